@@ -329,6 +329,122 @@ int ann_timing_read_each(int32_t kernel, int32_t capacity, int32_t *launches, fl
 int ann_priority_order(const int32_t *R, const double *W, const int32_t *C, const double *Wcur,
                        int32_t n, int32_t G, int32_t *level, int32_t *order, void *stream);
 
+/*
+ * ---- The step between two retrievals: one new token per request over a paged cache ----------------
+ *
+ * What retrieval returns is concatenated to the request's context and the model goes on from the keys and
+ * values that it has kept (Section 2.1, "PagedAttention" and prefix caching).  The entry points below are
+ * that step's operators around the matrix products: norms, rotation and the write into the cache
+ * (ann_qk_norm_rotate), attention of one new token per request (ann_paged_attention), cutting a cache that
+ * retrieved passages have made long (ann_cache_evict), and the rules that keep the output to its tags
+ * (ann_logit_rules).  The conventions at the top hold: device pointers, work only enqueued, no C++ exception
+ * crosses the boundary; an error means that nothing was enqueued.  Row strides are in elements.
+ *
+ * A paged cache holds the keys and values of many requests in pages of `slots` slots.  Slot j of request b
+ * lies in page page_table[b, j / slots] at place j % slots.  A page id outside [0, pages) is an empty page: its
+ * slots have no row.  Requests may share pages (a common prefix).
+ *   - Element (page, head, slot, i) of the keys is k[page k_page + head k_head + slot k_slot + i]; strides in
+ *     elements, multiples of 16 bytes, 16-byte aligned bases; the same for the values.  Any order of the
+ *     first three dimensions will do; [pages, heads, slots, d] is the fastest for short contexts.
+ *   - slots is a power of two, at most ANN_PAGE_MAX; d a multiple of 8, at most ANN_HEAD_MAX; offsets are 64 bits wide.
+ */
+#define ANN_PAGE_MAX   1024  /* most slots of a page */
+#define ANN_HEAD_MAX   256   /* largest dimension of a head */
+
+typedef struct ann_paged_cache {
+    void *k, *v;                          /* device */
+    int64_t k_page, k_head, k_slot;       /* strides */
+    int64_t v_page, v_head, v_slot;
+    int32_t pages, heads, slots, d;
+    int32_t dtype;
+} ann_paged_cache;
+
+/* Norms of queries and keys for each head, the rotation by position, and the write of keys and values into
+ * the cache, in one pass.  For token t and head h of qkv (q_heads query heads, then the cache's heads of keys,
+ * then as many of values), all in binary32 and rounded once:
+ *     y = x rsqrt(mean(x^2) + eps) w           (w: q_weight or k_weight, [d] of the cache's type)
+ *     with (c, s) = (cos_sin[p, i], cos_sin[p, rot / 2 + i]), p = positions[t], i < rot / 2, the pair (a, b) of
+ *     y becomes (a c - b s, b c + a s): elements i and rot / 2 + i, or 2 i and 2 i + 1 if `interleaved`;
+ *     elements from rot on stay.
+ * Queries go to q [T, q_heads, d]; keys, and values as they are, to place slots[t] % slots of page slots[t] / slots.
+ *   qkv         device, [T, q_heads + 2 heads, d]; strides token_stride, head_stride (multiples of 16 bytes)
+ *   cos_sin     device float [max_positions, rot]; rot a multiple of 16 in [0, d]
+ *   positions   device int32 [T].  A token whose position is not in [0, max_positions) is padding: its row of q
+ *               is zero and nothing is put into the cache.
+ *   slots       device int32 [T].  A token whose slot is not one of the cache's is not put there.  Two tokens
+ *               with one slot: either's row is left, or a mixture.
+ * T = 0 returns ANN_OK at once.  No workspace. */
+int ann_qk_norm_rotate(const void *qkv, int64_t token_stride, int64_t head_stride, int32_t T, int32_t q_heads,
+                       const void *q_weight, const void *k_weight, float eps,
+                       const int32_t *positions, const float *cos_sin, int32_t max_positions, int32_t rot,
+                       int32_t interleaved, const int32_t *slots, const ann_paged_cache *cache, void *q, void *stream);
+
+/* Attention of one new token per request over its paged cache.  Query head h of request b reads the keys and
+ * values of cache head h / (q_heads / heads):
+ *     x_j = scale <q, k_j>,  lse = log sum_j exp(x_j),  out = sum_j exp(x_j - lse) v_j
+ * over the slots j < n = lengths[b] whose page is not empty, and of these, with window > 0, the last `window`
+ * only (j >= n - window).  A request for which nothing is left gives out = 0, lse = -inf.  Sums, the softmax and its
+ * statistics are binary32; out is rounded once.
+ *   q           device [B, q_heads, d] of the cache's type; strides q_row, q_head (multiples of 16 bytes)
+ *   page_table  device int32 [B, width], rows one after the other; width >= 1
+ *   lengths     device int32 [B]; counts as no more than max_length (1 <= max_length <= width slots), and as 0 if negative
+ *   max_length  what the work is divided by: the largest length, where the host knows it
+ *   out         device [B, q_heads, d], contiguous;  lse  device float [B, q_heads], or NULL
+ *   mass        NULL, or device float [B, heads, mass_slots], mass_slots >= width slots: the weight
+ *               exp(x_j - lse) of slot j, summed over the query heads of a cache head, is added to mass[b, head, j]
+ * An infinite value with a weight above 0 gives an infinity or a NaN.  Same inputs give bitwise-same outputs.  Uses the workspace of the current device (conventions at the top;
+ * ann_set_workspace) for what the parts of a long context leave to be joined, and for scores if mass is given: the size below, where it is
+ * there; with less, or beyond 1 GiB, a few requests at a time.  B = 0 returns ANN_OK at once. */
+int ann_paged_attention(const void *q, int64_t q_row, int64_t q_head, int32_t B, int32_t q_heads,
+                        const ann_paged_cache *cache, const int32_t *page_table, int32_t width,
+                        const int32_t *lengths, int32_t max_length, float scale, int32_t window,
+                        void *out, float *lse, float *mass, int64_t mass_slots, void *stream);
+
+/* Bytes of workspace that ann_paged_attention uses for these sizes where it has them (with_mass: mass is given). */
+int64_t ann_paged_attention_workspace_bytes(int32_t B, int32_t q_heads, int32_t heads, int32_t d, int32_t dtype,
+                                            int32_t max_length, int32_t with_mass);
+
+/* Cuts caches to `budget` slots by accumulated attention weight (the mass of ann_paged_attention).  For each
+ * request b and cache head, with n = lengths[b]: all n slots if n <= budget; else the first `first`, the last
+ * `recent`, and of the others the budget - first - recent with the largest mass, of equal ones the lower slot (a NaN
+ * counts as less than any number).  Their rows are copied, in the order of the slots, to the slots 0, 1, ... of the new page
+ * table, bit for bit; the rows of an empty page are zeros.  What is read is not changed, so pages may be shared with other requests.
+ *   lengths     device int32 [B]; counts as no more than min(width slots, mass_slots), and as 0 if negative
+ *   mass        device float [B, heads, mass_slots]
+ *   new_page_table  device int32 [B, new_width]; its pages appear once each and are not pages of page_table that any request
+ *               still reads; rows that would go to an empty page are dropped
+ *   budget      1 <= budget <= min(new_width slots, new_mass_slots); first, recent >= 0, first + recent <= budget
+ *   kept        device int32 [B, heads, budget]: the slots, ascending, -1 behind the last (written)
+ *   new_lengths device int32 [B]: min(n, budget) (written)
+ *   new_mass    device float [B, heads, new_mass_slots]: the mass of the kept slots, 0 behind them (written)
+ * No workspace.  B = 0 returns ANN_OK at once. */
+int ann_cache_evict(const ann_paged_cache *cache, const int32_t *page_table, int32_t width, const int32_t *lengths, int32_t B,
+                    const float *mass, int64_t mass_slots, const int32_t *new_page_table, int32_t new_width,
+                    int32_t budget, int32_t first, int32_t recent,
+                    int32_t *kept, int32_t *new_lengths, float *new_mass, int64_t new_mass_slots, void *stream);
+
+/* Penalties for repeated tokens, biases and grammar masks on logits.  For request b and token v, l = logits[b, v], in
+ * binary32 and rounded once:
+ *     v among the n = lengths[b] tokens of the request:  l = l > 0 ? l / repetition[b] : l repetition[b]
+ *     v c > 0 times among those from prompt_lengths[b] on:  l = l - frequency[b] c - presence[b]
+ *     v = bias_tokens[b, i]:  l = l + bias_values[b, i]  (the last such i)
+ *     bit v % 32 of masks[mask_rows[b], v / 32] is 0:  l = -inf
+ *   logits, out     device [B, V] of dtype; strides row_stride, out_stride >= V; out may be logits
+ *   tokens          device int32 [B, T], T <= ANN_HISTORY_MAX; ids outside [0, V) are skipped
+ *   lengths, prompt_lengths  device int32 [B]; count as in [0, T];  repetition, presence, frequency  device float [B]
+ *   bias_tokens, bias_values device int32 / float [B, K], K <= ANN_BIAS_MAX; K = 0: NULL.  Ids outside [0, V) are skipped
+ *   masks           device uint32 [n_masks, ceil(V / 32)];  mask_rows  device int32 [B], outside [0, n_masks): no mask;
+ *                   both NULL with n_masks = 0
+ * No workspace.  B = 0 returns ANN_OK at once. */
+#define ANN_HISTORY_MAX 16777215
+#define ANN_BIAS_MAX    4096
+int ann_logit_rules(const void *logits, int64_t row_stride, int32_t B, int32_t V, int32_t dtype,
+                    const int32_t *tokens, int32_t T, const int32_t *lengths, const int32_t *prompt_lengths,
+                    const float *repetition, const float *presence, const float *frequency,
+                    const int32_t *bias_tokens, const float *bias_values, int32_t K,
+                    const uint32_t *masks, int32_t n_masks, const int32_t *mask_rows,
+                    void *out, int64_t out_stride, void *stream);
+
 /* Measurement support (no paper passage): the dense fp16 MFMA rate the current device sustains
  * on register-resident operands, in TFLOP/s, on the default stream (synchronises it).  With
  * random_operands != 0 the operands are random fp16 values that change from one MFMA to the

@@ -21,6 +21,7 @@ ANN_OK, ANN_ERR_INVALID, ANN_ERR_ALIGNMENT, ANN_ERR_UNKNOWN_CORPUS, ANN_ERR_LAUN
 ANN_F16, ANN_BF16, ANN_F32 = 0, 1, 2
 ANN_K_MAX, ANN_EF_MAX, ANN_R_MAX, ANN_D_MAX = 16, 16384, 256, 4096
 ANN_ENTRIES_MAX = 32
+ANN_PAGE_MAX, ANN_HEAD_MAX, ANN_HISTORY_MAX, ANN_BIAS_MAX = 1024, 256, 16777215, 4096
 
 _DTYPES = {torch.float16: ANN_F16, torch.bfloat16: ANN_BF16, torch.float32: ANN_F32}
 
@@ -31,7 +32,15 @@ EXPORTS = ("ann_version", "ann_last_error", "ann_flat_search_typed", "ann_flat_s
            "ann_graph_search_entries_typed", "ann_gather_ids", "ann_timing_enable", "ann_timing_read",
            "ann_measure_mfma_rate", "ann_priority_order", "ann_flat_search_static",
            "ann_graph_search_multi_typed", "ann_timing_read_each",
-           "ann_set_workspace", "ann_flat_search_after_typed")
+           "ann_set_workspace", "ann_flat_search_after_typed",
+           "ann_qk_norm_rotate", "ann_paged_attention", "ann_paged_attention_workspace_bytes", "ann_cache_evict", "ann_logit_rules")
+
+
+class PagedCache(ctypes.Structure):
+    """ann_paged_cache of include/ann.h."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p)] + \
+        [(name, ctypes.c_int64) for name in ("k_page", "k_head", "k_slot", "v_page", "v_head", "v_slot")] + \
+        [(name, ctypes.c_int32) for name in ("pages", "heads", "slots", "d", "dtype")]
 
 
 class AnnError(RuntimeError):
@@ -80,8 +89,16 @@ def lib() -> ctypes.CDLL:
         L.ann_timing_read_each.argtypes = [i32, i32, c.POINTER(i32), c.POINTER(c.c_float)]
         L.ann_graph_nonstall_workspace_bytes.argtypes = [i64, i32]
         L.ann_graph_nonstall_workspace_bytes.restype = i64
+        f32, cache = c.c_float, c.POINTER(PagedCache)
+        L.ann_qk_norm_rotate.argtypes = [vp, i64, i64, i32, i32, vp, vp, f32, vp, vp, i32, i32, i32, vp, cache, vp, vp]
+        L.ann_paged_attention.argtypes = [vp, i64, i64, i32, i32, cache, vp, i32, vp, i32, f32, i32, vp, vp, vp, i64, vp]
+        L.ann_paged_attention_workspace_bytes.argtypes = [i32] * 7
+        L.ann_paged_attention_workspace_bytes.restype = i64
+        L.ann_cache_evict.argtypes = [cache, vp, i32, vp, i32, vp, i64, vp, i32, i32, i32, i32, vp, vp, vp, i64, vp]
+        L.ann_logit_rules.argtypes = [vp, i64, i32, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, i32, vp, i32, vp, vp, i64, vp]
         for name in EXPORTS:
-            if name not in ("ann_last_error", "ann_flat_workspace_bytes", "ann_graph_nonstall_workspace_bytes"):
+            if name not in ("ann_last_error", "ann_flat_workspace_bytes", "ann_graph_nonstall_workspace_bytes",
+                            "ann_paged_attention_workspace_bytes"):
                 getattr(L, name).restype = c.c_int
         _lib = L
         _load_marshal(L)
@@ -471,3 +488,157 @@ def ann_set_workspace(buf: Optional[torch.Tensor]) -> None:
 
 def ann_release_workspace() -> None:
     _check(lib().ann_release_workspace())
+
+
+# ---- the step between two retrievals ---------------------------------------------------------
+
+def _array(t: torch.Tensor, name: str, dtype: torch.dtype, shape) -> torch.Tensor:
+    """A contiguous device tensor of that type and shape (-1: any size)."""
+    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or t.dim() != len(shape) or \
+            any(w not in (-1, n) for w, n in zip(shape, t.shape)):
+        raise ValueError(f"{name} must be a contiguous {str(dtype).replace('torch.', '')} device tensor of shape "
+                         f"{['any' if w == -1 else w for w in shape]}")
+    return t
+
+
+def _rows(t: torch.Tensor, name: str, dtype: torch.dtype, shape) -> torch.Tensor:
+    """A device tensor of that type and shape whose last dimension is contiguous."""
+    if t.dtype != dtype or not t.is_cuda or t.dim() != len(shape) or any(w not in (-1, n) for w, n in zip(shape, t.shape)) or \
+            (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name} must be a {str(dtype).replace('torch.', '')} device tensor of shape "
+                         f"{['any' if w == -1 else w for w in shape]} whose rows are contiguous")
+    return t
+
+
+def _strides(t: torch.Tensor):
+    """Strides of all dimensions but the last, 0 for those of size 1, which torch leaves anything."""
+    return [s if n > 1 else 0 for s, n in zip(t.stride()[:-1], t.shape)]
+
+
+def _cache(k_cache: torch.Tensor, v_cache: torch.Tensor) -> PagedCache:
+    for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+        if t.dim() != 4 or not t.is_cuda or t.dtype not in _DTYPES or (t.shape[3] > 1 and t.stride(3) != 1):
+            raise ValueError(f"{name} must be an fp16/bf16/fp32 device tensor [pages, heads, slots, d] whose rows are contiguous")
+    if k_cache.shape != v_cache.shape or k_cache.dtype != v_cache.dtype or k_cache.device != v_cache.device:
+        raise ValueError("k_cache and v_cache must have one shape and element type and be on one device")
+    pages, heads, slots, d = k_cache.shape
+    return PagedCache(k_cache.data_ptr(), v_cache.data_ptr(), *_strides(k_cache), *_strides(v_cache),
+                      pages, heads, slots, d, _DTYPES[k_cache.dtype])
+
+
+def _same_device(first: torch.Tensor, *others) -> None:
+    if any(t is not None and t.device != first.device for t in others):
+        raise ValueError("all tensors must be on one device")
+
+
+def ann_qk_norm_rotate(qkv: torch.Tensor, q_weight: torch.Tensor, k_weight: torch.Tensor, positions: torch.Tensor,
+                       cos_sin: torch.Tensor, slots: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, *,
+                       eps: float = 1e-6, interleaved: bool = False, q=None, stream=None) -> torch.Tensor:
+    """Norms of queries and keys for each head, the rotation by position, and the write of keys and values into the paged
+    cache [pages, heads, slots, d].  qkv is [T, query heads + 2 heads, d], cos_sin float32 [positions, rot], cosines before
+    sines; positions and slots int32 [T].  Returns the queries [T, query heads, d]."""
+    cache = _cache(k_cache, v_cache)
+    dtype, heads, d = k_cache.dtype, cache.heads, cache.d
+    _rows(qkv, "qkv", dtype, (-1, -1, d))
+    T, q_heads = qkv.shape[0], qkv.shape[1] - 2 * heads
+    if q_heads < 1:
+        raise ValueError("qkv must have query heads and the cache's heads twice")
+    _array(q_weight, "q_weight", dtype, (d,)), _array(k_weight, "k_weight", dtype, (d,))
+    _array(positions, "positions", torch.int32, (T,)), _array(slots, "slots", torch.int32, (T,))
+    _array(cos_sin, "cos_sin", torch.float32, (-1, -1))
+    if q is None:
+        q = torch.empty(T, q_heads, d, dtype=dtype, device=qkv.device)
+    _array(q, "q", dtype, (T, q_heads, d))
+    _same_device(k_cache, qkv, q_weight, k_weight, positions, cos_sin, slots, q)
+    _call(qkv.device, stream, lib().ann_qk_norm_rotate, qkv.data_ptr(), *_strides(qkv), T, q_heads, q_weight.data_ptr(),
+          k_weight.data_ptr(), float(eps), positions.data_ptr(), cos_sin.data_ptr(), cos_sin.shape[0], cos_sin.shape[1],
+          1 if interleaved else 0, slots.data_ptr(), ctypes.byref(cache), q.data_ptr())
+    return q
+
+
+def ann_paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor,
+                        lengths: torch.Tensor, *, scale: Optional[float] = None, window: int = 0, max_length: Optional[int] = None,
+                        mass: Optional[torch.Tensor] = None, out=None, lse=None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Attention of one new token per request over its paged cache.  q [B, query heads, d], page_table int32 [B, pages of a
+    request], lengths int32 [B]; scale 1 / sqrt(d) unless given; max_length: the largest length, where it is known.  mass
+    float32 [B, heads, slots]: the weight of every slot is added to it.  Returns (out [B, query heads, d], lse float32 [B, query heads])."""
+    cache = _cache(k_cache, v_cache)
+    d = cache.d
+    _rows(q, "q", k_cache.dtype, (-1, -1, d))
+    B, q_heads = q.shape[:2]
+    _array(page_table, "page_table", torch.int32, (B, -1)), _array(lengths, "lengths", torch.int32, (B,))
+    if mass is not None:
+        _array(mass, "mass", torch.float32, (B, cache.heads, -1))
+    width = page_table.shape[1]
+    out = torch.empty(B, q_heads, d, dtype=q.dtype, device=q.device) if out is None else _array(out, "out", q.dtype, (B, q_heads, d))
+    lse = torch.empty(B, q_heads, dtype=torch.float32, device=q.device) if lse is None else _array(lse, "lse", torch.float32, (B, q_heads))
+    _same_device(k_cache, q, page_table, lengths, mass, out, lse)
+    _call(q.device, stream, lib().ann_paged_attention, q.data_ptr(), *_strides(q), B, q_heads, ctypes.byref(cache),
+          page_table.data_ptr(), width, lengths.data_ptr(), width * cache.slots if max_length is None else int(max_length),
+          d ** -0.5 if scale is None else float(scale), int(window), out.data_ptr(), lse.data_ptr(),
+          0 if mass is None else mass.data_ptr(), 0 if mass is None else mass.shape[2])
+    return out, lse
+
+
+def ann_paged_attention_workspace_bytes(B: int, q_heads: int, heads: int, d: int, dtype: torch.dtype, max_length: int,
+                                        with_mass: bool = False) -> int:
+    return int(lib().ann_paged_attention_workspace_bytes(B, q_heads, heads, d, _DTYPES[dtype], max_length, 1 if with_mass else 0))
+
+
+def ann_cache_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor,
+                    mass: torch.Tensor, new_page_table: torch.Tensor, budget: int, *, first: int = 0, recent: int = 0,
+                    stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """The `budget` slots of every request and cache head that had the most attention (mass float32 [B, heads, slots]), its first
+    `first` and last `recent` among them, copied to the pages of new_page_table.  Returns (kept int32 [B, heads, budget], -1 behind
+    the last; new lengths int32 [B]; the kept slots' mass float32 [B, heads, new slots], 0 behind them)."""
+    cache = _cache(k_cache, v_cache)
+    _array(page_table, "page_table", torch.int32, (-1, -1))
+    B, device, budget = page_table.shape[0], k_cache.device, int(budget)
+    _array(lengths, "lengths", torch.int32, (B,)), _array(mass, "mass", torch.float32, (B, cache.heads, -1))
+    _array(new_page_table, "new_page_table", torch.int32, (B, -1))
+    _same_device(k_cache, page_table, lengths, mass, new_page_table)
+    new_slots = new_page_table.shape[1] * cache.slots
+    kept = torch.empty(B, cache.heads, max(0, budget), dtype=torch.int32, device=device)
+    new_lengths = torch.empty(B, dtype=torch.int32, device=device)
+    new_mass = torch.empty(B, cache.heads, new_slots, dtype=torch.float32, device=device)
+    _call(device, stream, lib().ann_cache_evict, ctypes.byref(cache), page_table.data_ptr(), page_table.shape[1], lengths.data_ptr(), B,
+          mass.data_ptr(), mass.shape[2], new_page_table.data_ptr(), new_page_table.shape[1], budget, int(first), int(recent),
+          kept.data_ptr(), new_lengths.data_ptr(), new_mass.data_ptr(), new_slots)
+    return kept, new_lengths, new_mass
+
+
+def ann_logit_rules(logits: torch.Tensor, tokens: torch.Tensor, lengths: torch.Tensor, prompt_lengths: torch.Tensor,
+                    repetition: torch.Tensor, presence: torch.Tensor, frequency: torch.Tensor, *,
+                    bias_tokens: Optional[torch.Tensor] = None, bias_values: Optional[torch.Tensor] = None,
+                    masks: Optional[torch.Tensor] = None, mask_rows: Optional[torch.Tensor] = None, out=None,
+                    stream=None) -> torch.Tensor:
+    """Penalties for repeated tokens, biases and grammar masks on logits [B, V] (fp16, bf16 or fp32).  tokens int32 [B, T], of which
+    lengths[b] count, the first prompt_lengths[b] of them as the prompt; repetition, presence, frequency float32 [B]; bias_tokens int32
+    and bias_values float32 [B, K]; masks int32 [M, ceil(V / 32)], a bit for each token, 1: allowed, and mask_rows int32 [B] into it,
+    -1: no mask.  out may be logits.  Returns out."""
+    if logits.dtype not in _DTYPES:
+        raise ValueError("logits must be an fp16/bf16/fp32 device tensor")
+    _rows(logits, "logits", logits.dtype, (-1, -1))
+    B, V = logits.shape
+    _array(tokens, "tokens", torch.int32, (B, -1)), _array(lengths, "lengths", torch.int32, (B,))
+    _array(prompt_lengths, "prompt_lengths", torch.int32, (B,))
+    for t, name in ((repetition, "repetition"), (presence, "presence"), (frequency, "frequency")):
+        _array(t, name, torch.float32, (B,))
+    K, M = 0, 0
+    if bias_tokens is not None or bias_values is not None:
+        if bias_tokens is None or bias_values is None:
+            raise ValueError("bias_tokens and bias_values go together")
+        K = _array(bias_tokens, "bias_tokens", torch.int32, (B, -1)).shape[1]
+        _array(bias_values, "bias_values", torch.float32, (B, K))
+    if masks is not None or mask_rows is not None:
+        if masks is None or mask_rows is None:
+            raise ValueError("masks and mask_rows go together")
+        M = _array(masks, "masks", torch.int32, (-1, (V + 31) // 32)).shape[0]
+        _array(mask_rows, "mask_rows", torch.int32, (B,))
+    out = torch.empty(B, V, dtype=logits.dtype, device=logits.device) if out is None else _rows(out, "out", logits.dtype, (B, V))
+    _same_device(logits, tokens, lengths, prompt_lengths, repetition, presence, frequency, bias_tokens, bias_values, masks, mask_rows, out)
+    _call(logits.device, stream, lib().ann_logit_rules, logits.data_ptr(), logits.stride(0) if B > 1 else V, B, V, _DTYPES[logits.dtype],
+          tokens.data_ptr(), tokens.shape[1], lengths.data_ptr(), prompt_lengths.data_ptr(), repetition.data_ptr(),
+          presence.data_ptr(), frequency.data_ptr(), bias_tokens.data_ptr() if K else 0, bias_values.data_ptr() if K else 0, K,
+          masks.data_ptr() if M else 0, M, mask_rows.data_ptr() if M else 0, out.data_ptr(), out.stride(0) if B > 1 else V)
+    return out

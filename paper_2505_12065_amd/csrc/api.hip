@@ -266,6 +266,52 @@ int flat_search_run(const FlatPlan &pl, const void *X, int64_t N, int d, int dty
     return check_launch("flat_merge_kernel", launch_flat_merge(partial, pl.st.P, B, k, ids, scores, stream));
 }
 
+// ---- the step between two retrievals -----------------------------------------------------------
+constexpr int64_t GRID_MAX = 1 << 22;                    // workgroups of a launch (of up to 1024 threads)
+
+int check_dtype(int32_t dtype) {
+    return dtype == ANN_F16 || dtype == ANN_BF16 || dtype == ANN_F32 ? ANN_OK : fail(ANN_ERR_INVALID, "unknown element type %d", dtype);
+}
+bool off16(const void *p) { return reinterpret_cast<uintptr_t>(p) & 15; }
+bool off4(std::initializer_list<const void *> ps) {
+    for (const void *p : ps)
+        if (reinterpret_cast<uintptr_t>(p) & 3) return true;
+    return false;
+}
+bool null_in(std::initializer_list<const void *> ps) {
+    for (const void *p : ps)
+        if (!p) return true;
+    return false;
+}
+
+int check_cache(const ann_paged_cache *c, Paged *out) {
+    if (!c || !c->k || !c->v) return fail(ANN_ERR_INVALID, "null pointer argument");
+    if (int rc = check_dtype(c->dtype)) return rc;
+    if (c->pages < 1 || c->heads < 1) return fail(ANN_ERR_INVALID, "a cache of %d pages and %d heads", c->pages, c->heads);
+    if (c->slots < 1 || c->slots > ANN_PAGE_MAX || (c->slots & (c->slots - 1)))
+        return fail(ANN_ERR_INVALID, "a page has %d slots: a power of two up to %d is wanted", c->slots, ANN_PAGE_MAX);
+    if (c->d < 8 || c->d > ANN_HEAD_MAX) return fail(ANN_ERR_INVALID, "d = %d out of range [8, %d]", c->d, ANN_HEAD_MAX);
+    if (c->d % 8) return fail(ANN_ERR_ALIGNMENT, "d = %d: a multiple of 8 is wanted", c->d);
+    const int e = elem_bytes(c->dtype);
+    const int64_t strides[] = {c->k_page, c->k_head, c->k_slot, c->v_page, c->v_head, c->v_slot};
+    for (int64_t s : strides) {
+        if (s < 0 || s > INT64_MAX / 8 / ((int64_t)c->pages + 1)) return fail(ANN_ERR_INVALID, "stride %lld out of range", (long long)s);
+        if (s * e % 16) return fail(ANN_ERR_ALIGNMENT, "stride %lld: rows must start at multiples of 16 bytes", (long long)s);
+    }
+    if (off16(c->k) || off16(c->v)) return fail(ANN_ERR_ALIGNMENT, "keys and values must be 16-byte aligned");
+    int log = 0;
+    while ((1 << log) < c->slots) ++log;
+    *out = Paged{static_cast<char *>(c->k), static_cast<char *>(c->v), c->k_page * e, c->k_head * e, c->k_slot * e,
+                 c->v_page * e, c->v_head * e, c->v_slot * e, c->pages, c->heads, log, c->d};
+    return ANN_OK;
+}
+int check_rows(const char *what, int64_t row, int64_t head, int e) {
+    if (row < 0 || head < 0 || row > INT64_MAX >> 34 || head > INT64_MAX >> 34)
+        return fail(ANN_ERR_INVALID, "strides of %s out of range", what);
+    if (row * e % 16 || head * e % 16) return fail(ANN_ERR_ALIGNMENT, "%s: rows must start at multiples of 16 bytes", what);
+    return ANN_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -374,6 +420,132 @@ int ann_priority_order(const int32_t *R, const double *W, const int32_t *C, cons
         return fail(ANN_ERR_ALIGNMENT, "R, C, level and order must be 4-byte aligned");
     return check_launch("priority kernels",
                         launch_priority(R, W, C, Wcur, n, G, level, order, static_cast<hipStream_t>(stream)));
+}
+
+int ann_qk_norm_rotate(const void *qkv, int64_t token_stride, int64_t head_stride, int32_t T, int32_t q_heads,
+                       const void *q_weight, const void *k_weight, float eps,
+                       const int32_t *positions, const float *cos_sin, int32_t max_positions, int32_t rot,
+                       int32_t interleaved, const int32_t *slots, const ann_paged_cache *cache, void *q, void *stream) {
+    if (T == 0) return ANN_OK;
+    RotateArgs a{};
+    if (int rc = check_cache(cache, &a.cache)) return rc;
+    if (null_in({qkv, q_weight, k_weight, positions, slots, q}) || (rot > 0 && !cos_sin)) return fail(ANN_ERR_INVALID, "null pointer argument");
+    if (T < 1 || T > GRID_MAX) return fail(ANN_ERR_INVALID, "T = %d out of range [0, %lld]", T, (long long)GRID_MAX);
+    if (q_heads < 1 || q_heads > 65536 || cache->heads > 65536)
+        return fail(ANN_ERR_INVALID, "%d query heads and %d heads of the cache", q_heads, cache->heads);
+    if (rot < 0 || rot > cache->d || rot % 16) return fail(ANN_ERR_INVALID, "rot = %d: a multiple of 16 up to d is wanted", rot);
+    if (max_positions < 0 || !(eps >= 0.f)) return fail(ANN_ERR_INVALID, "max_positions or eps out of range");
+    const int e = elem_bytes(cache->dtype);
+    if (int rc = check_rows("qkv", token_stride, head_stride, e)) return rc;
+    if (off16(qkv) || off16(q) || off16(q_weight) || off16(k_weight))
+        return fail(ANN_ERR_ALIGNMENT, "qkv, q and the weights must be 16-byte aligned");
+    if (off4({positions, cos_sin, slots})) return fail(ANN_ERR_ALIGNMENT, "positions, cos_sin and slots must be 4-byte aligned");
+    a.qkv = qkv; a.token = token_stride * e; a.head = head_stride * e; a.q_heads = q_heads;
+    a.q_weight = q_weight; a.k_weight = k_weight; a.eps = eps;
+    a.positions = positions; a.cos_sin = cos_sin; a.max_positions = max_positions; a.rot = rot; a.interleaved = interleaved != 0;
+    a.slots = slots; a.q = q;
+    return check_launch("qk_rotate_kernel", launch_qk_rotate(cache->dtype, a, T, static_cast<hipStream_t>(stream)));
+}
+
+int64_t ann_paged_attention_workspace_bytes(int32_t B, int32_t q_heads, int32_t heads, int32_t d, int32_t dtype,
+                                            int32_t max_length, int32_t with_mass) {
+    if (B < 1 || heads < 1 || q_heads < heads || q_heads % heads || d < 8 || d > ANN_HEAD_MAX || max_length < 1) return ANN_ERR_INVALID;
+    if (check_dtype(dtype) != ANN_OK) return ANN_ERR_INVALID;
+    return (int64_t)B * q_heads * 4 + 0 * with_mass;
+}
+
+int ann_paged_attention(const void *q, int64_t q_row, int64_t q_head, int32_t B, int32_t q_heads,
+                        const ann_paged_cache *cache, const int32_t *page_table, int32_t width,
+                        const int32_t *lengths, int32_t max_length, float scale, int32_t window,
+                        void *out, float *lse, float *mass, int64_t mass_slots, void *stream_) {
+    if (B == 0) return ANN_OK;
+    AttentionArgs a{};
+    if (int rc = check_cache(cache, &a.cache)) return rc;
+    if (null_in({q, page_table, lengths, out})) return fail(ANN_ERR_INVALID, "null pointer argument");
+    if (B < 1) return fail(ANN_ERR_INVALID, "B = %d out of range", B);
+    if (q_heads < 1 || q_heads % cache->heads)
+        return fail(ANN_ERR_INVALID, "%d query heads are no multiple of the cache's %d", q_heads, cache->heads);
+    if (width < 1 || (int64_t)width * cache->slots > INT32_MAX - 65536) return fail(ANN_ERR_INVALID, "width = %d out of range", width);
+    if (max_length < 1 || max_length > width * cache->slots)
+        return fail(ANN_ERR_INVALID, "max_length = %d out of range [1, width slots]", max_length);
+    if (window < 0 || !(fabsf(scale) < INFINITY)) return fail(ANN_ERR_INVALID, "window or scale out of range");
+    if (mass && mass_slots < (int64_t)width * cache->slots) return fail(ANN_ERR_INVALID, "mass has fewer slots than the page table");
+    const int e = elem_bytes(cache->dtype);
+    if (int rc = check_rows("q", q_row, q_head, e)) return rc;
+    if (off16(q) || off16(out)) return fail(ANN_ERR_ALIGNMENT, "q and out must be 16-byte aligned");
+    if (off4({page_table, lengths, lse, mass})) return fail(ANN_ERR_ALIGNMENT, "page_table, lengths, lse and mass must be 4-byte aligned");
+    if ((int64_t)B * q_heads > GRID_MAX) return fail(ANN_ERR_INVALID, "%d requests of %d heads are too many for a call", B, q_heads);
+    const hipStream_t stream = static_cast<hipStream_t>(stream_);
+    std::lock_guard<std::mutex> lock(g_mu);
+    DeviceState *st = nullptr;
+    if (int rc = device_state(&st)) return rc;
+    if (!lse) {
+        void *ws = nullptr;
+        if (int rc = workspace_for(st, &st->ws, (size_t)B * q_heads * 4, stream, &ws)) return rc;
+        lse = static_cast<float *>(ws);
+    }
+    a.q = q; a.q_row = q_row * e; a.q_head = q_head * e; a.q_heads = q_heads;
+    a.table = page_table; a.width = width; a.lengths = lengths; a.max_length = max_length; a.window = window; a.scale = scale;
+    a.out = out; a.lse = lse; a.mass = mass; a.mass_slots = mass_slots;
+    return check_launch("paged_attention_kernel", launch_paged_attention(cache->dtype, a, B, stream));
+}
+
+int ann_cache_evict(const ann_paged_cache *cache, const int32_t *page_table, int32_t width, const int32_t *lengths, int32_t B,
+                    const float *mass, int64_t mass_slots, const int32_t *new_page_table, int32_t new_width,
+                    int32_t budget, int32_t first, int32_t recent,
+                    int32_t *kept, int32_t *new_lengths, float *new_mass, int64_t new_mass_slots, void *stream) {
+    if (B == 0) return ANN_OK;
+    EvictArgs a{};
+    if (int rc = check_cache(cache, &a.cache)) return rc;
+    if (null_in({page_table, lengths, mass, new_page_table, kept, new_lengths, new_mass})) return fail(ANN_ERR_INVALID, "null pointer argument");
+    if (B < 1) return fail(ANN_ERR_INVALID, "B = %d out of range", B);
+    if (width < 1 || new_width < 1 || (int64_t)width * cache->slots > INT32_MAX - 65536 || (int64_t)new_width * cache->slots > INT32_MAX - 65536)
+        return fail(ANN_ERR_INVALID, "width or new_width out of range");
+    if (mass_slots < 1 || new_mass_slots < 1) return fail(ANN_ERR_INVALID, "mass without slots");
+    if (budget < 1 || budget > new_width * cache->slots || budget > new_mass_slots)
+        return fail(ANN_ERR_INVALID, "budget = %d does not fit the new page table or new_mass", budget);
+    if (first < 0 || recent < 0 || (int64_t)first + recent > budget)
+        return fail(ANN_ERR_INVALID, "first = %d and recent = %d do not fit the budget %d", first, recent, budget);
+    if (off4({page_table, lengths, mass, new_page_table, kept, new_lengths, new_mass}))
+        return fail(ANN_ERR_ALIGNMENT, "tables, lengths, masses and kept must be 4-byte aligned");
+    if ((int64_t)B * cache->heads * ((budget + 3) / 4) > GRID_MAX * 4)
+        return fail(ANN_ERR_INVALID, "%d requests of %d heads with a budget of %d are too many for a call", B, cache->heads, budget);
+    a.table = page_table; a.width = width; a.lengths = lengths; a.mass = mass; a.mass_slots = mass_slots;
+    a.most = (int)(mass_slots < (int64_t)width * cache->slots ? mass_slots : (int64_t)width * cache->slots);
+    a.new_table = new_page_table; a.new_width = new_width; a.budget = budget; a.first = first; a.recent = recent;
+    a.kept = kept; a.new_lengths = new_lengths; a.new_mass = new_mass; a.new_mass_slots = new_mass_slots;
+    return check_launch("evict kernels", launch_cache_evict(cache->dtype, a, B, static_cast<hipStream_t>(stream)));
+}
+
+int ann_logit_rules(const void *logits, int64_t row_stride, int32_t B, int32_t V, int32_t dtype,
+                    const int32_t *tokens, int32_t T, const int32_t *lengths, const int32_t *prompt_lengths,
+                    const float *repetition, const float *presence, const float *frequency,
+                    const int32_t *bias_tokens, const float *bias_values, int32_t K,
+                    const uint32_t *masks, int32_t n_masks, const int32_t *mask_rows,
+                    void *out, int64_t out_stride, void *stream) {
+    if (B == 0) return ANN_OK;
+    if (int rc = check_dtype(dtype)) return rc;
+    if (T < 0 || T > ANN_HISTORY_MAX) return fail(ANN_ERR_INVALID, "T = %d out of range [0, %d]", T, ANN_HISTORY_MAX);
+    if (K < 0 || K > ANN_BIAS_MAX) return fail(ANN_ERR_INVALID, "K = %d out of range [0, %d]", K, ANN_BIAS_MAX);
+    if (null_in({logits, lengths, prompt_lengths, repetition, presence, frequency, out}) || (T > 0 && !tokens) ||
+        (K > 0 && (!bias_tokens || !bias_values)) || (n_masks > 0 && (!masks || !mask_rows)))
+        return fail(ANN_ERR_INVALID, "null pointer argument");
+    if (B < 1 || V < 1 || V > INT32_MAX - 65536) return fail(ANN_ERR_INVALID, "B = %d or V = %d out of range", B, V);
+    if (n_masks < 0) return fail(ANN_ERR_INVALID, "n_masks = %d out of range", n_masks);
+    if (row_stride < V || out_stride < V || row_stride > INT64_MAX >> 34 || out_stride > INT64_MAX >> 34)
+        return fail(ANN_ERR_INVALID, "strides of logits or out out of range");
+    const uintptr_t odd = (uintptr_t)elem_bytes(dtype) - 1;
+    if ((reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(out)) & odd)
+        return fail(ANN_ERR_ALIGNMENT, "logits and out must be aligned to their elements");
+    if (off4({tokens, lengths, prompt_lengths, repetition, presence, frequency, bias_tokens, bias_values, masks, mask_rows}))
+        return fail(ANN_ERR_ALIGNMENT, "arrays of 32-bit values must be 4-byte aligned");
+    if ((int64_t)B * ((V + 1023) / 1024) > GRID_MAX) return fail(ANN_ERR_INVALID, "%d rows of %d logits are too many for a call", B, V);
+    RulesArgs a{};
+    a.logits = logits; a.row = row_stride; a.V = V; a.tokens = tokens; a.T = T; a.lengths = lengths; a.prompt = prompt_lengths;
+    a.repetition = repetition; a.presence = presence; a.frequency = frequency;
+    a.bias_tokens = bias_tokens; a.bias_values = bias_values; a.K = K;
+    a.masks = n_masks > 0 ? masks : nullptr; a.n_masks = n_masks; a.mask_rows = mask_rows; a.out = out; a.out_row = out_stride;
+    return check_launch("logit_rules_kernel", launch_logit_rules(dtype, a, B, static_cast<hipStream_t>(stream)));
 }
 
 int ann_measure_mfma_rate(int32_t random_operands, int32_t iters, double *tflops) {

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "common.hpp"
+#include "paged.hpp"
 #include "plan.hpp"
 
 namespace ann {
@@ -103,5 +104,72 @@ hipError_t launch_graph_search_nonstall(int dtype, const void *X, int64_t N, int
 // Scheduler priority levels (Section 3.2, Eq. 1-2) and execution order; all arrays device, length n.
 hipError_t launch_priority(const int32_t *R, const double *W, const int32_t *C, const double *Wcur, int n, int G,
                            int32_t *level, int32_t *order, hipStream_t stream);
+
+// ---- the step between two retrievals (strides in bytes unless said) ------------------------------
+struct RotateArgs {
+    const void *qkv;
+    int64_t token, head;
+    int q_heads;
+    const void *q_weight, *k_weight;
+    float eps;
+    const int32_t *positions;
+    const float *cos_sin;
+    int max_positions, rot, interleaved;
+    const int32_t *slots;
+    Paged cache;
+    void *q;
+};
+hipError_t launch_qk_rotate(int dtype, const RotateArgs &args, int T, hipStream_t stream);
+
+struct AttentionArgs {
+    const void *q;
+    int64_t q_row, q_head;
+    int q_heads;
+    Paged cache;
+    const int32_t *table;
+    int width;
+    const int32_t *lengths;
+    int max_length, window;
+    float scale;
+    void *out;
+    float *lse, *mass;
+    int64_t mass_slots;
+};
+hipError_t launch_paged_attention(int dtype, const AttentionArgs &args, int B, hipStream_t stream);
+
+struct EvictArgs {
+    Paged cache;
+    const int32_t *table;
+    int width;
+    const int32_t *lengths;
+    const float *mass;
+    int64_t mass_slots;
+    int most;                 // the largest length there can be
+    const int32_t *new_table;
+    int new_width, budget, first, recent;
+    int32_t *kept, *new_lengths;
+    float *new_mass;
+    int64_t new_mass_slots;
+};
+hipError_t launch_cache_evict(int dtype, const EvictArgs &args, int B, hipStream_t stream);
+
+struct RulesArgs {
+    const void *logits;
+    int64_t row;              // in elements
+    int V;
+    const int32_t *tokens;
+    int T;
+    const int32_t *lengths, *prompt;
+    const float *repetition, *presence, *frequency;
+    const int32_t *bias_tokens;
+    const float *bias_values;
+    int K;
+    const uint32_t *masks;
+    int n_masks;
+    const int32_t *mask_rows;
+    void *out;
+    int64_t out_row;
+};
+hipError_t launch_logit_rules(int dtype, const RulesArgs &args, int B, hipStream_t stream);
 
 }  // namespace ann
