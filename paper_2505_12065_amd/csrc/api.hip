@@ -449,9 +449,13 @@ int ann_qk_norm_rotate(const void *qkv, int64_t token_stride, int64_t head_strid
 
 int64_t ann_paged_attention_workspace_bytes(int32_t B, int32_t q_heads, int32_t heads, int32_t d, int32_t dtype,
                                             int32_t max_length, int32_t with_mass) {
-    if (B < 1 || heads < 1 || q_heads < heads || q_heads % heads || d < 8 || d > ANN_HEAD_MAX || max_length < 1) return ANN_ERR_INVALID;
+    if (B < 1 || heads < 1 || q_heads < heads || q_heads > 8192 || q_heads % heads || d < 8 || d > ANN_HEAD_MAX || max_length < 1) return ANN_ERR_INVALID;
     if (check_dtype(dtype) != ANN_OK) return ANN_ERR_INVALID;
-    return (int64_t)B * q_heads * 4 + 0 * with_mass;
+    std::lock_guard<std::mutex> lock(g_mu);
+    DeviceState *st = nullptr;
+    int cus = 256;
+    if (device_state(&st) == ANN_OK) cus = st->cus;
+    return (int64_t)attend_workspace(cus, B, q_heads, heads, d, elem_bytes(dtype), max_length, with_mass != 0, ATTEND_WS_MAX);
 }
 
 int ann_paged_attention(const void *q, int64_t q_row, int64_t q_head, int32_t B, int32_t q_heads,
@@ -463,8 +467,8 @@ int ann_paged_attention(const void *q, int64_t q_row, int64_t q_head, int32_t B,
     if (int rc = check_cache(cache, &a.cache)) return rc;
     if (null_in({q, page_table, lengths, out})) return fail(ANN_ERR_INVALID, "null pointer argument");
     if (B < 1) return fail(ANN_ERR_INVALID, "B = %d out of range", B);
-    if (q_heads < 1 || q_heads % cache->heads)
-        return fail(ANN_ERR_INVALID, "%d query heads are no multiple of the cache's %d", q_heads, cache->heads);
+    if (q_heads < 1 || q_heads > 8192 || q_heads % cache->heads)
+        return fail(ANN_ERR_INVALID, "%d query heads: a multiple of the cache's %d, at most 8192, is wanted", q_heads, cache->heads);
     if (width < 1 || (int64_t)width * cache->slots > INT32_MAX - 65536) return fail(ANN_ERR_INVALID, "width = %d out of range", width);
     if (max_length < 1 || max_length > width * cache->slots)
         return fail(ANN_ERR_INVALID, "max_length = %d out of range [1, width slots]", max_length);
@@ -479,15 +483,39 @@ int ann_paged_attention(const void *q, int64_t q_row, int64_t q_head, int32_t B,
     std::lock_guard<std::mutex> lock(g_mu);
     DeviceState *st = nullptr;
     if (int rc = device_state(&st)) return rc;
-    if (!lse) {
-        void *ws = nullptr;
-        if (int rc = workspace_for(st, &st->ws, (size_t)B * q_heads * 4, stream, &ws)) return rc;
-        lse = static_cast<float *>(ws);
+    AttendPlan pl = attend_plan(st->cus, B, q_heads, cache->heads, cache->d, e, max_length, window, mass != nullptr, ATTEND_WS_MAX);
+    // a buffer that a caller gave, or that a graph may not let grow, takes fewer requests at a time
+    if (!at_hand(st, st->ws, pl.one * pl.part, stream)) {
+        const size_t there = st->user_ws ? st->user_bytes : st->ws.bytes;
+        pl = attend_plan(st->cus, B, q_heads, cache->heads, cache->d, e, max_length, window, mass != nullptr, there);
+        if (pl.one > there)
+            return fail(ANN_ERR_NOMEM, "a request of %d slots needs %zu bytes of workspace, there are %zu", max_length, pl.one, there);
     }
-    a.q = q; a.q_row = q_row * e; a.q_head = q_head * e; a.q_heads = q_heads;
-    a.table = page_table; a.width = width; a.lengths = lengths; a.max_length = max_length; a.window = window; a.scale = scale;
-    a.out = out; a.lse = lse; a.mass = mass; a.mass_slots = mass_slots;
-    return check_launch("paged_attention_kernel", launch_paged_attention(cache->dtype, a, B, stream));
+    void *ws = nullptr;
+    if (pl.one)
+        if (int rc = workspace_for(st, &st->ws, pl.one * pl.part, stream, &ws)) return rc;
+    a.q_row = q_row * e; a.q_head = q_head * e; a.q_heads = q_heads;
+    a.width = width; a.max_length = max_length; a.window = window; a.scale = scale * 1.4426950408889634f;
+    a.mass_slots = mass_slots; a.groups = pl.groups; a.splits = pl.splits; a.chunk = pl.chunk; a.pad = pl.pad;
+    for (int b0 = 0; b0 < B; b0 += pl.part) {
+        const int b = B - b0 < pl.part ? B - b0 : pl.part;
+        a.q = static_cast<const char *>(q) + b0 * a.q_row;
+        a.table = page_table + (int64_t)b0 * width;
+        a.lengths = lengths + b0;
+        a.out = static_cast<char *>(out) + (int64_t)b0 * q_heads * cache->d * e;
+        a.lse = lse ? lse + (int64_t)b0 * q_heads : nullptr;
+        a.mass = mass ? mass + (int64_t)b0 * cache->heads * mass_slots : nullptr;
+        if (pl.one) {
+            a.partial = static_cast<float *>(ws);
+            float *scores = a.partial + (size_t)b * q_heads * pl.splits * cache->d;     // (whole multiples of 16 bytes)
+            a.scores = mass ? scores : nullptr;
+            a.stats = scores + (mass ? (size_t)b * q_heads * pl.pad : 0);
+        }
+        const hipError_t err = (cache->dtype == ANN_F16 ? launch_paged_attention_f16 : cache->dtype == ANN_BF16 ? launch_paged_attention_bf16
+                                : launch_paged_attention_f32)(a, b, stream);
+        if (int rc = check_launch("paged_attention_kernel", err)) return rc;
+    }
+    return ANN_OK;
 }
 
 int ann_cache_evict(const ann_paged_cache *cache, const int32_t *page_table, int32_t width, const int32_t *lengths, int32_t B,

@@ -1,0 +1,8 @@
+// Attention of one new token per request over a paged cache of BF16 elements.
+#include "paged_attention_kernel.hpp"
+
+namespace ann {
+
+hipError_t launch_paged_attention_bf16(const AttentionArgs &a, int B, hipStream_t stream) { return launch_attention<BF16>(a, B, stream); }
+
+}  // namespace ann

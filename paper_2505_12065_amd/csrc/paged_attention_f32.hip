@@ -1,0 +1,8 @@
+// Attention of one new token per request over a paged cache of F32 elements.
+#include "paged_attention_kernel.hpp"
+
+namespace ann {
+
+hipError_t launch_paged_attention_f32(const AttentionArgs &a, int B, hipStream_t stream) { return launch_attention<F32>(a, B, stream); }
+
+}  // namespace ann

@@ -1,0 +1,447 @@
+// Attention of one new token per request over a paged cache, on the matrix cores.
+//
+// A workgroup of four waves takes a part of one request's slots for the (at most 16) query heads of one cache head; a wave
+// takes NT tiles of 16 slots at a time.  Both products are turned so that the query heads are the columns of every tile:
+//     S^T [16 slots x 16 heads] = K Q^T          O^T [d x 16 heads] += V^T P^T
+// Lane 16 g + m then holds the scores of slots 4 g .. 4 g + 3 and head m, which is where the second product wants its operand P^T if
+// its 32 columns are numbered 8 g + 4 t + i for slot 4 g + i of tile t: nothing passes between lanes.  Its maximum, its sum
+// and its factor belong to head m too, so the accumulators are scaled in place.  Rows of V come as they lie in memory, 16 lanes
+// beside each other to a row, and are turned in registers, one byte permutation for two elements.
+#pragma once
+
+#include "launch.hpp"
+#include "paged.hpp"
+
+namespace ann {
+
+constexpr int ATTEND_THREADS = ATTEND_WAVES * WAVE;
+
+template <class T, int VE_>
+struct AttendShape {
+    static constexpr int VE = VE_, DP = 16 * VE;                     // elements of a row of V a lane holds; largest d
+    static constexpr int CE = T::bytes == 2 && VE > 4 ? 8 : 4;       // ... of which so many lie together
+    static constexpr int NU = VE / CE, CW = CE * T::bytes / 4;       // such chunks, and their registers
+    static constexpr int NS = DP * T::bytes / 64;                    // steps of 64 bytes of a row of K
+    static constexpr int NT = attend_tiles(T::bytes, VE);
+};
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// maximum, sum over the lanes with the same l % 16
+__device__ __forceinline__ float column_max(float x) {
+    uint32_t a, b;
+    row_pair<16>(__float_as_uint(x), a, b);
+    x = fmaxf(__uint_as_float(a), __uint_as_float(b));
+    row_pair<32>(__float_as_uint(x), a, b);
+    return fmaxf(__uint_as_float(a), __uint_as_float(b));
+}
+__device__ __forceinline__ float column_sum(float x) {
+    uint32_t a, b;
+    row_pair<16>(__float_as_uint(x), a, b);
+    x = __uint_as_float(a) + __uint_as_float(b);
+    row_pair<32>(__float_as_uint(x), a, b);
+    return __uint_as_float(a) + __uint_as_float(b);
+}
+
+template <int CW> struct Words;
+template <> struct Words<2> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
+template <> struct Words<4> { typedef u4 type; };
+
+// Eight weights as an operand of 16 bits and what that leaves, as another: the product with V then has 16 bits (bf16) or more of
+// them.  One part alone would be off by as much as the output's own rounding; the second product costs nothing here.
+template <class T>
+__device__ __forceinline__ void split_weights(const float (&p)[8], u4 &high, u4 &low);
+template <>
+__device__ __forceinline__ void split_weights<BF16>(const float (&p)[8], u4 &high, u4 &low) {
+    b8 h, l;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        h[i] = (__bf16)p[i];
+        l[i] = (__bf16)(p[i] - (float)h[i]);
+    }
+    high = __builtin_bit_cast(u4, h);
+    low = __builtin_bit_cast(u4, l);
+}
+template <>
+__device__ __forceinline__ void split_weights<F16>(const float (&p)[8], u4 &high, u4 &low) {
+    h8 h, l;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        h[i] = (_Float16)p[i];
+        l[i] = (_Float16)(p[i] - (float)h[i]);
+    }
+    high = __builtin_bit_cast(u4, h);
+    low = __builtin_bit_cast(u4, l);
+}
+
+template <class T>
+__device__ __forceinline__ f4 scores_step(u4 k, u4 q, f4 c) {
+    if constexpr (T::bytes == 2) {
+        return mfma16<T>(k, q, c);
+    } else {                                              // (which four columns meet in an instruction is all the same)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[j]), __uint_as_float(q[j]), c, 0, 0, 0);
+        return c;
+    }
+}
+
+// FINE: pages of less than 16 slots, looked up for every row and not for a tile.  FULL: d is 16 VE.
+template <class T, int VE, bool FINE, bool FULL>
+__global__ __launch_bounds__(ATTEND_THREADS, VE == 16 ? 1 : 2) void paged_attention_kernel(AttentionArgs a) {
+    typedef AttendShape<T, VE> Sh;
+    typedef typename Words<Sh::CW>::type VChunk;
+    constexpr int NT = Sh::NT, NS = Sh::NS, NU = Sh::NU, CE = Sh::CE, STEP = 16 * NT * ATTEND_WAVES;
+    extern __shared__ float lds[];
+    const int lane = threadIdx.x & (WAVE - 1), g = lane >> 4, m = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+    int id = xcd_block();
+    const int hg = id % a.groups;
+    id /= a.groups;
+    const int part = id % a.splits;
+    id /= a.splits;
+    const int h = id % a.cache.heads, b = id / a.cache.heads;
+    const int G = a.q_heads / a.cache.heads, rows = min(16, G - 16 * hg);     // query heads of this workgroup
+    const int n = min(a.lengths[b], a.max_length), lo = a.window > 0 ? max(0, n - a.window) : 0, start = lo & ~15;
+    const int first = start + part * a.chunk, end = min(n, first + a.chunk);
+    if (first >= n && a.splits > 1) return;
+    const int64_t hq0 = (int64_t)b * a.q_heads + h * G + 16 * hg;
+
+    u4 q[NS];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        q[s] = zero_chunk();
+        const int at = (4 * s + g) * 16;
+        if (m < rows && (FULL || at < a.cache.d * T::bytes))
+            q[s] = load_chunk(static_cast<const char *>(a.q) + b * a.q_row + (h * G + 16 * hg + m) * a.q_head + at);
+    }
+    const int32_t *table = a.table + (int64_t)b * a.width;
+    const int slots_log = a.cache.slots_log, mask = (1 << slots_log) - 1;
+    const char *k_head = a.cache.k + h * a.cache.k_head, *v_head = a.cache.v + h * a.cache.v_head;
+    // where a row is that may be read: its own, or for one that is not there the first of the cache
+    auto row_page = [&](int key) {
+        int page = -1;
+        if (key < end) page = table[key >> slots_log];
+        return (unsigned)page < (unsigned)a.cache.pages ? page : -1;
+    };
+
+    int page[NT], page_next[NT];                          // of a tile (uniform), -1: none
+    u4 kr[NT][NS];
+    auto pages_of = [&](int k0, int (&out)[NT]) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) out[t] = FINE ? 0 : __builtin_amdgcn_readfirstlane(row_page(k0 + 16 * t));
+    };
+    auto load_k = [&](int k0, const int (&pg)[NT]) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int key = k0 + 16 * t + m, p = FINE ? row_page(key) : pg[t];
+            const char *row = k_head + (int64_t)max(p, 0) * a.cache.k_page + (FINE && p < 0 ? 0 : key & mask) * a.cache.k_slot;
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                const int at = (4 * s + g) * 16;
+                if (FULL || at < a.cache.d * T::bytes) kr[t][s] = load_chunk(row + at);
+                else kr[t][s] = zero_chunk();
+            }
+        }
+    };
+
+    f4 o[VE];
+#pragma unroll
+    for (int c = 0; c < VE; ++c) o[c] = f4{0.f, 0.f, 0.f, 0.f};
+    float top = -INFINITY, sum = 0.f;                     // of head m; the sum of this lane's slots alone
+    int k0 = first + wave * 16 * NT;
+    if (k0 < end) {
+        pages_of(k0, page);
+        load_k(k0, page);
+    }
+    for (; k0 < end; k0 += STEP) {
+        const bool more = k0 + STEP < end;
+        if (more) pages_of(k0 + STEP, page_next);
+        VChunk vr[NT][4][NU];
+        unsigned there = 0;                               // FINE: which of the lane's slots have a row
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int key = k0 + 16 * t + 4 * g + i, p = FINE ? row_page(key) : page[t];
+                if (FINE && p >= 0 && key >= lo) there |= 1u << (4 * t + i);
+                const char *row = v_head + (int64_t)max(p, 0) * a.cache.v_page + (FINE && p < 0 ? 0 : key & mask) * a.cache.v_slot;
+#pragma unroll
+                for (int u = 0; u < NU; ++u) {
+                    const int at = (u * 16 + m) * CE;
+                    if (FULL || at < a.cache.d) vr[t][i][u] = *reinterpret_cast<const VChunk *>(row + at * T::bytes);
+                    else vr[t][i][u] = VChunk(0);
+                }
+            }
+        }
+        f4 x[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            x[t] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < NS; ++s) x[t] = scores_step<T>(kr[t][s], q[s], x[t]);
+        }
+        if (more) load_k(k0 + STEP, page_next);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) x[t] *= a.scale;
+        bool whole = k0 >= lo && k0 + 16 * NT <= end;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) whole = whole && page[t] >= 0;
+        if (FINE || !whole) {                             // slots that do not count: no score, and no value that could be NaN
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int key = k0 + 16 * t + 4 * g + i;
+                    const bool use = FINE ? (there >> (4 * t + i)) & 1 : page[t] >= 0 && key >= lo && key < end;
+                    if (!use) {
+                        x[t][i] = -INFINITY;
+#pragma unroll
+                        for (int u = 0; u < NU; ++u) vr[t][i][u] = VChunk(0);
+                    }
+                }
+            }
+        }
+        if (a.scores && m < rows) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+                *reinterpret_cast<f4 *>(a.scores + (hq0 + m) * a.pad + (k0 - start + 16 * t + 4 * g)) = x[t];
+        }
+        float most = x[0][0];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) most = fmaxf(most, x[t][i]);
+        const float now = fmaxf(top, column_max(most)), base = now == -INFINITY ? 0.f : now, keep = exp2_fast(top - base);
+        top = now;
+        sum *= keep;
+        float p[NT][4];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                p[t][i] = exp2_fast(x[t][i] - base);
+                sum += p[t][i];
+            }
+#pragma unroll
+        for (int c = 0; c < VE; ++c) o[c] *= keep;
+        if constexpr (T::bytes == 2) {
+#pragma unroll
+            for (int t = 0; t < NT; t += 2) {
+                const float w[8] = {p[t][0], p[t][1], p[t][2], p[t][3], p[t + 1][0], p[t + 1][1], p[t + 1][2], p[t + 1][3]};
+                u4 high, low;
+                split_weights<T>(w, high, low);
+#pragma unroll
+                for (int u = 0; u < NU; ++u)
+#pragma unroll
+                    for (int c = 0; c < CE; ++c) {
+                        u4 v;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            v[k] = __builtin_amdgcn_perm(vr[t + k / 2][2 * (k & 1) + 1][u][c / 2], vr[t + k / 2][2 * (k & 1)][u][c / 2],
+                                                         c & 1 ? 0x07060302u : 0x05040100u);
+                        f4 &acc = o[u * CE + c];
+                        acc = mfma16<T>(v, high, acc);
+                        acc = mfma16<T>(v, low, acc);
+                    }
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int u = 0; u < NU; ++u)
+#pragma unroll
+                        for (int c = 0; c < CE; ++c)
+                            o[u * CE + c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[t][i][u][c]), p[t][i], o[u * CE + c], 0, 0, 0);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) page[t] = page_next[t];
+    }
+
+    // the four waves' sums, joined: lane 16 g + m holds elements CE (4 g + i) .. of every 16 CE, head m
+    sum = column_sum(sum);
+    float *s_top = lds, *s_sum = lds + ATTEND_WAVES * 16, *s_o = lds + 2 * ATTEND_WAVES * 16;
+    constexpr int LD = attend_lds_row(VE);
+    if (g == 0) {
+        s_top[wave * 16 + m] = top;
+        s_sum[wave * 16 + m] = sum;
+    }
+    __syncthreads();
+    float all = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < ATTEND_WAVES; ++w) all = fmaxf(all, s_top[w * 16 + m]);
+    const float mine = top == -INFINITY ? 0.f : exp2_fast(top - all);
+    if (m < rows) {
+#pragma unroll
+        for (int u = 0; u < NU; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int c = 0; c < CE; c += 4) {
+                    const int at = (u * 16 + 4 * g + i) * CE + c;
+                    *reinterpret_cast<f4 *>(s_o + (wave * rows + m) * LD + at) =
+                        f4{o[u * CE + c][i], o[u * CE + c + 1][i], o[u * CE + c + 2][i], o[u * CE + c + 3][i]} * mine;
+                }
+    }
+    __syncthreads();
+    const int per_row = a.cache.d / 8;
+    for (int i = threadIdx.x; i < rows * per_row; i += ATTEND_THREADS) {
+        const int r = i / per_row, at = (i % per_row) * 8;
+        float most = -INFINITY, total = 0.f;
+#pragma unroll
+        for (int w = 0; w < ATTEND_WAVES; ++w) most = fmaxf(most, s_top[w * 16 + r]);
+#pragma unroll
+        for (int w = 0; w < ATTEND_WAVES; ++w) {
+            const float t = s_top[w * 16 + r];
+            // (a NaN among the scores is in the sum, whatever the maximum says)
+            total += s_sum[w * 16 + r] * (t == -INFINITY ? 1.f : exp2_fast(t - most));
+        }
+        float y[8] = {};
+#pragma unroll
+        for (int w = 0; w < ATTEND_WAVES; ++w) {
+            const float *z = s_o + (w * rows + r) * LD + at;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] += z[j];
+        }
+        if (a.splits > 1 || a.scores) {
+            float *to = a.partial + ((hq0 + r) * a.splits + part) * a.cache.d + at;
+            reinterpret_cast<f4 *>(to)[0] = f4{y[0], y[1], y[2], y[3]};
+            reinterpret_cast<f4 *>(to)[1] = f4{y[4], y[5], y[6], y[7]};
+            if (at == 0) {
+                a.stats[((hq0 + r) * a.splits + part) * 2] = most;
+                a.stats[((hq0 + r) * a.splits + part) * 2 + 1] = total;
+            }
+        } else {
+            const float f = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = total == 0.f ? 0.f : y[j] * f;
+            Eight<T> e;
+            e.set(y);
+            e.store(static_cast<char *>(a.out) + ((hq0 + r) * a.cache.d + at) * T::bytes);
+            if (at == 0 && a.lse) a.lse[hq0 + r] = total == 0.f ? -INFINITY : (most == -INFINITY ? 0.f : most) * 0.6931471805599453f + logf(total);
+        }
+    }
+}
+
+// What the parts of a context left, joined: the first B q_heads workgroups take a query head each; those behind them (scores given) take
+// 4 THREADS slots of a cache head each and add the weights of its query heads, in their order, to mass.
+template <class T>
+__global__ __launch_bounds__(ATTEND_THREADS) void paged_attention_join_kernel(AttentionArgs a, int B) {
+    __shared__ float lds[ATTEND_THREADS * 8];
+    const int G = a.q_heads / a.cache.heads, tid = threadIdx.x;
+    // of head row r, by one wave: largest exponent and total over its parts
+    auto stats_of = [&](int64_t r, int parts, float &most, float &total) {
+        const float *st = a.stats + r * a.splits * 2;
+        const int lane = tid & (WAVE - 1);
+        most = -INFINITY;
+        total = 0.f;
+        for (int s = lane; s < parts; s += WAVE) most = fmaxf(most, st[2 * s]);
+#pragma unroll
+        for (int k = 1; k < WAVE; k *= 2) most = fmaxf(most, __shfl_xor(most, k));
+        for (int s = lane; s < parts; s += WAVE) total += st[2 * s + 1] * (st[2 * s] == -INFINITY ? 1.f : exp2_fast(st[2 * s] - most));
+#pragma unroll
+        for (int k = 1; k < WAVE; k *= 2) total += __shfl_xor(total, k);
+    };
+    auto parts_of = [&](int b, int &n, int &lo, int &start) {
+        n = min(a.lengths[b], a.max_length);
+        lo = a.window > 0 ? max(0, n - a.window) : 0;
+        start = lo & ~15;
+        return n > 0 ? (n - start + a.chunk - 1) / a.chunk : 0;
+    };
+    int n, lo, start;
+    if ((int64_t)blockIdx.x < (int64_t)B * a.q_heads) {
+        const int64_t r = blockIdx.x;
+        const int parts = parts_of((int)(r / a.q_heads), n, lo, start);
+        const int per_row = a.cache.d / 8, side = ATTEND_THREADS / per_row;  // threads to a row; parts side by side
+        float most, total;
+        stats_of(r, parts, most, total);
+        float y[8] = {};
+        if (tid < side * per_row) {
+            const int at = (tid % per_row) * 8;
+            for (int s = tid / per_row; s < parts; s += side) {
+                const float t = a.stats[(r * a.splits + s) * 2], f = t == -INFINITY ? 1.f : exp2_fast(t - most);
+                const f4 *z = reinterpret_cast<const f4 *>(a.partial + (r * a.splits + s) * a.cache.d + at);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] = fmaf(z[j / 4][j % 4], f, y[j]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) lds[tid * 8 + j] = y[j];
+        __syncthreads();
+        if (tid < per_row) {
+            for (int s = 1; s < side && s < parts; ++s)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] += lds[(tid + s * per_row) * 8 + j];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = total == 0.f ? 0.f : y[j] / total;
+            Eight<T> e;
+            e.set(y);
+            e.store(static_cast<char *>(a.out) + (r * a.cache.d + 8 * tid) * T::bytes);
+            if (tid == 0 && a.lse) a.lse[r] = total == 0.f ? -INFINITY : (most == -INFINITY ? 0.f : most) * 0.6931471805599453f + logf(total);
+        }
+        return;
+    }
+    const int64_t id = blockIdx.x - (int64_t)B * a.q_heads;
+    const int pieces = (a.pad + 4 * ATTEND_THREADS - 1) / (4 * ATTEND_THREADS);
+    const int64_t row = id / pieces;
+    const int b = (int)(row / a.cache.heads), h = (int)(row % a.cache.heads);
+    const int parts = parts_of(b, n, lo, start), j0 = (int)(id % pieces) * 4 * ATTEND_THREADS;
+    if (start + j0 >= n) return;
+    const int j = j0 + 4 * tid;
+    f4 w = {0.f, 0.f, 0.f, 0.f};
+    for (int g0 = 0; g0 < G; g0 += ATTEND_THREADS) {      // (one round as a rule)
+        const int heads = min(ATTEND_THREADS, G - g0);
+        for (int i = tid / WAVE; i < heads; i += ATTEND_WAVES) {
+            float most, total;
+            stats_of((int64_t)b * a.q_heads + h * G + g0 + i, parts, most, total);
+            lds[2 * i] = most == -INFINITY ? 0.f : most;
+            lds[2 * i + 1] = total == 0.f ? 0.f : 1.f / total;
+        }
+        __syncthreads();
+        if (start + j < n) {
+            const float *x = a.scores + ((int64_t)b * a.q_heads + h * G + g0) * a.pad + j;
+            for (int i = 0; i < heads; ++i) {
+                const f4 s = *reinterpret_cast<const f4 *>(x + (int64_t)i * a.pad);
+                const float most = lds[2 * i], f = lds[2 * i + 1];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) w[c] += exp2_fast(s[c] - most) * f;
+            }
+        }
+        __syncthreads();
+    }
+    float *to = a.mass + row * a.mass_slots + start + j;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        if (start + j + c >= lo && start + j + c < n) to[c] += w[c];
+}
+
+template <class T, int VE, bool FINE, bool FULL>
+hipError_t attend(const AttentionArgs &a, int B, hipStream_t stream) {
+    static size_t granted = 0;
+    const int G = a.q_heads / a.cache.heads;
+    const size_t bytes = attend_lds_bytes(VE, G);
+    const void *kernel = reinterpret_cast<const void *>(paged_attention_kernel<T, VE, FINE, FULL>);
+    if (hipError_t e = allow_big_lds(kernel, bytes, &granted)) return e;
+    hipLaunchKernelGGL((paged_attention_kernel<T, VE, FINE, FULL>), dim3(B * a.cache.heads * a.splits * a.groups), dim3(ATTEND_THREADS), bytes, stream, a);
+    return hipGetLastError();
+}
+
+template <class T, int VE>
+hipError_t attend(const AttentionArgs &a, int B, hipStream_t stream) {
+    const bool fine = a.cache.slots_log < 4, full = a.cache.d == 16 * VE;
+    return fine ? full ? attend<T, VE, true, true>(a, B, stream) : attend<T, VE, true, false>(a, B, stream)
+                : full ? attend<T, VE, false, true>(a, B, stream) : attend<T, VE, false, false>(a, B, stream);
+}
+
+template <class T>
+hipError_t launch_attention(const AttentionArgs &a, int B, hipStream_t stream) {
+    const int ve = attend_ve(a.cache.d);
+    if (hipError_t e = ve == 4 ? attend<T, 4>(a, B, stream) : ve == 8 ? attend<T, 8>(a, B, stream) : attend<T, 16>(a, B, stream)) return e;
+    if (a.splits == 1 && !a.scores) return hipSuccess;
+    const int pieces = a.scores ? (a.pad + 4 * ATTEND_THREADS - 1) / (4 * ATTEND_THREADS) : 0;
+    hipLaunchKernelGGL((paged_attention_join_kernel<T>), dim3(B * a.q_heads + B * a.cache.heads * pieces), dim3(ATTEND_THREADS), 0, stream, a, B);
+    return hipGetLastError();
+}
+
+}  // namespace ann

@@ -986,4 +986,59 @@ inline bool graph_step_pays(int cus, int64_t N, int row_bytes, int R, int B, int
     return ef * reach >= N;                               // nodes per list entry up to which steps pay
 }
 
+// ---- attention over a paged cache ---------------------------------------------------------------------
+constexpr int ATTEND_WAVES = 4;
+constexpr size_t ATTEND_WS_MAX = (size_t)1 << 30;         // of the library's own workspace
+inline int attend_ve(int d) { return d <= 64 ? 4 : d <= 128 ? 8 : 16; }
+// Tiles of 16 slots that a wave takes at a time: as many as its registers hold twice (K of the next, V of this).
+constexpr int attend_tiles(int elem_bytes, int ve) { return elem_bytes == 2 ? (ve == 4 ? 4 : 2) : ve == 16 ? 1 : 2; }
+constexpr int attend_lds_row(int ve) { return 16 * ve + 4; }
+inline size_t attend_lds_bytes(int ve, int G) {
+    return (size_t)(2 * ATTEND_WAVES * 16 + ATTEND_WAVES * (G < 16 ? G : 16) * attend_lds_row(ve)) * 4;
+}
+
+// How a batch is divided: `groups` workgroups side by side for the query heads of a cache head, 16 each; `splits` parts of `chunk` slots of
+// every context; `part` requests at a time.
+struct AttendPlan {
+    int groups = 1, splits = 1, chunk = 0, pad = 0, part = 1;
+    size_t one = 0;              // bytes of workspace a request takes
+};
+constexpr int ATTEND_PARTS = 256, ATTEND_CHUNK = 1024, ATTEND_PER_CU = 4;
+constexpr int64_t ATTEND_GRID = 1 << 22;                  // workgroups of a launch
+inline int64_t attend_step(int elem_bytes, int d) { return 16 * ATTEND_WAVES * attend_tiles(elem_bytes, attend_ve(d)); }
+inline size_t attend_bytes(int q_heads, int d, int64_t splits, int64_t pad) { return (size_t)q_heads * ((size_t)splits * (d + 2) + (size_t)pad) * 4; }
+inline AttendPlan attend_plan(int cus, int B, int q_heads, int heads, int d, int elem_bytes, int max_length, int window, bool mass, size_t most) {
+    AttendPlan pl;
+    const int64_t step = attend_step(elem_bytes, d);
+    const int64_t range = window > 0 && (int64_t)window + 15 < max_length ? (int64_t)window + 15 : max_length;
+    pl.groups = (q_heads / heads + 15) / 16;
+    const int64_t units = (int64_t)B * heads * pl.groups;
+    int64_t chunk = (range * units / ((int64_t)cus * ATTEND_PER_CU) + step - 1) / step * step;
+    if (chunk > ATTEND_CHUNK) chunk = ATTEND_CHUNK;
+    if (chunk < step) chunk = step;
+    if (range > ATTEND_PARTS * chunk) chunk = (range + ATTEND_PARTS * step - 1) / (ATTEND_PARTS * step) * step;
+    pl.chunk = (int)chunk;
+    pl.splits = (int)((range + chunk - 1) / chunk);
+    pl.pad = (int)(pl.splits * chunk);
+    if (pl.splits > 1 || mass) pl.one = attend_bytes(q_heads, d, pl.splits, mass ? pl.pad : 0);
+    pl.part = B;
+    if (pl.one > 0 && pl.one * (size_t)B > most) pl.part = pl.one > most ? 1 : (int)(most / pl.one);
+    const int64_t grid = (int64_t)heads * pl.splits * pl.groups + (pl.one ? q_heads + (int64_t)heads * (mass ? pl.pad / 1024 + 1 : 0) : 0);
+    if (pl.part > ATTEND_GRID / grid) pl.part = ATTEND_GRID / grid < 1 ? 1 : (int)(ATTEND_GRID / grid);
+    return pl;
+}
+// Enough for these sizes and for shorter lengths and windows, which may be divided into more parts.
+inline size_t attend_workspace(int cus, int B, int q_heads, int heads, int d, int elem_bytes, int max_length, bool mass, size_t most) {
+    const int64_t step = attend_step(elem_bytes, d), units = (int64_t)B * heads * ((q_heads / heads + 15) / 16);
+    int64_t splits = ((int64_t)cus * ATTEND_PER_CU + units - 1) / units, by_chunk = ((int64_t)max_length + ATTEND_CHUNK - 1) / ATTEND_CHUNK;
+    const int64_t by_step = ((int64_t)max_length + step - 1) / step;
+    splits = splits > by_chunk ? splits : by_chunk;
+    splits = splits < by_step ? splits : by_step;
+    splits = splits < ATTEND_PARTS ? splits : ATTEND_PARTS;
+    const int64_t longest = (max_length + ATTEND_PARTS * step - 1) / (ATTEND_PARTS * step) * step;
+    const size_t one = attend_bytes(q_heads, d, splits, mass ? max_length + (longest > ATTEND_CHUNK ? longest : ATTEND_CHUNK) : 0);
+    const size_t part = one > most ? 1 : most / one;
+    return one * (part < (size_t)B ? part : (size_t)B);
+}
+
 }  // namespace ann
