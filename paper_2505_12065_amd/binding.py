@@ -125,6 +125,8 @@ def _load_marshal(L: ctypes.CDLL) -> None:
     module.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in
                   (L.ann_flat_search_typed, L.ann_flat_search_after_typed, L.ann_graph_search_typed, L.ann_graph_search_entries_typed,
                    L.ann_graph_search_nonstall_typed, L.ann_gather_ids, L.ann_priority_order)))
+    module.bind_decode(*(ctypes.cast(f, ctypes.c_void_p).value for f in
+                         (L.ann_qk_norm_rotate, L.ann_paged_attention, L.ann_cache_evict, L.ann_logit_rules)))
     _marshal = module
 
 
@@ -537,6 +539,10 @@ def ann_qk_norm_rotate(qkv: torch.Tensor, q_weight: torch.Tensor, k_weight: torc
     """Norms of queries and keys for each head, the rotation by position, and the write of keys and values into the paged
     cache [pages, heads, slots, d].  qkv is [T, query heads + 2 heads, d], cos_sin float32 [positions, rot], cosines before
     sines; positions and slots int32 [T].  Returns the queries [T, query heads, d]."""
+    if q is None and stream is None:
+        usual = _usual("rotate", qkv, q_weight, k_weight, positions, cos_sin, slots, k_cache, v_cache, eps, interleaved)
+        if usual is not None:
+            return usual[0]
     cache = _cache(k_cache, v_cache)
     dtype, heads, d = k_cache.dtype, cache.heads, cache.d
     _rows(qkv, "qkv", dtype, (-1, -1, d))
@@ -562,6 +568,10 @@ def ann_paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.T
     """Attention of one new token per request over its paged cache.  q [B, query heads, d], page_table int32 [B, pages of a
     request], lengths int32 [B]; scale 1 / sqrt(d) unless given; max_length: the largest length, where it is known.  mass
     float32 [B, heads, slots]: the weight of every slot is added to it.  Returns (out [B, query heads, d], lse float32 [B, query heads])."""
+    if out is None and lse is None and stream is None:
+        usual = _usual("attend", q, k_cache, v_cache, page_table, lengths, scale, window, max_length, mass)
+        if usual is not None:
+            return usual
     cache = _cache(k_cache, v_cache)
     d = cache.d
     _rows(q, "q", k_cache.dtype, (-1, -1, d))
@@ -591,6 +601,10 @@ def ann_cache_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: to
     """The `budget` slots of every request and cache head that had the most attention (mass float32 [B, heads, slots]), its first
     `first` and last `recent` among them, copied to the pages of new_page_table.  Returns (kept int32 [B, heads, budget], -1 behind
     the last; new lengths int32 [B]; the kept slots' mass float32 [B, heads, new slots], 0 behind them)."""
+    if stream is None:
+        usual = _usual("evict", k_cache, v_cache, page_table, lengths, mass, new_page_table, budget, first, recent)
+        if usual is not None:
+            return usual
     cache = _cache(k_cache, v_cache)
     _array(page_table, "page_table", torch.int32, (-1, -1))
     B, device, budget = page_table.shape[0], k_cache.device, int(budget)
@@ -616,6 +630,11 @@ def ann_logit_rules(logits: torch.Tensor, tokens: torch.Tensor, lengths: torch.T
     lengths[b] count, the first prompt_lengths[b] of them as the prompt; repetition, presence, frequency float32 [B]; bias_tokens int32
     and bias_values float32 [B, K]; masks int32 [M, ceil(V / 32)], a bit for each token, 1: allowed, and mask_rows int32 [B] into it,
     -1: no mask.  out may be logits.  Returns out."""
+    if out is None and stream is None:
+        usual = _usual("rules", logits, tokens, lengths, prompt_lengths, repetition, presence, frequency, bias_tokens, bias_values,
+                       masks, mask_rows)
+        if usual is not None:
+            return usual[0]
     if logits.dtype not in _DTYPES:
         raise ValueError("logits must be an fp16/bf16/fp32 device tensor")
     _rows(logits, "logits", logits.dtype, (-1, -1))

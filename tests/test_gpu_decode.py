@@ -481,3 +481,67 @@ def test_nothing_to_do():
     w = torch.zeros(64, dtype=BF16, device=DEV)
     assert ann.ann_qk_norm_rotate(torch.zeros(0, 8, 64, dtype=BF16, device=DEV), w, w, i(0), torch.zeros(4, 64, device=DEV), i(0), k, k).shape == (0, 4, 64)
     assert ann.ann_logit_rules(torch.zeros(0, 40, device=DEV), i(0, 5), i(0), i(0), f, f, f).shape == (0, 40)
+
+
+# ---- the binding's two halves -------------------------------------------------------------------------
+
+def test_both_halves_of_the_binding(monkeypatch):
+    """Native marshalling answers the usual calls with what the Python half gives, and leaves it the others."""
+    lengths = [300, 40, 511]
+    k, v, table = (dev(t) for t in D.paged(lengths, 16, 2, 64, BF16, 21, unused=0.0, spare=20))
+    free = torch.tensor([p for p in range(k.shape[0]) if p not in set(table.flatten().tolist())], dtype=torch.int32, device=DEV)
+    new_table, n = free[:12].view(3, 4).contiguous(), torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    qkv, w = dev(D.rows(3, 12, 64, dtype=BF16, seed=5)), torch.ones(64, dtype=BF16, device=DEV)
+    turn, slots = torch.randn(600, 32, generator=torch.Generator().manual_seed(4)).to(DEV), free[12:15] * 16
+    mass = torch.rand(3, 2, table.shape[1] * 16, device=DEV)
+    x = rule_inputs(F32, 3, 500, 100, 5, 2, 3)
+    x = [torch.nan_to_num(dev(x[0]), nan=3.0)] + [dev(t) for t in (x[1], x[2], x[3], *x[4], *x[5], x[6], x[7])]
+    q = qkv[:, :8]
+    rotate = lambda *a, **kw: (lambda: (ann.ann_qk_norm_rotate(qkv, w, w, n, turn, *a, k, v, **kw), k, v))  # noqa: E731
+    attend = lambda *a, **kw: (lambda: ann.ann_paged_attention(q, k, v, *a, **kw))  # noqa: E731
+    evict = lambda *a, **kw: (lambda: (*ann.ann_cache_evict(k, v, table, n, mass, *a, **kw), k, v))  # noqa: E731
+    rules = lambda *a, **kw: (lambda: ann.ann_logit_rules(*a, **kw))  # noqa: E731
+
+    def added():
+        m = mass.clone()
+        return (*ann.ann_paged_attention(q, k, v, table, n, mass=m), m)
+    answered_calls = [
+        rotate(slots), rotate(slots, eps=1e-3, interleaved=True), rotate(slots, eps=0), attend(table, n), attend(table, n, scale=0.3, window=7, max_length=400),
+        attend(table, n, scale=1), added, evict(new_table, 48), evict(new_table, 30, first=3, recent=9), rules(*x[:7]),
+        rules(*x[:7], bias_tokens=x[7], bias_values=x[8]), rules(*x[:7], masks=x[9], mask_rows=x[10]),
+        rules(*x[:7], bias_tokens=x[7], bias_values=x[8], masks=x[9], mask_rows=x[10])]
+    python_calls = [
+        rotate(slots, q=torch.empty(3, 8, 64, dtype=BF16, device=DEV)), attend(table, n, scale=np.float64(0.2)), evict(new_table, np.int64(7)),
+        rules(*x[:7], out=torch.empty_like(x[0]))]
+    refused = [
+        rotate(slots.long()), rotate(slots, eps=-1.0), attend(table, n.long()), attend(table, n, window=-2), attend(table, n, max_length=0), attend(table[:2], n),
+        evict(new_table, 0), evict(new_table, -3), evict(new_table, 65), evict(new_table, 8, first=9), rules(x[0].double(), *x[1:7]), rules(*x[:7], masks=x[9]),
+        rules(*x[:7], bias_tokens=x[7]), rules(x[0], x[1].long(), *x[2:7])]
+    answered = []
+    assert ann.binding._marshal is not None
+    for name in ("rotate", "attend", "evict", "rules"):
+        def spy(*args, native=getattr(ann.binding._marshal, name)):
+            out = native(*args)
+            answered.append(type(out) is tuple)
+            return out
+        monkeypatch.setattr(ann.binding._marshal, name, spy)
+    for group, kind in ((answered_calls, "native"), (python_calls, "python"), (refused, "refused")):
+        for number, call in enumerate(group):
+            got = []
+            for native in (True, False):
+                with monkeypatch.context() as m:
+                    if not native:
+                        m.setattr(ann.binding, "_marshal", None)
+                    del answered[:]
+                    try:
+                        out = call()
+                        got.append([t.cpu().clone() for t in (out if isinstance(out, tuple) else (out,))])
+                    except Exception as e:                # noqa: BLE001
+                        got.append((type(e), str(e)))
+                    assert any(answered) == (native and kind == "native"), (kind, number)
+            a, b = got
+            assert isinstance(a, tuple) == isinstance(b, tuple) == (kind == "refused"), (kind, number, a, b)
+            if kind == "refused":
+                assert a == b, (number, a, b)
+            else:
+                assert all(s.dtype == t.dtype and torch.equal(s, t) for s, t in zip(a, b)), (kind, number)
