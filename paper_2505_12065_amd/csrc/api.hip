@@ -573,7 +573,14 @@ int ann_logit_rules(const void *logits, int64_t row_stride, int32_t B, int32_t V
     a.repetition = repetition; a.presence = presence; a.frequency = frequency;
     a.bias_tokens = bias_tokens; a.bias_values = bias_values; a.K = K;
     a.masks = n_masks > 0 ? masks : nullptr; a.n_masks = n_masks; a.mask_rows = mask_rows; a.out = out; a.out_row = out_stride;
-    return check_launch("logit_rules_kernel", launch_logit_rules(dtype, a, B, static_cast<hipStream_t>(stream)));
+    int cus = 0;
+    {
+        std::lock_guard<std::mutex> lock(g_mu);
+        DeviceState *st = nullptr;
+        if (int rc = device_state(&st)) return rc;
+        cus = st->cus;
+    }
+    return check_launch("logit_rules_kernel", launch_logit_rules(dtype, cus, a, B, static_cast<hipStream_t>(stream)));
 }
 
 int ann_measure_mfma_rate(int32_t random_operands, int32_t iters, double *tflops) {

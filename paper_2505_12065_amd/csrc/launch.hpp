@@ -176,6 +176,6 @@ struct RulesArgs {
     void *out;
     int64_t out_row;
 };
-hipError_t launch_logit_rules(int dtype, const RulesArgs &args, int B, hipStream_t stream);
+hipError_t launch_logit_rules(int dtype, int cus, const RulesArgs &args, int B, hipStream_t stream);
 
 }  // namespace ann

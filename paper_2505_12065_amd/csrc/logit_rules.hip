@@ -1,4 +1,9 @@
 // Penalties for repeated tokens, biases and grammar masks on logits.
+//
+// The logits are read and written once.  What decides about a token is gathered beside them in LDS: a workgroup takes THREADS * 8 * R
+// tokens of the vocabulary of one request, asks for their logits (eight of a lane lie together), goes through the request's history and
+// biases while those are under way, and notes in a word for each token how often it was generated, whether it was seen, and its last bias.
+// Every workgroup of a request reads the whole history, so there are as few as keep the machine busy (rules_rounds).
 #include "launch.hpp"
 #include "paged.hpp"
 
@@ -6,64 +11,149 @@ namespace ann {
 
 namespace {
 
-constexpr int THREADS = 256, CHUNK = 4096;
-constexpr uint32_t SEEN = 1u << 31;                       // beside the count
+constexpr int THREADS = RULES_THREADS;
+
+// the same 16 bytes from any address that its element may have
+template <int ALIGN> struct Any;
+template <> struct Any<2> { typedef uint32_t type __attribute__((ext_vector_type(4), aligned(2))); };
+template <> struct Any<4> { typedef uint32_t type __attribute__((ext_vector_type(4), aligned(4))); };
 
 template <class T> struct Scalar;
 template <> struct Scalar<F16> { typedef _Float16 type; };
 template <> struct Scalar<BF16> { typedef __bf16 type; };
 template <> struct Scalar<F32> { typedef float type; };
 
-// A workgroup takes CHUNK tokens of the vocabulary of one request: it counts them in the request's history, finds the last
-// bias of each, and goes through its logits once.
 template <class T>
-__global__ __launch_bounds__(THREADS) void logit_rules_kernel(RulesArgs a) {
-    typedef typename Scalar<T>::type E;
-    __shared__ uint32_t count[CHUNK];
-    __shared__ int bias[CHUNK];
-    const int parts = (a.V + CHUNK - 1) / CHUNK, b = blockIdx.x / parts, v0 = blockIdx.x % parts * CHUNK, m = min(CHUNK, a.V - v0);
-    for (int i = threadIdx.x; i < m; i += THREADS) { count[i] = 0; bias[i] = -1; }
-    __syncthreads();
-    const int n = max(0, min(a.lengths[b], a.T)), prompt = max(0, a.prompt[b]);
-    const int32_t *tokens = a.tokens + (int64_t)b * a.T;
-    for (int t = threadIdx.x; t < n; t += THREADS) {
-        const uint32_t at = (uint32_t)(tokens[t] - v0);
-        if (tokens[t] < 0 || at >= (uint32_t)m) continue;
-        if (t < prompt) atomicOr(&count[at], SEEN);
-        else atomicAdd(&count[at], 1u);
+__device__ __forceinline__ Eight<T> load_any(const void *p) {
+    typedef typename Any<T::bytes>::type A;
+    Eight<T> e;
+    if constexpr (T::bytes == 2) {
+        e.raw = *static_cast<const A *>(p);
+    } else {
+        e.raw[0] = static_cast<const A *>(p)[0];
+        e.raw[1] = static_cast<const A *>(p)[1];
     }
-    for (int i = threadIdx.x; i < a.K; i += THREADS) {
-        const int token = a.bias_tokens[(int64_t)b * a.K + i];
-        if (token >= v0 && token - v0 < m) atomicMax(&bias[token - v0], i);
-    }
-    __syncthreads();
-    const float repetition = a.repetition[b], presence = a.presence[b], frequency = a.frequency[b];
-    const int mask_row = a.masks ? a.mask_rows[b] : -1;
-    const uint32_t *mask = (unsigned)mask_row < (unsigned)a.n_masks ? a.masks + (int64_t)mask_row * ((a.V + 31) / 32) : nullptr;
-    const E *in = static_cast<const E *>(a.logits) + b * a.row + v0;
-    E *out = static_cast<E *>(a.out) + b * a.out_row + v0;
-    for (int i = threadIdx.x; i < m; i += THREADS) {
-        float x = (float)in[i];
-        if (const uint32_t c = count[i]) {
-            x = x > 0.f ? x / repetition : x * repetition;
-            if (c & ~SEEN) x = x - frequency * (float)(c & ~SEEN) - presence;
-        }
-        if (bias[i] >= 0) x += a.bias_values[(int64_t)b * a.K + bias[i]];
-        if (mask && !((mask[(v0 + i) / 32] >> ((v0 + i) & 31)) & 1)) x = -INFINITY;
-        out[i] = (E)x;
+    return e;
+}
+template <class T>
+__device__ __forceinline__ void store_any(void *p, const Eight<T> &e) {
+    typedef typename Any<T::bytes>::type A;
+    if constexpr (T::bytes == 2) {
+        *static_cast<A *>(p) = e.raw;
+    } else {
+        static_cast<A *>(p)[0] = e.raw[0];
+        static_cast<A *>(p)[1] = e.raw[1];
     }
 }
 
-template <class T>
+// The word of a token: its count in the lowest CB bits, the mark of a token that was seen above them, and above that the number of its
+// last bias plus 1, in the same word (LONG: in a word of its own, for histories whose counts leave no room).
+template <class T, int R, bool LONG>
+__global__ __launch_bounds__(THREADS) void logit_rules_kernel(RulesArgs a, int parts) {
+    typedef typename Scalar<T>::type E;
+    constexpr int CHUNK = THREADS * 8 * R, CB = LONG ? 24 : RULES_COUNT_BITS;
+    constexpr uint32_t SEEN = 1u << CB, COUNT = SEEN - 1;
+    extern __shared__ uint32_t word[];
+    uint32_t *bias = LONG ? word + CHUNK : word;
+    const int b = blockIdx.x / parts, v0 = blockIdx.x % parts * CHUNK, m = min(CHUNK, a.V - v0), tid = threadIdx.x;
+    const E *in = static_cast<const E *>(a.logits) + b * a.row + v0;
+    E *out = static_cast<E *>(a.out) + b * a.out_row + v0;
+    Eight<T> x[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int i = (r * THREADS + tid) * 8;
+        if (i + 8 <= m) x[r] = load_any<T>(in + i);
+    }
+    for (int i = tid * 4; i < (LONG ? 2 * CHUNK : CHUNK); i += THREADS * 4) *reinterpret_cast<u4 *>(word + i) = zero_chunk();
+    __syncthreads();
+    const float repetition = a.repetition[b], presence = a.presence[b], frequency = a.frequency[b];
+    const float *bias_values = a.bias_values + (int64_t)b * a.K;
+    if (a.K > 0) {
+        for (int i = tid; i < a.K; i += THREADS) {
+            const int token = a.bias_tokens[(int64_t)b * a.K + i];
+            if (token >= v0 && token - v0 < m) atomicMax(&bias[token - v0], LONG ? (uint32_t)i + 1 : (uint32_t)(i + 1) << (CB + 1));
+        }
+        if (!LONG) __syncthreads();                       // (a maximum of what the counts have not been added to)
+    }
+    const int n = max(0, min(a.lengths[b], a.T)), prompt = max(0, a.prompt[b]);
+    const int32_t *tokens = a.tokens + (int64_t)b * a.T;
+    auto note = [&](int t, int token) {
+        const uint32_t at = (uint32_t)token - (uint32_t)v0;
+        if (at >= (uint32_t)m || token < 0) return;
+        if (t < prompt) atomicOr(&word[at], SEEN);
+        else atomicAdd(&word[at], 1u);
+    };
+    for (int t = 4 * tid; t + 4 <= n; t += 4 * THREADS) {
+        const u4 w = *reinterpret_cast<const Any<4>::type *>(tokens + t);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) note(t + i, (int)w[i]);
+    }
+    if ((n & ~3) + tid < n) note((n & ~3) + tid, tokens[(n & ~3) + tid]);
+    __syncthreads();
+    const int mask_row = a.masks ? a.mask_rows[b] : -1;
+    // (bit v % 32 of word v / 32 is bit v % 8 of byte v / 8)
+    const uint8_t *mask = (unsigned)mask_row < (unsigned)a.n_masks
+                              ? reinterpret_cast<const uint8_t *>(a.masks + (int64_t)mask_row * ((a.V + 31) / 32)) + v0 / 8 : nullptr;
+    auto ruled = [&](float y, uint32_t w, uint32_t k, bool allowed) {
+        if (w & (SEEN | COUNT)) {
+            y = y > 0.f ? y / repetition : y * repetition;
+            if (w & COUNT) y = y - frequency * (float)(w & COUNT) - presence;
+        }
+        if (k) y += bias_values[k - 1];
+        return allowed ? y : -INFINITY;
+    };
+    auto number = [&](int i) { return LONG ? bias[i] : word[i] >> (CB + 1); };
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int i = (r * THREADS + tid) * 8;
+        if (i + 8 <= m) {
+            const uint32_t bits = mask ? mask[i / 8] : 0xffu;
+            const u4 w0 = *reinterpret_cast<const u4 *>(word + i), w1 = *reinterpret_cast<const u4 *>(word + i + 4);
+            u4 k0 = zero_chunk(), k1 = zero_chunk();
+            if (LONG) {
+                k0 = *reinterpret_cast<const u4 *>(bias + i);
+                k1 = *reinterpret_cast<const u4 *>(bias + i + 4);
+            }
+            const u4 any = w0 | w1 | k0 | k1;
+            if ((any[0] | any[1] | any[2] | any[3]) || bits != 0xffu) {
+                float y[8];
+                x[r].get(y);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t w = j < 4 ? w0[j & 3] : w1[j & 3], k = LONG ? (j < 4 ? k0[j & 3] : k1[j & 3]) : w >> (CB + 1);
+                    y[j] = ruled(y[j], w, k, (bits >> j) & 1);
+                }
+                x[r].set(y);
+            }
+            store_any<T>(out + i, x[r]);
+        } else {
+            for (int j = i; j < m; ++j) out[j] = (E)ruled((float)in[j], word[j], number(j), !mask || ((mask[j / 8] >> (j & 7)) & 1));
+        }
+    }
+}
+
+template <class T, int R, bool LONG>
 hipError_t launch(const RulesArgs &a, int B, hipStream_t stream) {
-    hipLaunchKernelGGL((logit_rules_kernel<T>), dim3((a.V + CHUNK - 1) / CHUNK * B), dim3(THREADS), 0, stream, a);
+    static size_t granted = 0;
+    constexpr int CHUNK = THREADS * 8 * R;
+    const size_t bytes = (size_t)CHUNK * (LONG ? 8 : 4);
+    if (hipError_t e = allow_big_lds(reinterpret_cast<const void *>(logit_rules_kernel<T, R, LONG>), bytes, &granted)) return e;
+    const int parts = (a.V + CHUNK - 1) / CHUNK;
+    hipLaunchKernelGGL((logit_rules_kernel<T, R, LONG>), dim3(parts * B), dim3(THREADS), bytes, stream, a, parts);
     return hipGetLastError();
+}
+template <class T>
+hipError_t launch(const RulesArgs &a, int cus, int B, hipStream_t stream) {
+    if (a.T >= 1 << RULES_COUNT_BITS) return launch<T, 4, true>(a, B, stream);
+    const int rounds = rules_rounds(cus, B, a.V);
+    return rounds == 1 ? launch<T, 1, false>(a, B, stream) : rounds == 2 ? launch<T, 2, false>(a, B, stream)
+           : rounds == 4 ? launch<T, 4, false>(a, B, stream) : launch<T, 8, false>(a, B, stream);
 }
 
 }  // namespace
 
-hipError_t launch_logit_rules(int dtype, const RulesArgs &a, int B, hipStream_t stream) {
-    return dtype == ANN_F16 ? launch<F16>(a, B, stream) : dtype == ANN_BF16 ? launch<BF16>(a, B, stream) : launch<F32>(a, B, stream);
+hipError_t launch_logit_rules(int dtype, int cus, const RulesArgs &a, int B, hipStream_t stream) {
+    return dtype == ANN_F16 ? launch<F16>(a, cus, B, stream) : dtype == ANN_BF16 ? launch<BF16>(a, cus, B, stream) : launch<F32>(a, cus, B, stream);
 }
 
 }  // namespace ann

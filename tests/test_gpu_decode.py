@@ -378,6 +378,14 @@ def test_rules(dtype, B, V, T, K, M):
     assert (wide[:, :3] == 3).all() and (wide[:, V + 3:] == 3).all()
 
 
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("B,V,T,K,M", [(300, 16_391, 40, 3, 5), (130, 16_500, 300, 0, 2), (70, 16_380, 9, 20, 0), (513, 2049, 5, 1, 3),
+                                       (2, 9000, 262_143, 4096, 1), (2, 9000, 262_144, 4096, 1), (1, 40, 300_000, 9, 1)])
+def test_rules_many_rows_and_long_histories(dtype, B, V, T, K, M):
+    """Every number of logits that a lane takes, and counts that no longer share a word with a bias."""
+    test_rules(dtype, B, V, T, K, M)
+
+
 # ---- streams and graphs ----------------------------------------------------------------------------
 
 def all_four(stream=None):
