@@ -55,14 +55,23 @@ __global__ __launch_bounds__(THREADS) void logit_rules_kernel(RulesArgs a, int p
     constexpr uint32_t SEEN = 1u << CB, COUNT = SEEN - 1;
     extern __shared__ uint32_t word[];
     uint32_t *bias = LONG ? word + CHUNK : word;
-    const int b = blockIdx.x / parts, v0 = blockIdx.x % parts * CHUNK, m = min(CHUNK, a.V - v0), tid = threadIdx.x;
+    const int id = xcd_block(), b = id / parts, v0 = id % parts * CHUNK, m = min(CHUNK, a.V - v0), tid = threadIdx.x;
     const E *in = static_cast<const E *>(a.logits) + b * a.row + v0;
     E *out = static_cast<E *>(a.out) + b * a.out_row + v0;
+    const int mask_row = a.masks ? a.mask_rows[b] : -1;
+    // (bit v % 32 of word v / 32 is bit v % 8 of byte v / 8)
+    const uint8_t *mask = (unsigned)mask_row < (unsigned)a.n_masks
+                              ? reinterpret_cast<const uint8_t *>(a.masks + (int64_t)mask_row * ((a.V + 31) / 32)) + v0 / 8 : nullptr;
     Eight<T> x[R];
+    uint32_t bits[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int i = (r * THREADS + tid) * 8;
-        if (i + 8 <= m) x[r] = load_any<T>(in + i);
+        bits[r] = 0xffu;
+        if (i + 8 <= m) {
+            x[r] = load_any<T>(in + i);
+            if (mask) bits[r] = mask[i / 8];
+        }
     }
     for (int i = tid * 4; i < (LONG ? 2 * CHUNK : CHUNK); i += THREADS * 4) *reinterpret_cast<u4 *>(word + i) = zero_chunk();
     __syncthreads();
@@ -83,17 +92,22 @@ __global__ __launch_bounds__(THREADS) void logit_rules_kernel(RulesArgs a, int p
         if (t < prompt) atomicOr(&word[at], SEEN);
         else atomicAdd(&word[at], 1u);
     };
-    for (int t = 4 * tid; t + 4 <= n; t += 4 * THREADS) {
-        const u4 w = *reinterpret_cast<const Any<4>::type *>(tokens + t);
+    constexpr int AHEAD = 4;                              // loads of the history under way at a time
+    for (int t0 = 4 * tid; t0 < n; t0 += AHEAD * 4 * THREADS) {
+        u4 w[AHEAD];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) note(t + i, (int)w[i]);
+        for (int u = 0; u < AHEAD; ++u) {
+            const int t = t0 + u * 4 * THREADS;
+            w[u] = u4{~0u, ~0u, ~0u, ~0u};                // (no token)
+            if (t + 4 <= n) w[u] = *reinterpret_cast<const Any<4>::type *>(tokens + t);
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) note(t0 + u * 4 * THREADS + i, (int)w[u][i]);
     }
     if ((n & ~3) + tid < n) note((n & ~3) + tid, tokens[(n & ~3) + tid]);
     __syncthreads();
-    const int mask_row = a.masks ? a.mask_rows[b] : -1;
-    // (bit v % 32 of word v / 32 is bit v % 8 of byte v / 8)
-    const uint8_t *mask = (unsigned)mask_row < (unsigned)a.n_masks
-                              ? reinterpret_cast<const uint8_t *>(a.masks + (int64_t)mask_row * ((a.V + 31) / 32)) + v0 / 8 : nullptr;
     auto ruled = [&](float y, uint32_t w, uint32_t k, bool allowed) {
         if (w & (SEEN | COUNT)) {
             y = y > 0.f ? y / repetition : y * repetition;
@@ -107,7 +121,6 @@ __global__ __launch_bounds__(THREADS) void logit_rules_kernel(RulesArgs a, int p
     for (int r = 0; r < R; ++r) {
         const int i = (r * THREADS + tid) * 8;
         if (i + 8 <= m) {
-            const uint32_t bits = mask ? mask[i / 8] : 0xffu;
             const u4 w0 = *reinterpret_cast<const u4 *>(word + i), w1 = *reinterpret_cast<const u4 *>(word + i + 4);
             u4 k0 = zero_chunk(), k1 = zero_chunk();
             if (LONG) {
@@ -115,13 +128,13 @@ __global__ __launch_bounds__(THREADS) void logit_rules_kernel(RulesArgs a, int p
                 k1 = *reinterpret_cast<const u4 *>(bias + i + 4);
             }
             const u4 any = w0 | w1 | k0 | k1;
-            if ((any[0] | any[1] | any[2] | any[3]) || bits != 0xffu) {
+            if ((any[0] | any[1] | any[2] | any[3]) || bits[r] != 0xffu) {
                 float y[8];
                 x[r].get(y);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const uint32_t w = j < 4 ? w0[j & 3] : w1[j & 3], k = LONG ? (j < 4 ? k0[j & 3] : k1[j & 3]) : w >> (CB + 1);
-                    y[j] = ruled(y[j], w, k, (bits >> j) & 1);
+                    y[j] = ruled(y[j], w, k, (bits[r] >> j) & 1);
                 }
                 x[r].set(y);
             }
