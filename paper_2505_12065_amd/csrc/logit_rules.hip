@@ -3,15 +3,15 @@
 // The logits are read and written once.  What decides about a token is gathered beside them in LDS: a workgroup takes THREADS * 8 * R
 // tokens of the vocabulary of one request, asks for their logits (eight of a lane lie together), goes through the request's history and
 // biases while those are under way, and notes in a word for each token how often it was generated, whether it was seen, and its last bias.
-// Every workgroup of a request reads the whole history, so there are as few as keep the machine busy (rules_rounds).
+// Every workgroup of a request reads the whole history, so there are as few as keep the machine busy (rules_chunk).
+#include <type_traits>
+
 #include "launch.hpp"
 #include "paged.hpp"
 
 namespace ann {
 
 namespace {
-
-constexpr int THREADS = RULES_THREADS;
 
 // the same 16 bytes from any address that its element may have
 template <int ALIGN> struct Any;
@@ -46,9 +46,27 @@ __device__ __forceinline__ void store_any(void *p, const Eight<T> &e) {
     }
 }
 
+// -inf in the place of the elements whose bit is 0
+template <class T>
+__device__ __forceinline__ Eight<T> masked(Eight<T> x, uint32_t bits) {
+    if constexpr (T::bytes == 2) {
+        const uint32_t none = std::is_same_v<T, F16> ? 0xfc00fc00u : 0xff80ff80u;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t low = (uint32_t)((int32_t)(bits << (31 - 2 * j)) >> 31), high = (uint32_t)((int32_t)(bits << (30 - 2 * j)) >> 31);
+            const uint32_t keep = (low & 0xffffu) | (high & 0xffff0000u);
+            x.raw[j] = (x.raw[j] & keep) | (none & ~keep);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x.raw[j / 4][j % 4] = (bits >> j) & 1 ? x.raw[j / 4][j % 4] : 0xff800000u;
+    }
+    return x;
+}
+
 // The word of a token: its count in the lowest CB bits, the mark of a token that was seen above them, and above that the number of its
 // last bias plus 1, in the same word (LONG: in a word of its own, for histories whose counts leave no room).
-template <class T, int R, bool LONG>
+template <class T, int THREADS, int R, bool LONG>
 __global__ __launch_bounds__(THREADS) void logit_rules_kernel(RulesArgs a, int parts) {
     typedef typename Scalar<T>::type E;
     constexpr int CHUNK = THREADS * 8 * R, CB = LONG ? 24 : RULES_COUNT_BITS;
@@ -128,16 +146,17 @@ __global__ __launch_bounds__(THREADS) void logit_rules_kernel(RulesArgs a, int p
                 k1 = *reinterpret_cast<const u4 *>(bias + i + 4);
             }
             const u4 any = w0 | w1 | k0 | k1;
-            if ((any[0] | any[1] | any[2] | any[3]) || bits[r] != 0xffu) {
+            if (any[0] | any[1] | any[2] | any[3]) {
                 float y[8];
                 x[r].get(y);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const uint32_t w = j < 4 ? w0[j & 3] : w1[j & 3], k = LONG ? (j < 4 ? k0[j & 3] : k1[j & 3]) : w >> (CB + 1);
-                    y[j] = ruled(y[j], w, k, (bits[r] >> j) & 1);
+                    y[j] = ruled(y[j], w, k, true);
                 }
                 x[r].set(y);
             }
+            x[r] = masked<T>(x[r], bits[r]);
             store_any<T>(out + i, x[r]);
         } else {
             for (int j = i; j < m; ++j) out[j] = (E)ruled((float)in[j], word[j], number(j), !mask || ((mask[j / 8] >> (j & 7)) & 1));
@@ -145,22 +164,22 @@ __global__ __launch_bounds__(THREADS) void logit_rules_kernel(RulesArgs a, int p
     }
 }
 
-template <class T, int R, bool LONG>
+template <class T, int THREADS, int R, bool LONG>
 hipError_t launch(const RulesArgs &a, int B, hipStream_t stream) {
     static size_t granted = 0;
     constexpr int CHUNK = THREADS * 8 * R;
     const size_t bytes = (size_t)CHUNK * (LONG ? 8 : 4);
-    if (hipError_t e = allow_big_lds(reinterpret_cast<const void *>(logit_rules_kernel<T, R, LONG>), bytes, &granted)) return e;
+    if (hipError_t e = allow_big_lds(reinterpret_cast<const void *>(logit_rules_kernel<T, THREADS, R, LONG>), bytes, &granted)) return e;
     const int parts = (a.V + CHUNK - 1) / CHUNK;
-    hipLaunchKernelGGL((logit_rules_kernel<T, R, LONG>), dim3(parts * B), dim3(THREADS), bytes, stream, a, parts);
+    hipLaunchKernelGGL((logit_rules_kernel<T, THREADS, R, LONG>), dim3(parts * B), dim3(THREADS), bytes, stream, a, parts);
     return hipGetLastError();
 }
 template <class T>
 hipError_t launch(const RulesArgs &a, int cus, int B, hipStream_t stream) {
-    if (a.T >= 1 << RULES_COUNT_BITS) return launch<T, 4, true>(a, B, stream);
-    const int rounds = rules_rounds(cus, B, a.V);
-    return rounds == 1 ? launch<T, 1, false>(a, B, stream) : rounds == 2 ? launch<T, 2, false>(a, B, stream)
-           : rounds == 4 ? launch<T, 4, false>(a, B, stream) : launch<T, 8, false>(a, B, stream);
+    if (a.T >= 1 << RULES_COUNT_BITS) return launch<T, 1024, 1, true>(a, B, stream);
+    const int chunk = rules_chunk(cus, B, a.V);
+    return chunk == 2048 ? launch<T, 256, 1, false>(a, B, stream) : chunk == 4096 ? launch<T, 512, 1, false>(a, B, stream)
+           : chunk == 8192 ? launch<T, 1024, 1, false>(a, B, stream) : launch<T, 1024, 2, false>(a, B, stream);
 }
 
 }  // namespace

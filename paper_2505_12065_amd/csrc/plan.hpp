@@ -1042,14 +1042,13 @@ inline size_t attend_workspace(int cus, int B, int q_heads, int heads, int d, in
 }
 
 // ---- rules on logits ------------------------------------------------------------------------------------
-constexpr int RULES_THREADS = 256;
 constexpr int RULES_COUNT_BITS = 18;                      // of a token's word: the rest holds a mark and the number of one of ANN_BIAS_MAX biases
 static_assert(ANN_BIAS_MAX < 1 << (32 - RULES_COUNT_BITS - 1), "biases are numbered in what a count leaves");
-// Rounds of 8 logits a lane that a workgroup takes: the most that leave two workgroups for every compute unit.
-inline int rules_rounds(int cus, int B, int V) {
-    int rounds = 8;
-    while (rounds > 1 && (int64_t)B * ((V + RULES_THREADS * 8 * rounds - 1) / (RULES_THREADS * 8 * rounds)) < 2 * cus) rounds /= 2;
-    return rounds;
+// Logits of a workgroup: the most that leave two workgroups for every compute unit.
+inline int rules_chunk(int cus, int B, int V) {
+    int chunk = 16384;
+    while (chunk > 2048 && (int64_t)B * ((V + chunk - 1) / chunk) < 2 * cus) chunk /= 2;
+    return chunk;
 }
 
 }  // namespace ann
