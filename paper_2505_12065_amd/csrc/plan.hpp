@@ -1051,4 +1051,12 @@ inline int rules_chunk(int cus, int B, int V) {
     return chunk;
 }
 
+// ---- norms and rotation -----------------------------------------------------------------------------------
+// Rows (heads of a token) that a group of lanes takes, `groups` of them a workgroup: one where there are few tokens; else all
+// of a token's, or, beyond 4, the even share of as few workgroups as do with 4.
+inline int rotate_rows(int T, int heads, int groups) {
+    const int rows = (heads + groups - 1) / groups, parts = (rows + 3) / 4;
+    return T < 512 ? 1 : (rows + parts - 1) / parts;
+}
+
 }  // namespace ann

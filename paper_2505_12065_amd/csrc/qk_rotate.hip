@@ -8,79 +8,107 @@ namespace {
 
 constexpr int THREADS = 256;
 
-// LPR lanes for a row (a head of a token), eight elements a lane; a workgroup's rows are heads of one token.
-template <class T, int LPR, bool INTERLEAVED>
+// LPR lanes for a row (a head of a token), eight elements a lane.  A group of LPR lanes takes NR rows of one token, LANES / LPR heads apart:
+// all are asked for at once, and what belongs to the token and the lane (cosines and sines, four times the bytes of a row at 16 bits) or to the lane
+// alone (weights) is read once for all of them.
+template <class T, int LPR, int NR, bool INTERLEAVED>
 __global__ __launch_bounds__(THREADS) void qk_rotate_kernel(RotateArgs a) {
+    constexpr int GROUPS = THREADS / LPR;
     const int d = a.cache.d, group = threadIdx.x / LPR, lane = threadIdx.x % LPR, e = 8 * lane;
-    const int heads = a.q_heads + 2 * a.cache.heads, h = blockIdx.y * (THREADS / LPR) + group;
+    const int heads = a.q_heads + 2 * a.cache.heads, h0 = blockIdx.y * (GROUPS * NR) + group;
     const int64_t t = blockIdx.x;
-    if (h >= heads) return;                               // (whole rows: lanes that exchange values stay together)
     const int p = a.positions[t], slot = a.slots[t];
     const bool pad = (unsigned)p >= (unsigned)a.max_positions, mine = e < d;
     const int page = slot >> a.cache.slots_log, off = slot & ((1 << a.cache.slots_log) - 1);
     const bool stored = !pad && slot >= 0 && page < a.cache.pages;
-    const bool is_q = h < a.q_heads, is_k = !is_q && h < a.q_heads + a.cache.heads;
-    Eight<T> x;
-    x.zero();
-    if (mine && !pad) x.load(static_cast<const char *>(a.qkv) + t * a.token + h * a.head + e * T::bytes);
-    if (is_q || is_k) {
-        float y[8], w[8] = {}, sum = 0.f;
-        x.get(y);
+    Eight<T> x[NR], wq, wk;
+    const char *in = static_cast<const char *>(a.qkv) + t * a.token + e * T::bytes;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum = fmaf(y[i], y[i], sum);
-#pragma unroll
-        for (int s = 1; s < LPR; s *= 2) sum += __shfl_xor(sum, s);
-        const float r = 1.f / sqrtf(sum / (float)d + a.eps);
-        if (mine) {
-            Eight<T> wx;
-            wx.load(static_cast<const char *>(is_q ? a.q_weight : a.k_weight) + e * T::bytes);
-            wx.get(w);
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = y[i] * r * w[i];
-        const bool turns = e < a.rot && !pad;
-        const float *table = a.cos_sin + (int64_t)(pad ? 0 : p) * a.rot;
-        if (INTERLEAVED) {
-            if (turns) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float c = table[e / 2 + i], s = table[a.rot / 2 + e / 2 + i], u = y[2 * i], v = y[2 * i + 1];
-                    y[2 * i] = u * c - v * s;
-                    y[2 * i + 1] = v * c + u * s;
-                }
-            }
-        } else {
-            const bool low = e < a.rot / 2;
-            const int other = turns ? lane + (low ? a.rot / 16 : -(a.rot / 16)) : lane, i0 = low ? e : e - a.rot / 2;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float z = __shfl(y[i], other, LPR);
-                if (turns) {
-                    const float c = table[i0 + i], s = table[a.rot / 2 + i0 + i];
-                    y[i] = low ? y[i] * c - z * s : y[i] * c + z * s;
-                }
-            }
-        }
-        x.set(y);
+    for (int r = 0; r < NR; ++r) {
+        x[r].zero();
+        const int h = h0 + r * GROUPS;
+        if (mine && !pad && h < heads) x[r].load(in + h * a.head);
     }
-    if (!mine) return;
-    if (is_q) {
-        if (pad) x.zero();
-        x.store(static_cast<char *>(a.q) + ((t * a.q_heads + h) * d + e) * T::bytes);
-    } else if (stored) {
-        char *to = is_k ? a.cache.k + (int64_t)page * a.cache.k_page + (h - a.q_heads) * a.cache.k_head + off * a.cache.k_slot
-                        : a.cache.v + (int64_t)page * a.cache.v_page + (h - a.q_heads - a.cache.heads) * a.cache.v_head + off * a.cache.v_slot;
-        x.store(to + e * T::bytes);
+    wq.zero();
+    wk.zero();
+    if (mine) {
+        wq.load(static_cast<const char *>(a.q_weight) + e * T::bytes);
+        wk.load(static_cast<const char *>(a.k_weight) + e * T::bytes);
+    }
+    // cosine and sine of the lane's pairs; for pairs of halves its own eight, and the sine's sign is that of its half
+    constexpr int PAIRS = INTERLEAVED ? 4 : 8;
+    const bool turns = e < a.rot && !pad, low = e < a.rot / 2;
+    float c[PAIRS], s[PAIRS];
+    if (turns) {
+        const float *table = a.cos_sin + (int64_t)p * a.rot + (INTERLEAVED ? e / 2 : low ? e : e - a.rot / 2);
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) {
+            c[i] = table[i];
+            s[i] = table[a.rot / 2 + i];
+            if (!INTERLEAVED && low) s[i] = -s[i];
+        }
+    }
+    const int other = turns ? lane + (low ? a.rot / 16 : -(a.rot / 16)) : lane;
+    const float per_d = 1.f / (float)d;
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+        const int h = h0 + r * GROUPS;
+        if (h >= heads) break;                            // (whole groups: lanes that exchange values stay together)
+        const bool is_q = h < a.q_heads, is_v = h >= a.q_heads + a.cache.heads;
+        if (!is_v) {
+            float y[8], w[8], sum = 0.f;
+            x[r].get(y);
+            (is_q ? wq : wk).get(w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum = fmaf(y[i], y[i], sum);
+#pragma unroll
+            for (int k = 1; k < LPR; k *= 2) sum += __shfl_xor(sum, k);
+            const float f = rsqrtf(fmaf(sum, per_d, a.eps));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = y[i] * f * w[i];
+            if (INTERLEAVED) {
+                if (turns) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float u = y[2 * i], v = y[2 * i + 1];
+                        y[2 * i] = u * c[i % PAIRS] - v * s[i % PAIRS];
+                        y[2 * i + 1] = v * c[i % PAIRS] + u * s[i % PAIRS];
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float z = __shfl(y[i], other, LPR);
+                    if (turns) y[i] = y[i] * c[i % PAIRS] + z * s[i % PAIRS];
+                }
+            }
+            x[r].set(y);
+        }
+        if (!mine) continue;
+        if (is_q) {
+            if (pad) x[r].zero();
+            x[r].store(static_cast<char *>(a.q) + ((t * a.q_heads + h) * d + e) * T::bytes);
+        } else if (stored) {
+            char *to = is_v ? a.cache.v + (int64_t)page * a.cache.v_page + (h - a.q_heads - a.cache.heads) * a.cache.v_head + off * a.cache.v_slot
+                            : a.cache.k + (int64_t)page * a.cache.k_page + (h - a.q_heads) * a.cache.k_head + off * a.cache.k_slot;
+            x[r].store(to + e * T::bytes);
+        }
     }
 }
 
+template <class T, int LPR, int NR>
+hipError_t launch(const RotateArgs &a, int T_, hipStream_t stream) {
+    const int heads = a.q_heads + 2 * a.cache.heads, per = THREADS / LPR * NR;
+    const dim3 grid(T_, (heads + per - 1) / per);
+    if (a.interleaved) hipLaunchKernelGGL((qk_rotate_kernel<T, LPR, NR, true>), grid, dim3(THREADS), 0, stream, a);
+    else hipLaunchKernelGGL((qk_rotate_kernel<T, LPR, NR, false>), grid, dim3(THREADS), 0, stream, a);
+    return hipGetLastError();
+}
 template <class T, int LPR>
 hipError_t launch(const RotateArgs &a, int T_, hipStream_t stream) {
-    const int heads = a.q_heads + 2 * a.cache.heads, per = THREADS / LPR;
-    const dim3 grid(T_, (heads + per - 1) / per);
-    if (a.interleaved) hipLaunchKernelGGL((qk_rotate_kernel<T, LPR, true>), grid, dim3(THREADS), 0, stream, a);
-    else hipLaunchKernelGGL((qk_rotate_kernel<T, LPR, false>), grid, dim3(THREADS), 0, stream, a);
-    return hipGetLastError();
+    const int rows = rotate_rows(T_, a.q_heads + 2 * a.cache.heads, THREADS / LPR);
+    return rows == 1 ? launch<T, LPR, 1>(a, T_, stream) : rows == 2 ? launch<T, LPR, 2>(a, T_, stream)
+           : rows == 3 ? launch<T, LPR, 3>(a, T_, stream) : launch<T, LPR, 4>(a, T_, stream);
 }
 template <class T>
 hipError_t launch(const RotateArgs &a, int T_, hipStream_t stream) {

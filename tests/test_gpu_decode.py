@@ -246,6 +246,14 @@ def test_rotate(dtype, interleaved, T, Hq, heads, d, rot, page, layout):
     assert torch.equal(dv.cpu().double(), ev)
 
 
+@pytest.mark.parametrize("dtype,interleaved", [(F16, False), (BF16, True), (F32, False)])
+@pytest.mark.parametrize("Hq,heads,d,rot,layout", [(20, 1, 64, 64, "heads"), (40, 4, 56, 32, "slots"), (60, 3, 128, 16, "heads"), (12, 4, 256, 32, "heads"),
+                                                   (70, 2, 136, 48, "slots"), (36, 6, 80, 80, "heads"), (130, 1, 16, 16, "heads")])
+def test_rotate_many_tokens(dtype, interleaved, Hq, heads, d, rot, layout):
+    """Groups of lanes that take two, three or four heads of a token, the last of which may have none left."""
+    test_rotate(dtype, interleaved, 520, Hq, heads, d, rot, 16, layout)
+
+
 def test_rotate_part_of_a_larger_tensor_and_non_finite_values():
     T, Hq, heads, d = 6, 4, 2, 64
     big = D.rows(T, 2, Hq + 2 * heads, 96, dtype=BF16, seed=1)
