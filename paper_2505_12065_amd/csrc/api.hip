@@ -502,6 +502,7 @@ int ann_paged_attention(const void *q, int64_t q_row, int64_t q_head, int32_t B,
         a.q = static_cast<const char *>(q) + b0 * a.q_row;
         a.table = page_table + (int64_t)b0 * width;
         a.lengths = lengths + b0;
+        a.requests = b;
         a.out = static_cast<char *>(out) + (int64_t)b0 * q_heads * cache->d * e;
         a.lse = lse ? lse + (int64_t)b0 * q_heads : nullptr;
         a.mass = mass ? mass + (int64_t)b0 * cache->heads * mass_slots : nullptr;
@@ -512,7 +513,7 @@ int ann_paged_attention(const void *q, int64_t q_row, int64_t q_head, int32_t B,
             a.stats = scores + (mass ? (size_t)b * q_heads * pl.pad : 0);
         }
         const hipError_t err = (cache->dtype == ANN_F16 ? launch_paged_attention_f16 : cache->dtype == ANN_BF16 ? launch_paged_attention_bf16
-                                : launch_paged_attention_f32)(a, b, stream);
+                                : launch_paged_attention_f32)(a, pl.once, stream);
         if (int rc = check_launch("paged_attention_kernel", err)) return rc;
     }
     return ANN_OK;

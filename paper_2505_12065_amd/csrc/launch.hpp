@@ -134,14 +134,15 @@ struct AttentionArgs {
     void *out;
     float *lse, *mass;
     int64_t mass_slots;
+    int requests;
     int groups, splits, chunk, pad;   // attend_plan
     float *partial, *stats;   // [B, q_heads, splits, d], [B, q_heads, splits, 2] (largest exponent, sum), where the parts are joined
     float *scores;            // [B, q_heads, pad] if mass is given: exponents of 2, from the first tile of the window on
 };
-// (scale: times log2 e)
-hipError_t launch_paged_attention_f16(const AttentionArgs &args, int B, hipStream_t stream);
-hipError_t launch_paged_attention_bf16(const AttentionArgs &args, int B, hipStream_t stream);
-hipError_t launch_paged_attention_f32(const AttentionArgs &args, int B, hipStream_t stream);
+// (scale: times log2 e; once: read past the last cache)
+hipError_t launch_paged_attention_f16(const AttentionArgs &args, bool once, hipStream_t stream);
+hipError_t launch_paged_attention_bf16(const AttentionArgs &args, bool once, hipStream_t stream);
+hipError_t launch_paged_attention_f32(const AttentionArgs &args, bool once, hipStream_t stream);
 
 struct EvictArgs {
     Paged cache;

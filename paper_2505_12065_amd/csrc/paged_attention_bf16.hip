@@ -3,6 +3,6 @@
 
 namespace ann {
 
-hipError_t launch_paged_attention_bf16(const AttentionArgs &a, int B, hipStream_t stream) { return launch_attention<BF16>(a, B, stream); }
+hipError_t launch_paged_attention_bf16(const AttentionArgs &a, bool once, hipStream_t stream) { return launch_attention<BF16>(a, once, stream); }
 
 }  // namespace ann

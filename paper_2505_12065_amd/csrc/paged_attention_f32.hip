@@ -3,6 +3,6 @@
 
 namespace ann {
 
-hipError_t launch_paged_attention_f32(const AttentionArgs &a, int B, hipStream_t stream) { return launch_attention<F32>(a, B, stream); }
+hipError_t launch_paged_attention_f32(const AttentionArgs &a, bool once, hipStream_t stream) { return launch_attention<F32>(a, once, stream); }
 
 }  // namespace ann

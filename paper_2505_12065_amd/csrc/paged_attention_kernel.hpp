@@ -43,6 +43,12 @@ __device__ __forceinline__ float column_sum(float x) {
     return __uint_as_float(a) + __uint_as_float(b);
 }
 
+template <bool ONCE, class V>
+__device__ __forceinline__ V stream_load(const V *p) {
+    if constexpr (ONCE) return __builtin_nontemporal_load(p);
+    else return *p;
+}
+
 template <int CW> struct Words;
 template <> struct Words<2> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
 template <> struct Words<4> { typedef u4 type; };
@@ -85,8 +91,9 @@ __device__ __forceinline__ f4 scores_step(u4 k, u4 q, f4 c) {
     }
 }
 
-// FINE: pages of less than 16 slots, looked up for every row and not for a tile.  FULL: d is 16 VE.
-template <class T, int VE, bool FINE, bool FULL>
+// FINE: pages of less than 16 slots, looked up for every row and not for a tile.  FULL: d is 16 VE.  ONCE: keys and values are more than the
+// last cache holds, and are read past it.
+template <class T, int VE, bool FINE, bool FULL, bool ONCE>
 __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 ? 1 : 2) void paged_attention_kernel(AttentionArgs a) {
     typedef AttendShape<T, VE> Sh;
     typedef typename Words<Sh::CW>::type VChunk;
@@ -94,12 +101,12 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 ? 1 : 2) void paged_attent
     extern __shared__ float lds[];
     const int lane = threadIdx.x & (WAVE - 1), g = lane >> 4, m = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-    int id = xcd_block();
-    const int hg = id % a.groups;
-    id /= a.groups;
-    const int part = id % a.splits;
-    id /= a.splits;
-    const int h = id % a.cache.heads, b = id / a.cache.heads;
+    // First parts of all contexts first, each on any of the 8 XCDs, so that contexts of all lengths are spread over them; the workgroups
+    // that read the same slots follow each other on one.
+    const int hg = (blockIdx.x >> 3) % a.groups, item = (blockIdx.x >> 3) / a.groups * 8 + (blockIdx.x & 7);
+    const int units = a.requests * a.cache.heads, part = item / units, unit = item % units;
+    if (part >= a.splits) return;
+    const int h = unit % a.cache.heads, b = unit / a.cache.heads;
     const int G = a.q_heads / a.cache.heads, rows = min(16, G - 16 * hg);     // query heads of this workgroup
     const int n = min(a.lengths[b], a.max_length), lo = a.window > 0 ? max(0, n - a.window) : 0, start = lo & ~15;
     const int first = start + part * a.chunk, end = min(n, first + a.chunk);
@@ -138,7 +145,7 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 ? 1 : 2) void paged_attent
 #pragma unroll
             for (int s = 0; s < NS; ++s) {
                 const int at = (4 * s + g) * 16;
-                if (FULL || at < a.cache.d * T::bytes) kr[t][s] = load_chunk(row + at);
+                if (FULL || at < a.cache.d * T::bytes) kr[t][s] = stream_load<ONCE>(reinterpret_cast<const u4 *>(row + at));
                 else kr[t][s] = zero_chunk();
             }
         }
@@ -168,7 +175,7 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 ? 1 : 2) void paged_attent
 #pragma unroll
                 for (int u = 0; u < NU; ++u) {
                     const int at = (u * 16 + m) * CE;
-                    if (FULL || at < a.cache.d) vr[t][i][u] = *reinterpret_cast<const VChunk *>(row + at * T::bytes);
+                    if (FULL || at < a.cache.d) vr[t][i][u] = stream_load<ONCE>(reinterpret_cast<const VChunk *>(row + at * T::bytes));
                     else vr[t][i][u] = VChunk(0);
                 }
             }
@@ -324,10 +331,10 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 ? 1 : 2) void paged_attent
     }
 }
 
-// What the parts of a context left, joined: the first B q_heads workgroups take a query head each; those behind them (scores given) take
+// What the parts of a context left, joined: the first q_heads workgroups of every request take a query head each; those behind them (scores given) take
 // 4 THREADS slots of a cache head each and add the weights of its query heads, in their order, to mass.
 template <class T>
-__global__ __launch_bounds__(ATTEND_THREADS) void paged_attention_join_kernel(AttentionArgs a, int B) {
+__global__ __launch_bounds__(ATTEND_THREADS) void paged_attention_join_kernel(AttentionArgs a) {
     __shared__ float lds[ATTEND_THREADS * 8];
     const int G = a.q_heads / a.cache.heads, tid = threadIdx.x;
     // of head row r, by one wave: largest exponent and total over its parts
@@ -350,7 +357,7 @@ __global__ __launch_bounds__(ATTEND_THREADS) void paged_attention_join_kernel(At
         return n > 0 ? (n - start + a.chunk - 1) / a.chunk : 0;
     };
     int n, lo, start;
-    if ((int64_t)blockIdx.x < (int64_t)B * a.q_heads) {
+    if ((int64_t)blockIdx.x < (int64_t)a.requests * a.q_heads) {
         const int64_t r = blockIdx.x;
         const int parts = parts_of((int)(r / a.q_heads), n, lo, start);
         const int per_row = a.cache.d / 8, side = ATTEND_THREADS / per_row;  // threads to a row; parts side by side
@@ -382,7 +389,7 @@ __global__ __launch_bounds__(ATTEND_THREADS) void paged_attention_join_kernel(At
         }
         return;
     }
-    const int64_t id = blockIdx.x - (int64_t)B * a.q_heads;
+    const int64_t id = blockIdx.x - (int64_t)a.requests * a.q_heads;
     const int pieces = (a.pad + 4 * ATTEND_THREADS - 1) / (4 * ATTEND_THREADS);
     const int64_t row = id / pieces;
     const int b = (int)(row / a.cache.heads), h = (int)(row % a.cache.heads);
@@ -416,31 +423,34 @@ __global__ __launch_bounds__(ATTEND_THREADS) void paged_attention_join_kernel(At
         if (start + j + c >= lo && start + j + c < n) to[c] += w[c];
 }
 
-template <class T, int VE, bool FINE, bool FULL>
-hipError_t attend(const AttentionArgs &a, int B, hipStream_t stream) {
+template <class T, int VE, bool FINE, bool FULL, bool ONCE>
+hipError_t attend(const AttentionArgs &a, hipStream_t stream) {
     static size_t granted = 0;
-    const int G = a.q_heads / a.cache.heads;
-    const size_t bytes = attend_lds_bytes(VE, G);
-    const void *kernel = reinterpret_cast<const void *>(paged_attention_kernel<T, VE, FINE, FULL>);
+    const size_t bytes = attend_lds_bytes(VE, a.q_heads / a.cache.heads);
+    const void *kernel = reinterpret_cast<const void *>(paged_attention_kernel<T, VE, FINE, FULL, ONCE>);
     if (hipError_t e = allow_big_lds(kernel, bytes, &granted)) return e;
-    hipLaunchKernelGGL((paged_attention_kernel<T, VE, FINE, FULL>), dim3(B * a.cache.heads * a.splits * a.groups), dim3(ATTEND_THREADS), bytes, stream, a);
+    const int items = (a.requests * a.cache.heads * a.splits + 7) / 8 * 8;
+    hipLaunchKernelGGL((paged_attention_kernel<T, VE, FINE, FULL, ONCE>), dim3(items * a.groups), dim3(ATTEND_THREADS), bytes, stream, a);
     return hipGetLastError();
 }
 
+template <class T, int VE, bool FULL>
+hipError_t attend(const AttentionArgs &a, bool once, hipStream_t stream) {
+    return a.cache.slots_log < 4 ? attend<T, VE, true, FULL, false>(a, stream)
+           : once ? attend<T, VE, false, FULL, true>(a, stream) : attend<T, VE, false, FULL, false>(a, stream);
+}
 template <class T, int VE>
-hipError_t attend(const AttentionArgs &a, int B, hipStream_t stream) {
-    const bool fine = a.cache.slots_log < 4, full = a.cache.d == 16 * VE;
-    return fine ? full ? attend<T, VE, true, true>(a, B, stream) : attend<T, VE, true, false>(a, B, stream)
-                : full ? attend<T, VE, false, true>(a, B, stream) : attend<T, VE, false, false>(a, B, stream);
+hipError_t attend(const AttentionArgs &a, bool once, hipStream_t stream) {
+    return a.cache.d == 16 * VE ? attend<T, VE, true>(a, once, stream) : attend<T, VE, false>(a, once, stream);
 }
 
 template <class T>
-hipError_t launch_attention(const AttentionArgs &a, int B, hipStream_t stream) {
-    const int ve = attend_ve(a.cache.d);
-    if (hipError_t e = ve == 4 ? attend<T, 4>(a, B, stream) : ve == 8 ? attend<T, 8>(a, B, stream) : attend<T, 16>(a, B, stream)) return e;
+hipError_t launch_attention(const AttentionArgs &a, bool once, hipStream_t stream) {
+    const int ve = attend_ve(a.cache.d), B = a.requests;
+    if (hipError_t e = ve == 4 ? attend<T, 4>(a, once, stream) : ve == 8 ? attend<T, 8>(a, once, stream) : attend<T, 16>(a, once, stream)) return e;
     if (a.splits == 1 && !a.scores) return hipSuccess;
     const int pieces = a.scores ? (a.pad + 4 * ATTEND_THREADS - 1) / (4 * ATTEND_THREADS) : 0;
-    hipLaunchKernelGGL((paged_attention_join_kernel<T>), dim3(B * a.q_heads + B * a.cache.heads * pieces), dim3(ATTEND_THREADS), 0, stream, a, B);
+    hipLaunchKernelGGL((paged_attention_join_kernel<T>), dim3(B * a.q_heads + B * a.cache.heads * pieces), dim3(ATTEND_THREADS), 0, stream, a);
     return hipGetLastError();
 }
 
