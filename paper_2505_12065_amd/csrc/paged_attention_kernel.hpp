@@ -101,10 +101,12 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 ? 1 : 2) void paged_attent
     extern __shared__ float lds[];
     const int lane = threadIdx.x & (WAVE - 1), g = lane >> 4, m = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-    // First parts of all contexts first, each on any of the 8 XCDs, so that contexts of all lengths are spread over them; the workgroups
-    // that read the same slots follow each other on one.
+    // First parts of all contexts first.  Workgroups are dealt out in their order, to the 8 XCDs and inside an XCD to its 4 shader engines, whatever
+    // they have still to do; from part to part a context moves on by one XCD and by one engine, or the long ones of a batch would all be
+    // a few engines' (every second of 64 requests 8 times as long as the others: 542 -> 430 us).  The workgroups that read the same slots for
+    // other query heads follow each other on one XCD.
     const int hg = (blockIdx.x >> 3) % a.groups, item = (blockIdx.x >> 3) / a.groups * 8 + (blockIdx.x & 7);
-    const int units = a.requests * a.cache.heads, part = item / units, unit = item % units;
+    const int units = a.requests * a.cache.heads, part = item / units, unit = (item % units + 9 * part) % units;
     if (part >= a.splits) return;
     const int h = unit % a.cache.heads, b = unit / a.cache.heads;
     const int G = a.q_heads / a.cache.heads, rows = min(16, G - 16 * hg);     // query heads of this workgroup
@@ -333,6 +335,7 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 ? 1 : 2) void paged_attent
 
 // What the parts of a context left, joined: the first q_heads workgroups of every request take a query head each; those behind them (scores given) take
 // 4 THREADS slots of a cache head each and add the weights of its query heads, in their order, to mass.
+static_assert(ATTEND_PARTS <= ATTEND_THREADS, "a thread for every part");
 template <class T>
 __global__ __launch_bounds__(ATTEND_THREADS) void paged_attention_join_kernel(AttentionArgs a) {
     __shared__ float lds[ATTEND_THREADS * 8];
@@ -363,16 +366,27 @@ __global__ __launch_bounds__(ATTEND_THREADS) void paged_attention_join_kernel(At
         const int per_row = a.cache.d / 8, side = ATTEND_THREADS / per_row;  // threads to a row; parts side by side
         float most, total;
         stats_of(r, parts, most, total);
+        if (tid < parts) {                                // (at most ATTEND_PARTS of them)
+            const float t = a.stats[(r * a.splits + tid) * 2];
+            lds[tid] = t == -INFINITY ? 1.f : exp2_fast(t - most);
+        }
+        __syncthreads();
         float y[8] = {};
         if (tid < side * per_row) {
-            const int at = (tid % per_row) * 8;
+            const float *from = a.partial + r * a.splits * a.cache.d + (tid % per_row) * 8;
+#pragma unroll 4
             for (int s = tid / per_row; s < parts; s += side) {
-                const float t = a.stats[(r * a.splits + s) * 2], f = t == -INFINITY ? 1.f : exp2_fast(t - most);
-                const f4 *z = reinterpret_cast<const f4 *>(a.partial + (r * a.splits + s) * a.cache.d + at);
+                const f4 *z = reinterpret_cast<const f4 *>(from + (int64_t)s * a.cache.d);
+                const f4 z0 = z[0], z1 = z[1];
+                const float f = lds[s];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) y[j] = fmaf(z[j / 4][j % 4], f, y[j]);
+                for (int j = 0; j < 4; ++j) {
+                    y[j] = fmaf(z0[j], f, y[j]);
+                    y[4 + j] = fmaf(z1[j], f, y[4 + j]);
+                }
             }
         }
+        __syncthreads();
 #pragma unroll
         for (int j = 0; j < 8; ++j) lds[tid * 8 + j] = y[j];
         __syncthreads();

@@ -1001,11 +1001,11 @@ inline size_t attend_lds_bytes(int ve, int G) {
 // every context; `part` requests at a time.
 struct AttendPlan {
     int groups = 1, splits = 1, chunk = 0, pad = 0, part = 1;
-    bool once = false;           // keys and values may be more than the last cache holds (256 MiB)
+    bool once = false;           // keys and values are read once, and may be more than the last cache holds (256 MiB)
     size_t one = 0;              // bytes of workspace a request takes
 };
 constexpr int64_t ATTEND_CACHED = (int64_t)256 << 20;
-constexpr int ATTEND_PARTS = 256, ATTEND_CHUNK = 1024, ATTEND_PER_CU = 4;
+constexpr int ATTEND_PARTS = 256, ATTEND_CHUNK = 3328, ATTEND_PER_CU = 4;
 constexpr int64_t ATTEND_GRID = 1 << 22;                  // workgroups of a launch
 inline int64_t attend_step(int elem_bytes, int d) { return 16 * ATTEND_WAVES * attend_tiles(elem_bytes, attend_ve(d)); }
 inline size_t attend_bytes(int q_heads, int d, int64_t splits, int64_t pad) { return (size_t)q_heads * ((size_t)splits * (d + 2) + (size_t)pad) * 4; }
@@ -1023,7 +1023,7 @@ inline AttendPlan attend_plan(int cus, int B, int q_heads, int heads, int d, int
     pl.splits = (int)((range + chunk - 1) / chunk);
     pl.pad = (int)(pl.splits * chunk);
     if (pl.splits > 1 || mass) pl.one = attend_bytes(q_heads, d, pl.splits, mass ? pl.pad : 0);
-    pl.once = 2 * range * B * heads * d * elem_bytes > ATTEND_CACHED;
+    pl.once = pl.groups == 1 && 2 * range * B * heads * d * elem_bytes > ATTEND_CACHED;
     pl.part = B;
     if (pl.one > 0 && pl.one * (size_t)B > most) pl.part = pl.one > most ? 1 : (int)(most / pl.one);
     const int64_t grid = (int64_t)heads * pl.splits * pl.groups + (pl.one ? q_heads + (int64_t)heads * (mass ? pl.pad / 1024 + 1 : 0) : 0);
