@@ -71,7 +71,7 @@ __global__ __launch_bounds__(THREADS) void logit_rules_kernel(RulesArgs a, int p
     typedef typename Scalar<T>::type E;
     constexpr int CHUNK = THREADS * 8 * R, CB = LONG ? 24 : RULES_COUNT_BITS;
     constexpr uint32_t SEEN = 1u << CB, COUNT = SEEN - 1;
-    extern __shared__ uint32_t word[];
+    extern __shared__ __align__(16) uint32_t word[];
     uint32_t *bias = LONG ? word + CHUNK : word;
     const int id = xcd_block(), b = id / parts, v0 = id % parts * CHUNK, m = min(CHUNK, a.V - v0), tid = threadIdx.x;
     const E *in = static_cast<const E *>(a.logits) + b * a.row + v0;
@@ -91,40 +91,51 @@ __global__ __launch_bounds__(THREADS) void logit_rules_kernel(RulesArgs a, int p
             if (mask) bits[r] = mask[i / 8];
         }
     }
+    const int n = max(0, min(a.lengths[b], a.T)), prompt = max(0, a.prompt[b]);
+    const int32_t *tokens = a.tokens + (int64_t)b * a.T, *bias_tokens = a.bias_tokens + (int64_t)b * a.K;
+    const float *bias_values = a.bias_values + (int64_t)b * a.K;
+    const float repetition = a.repetition[b], presence = a.presence[b], frequency = a.frequency[b];
+    constexpr int AHEAD = 4;                              // loads of the history under way at a time
+    u4 told[AHEAD];
+    auto ask = [&](int t0) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int t = t0 + u * 4 * THREADS;
+            told[u] = u4{~0u, ~0u, ~0u, ~0u};             // (no token)
+            if (t + 4 <= n) told[u] = *reinterpret_cast<const Any<4>::type *>(tokens + t);
+        }
+    };
+    int rest = -1, biased = -1;                           // what the last whole four leave; the first biases
+    if ((n & ~3) + tid < n) rest = tokens[(n & ~3) + tid];
+    if (tid < a.K) biased = bias_tokens[tid];
+    ask(4 * tid);
     for (int i = tid * 4; i < (LONG ? 2 * CHUNK : CHUNK); i += THREADS * 4) *reinterpret_cast<u4 *>(word + i) = zero_chunk();
     __syncthreads();
-    const float repetition = a.repetition[b], presence = a.presence[b], frequency = a.frequency[b];
-    const float *bias_values = a.bias_values + (int64_t)b * a.K;
     if (a.K > 0) {
-        for (int i = tid; i < a.K; i += THREADS) {
-            const int token = a.bias_tokens[(int64_t)b * a.K + i];
+        auto note_bias = [&](int i, int token) {
             if (token >= v0 && token - v0 < m) atomicMax(&bias[token - v0], LONG ? (uint32_t)i + 1 : (uint32_t)(i + 1) << (CB + 1));
-        }
+        };
+        note_bias(tid, biased);
+        for (int i = tid + THREADS; i < a.K; i += THREADS) note_bias(i, bias_tokens[i]);
         if (!LONG) __syncthreads();                       // (a maximum of what the counts have not been added to)
     }
-    const int n = max(0, min(a.lengths[b], a.T)), prompt = max(0, a.prompt[b]);
-    const int32_t *tokens = a.tokens + (int64_t)b * a.T;
     auto note = [&](int t, int token) {
         const uint32_t at = (uint32_t)token - (uint32_t)v0;
         if (at >= (uint32_t)m || token < 0) return;
         if (t < prompt) atomicOr(&word[at], SEEN);
         else atomicAdd(&word[at], 1u);
     };
-    constexpr int AHEAD = 4;                              // loads of the history under way at a time
     for (int t0 = 4 * tid; t0 < n; t0 += AHEAD * 4 * THREADS) {
         u4 w[AHEAD];
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            const int t = t0 + u * 4 * THREADS;
-            w[u] = u4{~0u, ~0u, ~0u, ~0u};                // (no token)
-            if (t + 4 <= n) w[u] = *reinterpret_cast<const Any<4>::type *>(tokens + t);
-        }
+        for (int u = 0; u < AHEAD; ++u) w[u] = told[u];
+        if (t0 + AHEAD * 4 * THREADS < n) ask(t0 + AHEAD * 4 * THREADS);
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
             for (int i = 0; i < 4; ++i) note(t0 + u * 4 * THREADS + i, (int)w[u][i]);
     }
-    if ((n & ~3) + tid < n) note((n & ~3) + tid, tokens[(n & ~3) + tid]);
+    note((n & ~3) + tid, rest);
     __syncthreads();
     auto ruled = [&](float y, uint32_t w, uint32_t k, bool allowed) {
         if (w & (SEEN | COUNT)) {
@@ -176,10 +187,10 @@ hipError_t launch(const RulesArgs &a, int B, hipStream_t stream) {
 }
 template <class T>
 hipError_t launch(const RulesArgs &a, int cus, int B, hipStream_t stream) {
-    if (a.T >= 1 << RULES_COUNT_BITS) return launch<T, 1024, 1, true>(a, B, stream);
+    if (a.T >= 1 << RULES_COUNT_BITS) return launch<T, 512, 2, true>(a, B, stream);
     const int chunk = rules_chunk(cus, B, a.V);
     return chunk == 2048 ? launch<T, 256, 1, false>(a, B, stream) : chunk == 4096 ? launch<T, 512, 1, false>(a, B, stream)
-           : chunk == 8192 ? launch<T, 1024, 1, false>(a, B, stream) : launch<T, 1024, 2, false>(a, B, stream);
+           : launch<T, 512, 2, false>(a, B, stream);
 }
 
 }  // namespace

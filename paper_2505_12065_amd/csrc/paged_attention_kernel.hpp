@@ -98,7 +98,7 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 ? 1 : 2) void paged_attent
     typedef AttendShape<T, VE> Sh;
     typedef typename Words<Sh::CW>::type VChunk;
     constexpr int NT = Sh::NT, NS = Sh::NS, NU = Sh::NU, CE = Sh::CE, STEP = 16 * NT * ATTEND_WAVES;
-    extern __shared__ float lds[];
+    extern __shared__ __align__(16) float lds[];
     const int lane = threadIdx.x & (WAVE - 1), g = lane >> 4, m = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     // First parts of all contexts first.  Workgroups are dealt out in their order, to the 8 XCDs and inside an XCD to its 4 shader engines, whatever

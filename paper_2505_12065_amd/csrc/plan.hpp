@@ -1049,7 +1049,7 @@ constexpr int RULES_COUNT_BITS = 18;                      // of a token's word: 
 static_assert(ANN_BIAS_MAX < 1 << (32 - RULES_COUNT_BITS - 1), "biases are numbered in what a count leaves");
 // Logits of a workgroup: the most that leave two workgroups for every compute unit.
 inline int rules_chunk(int cus, int B, int V) {
-    int chunk = 16384;
+    int chunk = 8192;
     while (chunk > 2048 && (int64_t)B * ((V + chunk - 1) / chunk) < 2 * cus) chunk /= 2;
     return chunk;
 }
