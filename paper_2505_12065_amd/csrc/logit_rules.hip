@@ -119,11 +119,12 @@ __global__ __launch_bounds__(THREADS) void logit_rules_kernel(RulesArgs a, int p
         for (int i = tid + THREADS; i < a.K; i += THREADS) note_bias(i, bias_tokens[i]);
         if (!LONG) __syncthreads();                       // (a maximum of what the counts have not been added to)
     }
-    auto note = [&](int t, int token) {
-        const uint32_t at = (uint32_t)token - (uint32_t)v0;
-        if (at >= (uint32_t)m || token < 0) return;
-        if (t < prompt) atomicOr(&word[at], SEEN);
-        else atomicAdd(&word[at], 1u);
+    // (a token below 0 is beyond the last of the part as an unsigned number: V < 2^31 - 2^15)
+    auto note_seen = [&](uint32_t token) {
+        if (token - (uint32_t)v0 < (uint32_t)m) atomicOr(&word[token - v0], SEEN);
+    };
+    auto note_told = [&](uint32_t token) {
+        if (token - (uint32_t)v0 < (uint32_t)m) atomicAdd(&word[token - v0], 1u);
     };
     for (int t0 = 4 * tid; t0 < n; t0 += AHEAD * 4 * THREADS) {
         u4 w[AHEAD];
@@ -131,11 +132,18 @@ __global__ __launch_bounds__(THREADS) void logit_rules_kernel(RulesArgs a, int p
         for (int u = 0; u < AHEAD; ++u) w[u] = told[u];
         if (t0 + AHEAD * 4 * THREADS < n) ask(t0 + AHEAD * 4 * THREADS);
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
+        for (int u = 0; u < AHEAD; ++u) {
+            const int t = t0 + u * 4 * THREADS;
+            if (t >= prompt) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) note(t0 + u * 4 * THREADS + i, (int)w[u][i]);
+                for (int i = 0; i < 4; ++i) note_told(w[u][i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) t + i < prompt ? note_seen(w[u][i]) : note_told(w[u][i]);
+            }
+        }
     }
-    note((n & ~3) + tid, rest);
+    (n & ~3) + tid < prompt ? note_seen((uint32_t)rest) : note_told((uint32_t)rest);
     __syncthreads();
     auto ruled = [&](float y, uint32_t w, uint32_t k, bool allowed) {
         if (w & (SEEN | COUNT)) {
