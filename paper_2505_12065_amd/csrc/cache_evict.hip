@@ -17,39 +17,32 @@ __device__ __forceinline__ uint32_t rank_of(float x) {
     return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
 
-// The sum of x over the threads before this one, and over all.
-__device__ __forceinline__ uint32_t scan_before(uint32_t x, uint32_t *of_wave, uint32_t &all) {
-    const int lane = threadIdx.x & (WAVE - 1), wave = threadIdx.x / WAVE;
-    uint32_t y = x;
-#pragma unroll
-    for (int s = 1; s < WAVE; s *= 2) {
-        const uint32_t o = __shfl_up(y, s);
-        if (lane >= s) y += o;
-    }
-    if (lane == WAVE - 1) of_wave[wave] = y;
-    __syncthreads();
-    uint32_t before = y - x;
-    all = 0;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-        const uint32_t o = of_wave[w];
-        if (w < wave) before += o;
-        all += o;
-    }
-    __syncthreads();
-    return before;
+// The sum of x over the lanes up to this one.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+    int y = (int)x;
+    y += __builtin_amdgcn_update_dpp(0, y, 0x111, 0xf, 0xf, false);          // from 1, 2, 4, 8 lanes before, in rows of 16
+    y += __builtin_amdgcn_update_dpp(0, y, 0x112, 0xf, 0xf, false);
+    y += __builtin_amdgcn_update_dpp(0, y, 0x114, 0xf, 0xf, false);
+    y += __builtin_amdgcn_update_dpp(0, y, 0x118, 0xf, 0xf, false);
+    y += __builtin_amdgcn_update_dpp(0, y, 0x142, 0xa, 0xf, false);          // the last of a row to the next one
+    y += __builtin_amdgcn_update_dpp(0, y, 0x143, 0xc, 0xf, false);          // lane 31 to the upper half
+    return (uint32_t)y;
 }
 
-typedef float f4_any __attribute__((ext_vector_type(4), aligned(4)));
-
-// One workgroup for a cache head of a request.  The rank of the last slot that is kept is found digit by digit by counting in LDS, then every
-// thread learns from a scan where the kept ones of its KR neighbouring slots go.  HELD: the ranks stay in registers, a thread's slots are
-// all that it has; else they are read again for every digit, and the last step goes over the row in tiles.
+// One workgroup for a cache head of a request.  The rank of the last slot that is kept is found digit by digit by counting in LDS: thread
+// t owns the bins BINS / THREADS t on, from the top down.  Then a slot is kept if its rank is higher, or the same and not too many of those
+// lie before it; where it goes is the number of kept ones before it, which the slots of a wave (KR times 64 neighbours, THREADS apart) learn from a
+// ballot and the waves from a scan over all of their ballots.  HELD: the ranks stay in registers, a thread's KR slots are all that it has;
+// else they are read again for every digit, and the last step goes over the row in tiles of KR THREADS.
 template <int KR, bool HELD>
 __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
-    __shared__ uint32_t count[BINS], of_wave[WAVES], s_digit, s_need;
+    constexpr int EACH = BINS / THREADS, PER_LANE = KR * WAVES / WAVE;
+    static_assert(PER_LANE >= 1 && KR * WAVES <= BINS, "ballots of a tile, scanned by a wave");
+    __shared__ uint32_t count[BINS], of_wave[3][WAVES], s_digit[3], s_need[3];
+    __shared__ uint2 s_all;
     const int64_t row = blockIdx.x;
     const int b = blockIdx.x / a.cache.heads, h = blockIdx.x % a.cache.heads, tid = threadIdx.x;
+    const int lane = tid & (WAVE - 1), wave = tid / WAVE;
     const int n = max(0, min(a.lengths[b], a.most)), left = min(n, a.budget);
     const float *mass = a.mass + row * a.mass_slots;
     int32_t *kept = a.kept + row * a.budget;
@@ -64,92 +57,114 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
     const int lo = a.first, hi = n - a.recent;            // the slots that are chosen from
     float value[KR];
     uint32_t rank[KR];
-    auto load = [&](int i0) {
+    auto load = [&](int i0) {                             // slots i0, i0 + THREADS, ...
 #pragma unroll
-        for (int k = 0; k < KR; k += 4) {
-            if (i0 + k + 4 <= n) {
-                const f4_any x = *reinterpret_cast<const f4_any *>(mass + i0 + k);
+        for (int k = 0; k < KR; ++k) value[k] = i0 + k * THREADS < n ? mass[i0 + k * THREADS] : 0.f;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) value[k + j] = x[j];
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) value[k + j] = i0 + k + j < n ? mass[i0 + k + j] : 0.f;
-            }
+        for (int k = 0; k < KR; ++k) {
+            const int i = i0 + k * THREADS;
+            rank[k] = i < lo || i >= hi ? KEEP : rank_of(value[k]);
         }
-#pragma unroll
-        for (int k = 0; k < KR; ++k) rank[k] = i0 + k < lo || i0 + k >= hi ? KEEP : rank_of(value[k]);
     };
-    if (HELD) load(tid * KR);
+    if (HELD) load(tid);
     const int tiles = HELD ? 1 : (n + THREADS * KR - 1) / (THREADS * KR);
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) count[tid + j * THREADS] = 0;
+    __syncthreads();
     uint32_t prefix = 0, need = a.budget;                 // of the ranks that start with `prefix` so many are kept
-    for (int shift = 32 - DIGIT; ; shift = max(0, shift - DIGIT)) {
-        const int bits = shift > 0 ? DIGIT : 32 - 2 * DIGIT;
-        for (int i = tid; i < BINS; i += THREADS) count[i] = 0;
-        __syncthreads();
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+        const int bits = pass < 2 ? DIGIT : 32 - 2 * DIGIT, shift = pass < 2 ? 32 - (pass + 1) * DIGIT : 0;
         for (int tile = 0; tile < tiles; ++tile) {
-            const int i0 = (tile * THREADS + tid) * KR;
+            const int i0 = tile * THREADS * KR + tid;
             if (!HELD) load(i0);
 #pragma unroll
             for (int k = 0; k < KR; ++k) {
-                const bool in = i0 + k < n && (shift == 32 - DIGIT || rank[k] >> (shift + bits) == prefix >> (shift + bits));
+                const bool in = i0 + k * THREADS < n && (pass == 0 || rank[k] >> (shift + bits) == prefix >> (shift + bits));
                 if (!in) continue;
                 const uint32_t digit = (rank[k] >> shift) & ((1u << bits) - 1);
                 // (masses that are all the same would have the lanes wait for each other)
                 const uint32_t one = __builtin_amdgcn_readfirstlane(digit);
                 const uint64_t here = __ballot(true), same = __ballot(digit == one);
                 if (here == same) {
-                    if ((tid & (WAVE - 1)) == (int)__ffsll((unsigned long long)here) - 1) atomicAdd(&count[digit], (uint32_t)__popcll(here));
+                    if (lane == (int)__ffsll((unsigned long long)here) - 1) atomicAdd(&count[digit], (uint32_t)__popcll(here));
                 } else {
                     atomicAdd(&count[digit], 1u);
                 }
             }
         }
         __syncthreads();
-        // thread t takes the bins from the top down: how many lie above its own
-        constexpr int EACH = BINS / THREADS;
-        uint32_t mine = 0, c[EACH], all;
+        uint32_t mine = 0, c[EACH];
 #pragma unroll
-        for (int j = 0; j < EACH; ++j) mine += c[j] = count[BINS - 1 - (tid * EACH + j)];
-        uint32_t above = scan_before(mine, of_wave, all);
+        for (int j = 0; j < EACH; ++j) {
+            uint32_t &bin = count[BINS - 1 - (tid * EACH + j)];
+            mine += c[j] = bin;
+            bin = 0;
+        }
+        const uint32_t up_to = wave_scan(mine);
+        if (lane == WAVE - 1) of_wave[pass][wave] = up_to;
+        __syncthreads();
+        uint32_t above = up_to - mine;                    // slots in the bins above this thread's
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) above += w < wave ? of_wave[pass][w] : 0;
 #pragma unroll
         for (int j = 0; j < EACH; ++j) {
             if (above < need && above + c[j] >= need) {
-                s_digit = BINS - 1 - (tid * EACH + j);
-                s_need = need - above;
+                s_digit[pass] = BINS - 1 - (tid * EACH + j);
+                s_need[pass] = need - above;
             }
             above += c[j];
         }
         __syncthreads();
-        prefix |= s_digit << shift;
-        need = s_need;
-        if (shift == 0) break;
-        __syncthreads();
+        prefix |= s_digit[pass] << shift;
+        need = s_need[pass];
     }
     // all of a higher rank are kept, and the first `need` of rank `prefix`
-    uint32_t more = 0, equal = 0;                         // such slots in the tiles before
+    uint32_t *higher = count, *equal = count + BINS / 2;  // of the KR WAVES ballots: how many; then how many before
+    static_assert(KR * WAVES <= BINS / 2, "two counts of each");
+    uint32_t more = 0, as_much = 0;                       // such slots in the tiles before
     for (int tile = 0; tile < tiles; ++tile) {
-        const int i0 = (tile * THREADS + tid) * KR;
+        const int i0 = tile * THREADS * KR + tid;
         if (!HELD) load(i0);
-        uint32_t m = 0, e = 0, all_m, all_e;
+        const uint64_t before = (1ull << lane) - 1;
+        uint32_t m0[KR], e0[KR];                          // kept for sure, and of rank `prefix`, among the lanes before
 #pragma unroll
         for (int k = 0; k < KR; ++k) {
-            m += i0 + k < n && rank[k] > prefix;
-            e += i0 + k < n && rank[k] == prefix;
-        }
-        const uint32_t m0 = more + scan_before(m, of_wave, all_m);
-        uint32_t e0 = equal + scan_before(e, of_wave, all_e), at = m0 + min(e0, need);
-#pragma unroll
-        for (int k = 0; k < KR; ++k) {
-            const bool there = i0 + k < n, same = rank[k] == prefix;
-            if (there && (rank[k] > prefix || (same && e0 < need))) {
-                kept[at] = i0 + k;
-                new_mass[at] = value[k];
-                ++at;
+            const bool there = i0 + k * THREADS < n;
+            const uint64_t m = __ballot(there && rank[k] > prefix), e = __ballot(there && rank[k] == prefix);
+            m0[k] = __popcll(m & before);
+            e0[k] = __popcll(e & before);
+            if (lane == 0) {
+                higher[k * WAVES + wave] = __popcll(m);
+                equal[k * WAVES + wave] = __popcll(e);
             }
-            e0 += there && same;
         }
-        more += all_m;
-        equal += all_e;
+        __syncthreads();
+        if (wave < 2) {                                   // a wave for each of the two
+            uint32_t *x = wave == 0 ? higher : equal, v[PER_LANE], sum = 0;
+#pragma unroll
+            for (int j = 0; j < PER_LANE; ++j) sum += v[j] = x[lane * PER_LANE + j];
+            uint32_t up_to = wave_scan(sum), run = up_to - sum;
+#pragma unroll
+            for (int j = 0; j < PER_LANE; ++j) {
+                x[lane * PER_LANE + j] = run;
+                run += v[j];
+            }
+            if (lane == WAVE - 1) (wave == 0 ? s_all.x : s_all.y) = up_to;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < KR; ++k) {
+            const int i = i0 + k * THREADS;
+            const uint32_t m = more + higher[k * WAVES + wave] + m0[k], e = as_much + equal[k * WAVES + wave] + e0[k];
+            if (i < n && (rank[k] > prefix || (rank[k] == prefix && e < need))) {
+                kept[m + min(e, need)] = i;
+                new_mass[m + min(e, need)] = value[k];
+            }
+        }
+        more += s_all.x;
+        as_much += s_all.y;
+        if (!HELD) __syncthreads();
     }
 }
 
