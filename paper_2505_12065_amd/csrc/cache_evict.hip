@@ -37,8 +37,10 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
 template <int KR, bool HELD>
 __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
     constexpr int EACH = BINS / THREADS, PER_LANE = KR * WAVES / WAVE;
-    static_assert(PER_LANE >= 1 && KR * WAVES <= BINS, "ballots of a tile, scanned by a wave");
-    __shared__ uint32_t count[BINS], of_wave[3][WAVES], s_digit[3], s_need[3];
+    static_assert(PER_LANE >= 1 && 2 * KR * WAVES <= BINS && KR <= WAVE, "ballots of a tile, scanned by a wave");
+    // (four counts of a bin, a quarter of the lanes to each: masses that are all the same would have 64 lanes wait for each other)
+    __shared__ u4 count[BINS];
+    __shared__ uint32_t of_wave[3][WAVES], s_digit[3], s_need[3];
     __shared__ uint2 s_all;
     const int64_t row = blockIdx.x;
     const int b = blockIdx.x / a.cache.heads, h = blockIdx.x % a.cache.heads, tid = threadIdx.x;
@@ -63,43 +65,35 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
 #pragma unroll
         for (int k = 0; k < KR; ++k) {
             const int i = i0 + k * THREADS;
-            rank[k] = i < lo || i >= hi ? KEEP : rank_of(value[k]);
+            // (one that is not there comes after all that are, like a NaN behind them)
+            rank[k] = i >= n ? 0 : i < lo || i >= hi ? KEEP : rank_of(value[k]);
         }
     };
     if (HELD) load(tid);
     const int tiles = HELD ? 1 : (n + THREADS * KR - 1) / (THREADS * KR);
 #pragma unroll
-    for (int j = 0; j < EACH; ++j) count[tid + j * THREADS] = 0;
+    for (int j = 0; j < EACH; ++j) count[tid + j * THREADS] = zero_chunk();
     __syncthreads();
     uint32_t prefix = 0, need = a.budget;                 // of the ranks that start with `prefix` so many are kept
 #pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
         const int bits = pass < 2 ? DIGIT : 32 - 2 * DIGIT, shift = pass < 2 ? 32 - (pass + 1) * DIGIT : 0;
         for (int tile = 0; tile < tiles; ++tile) {
-            const int i0 = tile * THREADS * KR + tid;
-            if (!HELD) load(i0);
+            if (!HELD) load(tile * THREADS * KR + tid);
 #pragma unroll
             for (int k = 0; k < KR; ++k) {
-                const bool in = i0 + k * THREADS < n && (pass == 0 || rank[k] >> (shift + bits) == prefix >> (shift + bits));
-                if (!in) continue;
+                if (pass > 0 && (rank[k] ^ prefix) >> (shift + bits) != 0) continue;
                 const uint32_t digit = (rank[k] >> shift) & ((1u << bits) - 1);
-                // (masses that are all the same would have the lanes wait for each other)
-                const uint32_t one = __builtin_amdgcn_readfirstlane(digit);
-                const uint64_t here = __ballot(true), same = __ballot(digit == one);
-                if (here == same) {
-                    if (lane == (int)__ffsll((unsigned long long)here) - 1) atomicAdd(&count[digit], (uint32_t)__popcll(here));
-                } else {
-                    atomicAdd(&count[digit], 1u);
-                }
+                atomicAdd(reinterpret_cast<uint32_t *>(count) + 4 * digit + (lane & 3), 1u);
             }
         }
         __syncthreads();
         uint32_t mine = 0, c[EACH];
 #pragma unroll
         for (int j = 0; j < EACH; ++j) {
-            uint32_t &bin = count[BINS - 1 - (tid * EACH + j)];
-            mine += c[j] = bin;
-            bin = 0;
+            u4 &bin = count[BINS - 1 - (tid * EACH + j)];
+            mine += c[j] = (bin[0] + bin[1]) + (bin[2] + bin[3]);
+            bin = zero_chunk();
         }
         const uint32_t up_to = wave_scan(mine);
         if (lane == WAVE - 1) of_wave[pass][wave] = up_to;
@@ -120,24 +114,25 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
         need = s_need[pass];
     }
     // all of a higher rank are kept, and the first `need` of rank `prefix`
-    uint32_t *higher = count, *equal = count + BINS / 2;  // of the KR WAVES ballots: how many; then how many before
-    static_assert(KR * WAVES <= BINS / 2, "two counts of each");
+    uint32_t *higher = reinterpret_cast<uint32_t *>(count), *equal = higher + KR * WAVES;   // of the ballots: how many; then how many before
     uint32_t more = 0, as_much = 0;                       // such slots in the tiles before
     for (int tile = 0; tile < tiles; ++tile) {
         const int i0 = tile * THREADS * KR + tid;
         if (!HELD) load(i0);
-        const uint64_t before = (1ull << lane) - 1;
-        uint32_t m0[KR], e0[KR];                          // kept for sure, and of rank `prefix`, among the lanes before
+        uint32_t m0[KR], e0[KR], m_of = 0, e_of = 0;      // kept for sure, and of rank `prefix`, among the lanes before; lane k: in ballot k
 #pragma unroll
         for (int k = 0; k < KR; ++k) {
-            const bool there = i0 + k * THREADS < n;
-            const uint64_t m = __ballot(there && rank[k] > prefix), e = __ballot(there && rank[k] == prefix);
-            m0[k] = __popcll(m & before);
-            e0[k] = __popcll(e & before);
-            if (lane == 0) {
-                higher[k * WAVES + wave] = __popcll(m);
-                equal[k * WAVES + wave] = __popcll(e);
+            const uint64_t m = __ballot(rank[k] > prefix), e = __ballot(rank[k] == prefix);
+            m0[k] = __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+            e0[k] = __builtin_amdgcn_mbcnt_hi((uint32_t)(e >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)e, 0));
+            if (lane == k) {
+                m_of = __popcll(m);
+                e_of = __popcll(e);
             }
+        }
+        if (lane < KR) {
+            higher[lane * WAVES + wave] = m_of;
+            equal[lane * WAVES + wave] = e_of;
         }
         __syncthreads();
         if (wave < 2) {                                   // a wave for each of the two
@@ -157,7 +152,7 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
         for (int k = 0; k < KR; ++k) {
             const int i = i0 + k * THREADS;
             const uint32_t m = more + higher[k * WAVES + wave] + m0[k], e = as_much + equal[k * WAVES + wave] + e0[k];
-            if (i < n && (rank[k] > prefix || (rank[k] == prefix && e < need))) {
+            if (rank[k] > prefix || (rank[k] == prefix && e < need)) {
                 kept[m + min(e, need)] = i;
                 new_mass[m + min(e, need)] = value[k];
             }
