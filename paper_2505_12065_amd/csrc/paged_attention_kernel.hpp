@@ -333,17 +333,16 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 ? 1 : 2) void paged_attent
     }
 }
 
-// What the parts of a context left, joined: the first q_heads workgroups of every request take a query head each; those behind them (scores given) take
-// 4 THREADS slots of a cache head each and add the weights of its query heads, in their order, to mass.
+// What the parts of a context left, joined.  The first workgroups take query heads: FEW of them each, a wave to a head, if there are few parts, else one
+// head each.  Those behind them (scores given) take 4 THREADS slots of a cache head each and add the weights of its query heads, in their order, to mass.
 static_assert(ATTEND_PARTS <= ATTEND_THREADS, "a thread for every part");
-template <class T>
+template <class T, bool FEW>
 __global__ __launch_bounds__(ATTEND_THREADS) void paged_attention_join_kernel(AttentionArgs a) {
-    __shared__ float lds[ATTEND_THREADS * 8];
-    const int G = a.q_heads / a.cache.heads, tid = threadIdx.x;
+    __shared__ __align__(16) float lds[ATTEND_THREADS * 8];
+    const int G = a.q_heads / a.cache.heads, tid = threadIdx.x, lane = tid & (WAVE - 1);
     // of head row r, by one wave: largest exponent and total over its parts
     auto stats_of = [&](int64_t r, int parts, float &most, float &total) {
         const float *st = a.stats + r * a.splits * 2;
-        const int lane = tid & (WAVE - 1);
         most = -INFINITY;
         total = 0.f;
         for (int s = lane; s < parts; s += WAVE) most = fmaxf(most, st[2 * s]);
@@ -359,26 +358,33 @@ __global__ __launch_bounds__(ATTEND_THREADS) void paged_attention_join_kernel(At
         start = lo & ~15;
         return n > 0 ? (n - start + a.chunk - 1) / a.chunk : 0;
     };
+    auto write = [&](int64_t r, int i, float (&y)[8], float most, float total) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = total == 0.f ? 0.f : y[j] / total;
+        Eight<T> e;
+        e.set(y);
+        e.store(static_cast<char *>(a.out) + (r * a.cache.d + 8 * i) * T::bytes);
+        if (i == 0 && a.lse) a.lse[r] = total == 0.f ? -INFINITY : (most == -INFINITY ? 0.f : most) * 0.6931471805599453f + logf(total);
+    };
     int n, lo, start;
-    if ((int64_t)blockIdx.x < (int64_t)a.requests * a.q_heads) {
-        const int64_t r = blockIdx.x;
+    const int64_t heads_all = (int64_t)a.requests * a.q_heads, head_groups = FEW ? (heads_all + ATTEND_WAVES - 1) / ATTEND_WAVES : heads_all;
+    const int per_row = a.cache.d / 8;                    // lanes to a row, at most 32
+    if ((int64_t)blockIdx.x < head_groups) {
+        const int64_t r = FEW ? (int64_t)blockIdx.x * ATTEND_WAVES + tid / WAVE : blockIdx.x;
+        if (FEW && r >= heads_all) return;
         const int parts = parts_of((int)(r / a.q_heads), n, lo, start);
-        const int per_row = a.cache.d / 8, side = ATTEND_THREADS / per_row;  // threads to a row; parts side by side
+        const int member = FEW ? lane : tid, side = (FEW ? WAVE : ATTEND_THREADS) / per_row;   // parts side by side
+        const float *from = a.partial + r * a.splits * a.cache.d + (member % per_row) * 8;
+        const float *st = a.stats + r * a.splits * 2;
         float most, total;
         stats_of(r, parts, most, total);
-        if (tid < parts) {                                // (at most ATTEND_PARTS of them)
-            const float t = a.stats[(r * a.splits + tid) * 2];
-            lds[tid] = t == -INFINITY ? 1.f : exp2_fast(t - most);
-        }
-        __syncthreads();
         float y[8] = {};
-        if (tid < side * per_row) {
-            const float *from = a.partial + r * a.splits * a.cache.d + (tid % per_row) * 8;
+        if (member < side * per_row) {
 #pragma unroll 4
-            for (int s = tid / per_row; s < parts; s += side) {
+            for (int s = member / per_row; s < parts; s += side) {
                 const f4 *z = reinterpret_cast<const f4 *>(from + (int64_t)s * a.cache.d);
                 const f4 z0 = z[0], z1 = z[1];
-                const float f = lds[s];
+                const float t = st[2 * s], f = t == -INFINITY ? 1.f : exp2_fast(t - most);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     y[j] = fmaf(z0[j], f, y[j]);
@@ -386,24 +392,22 @@ __global__ __launch_bounds__(ATTEND_THREADS) void paged_attention_join_kernel(At
                 }
             }
         }
-        __syncthreads();
+        f4 *mine = reinterpret_cast<f4 *>(lds + tid * 8);
+        mine[0] = f4{y[0], y[1], y[2], y[3]};
+        mine[1] = f4{y[4], y[5], y[6], y[7]};
+        if (FEW) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // (what the wave itself wrote)
+        else __syncthreads();
+        if (member < per_row) {
+            for (int s = 1; s < side && s < parts; ++s) {
+                const f4 *z = reinterpret_cast<const f4 *>(lds + (tid + s * per_row) * 8);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) lds[tid * 8 + j] = y[j];
-        __syncthreads();
-        if (tid < per_row) {
-            for (int s = 1; s < side && s < parts; ++s)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) y[j] += lds[(tid + s * per_row) * 8 + j];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = total == 0.f ? 0.f : y[j] / total;
-            Eight<T> e;
-            e.set(y);
-            e.store(static_cast<char *>(a.out) + (r * a.cache.d + 8 * tid) * T::bytes);
-            if (tid == 0 && a.lse) a.lse[r] = total == 0.f ? -INFINITY : (most == -INFINITY ? 0.f : most) * 0.6931471805599453f + logf(total);
+                for (int j = 0; j < 8; ++j) y[j] += z[j / 4][j % 4];
+            }
+            write(r, member, y, most, total);
         }
         return;
     }
-    const int64_t id = blockIdx.x - (int64_t)a.requests * a.q_heads;
+    const int64_t id = blockIdx.x - head_groups;
     const int pieces = (a.pad + 4 * ATTEND_THREADS - 1) / (4 * ATTEND_THREADS);
     const int64_t row = id / pieces;
     const int b = (int)(row / a.cache.heads), h = (int)(row % a.cache.heads);
@@ -463,8 +467,12 @@ hipError_t launch_attention(const AttentionArgs &a, bool once, hipStream_t strea
     const int ve = attend_ve(a.cache.d), B = a.requests;
     if (hipError_t e = ve == 4 ? attend<T, 4>(a, once, stream) : ve == 8 ? attend<T, 8>(a, once, stream) : attend<T, 16>(a, once, stream)) return e;
     if (a.splits == 1 && !a.scores) return hipSuccess;
-    const int pieces = a.scores ? (a.pad + 4 * ATTEND_THREADS - 1) / (4 * ATTEND_THREADS) : 0;
-    hipLaunchKernelGGL((paged_attention_join_kernel<T>), dim3(B * a.q_heads + B * a.cache.heads * pieces), dim3(ATTEND_THREADS), 0, stream, a);
+    const int pieces = a.scores ? (a.pad + 4 * ATTEND_THREADS - 1) / (4 * ATTEND_THREADS) : 0, rows = B * a.q_heads, mass = B * a.cache.heads * pieces;
+    // (64 heads of 64 requests in 5 parts: 10.2 us a workgroup to a head, a wave to a head 5.9)
+    if (a.splits <= 16)
+        hipLaunchKernelGGL((paged_attention_join_kernel<T, true>), dim3((rows + ATTEND_WAVES - 1) / ATTEND_WAVES + mass), dim3(ATTEND_THREADS), 0, stream, a);
+    else
+        hipLaunchKernelGGL((paged_attention_join_kernel<T, false>), dim3(rows + mass), dim3(ATTEND_THREADS), 0, stream, a);
     return hipGetLastError();
 }
 
