@@ -91,6 +91,109 @@ __device__ __forceinline__ f4 scores_step(u4 k, u4 q, f4 c) {
     }
 }
 
+// What of request b is attended to: slots lo .. n - 1, in tiles from `start` on, in so many parts.
+struct AttendSpan { int n, lo, start, parts; };
+__device__ __forceinline__ AttendSpan attend_span(const AttentionArgs &a, int b) {
+    AttendSpan s;
+    s.n = min(a.lengths[b], a.max_length);
+    s.lo = a.window > 0 ? max(0, s.n - a.window) : 0;
+    s.start = s.lo & ~15;
+    s.parts = s.n > 0 ? (s.n - s.start + a.chunk - 1) / a.chunk : 0;
+    return s;
+}
+
+// By one wave: largest exponent of head row r and total over its parts.
+__device__ __forceinline__ void attend_stats(const AttentionArgs &a, int64_t r, int parts, float &most, float &total) {
+    const float *st = a.stats + r * a.splits * 2;
+    const int lane = threadIdx.x & (WAVE - 1);
+    most = -INFINITY;
+    total = 0.f;
+    for (int s = lane; s < parts; s += WAVE) most = fmaxf(most, st[2 * s]);
+#pragma unroll
+    for (int k = 1; k < WAVE; k *= 2) most = fmaxf(most, __shfl_xor(most, k));
+    for (int s = lane; s < parts; s += WAVE) total += st[2 * s + 1] * (st[2 * s] == -INFINITY ? 1.f : exp2_fast(st[2 * s] - most));
+#pragma unroll
+    for (int k = 1; k < WAVE; k *= 2) total += __shfl_xor(total, k);
+}
+__device__ __forceinline__ float attend_lse(float most, float total) {
+    return total == 0.f ? -INFINITY : (most == -INFINITY ? 0.f : most) * 0.6931471805599453f + logf(total);
+}
+
+// The parts of head row r, joined by one wave (WIDE: by the workgroup).  lds: 8 floats for each of its threads.
+template <class T, bool WIDE>
+__device__ __forceinline__ void attend_join(const AttentionArgs &a, int64_t r, int parts, float *lds) {
+    const int per_row = a.cache.d / 8;                    // lanes to a row, at most 32
+    const int member = WIDE ? threadIdx.x : threadIdx.x & (WAVE - 1), side = (WIDE ? ATTEND_THREADS : WAVE) / per_row;   // parts side by side
+    const float *from = a.partial + r * a.splits * a.cache.d + (member % per_row) * 8;
+    const float *st = a.stats + r * a.splits * 2;
+    float most, total, y[8] = {};
+    attend_stats(a, r, parts, most, total);
+    if (member < side * per_row) {
+#pragma unroll 4
+        for (int s = member / per_row; s < parts; s += side) {
+            const f4 *z = reinterpret_cast<const f4 *>(from + (int64_t)s * a.cache.d);
+            const f4 z0 = z[0], z1 = z[1];
+            const float t = st[2 * s], f = t == -INFINITY ? 1.f : exp2_fast(t - most);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                y[j] = fmaf(z0[j], f, y[j]);
+                y[4 + j] = fmaf(z1[j], f, y[4 + j]);
+            }
+        }
+    }
+    f4 *mine = reinterpret_cast<f4 *>(lds + threadIdx.x * 8);
+    mine[0] = f4{y[0], y[1], y[2], y[3]};
+    mine[1] = f4{y[4], y[5], y[6], y[7]};
+    if (WIDE) __syncthreads();
+    else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");             // (what the wave itself wrote)
+    if (member < per_row) {
+        for (int s = 1; s < side && s < parts; ++s) {
+            const f4 *z = reinterpret_cast<const f4 *>(lds + (threadIdx.x + s * per_row) * 8);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] += z[j / 4][j % 4];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = total == 0.f ? 0.f : y[j] / total;
+        Eight<T> e;
+        e.set(y);
+        e.store(static_cast<char *>(a.out) + (r * a.cache.d + 8 * member) * T::bytes);
+        if (member == 0 && a.lse) a.lse[r] = attend_lse(most, total);
+    }
+    if (!WIDE) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
+// By a workgroup: the weights of slots start + j0 .. of a cache head, ATTEND_PIECE of them, summed over its query heads in their order and added to mass.
+constexpr int ATTEND_PIECE = 4 * ATTEND_THREADS;
+__device__ __forceinline__ void attend_add_mass(const AttentionArgs &a, int b, int h, const AttendSpan &span, int j0, float *lds) {
+    const int G = a.q_heads / a.cache.heads, tid = threadIdx.x, j = j0 + 4 * tid;
+    f4 w = {0.f, 0.f, 0.f, 0.f};
+    for (int g0 = 0; g0 < G; g0 += ATTEND_THREADS) {      // (one round as a rule)
+        const int heads = min(ATTEND_THREADS, G - g0);
+        for (int i = tid / WAVE; i < heads; i += ATTEND_WAVES) {
+            float most, total;
+            attend_stats(a, (int64_t)b * a.q_heads + h * G + g0 + i, span.parts, most, total);
+            lds[2 * i] = most == -INFINITY ? 0.f : most;
+            lds[2 * i + 1] = total == 0.f ? 0.f : 1.f / total;
+        }
+        __syncthreads();
+        if (span.start + j < span.n) {
+            const float *x = a.scores + ((int64_t)b * a.q_heads + h * G + g0) * a.pad + j;
+#pragma unroll 4
+            for (int i = 0; i < heads; ++i) {
+                const f4 s = *reinterpret_cast<const f4 *>(x + (int64_t)i * a.pad);
+                const float most = lds[2 * i], f = lds[2 * i + 1];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) w[c] += exp2_fast(s[c] - most) * f;
+            }
+        }
+        __syncthreads();
+    }
+    float *to = a.mass + ((int64_t)b * a.cache.heads + h) * a.mass_slots + span.start + j;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        if (span.start + j + c >= span.lo && span.start + j + c < span.n) to[c] += w[c];
+}
+
 // FINE: pages of less than 16 slots, looked up for every row and not for a tile.  FULL: d is 16 VE.  ONCE: keys and values are more than the
 // last cache holds, and are read past it.
 template <class T, int VE, bool FINE, bool FULL, bool ONCE>
@@ -110,9 +213,9 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 ? 1 : 2) void paged_attent
     if (part >= a.splits) return;
     const int h = unit % a.cache.heads, b = unit / a.cache.heads;
     const int G = a.q_heads / a.cache.heads, rows = min(16, G - 16 * hg);     // query heads of this workgroup
-    const int n = min(a.lengths[b], a.max_length), lo = a.window > 0 ? max(0, n - a.window) : 0, start = lo & ~15;
-    const int first = start + part * a.chunk, end = min(n, first + a.chunk);
-    if (first >= n && a.splits > 1) return;
+    const AttendSpan span = attend_span(a, b);
+    const int n = span.n, lo = span.lo, start = span.start, first = start + part * a.chunk, end = min(n, first + a.chunk);
+    if (part >= max(span.parts, 1)) return;               // (the first part of nothing says so)
     const int64_t hq0 = (int64_t)b * a.q_heads + h * G + 16 * hg;
 
     u4 q[NS];
@@ -268,7 +371,7 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 ? 1 : 2) void paged_attent
         for (int t = 0; t < NT; ++t) page[t] = page_next[t];
     }
 
-    // the four waves' sums, joined: lane 16 g + m holds elements CE (4 g + i) .. of every 16 CE, head m
+    // the waves' sums, joined (of those that had a slot): lane 16 g + m holds elements CE (4 g + i) .. of every 16 CE, head m
     sum = column_sum(sum);
     float *s_top = lds, *s_sum = lds + ATTEND_WAVES * 16, *s_o = lds + 2 * ATTEND_WAVES * 16;
     constexpr int LD = attend_lds_row(VE);
@@ -276,12 +379,13 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 ? 1 : 2) void paged_attent
         s_top[wave * 16 + m] = top;
         s_sum[wave * 16 + m] = sum;
     }
+    const int used = min(ATTEND_WAVES, (max(end - first, 1) + 16 * NT - 1) / (16 * NT));
     __syncthreads();
     float all = -INFINITY;
 #pragma unroll
     for (int w = 0; w < ATTEND_WAVES; ++w) all = fmaxf(all, s_top[w * 16 + m]);
     const float mine = top == -INFINITY ? 0.f : exp2_fast(top - all);
-    if (m < rows) {
+    if (m < rows && wave < used) {
 #pragma unroll
         for (int u = 0; u < NU; ++u)
 #pragma unroll
@@ -307,8 +411,7 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 ? 1 : 2) void paged_attent
             total += s_sum[w * 16 + r] * (t == -INFINITY ? 1.f : exp2_fast(t - most));
         }
         float y[8] = {};
-#pragma unroll
-        for (int w = 0; w < ATTEND_WAVES; ++w) {
+        for (int w = 0; w < used; ++w) {
             const float *z = s_o + (w * rows + r) * LD + at;
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[j] += z[j];
@@ -328,117 +431,28 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 ? 1 : 2) void paged_attent
             Eight<T> e;
             e.set(y);
             e.store(static_cast<char *>(a.out) + ((hq0 + r) * a.cache.d + at) * T::bytes);
-            if (at == 0 && a.lse) a.lse[hq0 + r] = total == 0.f ? -INFINITY : (most == -INFINITY ? 0.f : most) * 0.6931471805599453f + logf(total);
+            if (at == 0 && a.lse) a.lse[hq0 + r] = attend_lse(most, total);
         }
     }
 }
 
-// What the parts of a context left, joined.  The first workgroups take query heads: FEW of them each, a wave to a head, if there are few parts, else one
-// head each.  Those behind them (scores given) take 4 THREADS slots of a cache head each and add the weights of its query heads, in their order, to mass.
-static_assert(ATTEND_PARTS <= ATTEND_THREADS, "a thread for every part");
+// What the parts of a context left, joined by a launch of its own: the workgroup that is done last could do it, but only behind fences that write back an XCD's
+// whole L2 (one request of 1500 slots: 16.9 us against 10.2).  The first workgroups take query heads: a wave to a head if there are few parts (FEW), else a
+// workgroup to a head.  Those behind them (scores given) take a piece of the slots of a cache head each.
 template <class T, bool FEW>
 __global__ __launch_bounds__(ATTEND_THREADS) void paged_attention_join_kernel(AttentionArgs a) {
     __shared__ __align__(16) float lds[ATTEND_THREADS * 8];
-    const int G = a.q_heads / a.cache.heads, tid = threadIdx.x, lane = tid & (WAVE - 1);
-    // of head row r, by one wave: largest exponent and total over its parts
-    auto stats_of = [&](int64_t r, int parts, float &most, float &total) {
-        const float *st = a.stats + r * a.splits * 2;
-        most = -INFINITY;
-        total = 0.f;
-        for (int s = lane; s < parts; s += WAVE) most = fmaxf(most, st[2 * s]);
-#pragma unroll
-        for (int k = 1; k < WAVE; k *= 2) most = fmaxf(most, __shfl_xor(most, k));
-        for (int s = lane; s < parts; s += WAVE) total += st[2 * s + 1] * (st[2 * s] == -INFINITY ? 1.f : exp2_fast(st[2 * s] - most));
-#pragma unroll
-        for (int k = 1; k < WAVE; k *= 2) total += __shfl_xor(total, k);
-    };
-    auto parts_of = [&](int b, int &n, int &lo, int &start) {
-        n = min(a.lengths[b], a.max_length);
-        lo = a.window > 0 ? max(0, n - a.window) : 0;
-        start = lo & ~15;
-        return n > 0 ? (n - start + a.chunk - 1) / a.chunk : 0;
-    };
-    auto write = [&](int64_t r, int i, float (&y)[8], float most, float total) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = total == 0.f ? 0.f : y[j] / total;
-        Eight<T> e;
-        e.set(y);
-        e.store(static_cast<char *>(a.out) + (r * a.cache.d + 8 * i) * T::bytes);
-        if (i == 0 && a.lse) a.lse[r] = total == 0.f ? -INFINITY : (most == -INFINITY ? 0.f : most) * 0.6931471805599453f + logf(total);
-    };
-    int n, lo, start;
     const int64_t heads_all = (int64_t)a.requests * a.q_heads, head_groups = FEW ? (heads_all + ATTEND_WAVES - 1) / ATTEND_WAVES : heads_all;
-    const int per_row = a.cache.d / 8;                    // lanes to a row, at most 32
     if ((int64_t)blockIdx.x < head_groups) {
-        const int64_t r = FEW ? (int64_t)blockIdx.x * ATTEND_WAVES + tid / WAVE : blockIdx.x;
-        if (FEW && r >= heads_all) return;
-        const int parts = parts_of((int)(r / a.q_heads), n, lo, start);
-        const int member = FEW ? lane : tid, side = (FEW ? WAVE : ATTEND_THREADS) / per_row;   // parts side by side
-        const float *from = a.partial + r * a.splits * a.cache.d + (member % per_row) * 8;
-        const float *st = a.stats + r * a.splits * 2;
-        float most, total;
-        stats_of(r, parts, most, total);
-        float y[8] = {};
-        if (member < side * per_row) {
-#pragma unroll 4
-            for (int s = member / per_row; s < parts; s += side) {
-                const f4 *z = reinterpret_cast<const f4 *>(from + (int64_t)s * a.cache.d);
-                const f4 z0 = z[0], z1 = z[1];
-                const float t = st[2 * s], f = t == -INFINITY ? 1.f : exp2_fast(t - most);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    y[j] = fmaf(z0[j], f, y[j]);
-                    y[4 + j] = fmaf(z1[j], f, y[4 + j]);
-                }
-            }
-        }
-        f4 *mine = reinterpret_cast<f4 *>(lds + tid * 8);
-        mine[0] = f4{y[0], y[1], y[2], y[3]};
-        mine[1] = f4{y[4], y[5], y[6], y[7]};
-        if (FEW) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // (what the wave itself wrote)
-        else __syncthreads();
-        if (member < per_row) {
-            for (int s = 1; s < side && s < parts; ++s) {
-                const f4 *z = reinterpret_cast<const f4 *>(lds + (tid + s * per_row) * 8);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) y[j] += z[j / 4][j % 4];
-            }
-            write(r, member, y, most, total);
-        }
+        const int64_t r = FEW ? (int64_t)blockIdx.x * ATTEND_WAVES + threadIdx.x / WAVE : blockIdx.x;
+        if (r < heads_all) attend_join<T, !FEW>(a, r, max(1, attend_span(a, (int)(r / a.q_heads)).parts), lds);
         return;
     }
     const int64_t id = blockIdx.x - head_groups;
-    const int pieces = (a.pad + 4 * ATTEND_THREADS - 1) / (4 * ATTEND_THREADS);
-    const int64_t row = id / pieces;
-    const int b = (int)(row / a.cache.heads), h = (int)(row % a.cache.heads);
-    const int parts = parts_of(b, n, lo, start), j0 = (int)(id % pieces) * 4 * ATTEND_THREADS;
-    if (start + j0 >= n) return;
-    const int j = j0 + 4 * tid;
-    f4 w = {0.f, 0.f, 0.f, 0.f};
-    for (int g0 = 0; g0 < G; g0 += ATTEND_THREADS) {      // (one round as a rule)
-        const int heads = min(ATTEND_THREADS, G - g0);
-        for (int i = tid / WAVE; i < heads; i += ATTEND_WAVES) {
-            float most, total;
-            stats_of((int64_t)b * a.q_heads + h * G + g0 + i, parts, most, total);
-            lds[2 * i] = most == -INFINITY ? 0.f : most;
-            lds[2 * i + 1] = total == 0.f ? 0.f : 1.f / total;
-        }
-        __syncthreads();
-        if (start + j < n) {
-            const float *x = a.scores + ((int64_t)b * a.q_heads + h * G + g0) * a.pad + j;
-            for (int i = 0; i < heads; ++i) {
-                const f4 s = *reinterpret_cast<const f4 *>(x + (int64_t)i * a.pad);
-                const float most = lds[2 * i], f = lds[2 * i + 1];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) w[c] += exp2_fast(s[c] - most) * f;
-            }
-        }
-        __syncthreads();
-    }
-    float *to = a.mass + row * a.mass_slots + start + j;
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-        if (start + j + c >= lo && start + j + c < n) to[c] += w[c];
+    const int pieces = (a.pad + ATTEND_PIECE - 1) / ATTEND_PIECE, j0 = (int)(id % pieces) * ATTEND_PIECE;
+    const int b = (int)(id / pieces / a.cache.heads), h = (int)(id / pieces % a.cache.heads);
+    const AttendSpan span = attend_span(a, b);
+    if (span.start + j0 < span.n) attend_add_mass(a, b, h, span, j0, lds);
 }
 
 template <class T, int VE, bool FINE, bool FULL, bool ONCE>
@@ -467,9 +481,9 @@ hipError_t launch_attention(const AttentionArgs &a, bool once, hipStream_t strea
     const int ve = attend_ve(a.cache.d), B = a.requests;
     if (hipError_t e = ve == 4 ? attend<T, 4>(a, once, stream) : ve == 8 ? attend<T, 8>(a, once, stream) : attend<T, 16>(a, once, stream)) return e;
     if (a.splits == 1 && !a.scores) return hipSuccess;
-    const int pieces = a.scores ? (a.pad + 4 * ATTEND_THREADS - 1) / (4 * ATTEND_THREADS) : 0, rows = B * a.q_heads, mass = B * a.cache.heads * pieces;
+    const int pieces = a.scores ? (a.pad + ATTEND_PIECE - 1) / ATTEND_PIECE : 0, rows = B * a.q_heads, mass = B * a.cache.heads * pieces;
     // (64 heads of 64 requests in 5 parts: 10.2 us a workgroup to a head, a wave to a head 5.9)
-    if (a.splits <= 16)
+    if (a.splits <= ATTEND_FEW)
         hipLaunchKernelGGL((paged_attention_join_kernel<T, true>), dim3((rows + ATTEND_WAVES - 1) / ATTEND_WAVES + mass), dim3(ATTEND_THREADS), 0, stream, a);
     else
         hipLaunchKernelGGL((paged_attention_join_kernel<T, false>), dim3(rows + mass), dim3(ATTEND_THREADS), 0, stream, a);

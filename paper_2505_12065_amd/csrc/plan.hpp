@@ -1004,6 +1004,7 @@ struct AttendPlan {
     bool once = false;           // keys and values are read once, and may be more than the last cache holds (256 MiB)
     size_t one = 0;              // bytes of workspace a request takes
 };
+constexpr int ATTEND_FEW = 16;                            // parts that a wave joins
 constexpr int64_t ATTEND_CACHED = (int64_t)256 << 20;
 constexpr int ATTEND_PARTS = 256, ATTEND_CHUNK = 3328, ATTEND_PER_CU = 4;
 constexpr int64_t ATTEND_GRID = 1 << 22;                  // workgroups of a launch
