@@ -1,6 +1,6 @@
 // Attention of one new token per request over a paged cache, on the matrix cores.
 //
-// A workgroup of four waves takes a part of one request's slots for the (at most 16) query heads of one cache head; a wave
+// A workgroup of four waves takes a part of one request's slots for at most 16 MT query heads of one cache head; a wave
 // takes NT tiles of 16 slots at a time.  Both products are turned so that the query heads are the columns of every tile:
 //     S^T [16 slots x 16 heads] = K Q^T          O^T [d x 16 heads] += V^T P^T
 // Lane 16 g + m then holds the scores of slots 4 g .. 4 g + 3 and head m, which is where the second product wants its operand P^T if
@@ -195,9 +195,9 @@ __device__ __forceinline__ void attend_add_mass(const AttentionArgs &a, int b, i
 }
 
 // FINE: pages of less than 16 slots, looked up for every row and not for a tile.  FULL: d is 16 VE.  ONCE: keys and values are more than the
-// last cache holds, and are read past it.
-template <class T, int VE, bool FINE, bool FULL, bool ONCE>
-__global__ __launch_bounds__(ATTEND_THREADS, VE == 16 ? 1 : 2) void paged_attention_kernel(AttentionArgs a) {
+// last cache holds, and are read past it.  MT: tiles of 16 query heads.
+template <class T, int VE, int MT, bool FINE, bool FULL, bool ONCE>
+__global__ __launch_bounds__(ATTEND_THREADS, VE == 16 || (MT > 1 && T::bytes == 4) ? 1 : 2) void paged_attention_kernel(AttentionArgs a) {
     typedef AttendShape<T, VE> Sh;
     typedef typename Words<Sh::CW>::type VChunk;
     constexpr int NT = Sh::NT, NS = Sh::NS, NU = Sh::NU, CE = Sh::CE, STEP = 16 * NT * ATTEND_WAVES;
@@ -212,20 +212,22 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 ? 1 : 2) void paged_attent
     const int units = a.requests * a.cache.heads, part = item / units, unit = (item % units + 9 * part) % units;
     if (part >= a.splits) return;
     const int h = unit % a.cache.heads, b = unit / a.cache.heads;
-    const int G = a.q_heads / a.cache.heads, rows = min(16, G - 16 * hg);     // query heads of this workgroup
+    const int G = a.q_heads / a.cache.heads, rows = min(16 * MT, G - 16 * MT * hg);   // query heads of this workgroup
     const AttendSpan span = attend_span(a, b);
     const int n = span.n, lo = span.lo, start = span.start, first = start + part * a.chunk, end = min(n, first + a.chunk);
     if (part >= max(span.parts, 1)) return;               // (the first part of nothing says so)
-    const int64_t hq0 = (int64_t)b * a.q_heads + h * G + 16 * hg;
+    const int64_t hq0 = (int64_t)b * a.q_heads + h * G + 16 * MT * hg;
 
-    u4 q[NS];
+    u4 q[MT][NS];
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-        q[s] = zero_chunk();
-        const int at = (4 * s + g) * 16;
-        if (m < rows && (FULL || at < a.cache.d * T::bytes))
-            q[s] = load_chunk(static_cast<const char *>(a.q) + b * a.q_row + (h * G + 16 * hg + m) * a.q_head + at);
-    }
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            q[mt][s] = zero_chunk();
+            const int at = (4 * s + g) * 16;
+            if (16 * mt + m < rows && (FULL || at < a.cache.d * T::bytes))
+                q[mt][s] = load_chunk(static_cast<const char *>(a.q) + b * a.q_row + (h * G + 16 * (MT * hg + mt) + m) * a.q_head + at);
+        }
     const int32_t *table = a.table + (int64_t)b * a.width;
     const int slots_log = a.cache.slots_log, mask = (1 << slots_log) - 1;
     const char *k_head = a.cache.k + h * a.cache.k_head, *v_head = a.cache.v + h * a.cache.v_head;
@@ -256,10 +258,15 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 ? 1 : 2) void paged_attent
         }
     };
 
-    f4 o[VE];
+    f4 o[MT][VE];
+    float top[MT], sum[MT];                               // of head 16 mt + m; the sum of this lane's slots alone
 #pragma unroll
-    for (int c = 0; c < VE; ++c) o[c] = f4{0.f, 0.f, 0.f, 0.f};
-    float top = -INFINITY, sum = 0.f;                     // of head m; the sum of this lane's slots alone
+    for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+        for (int c = 0; c < VE; ++c) o[mt][c] = f4{0.f, 0.f, 0.f, 0.f};
+        top[mt] = -INFINITY;
+        sum[mt] = 0.f;
+    }
     int k0 = first + wave * 16 * NT;
     if (k0 < end) {
         pages_of(k0, page);
@@ -285,16 +292,20 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 ? 1 : 2) void paged_attent
                 }
             }
         }
-        f4 x[NT];
+        f4 x[MT][NT];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            x[t] = f4{0.f, 0.f, 0.f, 0.f};
+        for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int s = 0; s < NS; ++s) x[t] = scores_step<T>(kr[t][s], q[s], x[t]);
-        }
+            for (int t = 0; t < NT; ++t) {
+                x[mt][t] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int s = 0; s < NS; ++s) x[mt][t] = scores_step<T>(kr[t][s], q[mt][s], x[mt][t]);
+            }
         if (more) load_k(k0 + STEP, page_next);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) x[t] *= a.scale;
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) x[mt][t] *= a.scale;
         bool whole = k0 >= lo && k0 + 16 * NT <= end;
 #pragma unroll
         for (int t = 0; t < NT; ++t) whole = whole && page[t] >= 0;
@@ -306,42 +317,53 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 ? 1 : 2) void paged_attent
                     const int key = k0 + 16 * t + 4 * g + i;
                     const bool use = FINE ? (there >> (4 * t + i)) & 1 : page[t] >= 0 && key >= lo && key < end;
                     if (!use) {
-                        x[t][i] = -INFINITY;
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) x[mt][t][i] = -INFINITY;
 #pragma unroll
                         for (int u = 0; u < NU; ++u) vr[t][i][u] = VChunk(0);
                     }
                 }
             }
         }
-        if (a.scores && m < rows) {
+        if (a.scores) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+                if (16 * mt + m < rows) {
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+                        *reinterpret_cast<f4 *>(a.scores + (hq0 + 16 * mt + m) * a.pad + (k0 - start + 16 * t + 4 * g)) = x[mt][t];
+                }
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {                 // x becomes the weights
+            float most = x[mt][0][0];
 #pragma unroll
             for (int t = 0; t < NT; ++t)
-                *reinterpret_cast<f4 *>(a.scores + (hq0 + m) * a.pad + (k0 - start + 16 * t + 4 * g)) = x[t];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) most = fmaxf(most, x[mt][t][i]);
+            const float now = fmaxf(top[mt], column_max(most)), base = now == -INFINITY ? 0.f : now, keep = exp2_fast(top[mt] - base);
+            top[mt] = now;
+            sum[mt] *= keep;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    x[mt][t][i] = exp2_fast(x[mt][t][i] - base);
+                    sum[mt] += x[mt][t][i];
+                }
+#pragma unroll
+            for (int c = 0; c < VE; ++c) o[mt][c] *= keep;
         }
-        float most = x[0][0];
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) most = fmaxf(most, x[t][i]);
-        const float now = fmaxf(top, column_max(most)), base = now == -INFINITY ? 0.f : now, keep = exp2_fast(top - base);
-        top = now;
-        sum *= keep;
-        float p[NT][4];
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                p[t][i] = exp2_fast(x[t][i] - base);
-                sum += p[t][i];
-            }
-#pragma unroll
-        for (int c = 0; c < VE; ++c) o[c] *= keep;
         if constexpr (T::bytes == 2) {
 #pragma unroll
             for (int t = 0; t < NT; t += 2) {
-                const float w[8] = {p[t][0], p[t][1], p[t][2], p[t][3], p[t + 1][0], p[t + 1][1], p[t + 1][2], p[t + 1][3]};
-                u4 high, low;
-                split_weights<T>(w, high, low);
+                u4 high[MT], low[MT];
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    const f4 x0 = x[mt][t], x1 = x[mt][t + 1];
+                    const float w[8] = {x0[0], x0[1], x0[2], x0[3], x1[0], x1[1], x1[2], x1[3]};
+                    split_weights<T>(w, high[mt], low[mt]);
+                }
 #pragma unroll
                 for (int u = 0; u < NU; ++u)
 #pragma unroll
@@ -351,9 +373,12 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 ? 1 : 2) void paged_attent
                         for (int k = 0; k < 4; ++k)
                             v[k] = __builtin_amdgcn_perm(vr[t + k / 2][2 * (k & 1) + 1][u][c / 2], vr[t + k / 2][2 * (k & 1)][u][c / 2],
                                                          c & 1 ? 0x07060302u : 0x05040100u);
-                        f4 &acc = o[u * CE + c];
-                        acc = mfma16<T>(v, high, acc);
-                        acc = mfma16<T>(v, low, acc);
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) {
+                            f4 &acc = o[mt][u * CE + c];
+                            acc = mfma16<T>(v, high[mt], acc);
+                            acc = mfma16<T>(v, low[mt], acc);
+                        }
                     }
             }
         } else {
@@ -365,37 +390,46 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 ? 1 : 2) void paged_attent
                     for (int u = 0; u < NU; ++u)
 #pragma unroll
                         for (int c = 0; c < CE; ++c)
-                            o[u * CE + c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[t][i][u][c]), p[t][i], o[u * CE + c], 0, 0, 0);
+#pragma unroll
+                            for (int mt = 0; mt < MT; ++mt)
+                                o[mt][u * CE + c] =
+                                    __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[t][i][u][c]), x[mt][t][i], o[mt][u * CE + c], 0, 0, 0);
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t) page[t] = page_next[t];
     }
 
-    // the waves' sums, joined (of those that had a slot): lane 16 g + m holds elements CE (4 g + i) .. of every 16 CE, head m
-    sum = column_sum(sum);
-    float *s_top = lds, *s_sum = lds + ATTEND_WAVES * 16, *s_o = lds + 2 * ATTEND_WAVES * 16;
-    constexpr int LD = attend_lds_row(VE);
-    if (g == 0) {
-        s_top[wave * 16 + m] = top;
-        s_sum[wave * 16 + m] = sum;
-    }
+    // the waves' sums, joined (of those that had a slot): lane 16 g + m holds elements CE (4 g + i) .. of every 16 CE, head 16 mt + m
+    constexpr int HEADS = 16 * MT, LD = attend_lds_row(VE);
+    float *s_top = lds, *s_sum = lds + ATTEND_WAVES * HEADS, *s_o = lds + 2 * ATTEND_WAVES * HEADS;
     const int used = min(ATTEND_WAVES, (max(end - first, 1) + 16 * NT - 1) / (16 * NT));
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        sum[mt] = column_sum(sum[mt]);
+        if (g == 0) {
+            s_top[wave * HEADS + 16 * mt + m] = top[mt];
+            s_sum[wave * HEADS + 16 * mt + m] = sum[mt];
+        }
+    }
     __syncthreads();
-    float all = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < ATTEND_WAVES; ++w) all = fmaxf(all, s_top[w * 16 + m]);
-    const float mine = top == -INFINITY ? 0.f : exp2_fast(top - all);
-    if (m < rows && wave < used) {
+    for (int mt = 0; mt < MT; ++mt) {
+        const int head = 16 * mt + m;
+        float all = -INFINITY;
 #pragma unroll
-        for (int u = 0; u < NU; ++u)
+        for (int w = 0; w < ATTEND_WAVES; ++w) all = fmaxf(all, s_top[w * HEADS + head]);
+        const float mine = top[mt] == -INFINITY ? 0.f : exp2_fast(top[mt] - all);
+        if (head < rows && wave < used) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int u = 0; u < NU; ++u)
 #pragma unroll
-                for (int c = 0; c < CE; c += 4) {
-                    const int at = (u * 16 + 4 * g + i) * CE + c;
-                    *reinterpret_cast<f4 *>(s_o + (wave * rows + m) * LD + at) =
-                        f4{o[u * CE + c][i], o[u * CE + c + 1][i], o[u * CE + c + 2][i], o[u * CE + c + 3][i]} * mine;
-                }
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int c = 0; c < CE; c += 4) {
+                        const int at = (u * 16 + 4 * g + i) * CE + c, e = u * CE + c;
+                        *reinterpret_cast<f4 *>(s_o + (wave * rows + head) * LD + at) = f4{o[mt][e][i], o[mt][e + 1][i], o[mt][e + 2][i], o[mt][e + 3][i]} * mine;
+                    }
+        }
     }
     __syncthreads();
     const int per_row = a.cache.d / 8;
@@ -403,12 +437,12 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 ? 1 : 2) void paged_attent
         const int r = i / per_row, at = (i % per_row) * 8;
         float most = -INFINITY, total = 0.f;
 #pragma unroll
-        for (int w = 0; w < ATTEND_WAVES; ++w) most = fmaxf(most, s_top[w * 16 + r]);
+        for (int w = 0; w < ATTEND_WAVES; ++w) most = fmaxf(most, s_top[w * HEADS + r]);
 #pragma unroll
         for (int w = 0; w < ATTEND_WAVES; ++w) {
-            const float t = s_top[w * 16 + r];
+            const float t = s_top[w * HEADS + r];
             // (a NaN among the scores is in the sum, whatever the maximum says)
-            total += s_sum[w * 16 + r] * (t == -INFINITY ? 1.f : exp2_fast(t - most));
+            total += s_sum[w * HEADS + r] * (t == -INFINITY ? 1.f : exp2_fast(t - most));
         }
         float y[8] = {};
         for (int w = 0; w < used; ++w) {
@@ -455,25 +489,30 @@ __global__ __launch_bounds__(ATTEND_THREADS) void paged_attention_join_kernel(At
     if (span.start + j0 < span.n) attend_add_mass(a, b, h, span, j0, lds);
 }
 
-template <class T, int VE, bool FINE, bool FULL, bool ONCE>
+template <class T, int VE, int MT, bool FINE, bool FULL, bool ONCE>
 hipError_t attend(const AttentionArgs &a, hipStream_t stream) {
     static size_t granted = 0;
-    const size_t bytes = attend_lds_bytes(VE, a.q_heads / a.cache.heads);
-    const void *kernel = reinterpret_cast<const void *>(paged_attention_kernel<T, VE, FINE, FULL, ONCE>);
+    const size_t bytes = attend_lds_bytes(VE, MT, a.q_heads / a.cache.heads);
+    const void *kernel = reinterpret_cast<const void *>(paged_attention_kernel<T, VE, MT, FINE, FULL, ONCE>);
     if (hipError_t e = allow_big_lds(kernel, bytes, &granted)) return e;
     const int items = (a.requests * a.cache.heads * a.splits + 7) / 8 * 8;
-    hipLaunchKernelGGL((paged_attention_kernel<T, VE, FINE, FULL, ONCE>), dim3(items * a.groups), dim3(ATTEND_THREADS), bytes, stream, a);
+    hipLaunchKernelGGL((paged_attention_kernel<T, VE, MT, FINE, FULL, ONCE>), dim3(items * a.groups), dim3(ATTEND_THREADS), bytes, stream, a);
     return hipGetLastError();
 }
 
-template <class T, int VE, bool FULL>
-hipError_t attend(const AttentionArgs &a, bool once, hipStream_t stream) {
-    return a.cache.slots_log < 4 ? attend<T, VE, true, FULL, false>(a, stream)
-           : once ? attend<T, VE, false, FULL, true>(a, stream) : attend<T, VE, false, FULL, false>(a, stream);
-}
+// (variants that few calls would tell apart share the general one: caches of small pages, and of many heads with d < 16 VE, are not read past the last cache)
 template <class T, int VE>
 hipError_t attend(const AttentionArgs &a, bool once, hipStream_t stream) {
-    return a.cache.d == 16 * VE ? attend<T, VE, true>(a, once, stream) : attend<T, VE, false>(a, once, stream);
+    constexpr int MT = attend_head_tiles(T::bytes, VE, 17);
+    const bool full = a.cache.d == 16 * VE, fine = a.cache.slots_log < 4;
+    if constexpr (MT > 1) {
+        if (a.q_heads / a.cache.heads > 16)
+            return fine ? attend<T, VE, MT, true, false, false>(a, stream) : !full ? attend<T, VE, MT, false, false, false>(a, stream)
+                   : once ? attend<T, VE, MT, false, true, true>(a, stream) : attend<T, VE, MT, false, true, false>(a, stream);
+    }
+    if (fine) return full ? attend<T, VE, 1, true, true, false>(a, stream) : attend<T, VE, 1, true, false, false>(a, stream);
+    if (once) return full ? attend<T, VE, 1, false, true, true>(a, stream) : attend<T, VE, 1, false, false, true>(a, stream);
+    return full ? attend<T, VE, 1, false, true, false>(a, stream) : attend<T, VE, 1, false, false, false>(a, stream);
 }
 
 template <class T>

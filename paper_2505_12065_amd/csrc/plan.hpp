@@ -993,11 +993,19 @@ inline int attend_ve(int d) { return d <= 64 ? 4 : d <= 128 ? 8 : 16; }
 // Tiles of 16 slots that a wave takes at a time: as many as its registers hold twice (K of the next, V of this).
 constexpr int attend_tiles(int elem_bytes, int ve) { return elem_bytes == 2 ? (ve == 4 ? 4 : 2) : ve == 16 ? 1 : 2; }
 constexpr int attend_lds_row(int ve) { return 16 * ve + 4; }
-inline size_t attend_lds_bytes(int ve, int G) {
-    return (size_t)(2 * ATTEND_WAVES * 16 + ATTEND_WAVES * (G < 16 ? G : 16) * attend_lds_row(ve)) * 4;
+inline size_t attend_lds_bytes(int ve, int mt, int G) {
+    return (size_t)(2 * ATTEND_WAVES * 16 * mt + ATTEND_WAVES * (G < 16 * mt ? G : 16 * mt) * attend_lds_row(ve)) * 4;
 }
 
-// How a batch is divided: `groups` workgroups side by side for the query heads of a cache head, 16 each; `splits` parts of `chunk` slots of
+// Tiles of 16 query heads that a workgroup takes, each reading of K and V then serving them all: two where there are more than 16 heads, except
+// where a wave's registers do not hold two (fp32, d > 128).
+constexpr int attend_head_tiles(int elem_bytes, int ve, int G) { return G <= 16 || (elem_bytes == 4 && ve == 16) ? 1 : 2; }
+inline int attend_groups(int elem_bytes, int d, int G) {
+    const int heads = 16 * attend_head_tiles(elem_bytes, attend_ve(d), G);
+    return (G + heads - 1) / heads;
+}
+
+// How a batch is divided: `groups` workgroups side by side for the query heads of a cache head; `splits` parts of `chunk` slots of
 // every context; `part` requests at a time.
 struct AttendPlan {
     int groups = 1, splits = 1, chunk = 0, pad = 0, part = 1;
@@ -1014,7 +1022,7 @@ inline AttendPlan attend_plan(int cus, int B, int q_heads, int heads, int d, int
     AttendPlan pl;
     const int64_t step = attend_step(elem_bytes, d);
     const int64_t range = window > 0 && (int64_t)window + 15 < max_length ? (int64_t)window + 15 : max_length;
-    pl.groups = (q_heads / heads + 15) / 16;
+    pl.groups = attend_groups(elem_bytes, d, q_heads / heads);
     const int64_t units = (int64_t)B * heads * pl.groups;
     int64_t chunk = (range * units / ((int64_t)cus * ATTEND_PER_CU) + step - 1) / step * step;
     if (chunk > ATTEND_CHUNK) chunk = ATTEND_CHUNK;
@@ -1033,7 +1041,7 @@ inline AttendPlan attend_plan(int cus, int B, int q_heads, int heads, int d, int
 }
 // Enough for these sizes and for shorter lengths and windows, which may be divided into more parts.
 inline size_t attend_workspace(int cus, int B, int q_heads, int heads, int d, int elem_bytes, int max_length, bool mass, size_t most) {
-    const int64_t step = attend_step(elem_bytes, d), units = (int64_t)B * heads * ((q_heads / heads + 15) / 16);
+    const int64_t step = attend_step(elem_bytes, d), units = (int64_t)B * heads * attend_groups(elem_bytes, d, q_heads / heads);
     int64_t splits = ((int64_t)cus * ATTEND_PER_CU + units - 1) / units, by_chunk = ((int64_t)max_length + ATTEND_CHUNK - 1) / ATTEND_CHUNK;
     const int64_t by_step = ((int64_t)max_length + step - 1) / step;
     splits = splits > by_chunk ? splits : by_chunk;
