@@ -238,16 +238,31 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 || (MT > 1 && T::bytes == 
         return (unsigned)page < (unsigned)a.cache.pages ? page : -1;
     };
 
-    int page[NT], page_next[NT];                          // of a tile (uniform), -1: none
+    // pages of tiles, looked up a step ahead; -1: none.  FINE: of the lane's row of K, and of its four rows of V
+    struct Pages { int k[NT], v[NT][FINE ? 4 : 1]; };
+    Pages page, page_next;
     u4 kr[NT][NS];
-    auto pages_of = [&](int k0, int (&out)[NT]) {
-#pragma unroll
-        for (int t = 0; t < NT; ++t) out[t] = FINE ? 0 : __builtin_amdgcn_readfirstlane(row_page(k0 + 16 * t));
-    };
-    auto load_k = [&](int k0, const int (&pg)[NT]) {
+    auto pages_of = [&](int k0, Pages &out) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const int key = k0 + 16 * t + m, p = FINE ? row_page(key) : pg[t];
+            if (!FINE) {
+                out.k[t] = __builtin_amdgcn_readfirstlane(row_page(k0 + 16 * t));
+                continue;
+            }
+            const int key = k0 + 16 * t + 4 * g;
+            out.k[t] = row_page(k0 + 16 * t + m);
+            out.v[t][0] = row_page(key);
+#pragma unroll
+            for (int i = 1; i < (FINE ? 4 : 1); ++i) {
+                if (slots_log >= 2) out.v[t][i] = key + i < end ? out.v[t][0] : -1;
+                else out.v[t][i] = row_page(key + i);
+            }
+        }
+    };
+    auto load_k = [&](int k0, const Pages &pg) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int key = k0 + 16 * t + m, p = pg.k[t];
             const char *row = k_head + (int64_t)max(p, 0) * a.cache.k_page + (FINE && p < 0 ? 0 : key & mask) * a.cache.k_slot;
 #pragma unroll
             for (int s = 0; s < NS; ++s) {
@@ -281,7 +296,7 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 || (MT > 1 && T::bytes == 
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int key = k0 + 16 * t + 4 * g + i, p = FINE ? row_page(key) : page[t];
+                const int key = k0 + 16 * t + 4 * g + i, p = FINE ? page.v[t][FINE ? i : 0] : page.k[t];
                 if (FINE && p >= 0 && key >= lo) there |= 1u << (4 * t + i);
                 const char *row = v_head + (int64_t)max(p, 0) * a.cache.v_page + (FINE && p < 0 ? 0 : key & mask) * a.cache.v_slot;
 #pragma unroll
@@ -308,14 +323,14 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 || (MT > 1 && T::bytes == 
             for (int t = 0; t < NT; ++t) x[mt][t] *= a.scale;
         bool whole = k0 >= lo && k0 + 16 * NT <= end;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) whole = whole && page[t] >= 0;
+        for (int t = 0; t < NT; ++t) whole = whole && page.k[t] >= 0;
         if (FINE || !whole) {                             // slots that do not count: no score, and no value that could be NaN
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int key = k0 + 16 * t + 4 * g + i;
-                    const bool use = FINE ? (there >> (4 * t + i)) & 1 : page[t] >= 0 && key >= lo && key < end;
+                    const bool use = FINE ? (there >> (4 * t + i)) & 1 : page.k[t] >= 0 && key >= lo && key < end;
                     if (!use) {
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt) x[mt][t][i] = -INFINITY;
@@ -395,8 +410,7 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 || (MT > 1 && T::bytes == 
                                 o[mt][u * CE + c] =
                                     __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[t][i][u][c]), x[mt][t][i], o[mt][u * CE + c], 0, 0, 0);
         }
-#pragma unroll
-        for (int t = 0; t < NT; ++t) page[t] = page_next[t];
+        page = page_next;
     }
 
     // the waves' sums, joined (of those that had a slot): lane 16 g + m holds elements CE (4 g + i) .. of every 16 CE, head 16 mt + m
