@@ -400,7 +400,8 @@ int ann_paged_attention(const void *q, int64_t q_row, int64_t q_head, int32_t B,
                         const int32_t *lengths, int32_t max_length, float scale, int32_t window,
                         void *out, float *lse, float *mass, int64_t mass_slots, void *stream);
 
-/* Bytes of workspace that ann_paged_attention uses for these sizes where it has them (with_mass: mass is given). */
+/* Bytes of workspace that are enough for ann_paged_attention at these sizes, shorter lengths and windows included, without taking fewer
+ * requests at a time than it would anyway (with_mass: mass is given).  The size of one request is the least that will do. */
 int64_t ann_paged_attention_workspace_bytes(int32_t B, int32_t q_heads, int32_t heads, int32_t d, int32_t dtype,
                                             int32_t max_length, int32_t with_mass);
 

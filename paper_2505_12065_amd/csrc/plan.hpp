@@ -1024,7 +1024,8 @@ inline AttendPlan attend_plan(int cus, int B, int q_heads, int heads, int d, int
     const int64_t range = window > 0 && (int64_t)window + 15 < max_length ? (int64_t)window + 15 : max_length;
     pl.groups = attend_groups(elem_bytes, d, q_heads / heads);
     const int64_t units = (int64_t)B * heads * pl.groups;
-    int64_t chunk = (range * units / ((int64_t)cus * ATTEND_PER_CU) + step - 1) / step * step;
+    const int64_t fill = (int64_t)cus * ATTEND_PER_CU;
+    int64_t chunk = (range * units + fill * step - 1) / (fill * step) * step;
     if (chunk > ATTEND_CHUNK) chunk = ATTEND_CHUNK;
     if (chunk < step) chunk = step;
     if (range > ATTEND_PARTS * chunk) chunk = (range + ATTEND_PARTS * step - 1) / (ATTEND_PARTS * step) * step;
@@ -1049,8 +1050,7 @@ inline size_t attend_workspace(int cus, int B, int q_heads, int heads, int d, in
     splits = splits < ATTEND_PARTS ? splits : ATTEND_PARTS;
     const int64_t longest = (max_length + ATTEND_PARTS * step - 1) / (ATTEND_PARTS * step) * step;
     const size_t one = attend_bytes(q_heads, d, splits, mass ? max_length + (longest > ATTEND_CHUNK ? longest : ATTEND_CHUNK) : 0);
-    const size_t part = one > most ? 1 : most / one;
-    return one * (part < (size_t)B ? part : (size_t)B);
+    return one > most ? one : one * (size_t)B < most ? one * (size_t)B : most;
 }
 
 // ---- rules on logits ------------------------------------------------------------------------------------
