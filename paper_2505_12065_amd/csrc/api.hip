@@ -267,7 +267,7 @@ int flat_search_run(const FlatPlan &pl, const void *X, int64_t N, int d, int dty
 }
 
 // ---- the step between two retrievals -----------------------------------------------------------
-constexpr int64_t GRID_MAX = 1 << 22;                    // workgroups of a launch (of up to 1024 threads)
+constexpr int64_t GRID_MAX = 1 << 22;                    // workgroups of a launch (a launch has fewer than 2^32 threads)
 
 int check_dtype(int32_t dtype) {
     return dtype == ANN_F16 || dtype == ANN_BF16 || dtype == ANN_F32 ? ANN_OK : fail(ANN_ERR_INVALID, "unknown element type %d", dtype);
@@ -537,7 +537,7 @@ int ann_cache_evict(const ann_paged_cache *cache, const int32_t *page_table, int
         return fail(ANN_ERR_INVALID, "first = %d and recent = %d do not fit the budget %d", first, recent, budget);
     if (off4({page_table, lengths, mass, new_page_table, kept, new_lengths, new_mass}))
         return fail(ANN_ERR_ALIGNMENT, "tables, lengths, masses and kept must be 4-byte aligned");
-    if ((int64_t)B * cache->heads * ((budget + 3) / 4) > GRID_MAX * 4)
+    if ((int64_t)B * cache->heads > GRID_MAX / 4 || (int64_t)B * cache->heads * (((int64_t)budget + 3) / 4) > GRID_MAX * 2)
         return fail(ANN_ERR_INVALID, "%d requests of %d heads with a budget of %d are too many for a call", B, cache->heads, budget);
     a.table = page_table; a.width = width; a.lengths = lengths; a.mass = mass; a.mass_slots = mass_slots;
     a.most = (int)(mass_slots < (int64_t)width * cache->slots ? mass_slots : (int64_t)width * cache->slots);

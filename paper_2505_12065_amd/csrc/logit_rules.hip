@@ -73,6 +73,7 @@ __global__ __launch_bounds__(THREADS) void logit_rules_kernel(RulesArgs a, int p
     constexpr uint32_t SEEN = 1u << CB, COUNT = SEEN - 1;
     extern __shared__ __align__(16) uint32_t word[];
     uint32_t *bias = LONG ? word + CHUNK : word;
+    __shared__ float first_values[THREADS];               // of the first biases
     const int id = xcd_block(), b = id / parts, v0 = id % parts * CHUNK, m = min(CHUNK, a.V - v0), tid = threadIdx.x;
     const E *in = static_cast<const E *>(a.logits) + b * a.row + v0;
     E *out = static_cast<E *>(a.out) + b * a.out_row + v0;
@@ -95,7 +96,7 @@ __global__ __launch_bounds__(THREADS) void logit_rules_kernel(RulesArgs a, int p
     const int32_t *tokens = a.tokens + (int64_t)b * a.T, *bias_tokens = a.bias_tokens + (int64_t)b * a.K;
     const float *bias_values = a.bias_values + (int64_t)b * a.K;
     const float repetition = a.repetition[b], presence = a.presence[b], frequency = a.frequency[b];
-    constexpr int AHEAD = 4;                              // loads of the history under way at a time
+    constexpr int AHEAD = 2;                              // loads of the history under way at a time
     u4 told[AHEAD];
     auto ask = [&](int t0) {
 #pragma unroll
@@ -107,11 +108,16 @@ __global__ __launch_bounds__(THREADS) void logit_rules_kernel(RulesArgs a, int p
     };
     int rest = -1, biased = -1;                           // what the last whole four leave; the first biases
     if ((n & ~3) + tid < n) rest = tokens[(n & ~3) + tid];
-    if (tid < a.K) biased = bias_tokens[tid];
+    float worth = 0.f;
+    if (tid < a.K) {
+        biased = bias_tokens[tid];
+        worth = bias_values[tid];
+    }
     ask(4 * tid);
     for (int i = tid * 4; i < (LONG ? 2 * CHUNK : CHUNK); i += THREADS * 4) *reinterpret_cast<u4 *>(word + i) = zero_chunk();
     __syncthreads();
     if (a.K > 0) {
+        first_values[tid] = worth;
         auto note_bias = [&](int i, int token) {
             if (token >= v0 && token - v0 < m) atomicMax(&bias[token - v0], LONG ? (uint32_t)i + 1 : (uint32_t)(i + 1) << (CB + 1));
         };
@@ -150,7 +156,7 @@ __global__ __launch_bounds__(THREADS) void logit_rules_kernel(RulesArgs a, int p
             y = y > 0.f ? y / repetition : y * repetition;
             if (w & COUNT) y = y - frequency * (float)(w & COUNT) - presence;
         }
-        if (k) y += bias_values[k - 1];
+        if (k) y += k <= THREADS ? first_values[k - 1] : bias_values[k - 1];
         return allowed ? y : -INFINITY;
     };
     auto number = [&](int i) { return LONG ? bias[i] : word[i] >> (CB + 1); };
@@ -185,17 +191,16 @@ __global__ __launch_bounds__(THREADS) void logit_rules_kernel(RulesArgs a, int p
 
 template <class T, int THREADS, int R, bool LONG>
 hipError_t launch(const RulesArgs &a, int B, hipStream_t stream) {
-    static size_t granted = 0;
     constexpr int CHUNK = THREADS * 8 * R;
-    const size_t bytes = (size_t)CHUNK * (LONG ? 8 : 4);
-    if (hipError_t e = allow_big_lds(reinterpret_cast<const void *>(logit_rules_kernel<T, THREADS, R, LONG>), bytes, &granted)) return e;
+    constexpr size_t bytes = (size_t)CHUNK * (LONG ? 8 : 4);
+    static_assert(bytes + THREADS * 4 <= 64 * 1024, "what a launch may take unasked");
     const int parts = (a.V + CHUNK - 1) / CHUNK;
     hipLaunchKernelGGL((logit_rules_kernel<T, THREADS, R, LONG>), dim3(parts * B), dim3(THREADS), bytes, stream, a, parts);
     return hipGetLastError();
 }
 template <class T>
 hipError_t launch(const RulesArgs &a, int cus, int B, hipStream_t stream) {
-    if (a.T >= 1 << RULES_COUNT_BITS) return launch<T, 512, 2, true>(a, B, stream);
+    if (a.T >= 1 << RULES_COUNT_BITS) return launch<T, 512, 1, true>(a, B, stream);
     const int chunk = rules_chunk(cus, B, a.V);
     return chunk == 2048 ? launch<T, 256, 1, false>(a, B, stream) : chunk == 4096 ? launch<T, 512, 1, false>(a, B, stream)
            : launch<T, 512, 2, false>(a, B, stream);
