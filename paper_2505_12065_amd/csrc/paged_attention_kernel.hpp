@@ -9,6 +9,8 @@
 // beside each other to a row, and are turned in registers, one byte permutation for two elements.
 #pragma once
 
+#include <type_traits>
+
 #include "launch.hpp"
 #include "paged.hpp"
 
@@ -52,6 +54,10 @@ __device__ __forceinline__ V stream_load(const V *p) {
 template <int CW> struct Words;
 template <> struct Words<2> { typedef uint32_t type __attribute__((ext_vector_type(2))); };
 template <> struct Words<4> { typedef u4 type; };
+
+// fp16 has no numbers below 2^-24, and a long context may have its weight in many slots that get less than that of the largest: weights are
+// 2^12 times as large in the loop, which keeps what makes up a millionth of the sum of 2^17 slots.
+template <class T> constexpr int ATTEND_LIFT = std::is_same_v<T, F16> ? 12 : 0;
 
 // Eight weights as an operand of 16 bits and what that leaves, as another: the product with V then has 16 bits (bf16) or more of
 // them.  One part alone would be off by as much as the output's own rounding; the second product costs nothing here.
@@ -356,14 +362,14 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 || (MT > 1 && T::bytes == 
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) most = fmaxf(most, x[mt][t][i]);
-            const float now = fmaxf(top[mt], column_max(most)), base = now == -INFINITY ? 0.f : now, keep = exp2_fast(top[mt] - base);
+            const float now = fmaxf(top[mt], column_max(most)), base = now == -INFINITY ? 0.f : now, keep = exp2_fast(top[mt] - base), lifted = base - ATTEND_LIFT<T>;
             top[mt] = now;
             sum[mt] *= keep;
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    x[mt][t][i] = exp2_fast(x[mt][t][i] - base);
+                    x[mt][t][i] = exp2_fast(x[mt][t][i] - lifted);
                     sum[mt] += x[mt][t][i];
                 }
 #pragma unroll
@@ -419,7 +425,7 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 || (MT > 1 && T::bytes == 
     const int used = min(ATTEND_WAVES, (max(end - first, 1) + 16 * NT - 1) / (16 * NT));
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-        sum[mt] = column_sum(sum[mt]);
+        sum[mt] = column_sum(sum[mt]) * (1.f / (1 << ATTEND_LIFT<T>));
         if (g == 0) {
             s_top[wave * HEADS + 16 * mt + m] = top[mt];
             s_sum[wave * HEADS + 16 * mt + m] = sum[mt];
@@ -432,7 +438,7 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 || (MT > 1 && T::bytes == 
         float all = -INFINITY;
 #pragma unroll
         for (int w = 0; w < ATTEND_WAVES; ++w) all = fmaxf(all, s_top[w * HEADS + head]);
-        const float mine = top[mt] == -INFINITY ? 0.f : exp2_fast(top[mt] - all);
+        const float mine = top[mt] == -INFINITY ? 0.f : exp2_fast(top[mt] - all) * (1.f / (1 << ATTEND_LIFT<T>));
         if (head < rows && wave < used) {
 #pragma unroll
             for (int u = 0; u < NU; ++u)

@@ -106,6 +106,25 @@ def test_attention_large_scores(dtype):
     attend(dtype, [700, 33, 129, 2000], 6, 2, 128, 16, seed=8, mass=True, edit=late)
 
 
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("below", [10.0, 16.0, 16.6, 17.5, 20.0, 24.0])
+def test_attention_weight_in_many_small_slots(dtype, below):
+    """One slot has the largest score and a value of zero; all of the output comes from thousands whose weight is e^-below of its."""
+    n, d = 20_000, 64
+
+    def edit(q, k, v, table, lens):
+        q[:] = 0
+        q[..., 0] = 4.0
+        k[:] = 0
+        v[:] = 1.0
+        at = table[0, 3000 // 16], slice(None), 3000 % 16
+        k[at] = 0
+        k[(*at, 0)] = below / 4
+        v[at] = 0
+        return q, k, v, table, lens
+    attend(dtype, [n], 4, 2, d, 16, scale=1.0, seed=12, mass=True, edit=edit)
+
+
 @pytest.mark.parametrize("page", [4, 16])
 @pytest.mark.parametrize("dtype", [F16, BF16, F32])
 def test_attention_empty_and_shared_pages(dtype, page):
