@@ -508,7 +508,7 @@ int ann_paged_attention(const void *q, int64_t q_row, int64_t q_head, int32_t B,
         a.mass = mass ? mass + (int64_t)b0 * cache->heads * mass_slots : nullptr;
         if (pl.one) {
             a.partial = static_cast<float *>(ws);
-            float *scores = a.partial + (size_t)b * q_heads * pl.splits * cache->d;     // (whole multiples of 16 bytes)
+            float *scores = a.partial + (pl.splits > 1 ? (size_t)b * q_heads * pl.splits * cache->d : 0);     // (whole multiples of 16 bytes)
             a.scores = mass ? scores : nullptr;
             a.stats = scores + (mass ? (size_t)b * q_heads * pl.pad : 0);
         }

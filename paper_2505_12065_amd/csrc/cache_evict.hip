@@ -198,7 +198,7 @@ hipError_t launch_cache_evict(int dtype, const EvictArgs &a, int B, hipStream_t 
     if (a.most <= 4 * THREADS) hipLaunchKernelGGL((evict_select_kernel<4, true>), dim3(rows), dim3(THREADS), 0, stream, a);
     else if (a.most <= 8 * THREADS) hipLaunchKernelGGL((evict_select_kernel<8, true>), dim3(rows), dim3(THREADS), 0, stream, a);
     else if (a.most <= 16 * THREADS) hipLaunchKernelGGL((evict_select_kernel<16, true>), dim3(rows), dim3(THREADS), 0, stream, a);
-    else hipLaunchKernelGGL((evict_select_kernel<4, false>), dim3(rows), dim3(THREADS), 0, stream, a);
+    else hipLaunchKernelGGL((evict_select_kernel<16, false>), dim3(rows), dim3(THREADS), 0, stream, a);
     if (hipError_t e = hipGetLastError()) return e;
     return chunks <= 8 ? copy<8>(a, rows, chunks, stream) : chunks <= 16 ? copy<16>(a, rows, chunks, stream)
            : chunks <= 32 ? copy<32>(a, rows, chunks, stream) : copy<64>(a, rows, chunks, stream);

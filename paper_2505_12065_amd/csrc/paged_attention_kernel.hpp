@@ -470,14 +470,14 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 || (MT > 1 && T::bytes == 
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[j] += z[j];
         }
-        if (a.splits > 1 || a.scores) {
+        if (at == 0 && a.stats) {
+            a.stats[((hq0 + r) * a.splits + part) * 2] = most;
+            a.stats[((hq0 + r) * a.splits + part) * 2 + 1] = total;
+        }
+        if (a.splits > 1) {
             float *to = a.partial + ((hq0 + r) * a.splits + part) * a.cache.d + at;
             reinterpret_cast<f4 *>(to)[0] = f4{y[0], y[1], y[2], y[3]};
             reinterpret_cast<f4 *>(to)[1] = f4{y[4], y[5], y[6], y[7]};
-            if (at == 0) {
-                a.stats[((hq0 + r) * a.splits + part) * 2] = most;
-                a.stats[((hq0 + r) * a.splits + part) * 2 + 1] = total;
-            }
         } else {
             const float f = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
@@ -492,11 +492,11 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 || (MT > 1 && T::bytes == 
 
 // What the parts of a context left, joined by a launch of its own: the workgroup that is done last could do it, but only behind fences that write back an XCD's
 // whole L2 (one request of 1500 slots: 16.9 us against 10.2).  The first workgroups take query heads: a wave to a head if there are few parts (FEW), else a
-// workgroup to a head.  Those behind them (scores given) take a piece of the slots of a cache head each.
+// workgroup to a head; none do where there is one part only.  Those behind them (scores given) take a piece of the slots of a cache head each.
 template <class T, bool FEW>
 __global__ __launch_bounds__(ATTEND_THREADS) void paged_attention_join_kernel(AttentionArgs a) {
     __shared__ __align__(16) float lds[ATTEND_THREADS * 8];
-    const int64_t heads_all = (int64_t)a.requests * a.q_heads, head_groups = FEW ? (heads_all + ATTEND_WAVES - 1) / ATTEND_WAVES : heads_all;
+    const int64_t heads_all = a.splits > 1 ? (int64_t)a.requests * a.q_heads : 0, head_groups = FEW ? (heads_all + ATTEND_WAVES - 1) / ATTEND_WAVES : heads_all;
     if ((int64_t)blockIdx.x < head_groups) {
         const int64_t r = FEW ? (int64_t)blockIdx.x * ATTEND_WAVES + threadIdx.x / WAVE : blockIdx.x;
         if (r < heads_all) attend_join<T, !FEW>(a, r, max(1, attend_span(a, (int)(r / a.q_heads)).parts), lds);
@@ -540,7 +540,7 @@ hipError_t launch_attention(const AttentionArgs &a, bool once, hipStream_t strea
     const int ve = attend_ve(a.cache.d), B = a.requests;
     if (hipError_t e = ve == 4 ? attend<T, 4>(a, once, stream) : ve == 8 ? attend<T, 8>(a, once, stream) : attend<T, 16>(a, once, stream)) return e;
     if (a.splits == 1 && !a.scores) return hipSuccess;
-    const int pieces = a.scores ? (a.pad + ATTEND_PIECE - 1) / ATTEND_PIECE : 0, rows = B * a.q_heads, mass = B * a.cache.heads * pieces;
+    const int pieces = a.scores ? (a.pad + ATTEND_PIECE - 1) / ATTEND_PIECE : 0, rows = a.splits > 1 ? B * a.q_heads : 0, mass = B * a.cache.heads * pieces;
     // (64 heads of 64 requests in 5 parts: 10.2 us a workgroup to a head, a wave to a head 5.9)
     if (a.splits <= ATTEND_FEW)
         hipLaunchKernelGGL((paged_attention_join_kernel<T, true>), dim3((rows + ATTEND_WAVES - 1) / ATTEND_WAVES + mass), dim3(ATTEND_THREADS), 0, stream, a);

@@ -1017,7 +1017,9 @@ constexpr int64_t ATTEND_CACHED = (int64_t)256 << 20;
 constexpr int ATTEND_PARTS = 256, ATTEND_CHUNK = 3328, ATTEND_PER_CU = 4;
 constexpr int64_t ATTEND_GRID = 1 << 22;                  // workgroups of a launch
 inline int64_t attend_step(int elem_bytes, int d) { return 16 * ATTEND_WAVES * attend_tiles(elem_bytes, attend_ve(d)); }
-inline size_t attend_bytes(int q_heads, int d, int64_t splits, int64_t pad) { return (size_t)q_heads * ((size_t)splits * (d + 2) + (size_t)pad) * 4; }
+inline size_t attend_bytes(int q_heads, int d, int64_t splits, int64_t pad) {
+    return (size_t)q_heads * ((splits > 1 ? (size_t)splits * d : 0) + (size_t)splits * 2 + (size_t)pad) * 4;
+}
 inline AttendPlan attend_plan(int cus, int B, int q_heads, int heads, int d, int elem_bytes, int max_length, int window, bool mass, size_t most) {
     AttendPlan pl;
     const int64_t step = attend_step(elem_bytes, d);
