@@ -4,6 +4,9 @@
 // tokens of the vocabulary of one request, asks for their logits (eight of a lane lie together), goes through the request's history and
 // biases while those are under way, and notes in a word for each token how often it was generated, whether it was seen, and its last bias.
 // Every workgroup of a request reads the whole history, so there are as few as keep the machine busy (rules_chunk).
+//
+// Bytes are the bound, and the histories' share of instructions comes on top.  192 rows of 128000 bf16 logits, a mask each, histories of up to 8100 tokens, 64 biases (0.11 GB): 27 us, 3.9 TB/s;
+// without histories and biases 16.5.  One row of 32000 fp32 logits: 4.5 us on the GPU, 5.6 a call.
 #include <type_traits>
 
 #include "launch.hpp"

@@ -998,7 +998,8 @@ inline size_t attend_lds_bytes(int ve, int mt, int G) {
 }
 
 // Tiles of 16 query heads that a workgroup takes, each reading of K and V then serving them all: two where there are more than 16 heads, except
-// where a wave's registers do not hold two (fp32, d > 128).
+// where a wave's registers do not hold two (fp32, d > 128).  32 heads to a cache head, d = 128, bf16, two tiles against two workgroups side by side: 64 x 4 cache heads of
+// 9216 slots 238 us against 279, 64 of 1000 17.3 and 19.7, of 8000 64 and 68; few contexts lose: 8 of 1000 11.0 and 9.7, of 16000 28.7 and 25.3.
 constexpr int attend_head_tiles(int elem_bytes, int ve, int G) { return G <= 16 || (elem_bytes == 4 && ve == 16) ? 1 : 2; }
 inline int attend_groups(int elem_bytes, int d, int G) {
     const int heads = 16 * attend_head_tiles(elem_bytes, attend_ve(d), G);
@@ -1013,7 +1014,13 @@ struct AttendPlan {
     size_t one = 0;              // bytes of workspace a request takes
 };
 constexpr int ATTEND_FEW = 16;                            // parts that a wave joins
+// Read past the last cache from this size on (which is that cache's): 64 x 8 cache heads of 9216 slots, 2.4 GB, 421 us without and 380 with it; one request of 30000,
+// 0.12 GB, 29.6 and 32.1 when it is read again and again.
 constexpr int64_t ATTEND_CACHED = (int64_t)256 << 20;
+// A part has at most ATTEND_CHUNK slots.  What it leaves is 8 d bytes of traffic for each query head, in the way of the reads: those 64 x 8 cache heads with 8 query heads each took 431 us
+// in parts of 1024, 405 of 2048, 393 of 3328 and 396 of 4096; ragged contexts, which larger parts divide less evenly, 460, 456, 454 and 462.
+// Where contexts are short or few there are ATTEND_PER_CU parts for a compute unit if all are of max_length: even contexts would do with fewer (8 x 1 cache head of 16000 slots, 8 query heads: 21.1 us with 4,
+// 19.7 with 2), ragged ones not (48 x 4 of up to 8100: 93 us with 4, 112 with 3, 136 with 2; 92 with 8, but one request of 131072 then 99.7 for 97.9).
 constexpr int ATTEND_PARTS = 256, ATTEND_CHUNK = 3328, ATTEND_PER_CU = 4;
 constexpr int64_t ATTEND_GRID = 1 << 22;                  // workgroups of a launch
 inline int64_t attend_step(int elem_bytes, int d) { return 16 * ATTEND_WAVES * attend_tiles(elem_bytes, attend_ve(d)); }
@@ -1035,7 +1042,7 @@ inline AttendPlan attend_plan(int cus, int B, int q_heads, int heads, int d, int
     pl.splits = (int)((range + chunk - 1) / chunk);
     pl.pad = (int)(pl.splits * chunk);
     if (pl.splits > 1 || mass) pl.one = attend_bytes(q_heads, d, pl.splits, mass ? pl.pad : 0);
-    pl.once = pl.groups == 1 && 2 * range * B * heads * d * elem_bytes > ATTEND_CACHED;
+    pl.once = pl.groups == 1 && 2.0 * range * B * heads * d * elem_bytes > ATTEND_CACHED;
     pl.part = B;
     if (pl.one > 0 && pl.one * (size_t)B > most) pl.part = pl.one > most ? 1 : (int)(most / pl.one);
     const int64_t grid = (int64_t)heads * pl.splits * pl.groups + (pl.one ? q_heads + (int64_t)heads * (mass ? pl.pad / 1024 + 1 : 0) : 0);
@@ -1058,16 +1065,19 @@ inline size_t attend_workspace(int cus, int B, int q_heads, int heads, int d, in
 // ---- rules on logits ------------------------------------------------------------------------------------
 constexpr int RULES_COUNT_BITS = 18;                      // of a token's word: the rest holds a mark and the number of one of ANN_BIAS_MAX biases
 static_assert(ANN_BIAS_MAX < 1 << (32 - RULES_COUNT_BITS - 1), "biases are numbered in what a count leaves");
-// Logits of a workgroup: the most that leave two workgroups for every compute unit.
+// Logits of a workgroup: the most that leave a workgroup for every compute unit.  Larger parts read the histories fewer times, smaller ones are more at once (histories of
+// 3000 to 6000 tokens, with this rule, and with two workgroups to a unit): 33 rows of 50001 5.8 us and 6.5, 8 of 128000 4.7 and 5.2, 16 of 128000 6.2 and 5.8;
+// 192 rows of 128000: 27.2 us with parts of 8192, 29.1 with 16384 (fewer fit a compute unit), 40 with 4096.
 inline int rules_chunk(int cus, int B, int V) {
     int chunk = 8192;
-    while (chunk > 2048 && (int64_t)B * ((V + chunk - 1) / chunk) < 2 * cus) chunk /= 2;
+    while (chunk > 2048 && (int64_t)B * ((V + chunk - 1) / chunk) < cus) chunk /= 2;
     return chunk;
 }
 
 // ---- norms and rotation -----------------------------------------------------------------------------------
 // Rows (heads of a token) that a group of lanes takes, `groups` of them a workgroup: one where there are few tokens; else all
-// of a token's, or, beyond 4, the even share of as few workgroups as do with 4.
+// of a token's, or, beyond 4, the even share of as few workgroups as do with 4.  48 heads of 128, one row and three: 128 tokens 3.1 us and 4.0, 256 3.5 and 4.3,
+// 512 4.6 and 5.0, 2048 11.6 and 11.6, 4096 20.1 and 19.0, 8192 45 and 39.
 inline int rotate_rows(int T, int heads, int groups) {
     const int rows = (heads + groups - 1) / groups, parts = (rows + 3) / 4;
     return T < 512 ? 1 : (rows + parts - 1) / parts;
