@@ -26,7 +26,8 @@ def close(got, want, bound, what):
     got = got.double().cpu().numpy() if isinstance(got, torch.Tensor) else got
     finite = np.isfinite(want)
     assert np.array_equal(np.isfinite(got), finite) and np.array_equal(got[~finite], want[~finite], equal_nan=True), what
-    off = np.abs(got - want)[finite] - np.broadcast_to(bound, want.shape)[finite]
+    with np.errstate(invalid="ignore"):
+        off = np.abs(got - want)[finite] - np.broadcast_to(bound, want.shape)[finite]
     assert off.size == 0 or off.max() <= 0, (what, off.max(), np.abs(got - want)[finite].max())
 
 
@@ -91,6 +92,21 @@ def test_attention_window(dtype, window):
 def test_attention_long(dtype, lengths, Hq, heads, d, page):
     attend(dtype, lengths, Hq, heads, d, page, seed=3)
     attend(dtype, lengths, Hq, heads, d, page, seed=3, mass=True, window=lengths[0] // 2, layout="slots")
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("Hq,heads,d", [(20, 1, 64), (40, 2, 128), (18, 1, 256), (34, 2, 104), (65, 1, 128), (6, 2, 64), (16, 1, 128), (8, 2, 256), (6, 3, 72), (4, 1, 200)])
+def test_attention_tiles_of_heads_and_wide_tables(dtype, wide, Hq, heads, d):
+    """More query heads than a tile has, and tables that are wide enough for 256 MiB of keys and values, of which only a little is there: caches of that size
+    are read past the last cache, and a context has the most parts that there can be."""
+    def edit(q, k, v, table, lens):
+        if wide:
+            width = (300 << 20) // (2 * len(lens) * heads * d * k.element_size() * 16)
+            table = torch.nn.functional.pad(table, (0, width - table.shape[1]), value=-1)
+        return q, k, v, table, lens
+    attend(dtype, [900, 0, 33, 4097], Hq, heads, d, 16, seed=d + Hq, edit=edit)
+    attend(dtype, [900, 0, 33, 4097], Hq, heads, d, 16, seed=d + Hq + 1, edit=edit, mass=True, window=700, layout="slots")
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16, F32])
