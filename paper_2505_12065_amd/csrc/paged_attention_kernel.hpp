@@ -50,6 +50,22 @@ __device__ __forceinline__ float column_sum(float x) {
     return __uint_as_float(a) + __uint_as_float(b);
 }
 
+// ... over all lanes of a wave
+__device__ __forceinline__ float wave_max(float x) {
+    x = fmaxf(x, __uint_as_float(lane_swap<1>(__float_as_uint(x))));
+    x = fmaxf(x, __uint_as_float(lane_swap<2>(__float_as_uint(x))));
+    x = fmaxf(x, __uint_as_float(lane_swap<4>(__float_as_uint(x))));
+    x = fmaxf(x, __uint_as_float(lane_swap<8>(__float_as_uint(x))));
+    return column_max(x);
+}
+__device__ __forceinline__ float wave_sum(float x) {
+    x += __uint_as_float(lane_swap<1>(__float_as_uint(x)));
+    x += __uint_as_float(lane_swap<2>(__float_as_uint(x)));
+    x += __uint_as_float(lane_swap<4>(__float_as_uint(x)));
+    x += __uint_as_float(lane_swap<8>(__float_as_uint(x)));
+    return column_sum(x);
+}
+
 template <bool ONCE, class V>
 __device__ __forceinline__ V stream_load(const V *p) {
     if constexpr (ONCE) return __builtin_nontemporal_load(p);
@@ -117,31 +133,86 @@ __device__ __forceinline__ AttendSpan attend_span(const AttentionArgs &a, int b)
 __device__ __forceinline__ void attend_stats(const AttentionArgs &a, int64_t r, int parts, float &most, float &total) {
     const float *st = a.stats + r * a.splits * 2;
     const int lane = threadIdx.x & (WAVE - 1);
-    most = -INFINITY;
-    total = 0.f;
-    for (int s = lane; s < parts; s += WAVE) most = fmaxf(most, st[2 * s]);
-#pragma unroll
-    for (int k = 1; k < WAVE; k *= 2) most = fmaxf(most, __shfl_xor(most, k));
-    for (int s = lane; s < parts; s += WAVE) total += st[2 * s + 1] * (st[2 * s] == -INFINITY ? 1.f : exp2_fast(st[2 * s] - most));
-#pragma unroll
-    for (int k = 1; k < WAVE; k *= 2) total += __shfl_xor(total, k);
+    float m = -INFINITY, t = 0.f;
+    for (int s = lane; s < parts; s += WAVE) m = fmaxf(m, st[2 * s]);
+    most = wave_max(m);
+    for (int s = lane; s < parts; s += WAVE) t += st[2 * s + 1] * (st[2 * s] == -INFINITY ? 1.f : exp2_fast(st[2 * s] - most));
+    total = wave_sum(t);
 }
 __device__ __forceinline__ float attend_lse(float most, float total) {
     return total == 0.f ? -INFINITY : (most == -INFINITY ? 0.f : most) * 0.6931471805599453f + logf(total);
 }
+// Eight elements of head row r, a sum of its parts
+template <class T>
+__device__ __forceinline__ void attend_write(const AttentionArgs &a, int64_t r, int at, float (&y)[8], float most, float total) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] = total == 0.f ? 0.f : y[j] / total;
+    Eight<T> e;
+    e.set(y);
+    e.store(static_cast<char *>(a.out) + (r * a.cache.d + at) * T::bytes);
+    if (at == 0 && a.lse) a.lse[r] = attend_lse(most, total);
+}
 
-// The parts of head row r, joined by one wave (WIDE: by the workgroup).  lds: 8 floats for each of its threads.
-template <class T, bool WIDE>
-__device__ __forceinline__ void attend_join(const AttentionArgs &a, int64_t r, int parts, float *lds) {
-    const int per_row = a.cache.d / 8;                    // lanes to a row, at most 32
-    const int member = WIDE ? threadIdx.x : threadIdx.x & (WAVE - 1), side = (WIDE ? ATTEND_THREADS : WAVE) / per_row;   // parts side by side
-    const float *from = a.partial + r * a.splits * a.cache.d + (member % per_row) * 8;
+// The parts of head row r, joined: by a wave if there are at most ATTEND_FEW of them, which are then all asked for before the request's length says how many
+// there are; else by the workgroup.  per_row lanes (at most 32) share a row, and rows lie side by side.  lds: 8 floats for each thread.
+template <class T>
+__device__ __forceinline__ void attend_join_few(const AttentionArgs &a, int64_t r, float *lds) {
+    const int per_row = a.cache.d / 8, lane = threadIdx.x & (WAVE - 1), side = WAVE / per_row, first = lane / per_row;
+    const float *from = a.partial + r * a.splits * a.cache.d + (lane % per_row) * 8;
+    const float2 own = lane < a.splits ? reinterpret_cast<const float2 *>(a.stats)[r * a.splits + lane] : float2{-INFINITY, 0.f};
+    constexpr int AHEAD = 4;
+    f4 z[AHEAD][2];
+    auto ask = [&](int s0) {
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int s = s0 + k * side;
+            if (first < side && s < a.splits) {
+                z[k][0] = reinterpret_cast<const f4 *>(from + (int64_t)s * a.cache.d)[0];
+                z[k][1] = reinterpret_cast<const f4 *>(from + (int64_t)s * a.cache.d)[1];
+            }
+        }
+    };
+    ask(first);
+    const int parts = max(1, attend_span(a, (int)(r / a.q_heads)).parts);
+    const float t = lane < parts ? own.x : -INFINITY, most = wave_max(t);
+    // (a part without a score has a sum of 0, or NaN, and counts as it is)
+    const float f = lane >= parts ? 0.f : t == -INFINITY ? 1.f : exp2_fast(t - most), total = wave_sum(lane < parts ? own.y * f : 0.f);
+    float y[8] = {};
+    for (int s0 = first; s0 - first < parts; s0 += AHEAD * side) {
+        if (s0 != first) ask(s0);
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int s = s0 + k * side;
+            const float g = __shfl(f, s & (WAVE - 1));
+            if (first < side && s < parts) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] = fmaf(z[k][j / 4][j % 4], g, y[j]);
+            }
+        }
+    }
+    f4 *mine = reinterpret_cast<f4 *>(lds + threadIdx.x * 8);
+    mine[0] = f4{y[0], y[1], y[2], y[3]};
+    mine[1] = f4{y[4], y[5], y[6], y[7]};
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");                  // (what the wave itself wrote)
+    if (lane < per_row) {
+        for (int s = 1; s < side && s < parts; ++s) {
+            const f4 *o = reinterpret_cast<const f4 *>(lds + (threadIdx.x + s * per_row) * 8);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] += o[j / 4][j % 4];
+        }
+        attend_write<T>(a, r, 8 * lane, y, most, total);
+    }
+}
+template <class T>
+__device__ __forceinline__ void attend_join(const AttentionArgs &a, int64_t r, float *lds) {
+    const int parts = max(1, attend_span(a, (int)(r / a.q_heads)).parts), per_row = a.cache.d / 8, tid = threadIdx.x, side = ATTEND_THREADS / per_row;
+    const float *from = a.partial + r * a.splits * a.cache.d + (tid % per_row) * 8;
     const float *st = a.stats + r * a.splits * 2;
     float most, total, y[8] = {};
     attend_stats(a, r, parts, most, total);
-    if (member < side * per_row) {
+    if (tid < side * per_row) {
 #pragma unroll 4
-        for (int s = member / per_row; s < parts; s += side) {
+        for (int s = tid / per_row; s < parts; s += side) {
             const f4 *z = reinterpret_cast<const f4 *>(from + (int64_t)s * a.cache.d);
             const f4 z0 = z[0], z1 = z[1];
             const float t = st[2 * s], f = t == -INFINITY ? 1.f : exp2_fast(t - most);
@@ -152,25 +223,18 @@ __device__ __forceinline__ void attend_join(const AttentionArgs &a, int64_t r, i
             }
         }
     }
-    f4 *mine = reinterpret_cast<f4 *>(lds + threadIdx.x * 8);
+    f4 *mine = reinterpret_cast<f4 *>(lds + tid * 8);
     mine[0] = f4{y[0], y[1], y[2], y[3]};
     mine[1] = f4{y[4], y[5], y[6], y[7]};
-    if (WIDE) __syncthreads();
-    else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");             // (what the wave itself wrote)
-    if (member < per_row) {
+    __syncthreads();
+    if (tid < per_row) {
         for (int s = 1; s < side && s < parts; ++s) {
-            const f4 *z = reinterpret_cast<const f4 *>(lds + (threadIdx.x + s * per_row) * 8);
+            const f4 *o = reinterpret_cast<const f4 *>(lds + (tid + s * per_row) * 8);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] += z[j / 4][j % 4];
+            for (int j = 0; j < 8; ++j) y[j] += o[j / 4][j % 4];
         }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = total == 0.f ? 0.f : y[j] / total;
-        Eight<T> e;
-        e.set(y);
-        e.store(static_cast<char *>(a.out) + (r * a.cache.d + 8 * member) * T::bytes);
-        if (member == 0 && a.lse) a.lse[r] = attend_lse(most, total);
+        attend_write<T>(a, r, 8 * tid, y, most, total);
     }
-    if (!WIDE) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
 // By a workgroup: the weights of slots start + j0 .. of a cache head, ATTEND_PIECE of them, summed over its query heads in their order and added to mass.
@@ -504,7 +568,10 @@ __global__ __launch_bounds__(ATTEND_THREADS) void paged_attention_join_kernel(At
     const int64_t heads_all = a.splits > 1 ? (int64_t)a.requests * a.q_heads : 0, head_groups = FEW ? (heads_all + ATTEND_WAVES - 1) / ATTEND_WAVES : heads_all;
     if ((int64_t)blockIdx.x < head_groups) {
         const int64_t r = FEW ? (int64_t)blockIdx.x * ATTEND_WAVES + threadIdx.x / WAVE : blockIdx.x;
-        if (r < heads_all) attend_join<T, !FEW>(a, r, max(1, attend_span(a, (int)(r / a.q_heads)).parts), lds);
+        if (r < heads_all) {
+            if (FEW) attend_join_few<T>(a, r, lds);
+            else attend_join<T>(a, r, lds);
+        }
         return;
     }
     const int64_t id = blockIdx.x - head_groups;
