@@ -60,16 +60,23 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
         return;
     }
     const int lo = a.first, hi = n - a.recent;            // the slots that are chosen from
-    float value[KR];
+    constexpr bool VALUES = KR <= 16;                     // (registers: else the kept ones' are read again)
+    float value[VALUES ? KR : 1];
     uint32_t rank[KR];
     auto load = [&](int i0) {                             // slots i0, i0 + THREADS, ...
+        constexpr int AT_ONCE = KR < 16 ? KR : 16;
 #pragma unroll
-        for (int k = 0; k < KR; ++k) value[k] = i0 + k * THREADS < n ? mass[i0 + k * THREADS] : 0.f;
+        for (int k0 = 0; k0 < KR; k0 += AT_ONCE) {
+            float x[AT_ONCE];
 #pragma unroll
-        for (int k = 0; k < KR; ++k) {
-            const int i = i0 + k * THREADS;
-            // (one that is not there comes after all that are, like a NaN behind them)
-            rank[k] = i >= n ? 0 : i < lo || i >= hi ? KEEP : rank_of(value[k]);
+            for (int k = 0; k < AT_ONCE; ++k) x[k] = i0 + (k0 + k) * THREADS < n ? mass[i0 + (k0 + k) * THREADS] : 0.f;
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) {
+                const int i = i0 + (k0 + k) * THREADS;
+                // (one that is not there comes after all that are, like a NaN behind them)
+                rank[k0 + k] = i >= n ? 0 : i < lo || i >= hi ? KEEP : rank_of(x[k]);
+                if (VALUES) value[VALUES ? k0 + k : 0] = x[k];
+            }
         }
     };
     if (HELD) load(tid);
@@ -122,12 +129,10 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
     for (int tile = 0; tile < tiles; ++tile) {
         const int i0 = tile * THREADS * KR + tid;
         if (!HELD) load(i0);
-        uint32_t m0[KR], e0[KR], m_of = 0, e_of = 0;      // kept for sure, and of rank `prefix`, among the lanes before; lane k: in ballot k
+        uint32_t m_of = 0, e_of = 0;                      // kept for sure, and of rank `prefix`; lane k: in ballot k
 #pragma unroll
         for (int k = 0; k < KR; ++k) {
             const uint64_t m = __ballot(rank[k] > prefix), e = __ballot(rank[k] == prefix);
-            m0[k] = __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
-            e0[k] = __builtin_amdgcn_mbcnt_hi((uint32_t)(e >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)e, 0));
             if (lane == k) {
                 m_of = __popcll(m);
                 e_of = __popcll(e);
@@ -153,11 +158,13 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a) {
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < KR; ++k) {
-            const int i = i0 + k * THREADS;
-            const uint32_t m = more + higher[k * WAVES + wave] + m0[k], e = as_much + equal[k * WAVES + wave] + e0[k];
+            const uint64_t mb = __ballot(rank[k] > prefix), eb = __ballot(rank[k] == prefix);   // (those among the lanes before)
+            const uint32_t m = more + higher[k * WAVES + wave] + __builtin_amdgcn_mbcnt_hi((uint32_t)(mb >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mb, 0));
+            const uint32_t e = as_much + equal[k * WAVES + wave] + __builtin_amdgcn_mbcnt_hi((uint32_t)(eb >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)eb, 0));
             if (rank[k] > prefix || (rank[k] == prefix && e < need)) {
+                const int i = i0 + k * THREADS;
                 kept[m + min(e, need)] = i;
-                new_mass[m + min(e, need)] = value[k];
+                new_mass[m + min(e, need)] = VALUES ? value[VALUES ? k : 0] : mass[i];
             }
         }
         more += s_all.x;
@@ -197,11 +204,12 @@ hipError_t copy(const EvictArgs &a, int rows, int chunks, hipStream_t stream) {
 
 hipError_t launch_cache_evict(int dtype, const EvictArgs &a, int B, hipStream_t stream) {
     const int rows = B * a.cache.heads, chunks = a.cache.d * elem_bytes(dtype) / 16;
-    // A row has at most a.most slots.  As few ranks a thread as hold it (a choice among 6000 with 8: 9.2 us; among 16000 with 16: 13.6); longer rows are read again for every digit
-    // (among 25000: 24 us).
+    // A row has at most a.most slots.  As few ranks a thread as hold it (a choice among 6000 with 8: 9.2 us; among 16000 with 16: 13.6; among
+    // 32000 with 32: 20.5, or 27 if they are read again for every digit), longer rows are read again (60000: 53; 64 ranks do not fit a thread's registers: 61; 130000: 102).
     if (a.most <= 4 * THREADS) hipLaunchKernelGGL((evict_select_kernel<4, true>), dim3(rows), dim3(THREADS), 0, stream, a);
     else if (a.most <= 8 * THREADS) hipLaunchKernelGGL((evict_select_kernel<8, true>), dim3(rows), dim3(THREADS), 0, stream, a);
     else if (a.most <= 16 * THREADS) hipLaunchKernelGGL((evict_select_kernel<16, true>), dim3(rows), dim3(THREADS), 0, stream, a);
+    else if (a.most <= 32 * THREADS) hipLaunchKernelGGL((evict_select_kernel<32, true>), dim3(rows), dim3(THREADS), 0, stream, a);
     else hipLaunchKernelGGL((evict_select_kernel<16, false>), dim3(rows), dim3(THREADS), 0, stream, a);
     if (hipError_t e = hipGetLastError()) return e;
     return chunks <= 8 ? copy<8>(a, rows, chunks, stream) : chunks <= 16 ? copy<16>(a, rows, chunks, stream)

@@ -333,7 +333,8 @@ def test_rotate_part_of_a_larger_tensor_and_non_finite_values():
 @pytest.mark.parametrize("lengths,budget,first,recent,page,layout", [
     ([0, 1, 63, 64, 65, 200], 64, 0, 0, 16, "heads"), ([300, 5, 299], 100, 4, 32, 8, "slots"), ([1000], 1, 0, 0, 16, "heads"),
     ([1000, 70], 60, 60, 0, 4, "heads"), ([1000, 61], 60, 0, 60, 32, "slots"), ([5000, 4999, 77], 2000, 16, 500, 64, "heads"),
-    ([2100, 2000], 33, 1, 1, 1, "heads"), ([20_000], 1500, 0, 7, 128, "heads")])
+    ([2100, 2000], 33, 1, 1, 1, "heads"), ([20_000], 1500, 0, 7, 128, "heads"),
+    ([40_000, 33_000], 3000, 5, 100, 64, "slots")])
 def test_evict(dtype, d, lengths, budget, first, recent, page, layout):
     heads, seed = 3, budget + d
     g = torch.Generator().manual_seed(seed)
