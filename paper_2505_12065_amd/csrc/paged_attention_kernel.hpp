@@ -11,7 +11,7 @@
 // Bound by reading K and V once: G = q_heads / heads query heads make G multiply-adds of a 16-bit element, a tenth of what the matrix cores do in the
 // time even where 15 of 16 columns are empty (G = 1).  So the loop asks for V of these slots and K of the next before it needs either, 16 KB a wave at d = 128, three
 // workgroups to a compute unit.  64 requests of 9216 slots, 8 cache heads of 128, bf16 (2.4 GB): 390 us, 6.2 TB/s, which is what a loop of loads reads; G = 1: 6.35,
-// d = 256: 5.8, fp32: 5.6, pages of 8 slots 5.5, of one 4.2 (a look-up for each row).  One request of 131072 slots (0.54 GB): 103 us a call.
+// d = 256: 6.1, fp32: 6.2, pages of 8 slots 5.7, of one 4.2 (a look-up for each row).  One request of 131072 slots (0.54 GB): 103 us a call.
 #pragma once
 
 #include <type_traits>
@@ -272,7 +272,7 @@ __device__ __forceinline__ void attend_add_mass(const AttentionArgs &a, int b, i
 // FINE: pages of less than 16 slots, looked up for every row and not for a tile.  FULL: d is 16 VE.  ONCE: keys and values are more than the
 // last cache holds, and are read past it.  MT: tiles of 16 query heads.
 template <class T, int VE, int MT, bool FINE, bool FULL, bool ONCE>
-__global__ __launch_bounds__(ATTEND_THREADS, VE == 16 || (MT > 1 && T::bytes == 4) ? 1 : 2) void paged_attention_kernel(AttentionArgs a) {
+__global__ __launch_bounds__(ATTEND_THREADS, (MT > 1 && (VE == 16 || T::bytes == 4)) || (VE == 16 && T::bytes == 2 && (FINE || !FULL)) ? 1 : 2) void paged_attention_kernel(AttentionArgs a) {
     typedef AttendShape<T, VE> Sh;
     typedef typename Words<Sh::CW>::type VChunk;
     constexpr int NT = Sh::NT, NS = Sh::NS, NU = Sh::NU, CE = Sh::CE, STEP = 16 * NT * ATTEND_WAVES;
@@ -293,16 +293,26 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 || (MT > 1 && T::bytes == 
     if (part >= max(span.parts, 1)) return;               // (the first part of nothing says so)
     const int64_t hq0 = (int64_t)b * a.q_heads + h * G + 16 * MT * hg;
 
-    u4 q[MT][NS];
+    // (LDS: what the waves' sums are written over afterwards)
+    constexpr bool Q_LDS = attend_q_in_lds(VE);
+    constexpr int HEADS = 16 * MT, LD = attend_lds_row(VE);
+    float *s_top = lds, *s_sum = lds + ATTEND_WAVES * HEADS, *s_o = lds + 2 * ATTEND_WAVES * HEADS;
+    u4 *s_q = reinterpret_cast<u4 *>(s_o), q[Q_LDS ? 1 : MT][Q_LDS ? 1 : NS];
+    auto query = [&](int mt, int s) {                     // this lane's operand of step s
+        u4 x = zero_chunk();
+        const int at = (4 * s + g) * 16;
+        if (16 * mt + m < rows && (FULL || at < a.cache.d * T::bytes))
+            x = load_chunk(static_cast<const char *>(a.q) + b * a.q_row + (h * G + 16 * (MT * hg + mt) + m) * a.q_head + at);
+        return x;
+    };
+    if constexpr (Q_LDS) {
+        for (int i = wave; i < MT * NS; i += ATTEND_WAVES) s_q[i * WAVE + lane] = query(i / NS, i % NS);
+    } else {
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+        for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            q[mt][s] = zero_chunk();
-            const int at = (4 * s + g) * 16;
-            if (16 * mt + m < rows && (FULL || at < a.cache.d * T::bytes))
-                q[mt][s] = load_chunk(static_cast<const char *>(a.q) + b * a.q_row + (h * G + 16 * (MT * hg + mt) + m) * a.q_head + at);
-        }
+            for (int s = 0; s < NS; ++s) q[mt][s] = query(mt, s);
+    }
     const int32_t *table = a.table + (int64_t)b * a.width;
     const int slots_log = a.cache.slots_log, mask = (1 << slots_log) - 1;
     const char *k_head = a.cache.k + h * a.cache.k_head, *v_head = a.cache.v + h * a.cache.v_head;
@@ -362,6 +372,7 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 || (MT > 1 && T::bytes == 
         pages_of(k0, page);
         load_k(k0, page);
     }
+    if constexpr (Q_LDS) __syncthreads();
     for (; k0 < end; k0 += STEP) {
         const bool more = k0 + STEP < end;
         if (more) pages_of(k0 + STEP, page_next);
@@ -382,6 +393,7 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 || (MT > 1 && T::bytes == 
                 }
             }
         }
+        if constexpr (Q_LDS) asm volatile("" ::: "memory");                 // (the queries stay where they are)
         f4 x[MT][NT];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
@@ -389,7 +401,7 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 || (MT > 1 && T::bytes == 
             for (int t = 0; t < NT; ++t) {
                 x[mt][t] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int s = 0; s < NS; ++s) x[mt][t] = scores_step<T>(kr[t][s], q[mt][s], x[mt][t]);
+                for (int s = 0; s < NS; ++s) x[mt][t] = scores_step<T>(kr[t][s], Q_LDS ? s_q[(mt * NS + s) * WAVE + lane] : q[Q_LDS ? 0 : mt][Q_LDS ? 0 : s], x[mt][t]);
             }
         if (more) load_k(k0 + STEP, page_next);
 #pragma unroll
@@ -489,8 +501,6 @@ __global__ __launch_bounds__(ATTEND_THREADS, VE == 16 || (MT > 1 && T::bytes == 
     }
 
     // the waves' sums, joined (of those that had a slot): lane 16 g + m holds elements CE (4 g + i) .. of every 16 CE, head 16 mt + m
-    constexpr int HEADS = 16 * MT, LD = attend_lds_row(VE);
-    float *s_top = lds, *s_sum = lds + ATTEND_WAVES * HEADS, *s_o = lds + 2 * ATTEND_WAVES * HEADS;
     const int used = min(ATTEND_WAVES, (max(end - first, 1) + 16 * NT - 1) / (16 * NT));
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
@@ -584,7 +594,7 @@ __global__ __launch_bounds__(ATTEND_THREADS) void paged_attention_join_kernel(At
 template <class T, int VE, int MT, bool FINE, bool FULL, bool ONCE>
 hipError_t attend(const AttentionArgs &a, hipStream_t stream) {
     static size_t granted = 0;
-    const size_t bytes = attend_lds_bytes(VE, MT, a.q_heads / a.cache.heads);
+    const size_t bytes = attend_lds_bytes(T::bytes, VE, MT, a.q_heads / a.cache.heads);
     const void *kernel = reinterpret_cast<const void *>(paged_attention_kernel<T, VE, MT, FINE, FULL, ONCE>);
     if (hipError_t e = allow_big_lds(kernel, bytes, &granted)) return e;
     const int items = (a.requests * a.cache.heads * a.splits + 7) / 8 * 8;

@@ -993,8 +993,12 @@ inline int attend_ve(int d) { return d <= 64 ? 4 : d <= 128 ? 8 : 16; }
 // Tiles of 16 slots that a wave takes at a time: as many as its registers hold twice (K of the next, V of this).
 constexpr int attend_tiles(int elem_bytes, int ve) { return elem_bytes == 2 ? (ve == 4 ? 4 : 2) : ve == 16 ? 1 : 2; }
 constexpr int attend_lds_row(int ve) { return 16 * ve + 4; }
-inline size_t attend_lds_bytes(int ve, int mt, int G) {
-    return (size_t)(2 * ATTEND_WAVES * 16 * mt + ATTEND_WAVES * (G < 16 * mt ? G : 16 * mt) * attend_lds_row(ve)) * 4;
+// Queries of d > 128 are in LDS and not in registers: K, V and the sums alone take 192 of a lane's 256, beyond which every step moves them (8 cache heads of 256, fp16: 16 x 1000 slots 45 us
+// with all in registers, 29 so; 64 requests of 9216 of 4 heads 420 and 394).
+constexpr bool attend_q_in_lds(int ve) { return ve == 16; }
+inline size_t attend_lds_bytes(int elem_bytes, int ve, int mt, int G) {
+    const int o = ATTEND_WAVES * (G < 16 * mt ? G : 16 * mt) * attend_lds_row(ve), q = attend_q_in_lds(ve) ? 16 * mt * 16 * ve * elem_bytes / 4 : 0;
+    return (size_t)(2 * ATTEND_WAVES * 16 * mt + (o > q ? o : q)) * 4;
 }
 
 // Tiles of 16 query heads that a workgroup takes, each reading of K and V then serving them all: two where there are more than 16 heads, except
@@ -1037,6 +1041,9 @@ inline AttendPlan attend_plan(int cus, int B, int q_heads, int heads, int d, int
     int64_t chunk = (range * units + fill * step - 1) / (fill * step) * step;
     if (chunk > ATTEND_CHUNK) chunk = ATTEND_CHUNK;
     if (chunk < step) chunk = step;
+    // (A second step costs less than a second launch: 8 cache heads of 128, bf16, 150 slots 6.0 us against 8.2, 250 6.7 and 8.3; d = 64, 500 slots 7.6 and 9.0; fp32 10.1 and 10.8, 11.0 and 10.9.
+    // A third costs as much, or more: 380 slots 8.2 and 8.2, fp32 14.8 and 10.9.)
+    if (range <= 2 * step) chunk = 2 * step;
     if (range > ATTEND_PARTS * chunk) chunk = (range + ATTEND_PARTS * step - 1) / (ATTEND_PARTS * step) * step;
     pl.chunk = (int)chunk;
     pl.splits = (int)((range + chunk - 1) / chunk);

@@ -14,7 +14,7 @@ using namespace ann;
 extern "C" void attend(int cus, int B, int q_heads, int heads, int d, int eb, int max_length, int window, int mass, int64_t most, int64_t *out) {
     const AttendPlan p = attend_plan(cus, B, q_heads, heads, d, eb, max_length, window, mass != 0, (size_t)most);
     const int G = q_heads / heads, mt = attend_head_tiles(eb, attend_ve(d), G);
-    const int64_t v[] = {p.groups, p.splits, p.chunk, p.pad, p.part, p.once, (int64_t)p.one, attend_step(eb, d), mt, (int64_t)attend_lds_bytes(attend_ve(d), mt, G)};
+    const int64_t v[] = {p.groups, p.splits, p.chunk, p.pad, p.part, p.once, (int64_t)p.one, attend_step(eb, d), mt, (int64_t)attend_lds_bytes(eb, attend_ve(d), mt, G)};
     for (int i = 0; i < 10; ++i) out[i] = v[i];
 }
 extern "C" int64_t workspace(int cus, int B, int q_heads, int heads, int d, int eb, int max_length, int mass, int64_t most) {
