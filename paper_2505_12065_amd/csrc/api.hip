@@ -496,7 +496,7 @@ int ann_paged_attention(const void *q, int64_t q_row, int64_t q_head, int32_t B,
         if (int rc = workspace_for(st, &st->ws, pl.one * pl.part, stream, &ws)) return rc;
     a.q_row = q_row * e; a.q_head = q_head * e; a.q_heads = q_heads;
     a.width = width; a.max_length = max_length; a.window = window; a.scale = scale * 1.4426950408889634f;
-    a.mass_slots = mass_slots; a.groups = pl.groups; a.splits = pl.splits; a.chunk = pl.chunk; a.pad = pl.pad;
+    a.mass_slots = mass_slots; a.groups = pl.groups; a.splits = pl.splits; a.chunk = pl.chunk; a.pad = pl.pad; a.keep = pl.keep;
     for (int b0 = 0; b0 < B; b0 += pl.part) {
         const int b = B - b0 < pl.part ? B - b0 : pl.part;
         a.q = static_cast<const char *>(q) + b0 * a.q_row;

@@ -135,9 +135,9 @@ struct AttentionArgs {
     float *lse, *mass;
     int64_t mass_slots;
     int requests;
-    int groups, splits, chunk, pad;   // attend_plan
+    int groups, splits, chunk, pad, keep;   // attend_plan
     float *partial, *stats;   // [B, q_heads, splits, d], [B, q_heads, splits, 2] (largest exponent, sum), where the parts are joined
-    float *scores;            // [B, q_heads, pad] if mass is given: exponents of 2, from the first tile of the window on
+    float *scores;            // [B, q_heads, pad] if mass is given and keep is 0: exponents of 2, from the first tile of the window on
 };
 // (scale: times log2 e; once: read past the last cache)
 hipError_t launch_paged_attention_f16(const AttentionArgs &args, bool once, hipStream_t stream);

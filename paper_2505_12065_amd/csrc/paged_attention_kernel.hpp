@@ -297,6 +297,7 @@ __global__ __launch_bounds__(ATTEND_THREADS, (MT > 1 && (VE == 16 || T::bytes ==
     constexpr bool Q_LDS = attend_q_in_lds(VE);
     constexpr int HEADS = 16 * MT, LD = attend_lds_row(VE);
     float *s_top = lds, *s_sum = lds + ATTEND_WAVES * HEADS, *s_o = lds + 2 * ATTEND_WAVES * HEADS;
+    float *s_x = s_o + max(ATTEND_WAVES * rows * LD, Q_LDS ? MT * NS * WAVE * 4 : 0);   // scores that stay here
     u4 *s_q = reinterpret_cast<u4 *>(s_o), q[Q_LDS ? 1 : MT][Q_LDS ? 1 : NS];
     auto query = [&](int mt, int s) {                     // this lane's operand of step s
         u4 x = zero_chunk();
@@ -427,13 +428,16 @@ __global__ __launch_bounds__(ATTEND_THREADS, (MT > 1 && (VE == 16 || T::bytes ==
                 }
             }
         }
-        if (a.scores) {
+        if (a.scores || a.keep) {
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
                 if (16 * mt + m < rows) {
+                    float *to = a.keep ? s_x + (16 * mt + m) * a.keep : a.scores + (hq0 + 16 * mt + m) * a.pad;
 #pragma unroll
-                    for (int t = 0; t < NT; ++t)
-                        *reinterpret_cast<f4 *>(a.scores + (hq0 + 16 * mt + m) * a.pad + (k0 - start + 16 * t + 4 * g)) = x[mt][t];
+                    for (int t = 0; t < NT; ++t) {
+                        const int at = k0 - start + 16 * t + 4 * g;
+                        if (!a.keep || at < n - start) *reinterpret_cast<f4 *>(to + at) = x[mt][t];
+                    }
                 }
         }
 #pragma unroll
@@ -567,6 +571,27 @@ __global__ __launch_bounds__(ATTEND_THREADS, (MT > 1 && (VE == 16 || T::bytes ==
             if (at == 0 && a.lse) a.lse[hq0 + r] = attend_lse(most, total);
         }
     }
+    if (!a.keep) return;
+
+    // the only part: the weights of its slots, summed over the query heads in their order, are added to mass
+    __syncthreads();
+    for (int r = threadIdx.x; r < rows; r += ATTEND_THREADS) {
+        float most = -INFINITY, total = 0.f;
+        for (int w = 0; w < ATTEND_WAVES; ++w) most = fmaxf(most, s_top[w * HEADS + r]);
+        for (int w = 0; w < ATTEND_WAVES; ++w) {
+            const float t = s_top[w * HEADS + r];
+            total += s_sum[w * HEADS + r] * (t == -INFINITY ? 1.f : exp2_fast(t - most));
+        }
+        s_o[2 * r] = most == -INFINITY ? 0.f : most;
+        s_o[2 * r + 1] = total == 0.f ? 0.f : 1.f / total;
+    }
+    __syncthreads();
+    float *mass = a.mass + ((int64_t)b * a.cache.heads + h) * a.mass_slots;
+    for (int j = lo + threadIdx.x; j < n; j += ATTEND_THREADS) {
+        float w = 0.f;
+        for (int r = 0; r < rows; ++r) w += exp2_fast(s_x[r * a.keep + j - start] - s_o[2 * r]) * s_o[2 * r + 1];
+        mass[j] += w;
+    }
 }
 
 // What the parts of a context left, joined by a launch of its own: the workgroup that is done last could do it, but only behind fences that write back an XCD's
@@ -594,7 +619,7 @@ __global__ __launch_bounds__(ATTEND_THREADS) void paged_attention_join_kernel(At
 template <class T, int VE, int MT, bool FINE, bool FULL, bool ONCE>
 hipError_t attend(const AttentionArgs &a, hipStream_t stream) {
     static size_t granted = 0;
-    const size_t bytes = attend_lds_bytes(T::bytes, VE, MT, a.q_heads / a.cache.heads);
+    const size_t bytes = attend_lds_bytes(T::bytes, VE, MT, a.q_heads / a.cache.heads, a.keep);
     const void *kernel = reinterpret_cast<const void *>(paged_attention_kernel<T, VE, MT, FINE, FULL, ONCE>);
     if (hipError_t e = allow_big_lds(kernel, bytes, &granted)) return e;
     const int items = (a.requests * a.cache.heads * a.splits + 7) / 8 * 8;

@@ -996,9 +996,10 @@ constexpr int attend_lds_row(int ve) { return 16 * ve + 4; }
 // Queries of d > 128 are in LDS and not in registers: K, V and the sums alone take 192 of a lane's 256, beyond which every step moves them (8 cache heads of 256, fp16: 16 x 1000 slots 45 us
 // with all in registers, 29 so; 64 requests of 9216 of 4 heads 420 and 394).
 constexpr bool attend_q_in_lds(int ve) { return ve == 16; }
-inline size_t attend_lds_bytes(int elem_bytes, int ve, int mt, int G) {
+// keep: floats of a head's scores that stay in LDS behind the rest.
+inline size_t attend_lds_bytes(int elem_bytes, int ve, int mt, int G, int keep) {
     const int o = ATTEND_WAVES * (G < 16 * mt ? G : 16 * mt) * attend_lds_row(ve), q = attend_q_in_lds(ve) ? 16 * mt * 16 * ve * elem_bytes / 4 : 0;
-    return (size_t)(2 * ATTEND_WAVES * 16 * mt + (o > q ? o : q)) * 4;
+    return (size_t)(2 * ATTEND_WAVES * 16 * mt + (o > q ? o : q) + (G < 16 * mt ? G : 16 * mt) * keep) * 4;
 }
 
 // Tiles of 16 query heads that a workgroup takes, each reading of K and V then serving them all: two where there are more than 16 heads, except
@@ -1014,10 +1015,12 @@ inline int attend_groups(int elem_bytes, int d, int G) {
 // every context; `part` requests at a time.
 struct AttendPlan {
     int groups = 1, splits = 1, chunk = 0, pad = 0, part = 1;
+    int keep = 0;                // with mass: floats from head to head of scores that stay in LDS, for contexts of one part; 0: they do not
     bool once = false;           // keys and values are read once, and may be more than the last cache holds (256 MiB)
     size_t one = 0;              // bytes of workspace a request takes
 };
 constexpr int ATTEND_FEW = 16;                            // parts that a wave joins
+constexpr int ATTEND_KEEP = 40 * 1024;                    // bytes of scores that leave room for a second workgroup in a compute unit's LDS
 // Read past the last cache from this size on (which is that cache's): 64 x 8 cache heads of 9216 slots, 2.4 GB, 421 us without and 380 with it; one request of 30000,
 // 0.12 GB, 29.6 and 32.1 when it is read again and again.
 constexpr int64_t ATTEND_CACHED = (int64_t)256 << 20;
@@ -1048,11 +1051,13 @@ inline AttendPlan attend_plan(int cus, int B, int q_heads, int heads, int d, int
     pl.chunk = (int)chunk;
     pl.splits = (int)((range + chunk - 1) / chunk);
     pl.pad = (int)(pl.splits * chunk);
-    if (pl.splits > 1 || mass) pl.one = attend_bytes(q_heads, d, pl.splits, mass ? pl.pad : 0);
+    const int64_t keep = (range + 63) / 64 * 64 + 4;      // (heads lie 4 banks apart)
+    if (mass && pl.splits == 1 && pl.groups == 1 && q_heads / heads * keep * 4 <= ATTEND_KEEP) pl.keep = (int)keep;
+    if (pl.splits > 1 || (mass && !pl.keep)) pl.one = attend_bytes(q_heads, d, pl.splits, mass ? pl.pad : 0);
     pl.once = pl.groups == 1 && 2.0 * range * B * heads * d * elem_bytes > ATTEND_CACHED;
     pl.part = B;
     if (pl.one > 0 && pl.one * (size_t)B > most) pl.part = pl.one > most ? 1 : (int)(most / pl.one);
-    const int64_t grid = (int64_t)heads * pl.splits * pl.groups + (pl.one ? q_heads + (int64_t)heads * (mass ? pl.pad / 1024 + 1 : 0) : 0);
+    const int64_t grid = (int64_t)heads * pl.splits * pl.groups + (pl.one ? q_heads + (int64_t)heads * (mass && !pl.keep ? pl.pad / 1024 + 1 : 0) : 0);
     if (pl.part > ATTEND_GRID / grid) pl.part = ATTEND_GRID / grid < 1 ? 1 : (int)(ATTEND_GRID / grid);
     return pl;
 }

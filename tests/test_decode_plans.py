@@ -10,12 +10,12 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 SHIM = r"""
 #include "plan.hpp"
 using namespace ann;
-// out: groups, splits, chunk, pad, part, once, bytes of a request, step, head tiles, LDS bytes
+// out: groups, splits, chunk, pad, part, once, bytes of a request, step, head tiles, LDS bytes, floats from head to head of scores in LDS
 extern "C" void attend(int cus, int B, int q_heads, int heads, int d, int eb, int max_length, int window, int mass, int64_t most, int64_t *out) {
     const AttendPlan p = attend_plan(cus, B, q_heads, heads, d, eb, max_length, window, mass != 0, (size_t)most);
     const int G = q_heads / heads, mt = attend_head_tiles(eb, attend_ve(d), G);
-    const int64_t v[] = {p.groups, p.splits, p.chunk, p.pad, p.part, p.once, (int64_t)p.one, attend_step(eb, d), mt, (int64_t)attend_lds_bytes(eb, attend_ve(d), mt, G)};
-    for (int i = 0; i < 10; ++i) out[i] = v[i];
+    const int64_t v[] = {p.groups, p.splits, p.chunk, p.pad, p.part, p.once, (int64_t)p.one, attend_step(eb, d), mt, (int64_t)attend_lds_bytes(eb, attend_ve(d), mt, G, p.keep), p.keep};
+    for (int i = 0; i < 11; ++i) out[i] = v[i];
 }
 extern "C" int64_t workspace(int cus, int B, int q_heads, int heads, int d, int eb, int max_length, int mass, int64_t most) {
     return (int64_t)attend_workspace(cus, B, q_heads, heads, d, eb, max_length, mass != 0, (size_t)most);
@@ -38,7 +38,7 @@ def plans(tmp_path_factory):
     return lib
 
 
-NAMES = ("groups", "splits", "chunk", "pad", "part", "once", "one", "step", "tiles", "lds")
+NAMES = ("groups", "splits", "chunk", "pad", "part", "once", "one", "step", "tiles", "lds", "keep")
 
 
 def attend(lib, *args, most=1 << 30):
@@ -65,7 +65,9 @@ def test_attention_covers_every_slot_and_head(plans):
         assert (p["splits"] - 1) * p["chunk"] < reach <= p["pad"]           # nothing left out, no part empty by construction
         assert p["groups"] * 16 * p["tiles"] >= G and (p["groups"] - 1) * 16 * p["tiles"] < G
         assert p["lds"] <= 160 * 1024 and 1 <= p["part"] <= B
-        assert (p["one"] > 0) == (p["splits"] > 1 or bool(mass))
+        assert (p["one"] > 0) == (p["splits"] > 1 or (bool(mass) and not p["keep"]))
+        if p["keep"]:                                     # all scores of a cache head, and room for a second workgroup
+            assert mass and p["splits"] == p["groups"] == 1 and p["keep"] >= reach and p["keep"] * G * 4 <= 40 * 1024
         assert p["one"] * p["part"] <= most or p["part"] == 1
         assert p["part"] == 1 or p["part"] * heads * p["splits"] * p["groups"] <= 1 << 22
 
