@@ -1020,11 +1020,11 @@ struct AttendPlan {
     size_t one = 0;              // bytes of workspace a request takes
 };
 constexpr int ATTEND_FEW = 16;                            // parts that a wave joins
-constexpr int ATTEND_KEEP = 40 * 1024;                    // bytes of scores that leave room for a second workgroup in a compute unit's LDS
+constexpr int ATTEND_KEEP = 64 * 1024;                    // bytes of scores that leave room for a second workgroup in a compute unit's LDS
 // Read past the last cache from this size on (which is that cache's): 64 x 8 cache heads of 9216 slots, 2.4 GB, 421 us without and 380 with it; one request of 30000,
 // 0.12 GB, 29.6 and 32.1 when it is read again and again.
 constexpr int64_t ATTEND_CACHED = (int64_t)256 << 20;
-// A part has at most ATTEND_CHUNK slots.  What it leaves is 8 d bytes of traffic for each query head, in the way of the reads: those 64 x 8 cache heads with 8 query heads each took 431 us
+// A part has at most ATTEND_CHUNK slots as a rule.  What it leaves is 8 d bytes of traffic for each query head, in the way of the reads: those 64 x 8 cache heads with 8 query heads each took 431 us
 // in parts of 1024, 405 of 2048, 393 of 3328 and 396 of 4096; ragged contexts, which larger parts divide less evenly, 460, 456, 454 and 462.
 // Where contexts are short or few there are ATTEND_PER_CU parts for a compute unit if all are of max_length: even contexts would do with fewer (8 x 1 cache head of 16000 slots, 8 query heads: 21.1 us with 4,
 // 19.7 with 2), ragged ones not (48 x 4 of up to 8100: 93 us with 4, 112 with 3, 136 with 2; 92 with 8, but one request of 131072 then 99.7 for 97.9).
@@ -1047,12 +1047,18 @@ inline AttendPlan attend_plan(int cus, int B, int q_heads, int heads, int d, int
     // (A second step costs less than a second launch: 8 cache heads of 128, bf16, 150 slots 6.0 us against 8.2, 250 6.7 and 8.3; d = 64, 500 slots 7.6 and 9.0; fp32 10.1 and 10.8, 11.0 and 10.9.
     // A third costs as much, or more: 380 slots 8.2 and 8.2, fp32 14.8 and 10.9.)
     if (range <= 2 * step) chunk = 2 * step;
+    // With a cache head for every compute unit, contexts of up to 1024 slots are one part, and with mass of up to 4096 if their scores stay in LDS.  64 x 8 cache heads, d = 128, bf16,
+    // all of that length or ragged up to it, in one part and otherwise: 8 query heads each, 1000 slots 50 us and 58, ragged 35.5 and 37, with mass 54 and 70, ragged 38 and 44; 4 query heads, with
+    // mass, 4000 slots 177 and 227, ragged 134 and 155; 2000 slots 91 and 114, but ragged 73 and 71.  Longer ones lose more when they are ragged (10000 slots, one query head, d = 64, with mass
+    // 207 and 190), and so do scores that leave no room for a second workgroup (48 x 8 of up to 3500, 7 query heads, ragged, with mass 137 and 116).
+    const int64_t keep = (range + 63) / 64 * 64 + 4;      // floats from head to head: 4 banks apart
+    const bool keeps = mass && pl.groups == 1 && q_heads / heads * keep * 4 <= ATTEND_KEEP;
+    if (units >= cus && (range <= 1024 || (keeps && range <= 4096))) chunk = (range + step - 1) / step * step;
     if (range > ATTEND_PARTS * chunk) chunk = (range + ATTEND_PARTS * step - 1) / (ATTEND_PARTS * step) * step;
     pl.chunk = (int)chunk;
     pl.splits = (int)((range + chunk - 1) / chunk);
     pl.pad = (int)(pl.splits * chunk);
-    const int64_t keep = (range + 63) / 64 * 64 + 4;      // (heads lie 4 banks apart)
-    if (mass && pl.splits == 1 && pl.groups == 1 && q_heads / heads * keep * 4 <= ATTEND_KEEP) pl.keep = (int)keep;
+    if (keeps && pl.splits == 1) pl.keep = (int)keep;
     if (pl.splits > 1 || (mass && !pl.keep)) pl.one = attend_bytes(q_heads, d, pl.splits, mass ? pl.pad : 0);
     pl.once = pl.groups == 1 && 2.0 * range * B * heads * d * elem_bytes > ATTEND_CACHED;
     pl.part = B;

@@ -95,6 +95,17 @@ def test_attention_long(dtype, lengths, Hq, heads, d, page):
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("Hq,heads,d,page,longest,window", [
+    (32, 32, 64, 16, 1020, 0), (128, 32, 16, 8, 1024, 0), (64, 32, 128, 32, 1025, 0), (64, 32, 96, 16, 1020, 333),
+    (128, 32, 8, 64, 4030, 0), (32, 32, 8, 16, 4096, 0), (64, 32, 16, 16, 4200, 0)])
+def test_attention_contexts_of_one_part_in_a_large_batch(dtype, Hq, heads, d, page, longest, window):
+    """A cache head for every compute unit: contexts in one part up to some length, and weights added from scores that stay on the chip."""
+    lengths = [longest, 0, 1, longest - 1, 64, 65, longest // 2, 300]
+    for mass in (False, True):
+        attend(dtype, lengths, Hq, heads, d, page, window, mass)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
 @pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("Hq,heads,d", [(20, 1, 64), (40, 2, 128), (18, 1, 256), (34, 2, 104), (65, 1, 128), (6, 2, 64), (16, 1, 128), (8, 2, 256), (6, 3, 72), (4, 1, 200)])
 def test_attention_tiles_of_heads_and_wide_tables(dtype, wide, Hq, heads, d):
