@@ -118,15 +118,8 @@ __device__ __forceinline__ f4 scores_step(u4 k, u4 q, f4 c) {
     }
 }
 
-// What of request b is attended to: slots lo .. n - 1, in tiles from `start` on, in so many parts.
-struct AttendSpan { int n, lo, start, parts; };
 __device__ __forceinline__ AttendSpan attend_span(const AttentionArgs &a, int b) {
-    AttendSpan s;
-    s.n = min(a.lengths[b], a.max_length);
-    s.lo = a.window > 0 ? max(0, s.n - a.window) : 0;
-    s.start = s.lo & ~15;
-    s.parts = s.n > 0 ? (s.n - s.start + a.chunk - 1) / a.chunk : 0;
-    return s;
+    return attend_span(a.lengths[b], a.max_length, a.window, a.chunk);
 }
 
 // By one wave: largest exponent of head row r and total over its parts.

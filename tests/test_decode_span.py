@@ -1,0 +1,45 @@
+"""Which slots of a request attention goes through, decided without a GPU: the arithmetic of plan.hpp that the kernels run too, compiled with the C++
+compiler alone and checked over the whole range of lengths and windows."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+SHIM = r"""
+#include "plan.hpp"
+extern "C" void span(int length, int max_length, int window, int chunk, int *out) {
+    const ann::AttendSpan s = ann::attend_span(length, max_length, window, chunk);
+    out[0] = s.n, out[1] = s.lo, out[2] = s.start, out[3] = s.parts;
+}
+"""
+LEAST, MOST = -2 ** 31, 2 ** 31 - 1
+LENGTHS = [LEAST, LEAST + 1, LEAST + 1000, -65536, -1000, -3, -1, 0, 1, 2, 15, 16, 17, 100, 1499, 1500, 1501, 65536, MOST - 1, MOST]
+WINDOWS = [0, 1, 2, 15, 16, 17, 999, 1001, 1500, 65535, 2 ** 30, MOST - 1, MOST]
+
+
+@pytest.fixture(scope="module")
+def span(tmp_path_factory):
+    folder = tmp_path_factory.mktemp("span")
+    (folder / "shim.cpp").write_text(SHIM)
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-fwrapv", "-shared", "-fPIC", "-I", os.path.join(ROOT, "paper_2505_12065_amd", "csrc"),
+                           str(folder / "shim.cpp"), "-o", str(folder / "shim.so")])
+    lib = ctypes.CDLL(str(folder / "shim.so"))
+    out = (ctypes.c_int * 4)()
+
+    def call(*args):
+        lib.span(*args, out)
+        return list(out)
+    return call
+
+
+@pytest.mark.parametrize("max_length,chunk", [(1, 128), (1500, 128), (1500, 256), (65536, 1024), (1_000_000, 3328)])
+def test_span(span, max_length, chunk):
+    """No length and no window reaches a slot before the first or behind the last; a negative length is none."""
+    for length in LENGTHS:
+        for window in WINDOWS:
+            n, lo, start, parts = span(length, max_length, window, chunk)
+            assert n == max(0, min(length, max_length)), (length, window)
+            assert lo == (max(0, n - window) if window else 0), (length, window)
+            assert start == lo - lo % 16 and parts == -(-(n - start) // chunk), (length, window)
