@@ -233,7 +233,7 @@ __device__ __forceinline__ void attend_join(const AttentionArgs &a, int64_t r, f
 // By a workgroup: the weights of slots start + j0 .. of a cache head, ATTEND_PIECE of them, summed over its query heads in their order and added to mass.
 constexpr int ATTEND_PIECE = 4 * ATTEND_THREADS;
 __device__ __forceinline__ void attend_add_mass(const AttentionArgs &a, int b, int h, const AttendSpan &span, int j0, float *lds) {
-    const int G = a.q_heads / a.cache.heads, tid = threadIdx.x, j = j0 + 4 * tid;
+    const int G = a.q_heads / a.cache.heads, tid = threadIdx.x, j = j0 + 4 * tid, from = span.lo - span.start, count = span.n - span.start;
     f4 w = {0.f, 0.f, 0.f, 0.f};
     for (int g0 = 0; g0 < G; g0 += ATTEND_THREADS) {      // (one round as a rule)
         const int heads = min(ATTEND_THREADS, G - g0);
@@ -244,7 +244,7 @@ __device__ __forceinline__ void attend_add_mass(const AttentionArgs &a, int b, i
             lds[2 * i + 1] = total == 0.f ? 0.f : 1.f / total;
         }
         __syncthreads();
-        if (span.start + j < span.n) {
+        if (j < count) {
             const float *x = a.scores + ((int64_t)b * a.q_heads + h * G + g0) * a.pad + j;
 #pragma unroll 4
             for (int i = 0; i < heads; ++i) {
@@ -259,7 +259,7 @@ __device__ __forceinline__ void attend_add_mass(const AttentionArgs &a, int b, i
     float *to = a.mass + ((int64_t)b * a.cache.heads + h) * a.mass_slots + span.start + j;
 #pragma unroll
     for (int c = 0; c < 4; ++c)
-        if (span.start + j + c >= span.lo && span.start + j + c < span.n) to[c] += w[c];
+        if (j + c >= from && j + c < count) to[c] += w[c];
 }
 
 // FINE: pages of less than 16 slots, looked up for every row and not for a tile.  FULL: d is 16 VE.  ONCE: keys and values are more than the
@@ -282,7 +282,7 @@ __global__ __launch_bounds__(ATTEND_THREADS, (MT > 1 && (VE == 16 || T::bytes ==
     const int h = unit % a.cache.heads, b = unit / a.cache.heads;
     const int G = a.q_heads / a.cache.heads, rows = min(16 * MT, G - 16 * MT * hg);   // query heads of this workgroup
     const AttendSpan span = attend_span(a, b);
-    const int n = span.n, lo = span.lo, start = span.start, first = start + part * a.chunk, end = min(n, first + a.chunk);
+    const int n = span.n, lo = span.lo, start = span.start, first = start + part * a.chunk, end = attend_end(n, first, a.chunk);
     if (part >= max(span.parts, 1)) return;               // (the first part of nothing says so)
     const int64_t hq0 = (int64_t)b * a.q_heads + h * G + 16 * MT * hg;
 
@@ -606,7 +606,7 @@ __global__ __launch_bounds__(ATTEND_THREADS) void paged_attention_join_kernel(At
     const int pieces = (a.pad + ATTEND_PIECE - 1) / ATTEND_PIECE, j0 = (int)(id % pieces) * ATTEND_PIECE;
     const int b = (int)(id / pieces / a.cache.heads), h = (int)(id / pieces % a.cache.heads);
     const AttendSpan span = attend_span(a, b);
-    if (span.start + j0 < span.n) attend_add_mass(a, b, h, span, j0, lds);
+    if (j0 < span.n - span.start) attend_add_mass(a, b, h, span, j0, lds);
 }
 
 template <class T, int VE, int MT, bool FINE, bool FULL, bool ONCE>

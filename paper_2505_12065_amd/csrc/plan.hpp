@@ -1030,16 +1030,18 @@ constexpr int64_t ATTEND_CACHED = (int64_t)256 << 20;
 // 19.7 with 2), ragged ones not (48 x 4 of up to 8100: 93 us with 4, 112 with 3, 136 with 2; 92 with 8, but one request of 131072 then 99.7 for 97.9).
 constexpr int ATTEND_PARTS = 256, ATTEND_CHUNK = 3328, ATTEND_PER_CU = 4;
 // What is attended to of a request: slots lo .. n - 1, in tiles from `start` on, in so many parts.  (Also on the device.  A negative length is 0 before
-// the window is taken off it, or the difference could pass the least integer and start far behind all tables.)
+// the window is taken off it, or the difference could pass the least integer and start far behind all tables; a length within a part of 2^31 is no reason to pass that.)
 struct AttendSpan { int n, lo, start, parts; };
 constexpr AttendSpan attend_span(int length, int max_length, int window, int chunk) {
     AttendSpan s{};
     s.n = length < 0 ? 0 : length < max_length ? length : max_length;
     s.lo = window > 0 && s.n > window ? s.n - window : 0;
     s.start = s.lo & ~15;
-    s.parts = s.n > 0 ? (s.n - s.start + chunk - 1) / chunk : 0;
+    s.parts = s.n > 0 ? (s.n - s.start - 1) / chunk + 1 : 0;
     return s;
 }
+// Behind the last slot of the part that begins with slot `first`.
+constexpr int attend_end(int n, int first, int chunk) { return n - first < chunk ? n : first + chunk; }
 constexpr int64_t ATTEND_GRID = 1 << 22;                  // workgroups of a launch
 inline int64_t attend_step(int elem_bytes, int d) { return 16 * ATTEND_WAVES * attend_tiles(elem_bytes, attend_ve(d)); }
 inline size_t attend_bytes(int q_heads, int d, int64_t splits, int64_t pad) {

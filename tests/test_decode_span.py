@@ -13,8 +13,14 @@ extern "C" void span(int length, int max_length, int window, int chunk, int *out
     const ann::AttendSpan s = ann::attend_span(length, max_length, window, chunk);
     out[0] = s.n, out[1] = s.lo, out[2] = s.start, out[3] = s.parts;
 }
+extern "C" int end(int n, int first, int chunk) { return ann::attend_end(n, first, chunk); }
+extern "C" void plan(int heads, int G, int d, int elem_bytes, int max_length, int window, int mass, int *out) {
+    const ann::AttendPlan p = ann::attend_plan(256, 1, heads * G, heads, d, elem_bytes, max_length, window, mass != 0, (size_t)1 << 30);
+    out[0] = p.chunk, out[1] = p.splits, out[2] = p.pad;
+}
 """
 LEAST, MOST = -2 ** 31, 2 ** 31 - 1
+LONGEST = MOST - 65536                                    # what a page table may hold
 LENGTHS = [LEAST, LEAST + 1, LEAST + 1000, -65536, -1000, -3, -1, 0, 1, 2, 15, 16, 17, 100, 1499, 1500, 1501, 65536, MOST - 1, MOST]
 WINDOWS = [0, 1, 2, 15, 16, 17, 999, 1001, 1500, 65535, 2 ** 30, MOST - 1, MOST]
 
@@ -31,6 +37,7 @@ def span(tmp_path_factory):
     def call(*args):
         lib.span(*args, out)
         return list(out)
+    call.lib = lib
     return call
 
 
@@ -43,3 +50,24 @@ def test_span(span, max_length, chunk):
             assert n == max(0, min(length, max_length)), (length, window)
             assert lo == (max(0, n - window) if window else 0), (length, window)
             assert start == lo - lo % 16 and parts == -(-(n - start) // chunk), (length, window)
+
+
+@pytest.mark.parametrize("d,elem_bytes", [(8, 2), (64, 4), (128, 2), (128, 4), (256, 2), (256, 4)])
+def test_parts_of_the_longest_contexts(span, d, elem_bytes):
+    """Every slot is in one part, for contexts whose length and part together pass 2^31."""
+    out = (ctypes.c_int * 3)()
+    for max_length in (LONGEST, LONGEST - 1, LONGEST - 15, LONGEST - 8_000_000, 2 ** 30, 2 ** 30 + 1):
+        for window in (0, max_length, max_length - 1, max_length - 17, 2 ** 30, MOST):
+            span.lib.plan(1, 4, d, elem_bytes, max_length, window, 1, out)
+            chunk, splits, pad = out
+            assert pad == splits * chunk <= MOST - 2048
+            for length in (max_length, max_length - 1, max_length - 16, max_length - chunk):
+                n, lo, start, parts = span(length, max_length, window, chunk)
+                assert n == length and parts == -(-(n - start) // chunk) <= splits, (max_length, window, length)
+                assert start + (splits - 1) * chunk <= MOST               # (parts that this request has not are looked at too)
+                reached = start
+                for part in range(parts):
+                    end = span.lib.end(n, reached, chunk)
+                    assert end == min(n, reached + chunk) > reached
+                    reached = end
+                assert reached == n

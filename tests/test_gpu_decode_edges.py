@@ -22,3 +22,36 @@ def test_attention_negative_lengths_with_any_window(dtype, page, window):
         return q, k, v, table, lens
     out = attend(dtype, [700, 10, 10, 10, 10, 0, 33], 4, 2, 64, page, window=window, mass=True, seed=31, edit=edit)
     assert (out[1:6] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("with_mass", [False, True])
+def test_attention_of_the_longest_context(dtype, with_mass):
+    """As many slots as a page table may hold (its pages are the same three).  All scores are 0, so every sum of a part is a whole number below 2^24 and exact;
+    the parts' are added up with a relative 2^-24 each, the logarithm (21.5) is right to a few of its last places, 2^-19."""
+    page, d, short = 1024, 8, 5
+    width = (MOST - 65536) // page
+    n = width * page - short
+    k, v = torch.randn(3, 1, page, d, device=DEV).to(dtype), torch.zeros(3, 1, page, d, dtype=dtype, device=DEV)
+    v[..., 0], v[1, ..., 1], v[2, ..., 2] = 1, 1024, 1024
+    table = torch.zeros(1, width, dtype=torch.int32, device=DEV)
+    table[0, -1], table[0, 0] = 1, 2                      # the last page, of which `short` slots are behind the end, and the first
+    lens = torch.tensor([n], dtype=torch.int32, device=DEV)
+    mass = torch.zeros(1, 1, width * page, device=DEV) if with_mass else None
+    q = torch.zeros(1, 1, d, dtype=dtype, device=DEV)
+    if with_mass:                                         # (the library's own buffer stays as small as it is)
+        space = torch.empty(ann.ann_paged_attention_workspace_bytes(1, 1, 1, d, dtype, width * page, True), dtype=torch.uint8, device=DEV)
+        ann.ann_set_workspace(space)
+    try:
+        out, lse = ann.ann_paged_attention(q, k, v, table, lens, mass=mass)
+        torch.cuda.synchronize()
+    finally:
+        if with_mass:
+            ann.ann_set_workspace(None)
+    want = torch.tensor([1.0, (page - short) * 1024 / n, page * 1024 / n, 0, 0, 0, 0, 0], dtype=torch.float64)
+    off = (out[0, 0].double().cpu() - want).abs()
+    assert (off <= want * (D.HALF_ULP[dtype] * 1.01 + 2.0 ** -18) + D.TINY[dtype]).all(), off
+    assert abs(lse.item() - torch.tensor(float(n), dtype=torch.float64).log().item()) <= 2.0 ** -17
+    if with_mass:
+        low, high = torch.aminmax(mass[0, 0, :n])
+        assert abs(low.item() * n - 1) <= 2.0 ** -16 and abs(high.item() * n - 1) <= 2.0 ** -16 and not mass[0, 0, n:].any()
