@@ -484,6 +484,7 @@ int ann_paged_attention(const void *q, int64_t q_row, int64_t q_head, int32_t B,
     DeviceState *st = nullptr;
     if (int rc = device_state(&st)) return rc;
     AttendPlan pl = attend_plan(st->cus, B, q_heads, cache->heads, cache->d, e, max_length, window, mass != nullptr, ATTEND_WS_MAX);
+    if (pl.grid > ATTEND_GRID_ONE) return fail(ANN_ERR_INVALID, "weights of %d slots for %d heads of the cache are too many for a call", max_length, cache->heads);
     // a buffer that a caller gave, or that a graph may not let grow, takes fewer requests at a time
     if (!at_hand(st, st->ws, pl.one * pl.part, stream)) {
         const size_t there = st->user_ws ? st->user_bytes : st->ws.bytes;

@@ -1018,6 +1018,7 @@ struct AttendPlan {
     int keep = 0;                // with mass: floats from head to head of scores that stay in LDS, for contexts of one part; 0: they do not
     bool once = false;           // keys and values are read once, and may be more than the last cache holds (256 MiB)
     size_t one = 0;              // bytes of workspace a request takes
+    int64_t grid = 0;            // workgroups of the two launches for one request
 };
 constexpr int ATTEND_FEW = 16;                            // parts that a wave joins
 constexpr int ATTEND_KEEP = 64 * 1024;                    // bytes of scores that leave room for a second workgroup in a compute unit's LDS
@@ -1042,7 +1043,8 @@ constexpr AttendSpan attend_span(int length, int max_length, int window, int chu
 }
 // Behind the last slot of the part that begins with slot `first`.
 constexpr int attend_end(int n, int first, int chunk) { return n - first < chunk ? n : first + chunk; }
-constexpr int64_t ATTEND_GRID = 1 << 22;                  // workgroups of a launch
+constexpr int64_t ATTEND_GRID = 1 << 22;                  // workgroups of a launch, where there is more than one request
+constexpr int64_t ATTEND_GRID_ONE = (1 << 24) - 1;        // ... of one request: a launch has fewer than 2^32 threads
 inline int64_t attend_step(int elem_bytes, int d) { return 16 * ATTEND_WAVES * attend_tiles(elem_bytes, attend_ve(d)); }
 inline size_t attend_bytes(int q_heads, int d, int64_t splits, int64_t pad) {
     return (size_t)q_heads * ((splits > 1 ? (size_t)splits * d : 0) + (size_t)splits * 2 + (size_t)pad) * 4;
@@ -1076,8 +1078,8 @@ inline AttendPlan attend_plan(int cus, int B, int q_heads, int heads, int d, int
     pl.once = pl.groups == 1 && 2.0 * range * B * heads * d * elem_bytes > ATTEND_CACHED;
     pl.part = B;
     if (pl.one > 0 && pl.one * (size_t)B > most) pl.part = pl.one > most ? 1 : (int)(most / pl.one);
-    const int64_t grid = (int64_t)heads * pl.splits * pl.groups + (pl.one ? q_heads + (int64_t)heads * (mass && !pl.keep ? pl.pad / 1024 + 1 : 0) : 0);
-    if (pl.part > ATTEND_GRID / grid) pl.part = ATTEND_GRID / grid < 1 ? 1 : (int)(ATTEND_GRID / grid);
+    pl.grid = (int64_t)heads * pl.splits * pl.groups + (pl.one ? q_heads + (int64_t)heads * (mass && !pl.keep ? pl.pad / 1024 + 1 : 0) : 0);
+    if (pl.part > ATTEND_GRID / pl.grid) pl.part = ATTEND_GRID / pl.grid < 1 ? 1 : (int)(ATTEND_GRID / pl.grid);
     return pl;
 }
 // Enough for these sizes and for shorter lengths and windows, which may be divided into more parts.

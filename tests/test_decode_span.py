@@ -14,9 +14,9 @@ extern "C" void span(int length, int max_length, int window, int chunk, int *out
     out[0] = s.n, out[1] = s.lo, out[2] = s.start, out[3] = s.parts;
 }
 extern "C" int end(int n, int first, int chunk) { return ann::attend_end(n, first, chunk); }
-extern "C" void plan(int heads, int G, int d, int elem_bytes, int max_length, int window, int mass, int *out) {
+extern "C" void plan(int heads, int G, int d, int elem_bytes, int max_length, int window, int mass, int64_t *out) {
     const ann::AttendPlan p = ann::attend_plan(256, 1, heads * G, heads, d, elem_bytes, max_length, window, mass != 0, (size_t)1 << 30);
-    out[0] = p.chunk, out[1] = p.splits, out[2] = p.pad;
+    out[0] = p.chunk, out[1] = p.splits, out[2] = p.pad, out[3] = p.grid, out[4] = ann::ATTEND_GRID_ONE, out[5] = p.keep;
 }
 """
 LEAST, MOST = -2 ** 31, 2 ** 31 - 1
@@ -55,11 +55,11 @@ def test_span(span, max_length, chunk):
 @pytest.mark.parametrize("d,elem_bytes", [(8, 2), (64, 4), (128, 2), (128, 4), (256, 2), (256, 4)])
 def test_parts_of_the_longest_contexts(span, d, elem_bytes):
     """Every slot is in one part, for contexts whose length and part together pass 2^31."""
-    out = (ctypes.c_int * 3)()
+    out = (ctypes.c_int64 * 6)()
     for max_length in (LONGEST, LONGEST - 1, LONGEST - 15, LONGEST - 8_000_000, 2 ** 30, 2 ** 30 + 1):
         for window in (0, max_length, max_length - 1, max_length - 17, 2 ** 30, MOST):
             span.lib.plan(1, 4, d, elem_bytes, max_length, window, 1, out)
-            chunk, splits, pad = out
+            chunk, splits, pad = out[:3]
             assert pad == splits * chunk <= MOST - 2048
             for length in (max_length, max_length - 1, max_length - 16, max_length - chunk):
                 n, lo, start, parts = span(length, max_length, window, chunk)
@@ -71,3 +71,19 @@ def test_parts_of_the_longest_contexts(span, d, elem_bytes):
                     assert end == min(n, reached + chunk) > reached
                     reached = end
                 assert reached == n
+
+
+def test_launches_of_one_request(span):
+    """The second launch has a workgroup for 1024 slots of a cache head, so the most heads and the longest contexts together are more than a launch may have:
+    what the plan counts is never less than either launch, and a call is refused from where 256 threads to a workgroup would pass 2^32."""
+    out, refused = (ctypes.c_int64 * 6)(), 0
+    for heads in (1, 7, 8, 9, 64, 1024, 8192):
+        for length in (1, 1500, 2 ** 20, 2 ** 28, LONGEST):
+            for mass in (0, 1):
+                span.lib.plan(heads, 1, 128, 2, length, 0, mass, out)
+                chunk, splits, pad, grid, most, keep = out
+                assert grid >= heads * splits and grid >= (heads if splits > 1 else 0) + (heads * -(-pad // 1024) if mass and not keep else 0)
+                assert most * 256 < 2 ** 32
+                refused += grid > most
+                assert mass or grid <= most
+    assert 0 < refused < 20
