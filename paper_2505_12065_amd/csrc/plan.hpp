@@ -1021,7 +1021,10 @@ struct AttendPlan {
     int64_t grid = 0;            // workgroups of the two launches for one request
 };
 constexpr int ATTEND_FEW = 16;                            // parts that a wave joins
-constexpr int ATTEND_KEEP = 64 * 1024;                    // bytes of scores that leave room for a second workgroup in a compute unit's LDS
+// Bytes of scores, at most, that stay in LDS, if all that the workgroup has there fits a compute unit.  A second workgroup need not fit beside it: 64 x 8 cache heads, bf16, with mass,
+// scores that take its room in LDS and in memory: 16 query heads of 128, 960 slots 62 us and 72, ragged 55 and 58; 8 of 256, 1900 slots 182 and 217, 134 and 155; 10 of 128, 1500 slots 87
+// and 101, but ragged 77 and 75.
+constexpr int ATTEND_KEEP = 64 * 1024;
 // Read past the last cache from this size on (which is that cache's): 64 x 8 cache heads of 9216 slots, 2.4 GB, 421 us without and 380 with it; one request of 30000,
 // 0.12 GB, 29.6 and 32.1 when it is read again and again.
 constexpr int64_t ATTEND_CACHED = (int64_t)256 << 20;
@@ -1065,9 +1068,11 @@ inline AttendPlan attend_plan(int cus, int B, int q_heads, int heads, int d, int
     // With a cache head for every compute unit, contexts of up to 1024 slots are one part, and with mass of up to 4096 if their scores stay in LDS.  64 x 8 cache heads, d = 128, bf16,
     // all of that length or ragged up to it, in one part and otherwise: 8 query heads each, 1000 slots 50 us and 58, ragged 35.5 and 37, with mass 54 and 70, ragged 38 and 44; 4 query heads, with
     // mass, 4000 slots 177 and 227, ragged 134 and 155; 2000 slots 91 and 114, but ragged 73 and 71.  Longer ones lose more when they are ragged (10000 slots, one query head, d = 64, with mass
-    // 207 and 190), and so do scores that leave no room for a second workgroup (48 x 8 of up to 3500, 7 query heads, ragged, with mass 137 and 116).
+    // 207 and 190), and so do scores beyond ATTEND_KEEP (48 x 8 of up to 3500, 7 query heads, ragged, with mass 137 and 116).
     const int64_t keep = (range + 63) / 64 * 64 + 4;      // floats from head to head: 4 banks apart
-    const bool keeps = mass && pl.groups == 1 && q_heads / heads * keep * 4 <= ATTEND_KEEP;
+    const int G = q_heads / heads, ve = attend_ve(d);
+    const bool keeps = mass && pl.groups == 1 && G * keep * 4 <= ATTEND_KEEP &&
+                       attend_lds_bytes(elem_bytes, ve, attend_head_tiles(elem_bytes, ve, G), G, (int)keep) <= LDS_MAX;
     if (units >= cus && (range <= 1024 || (keeps && range <= 4096))) chunk = (range + step - 1) / step * step;
     if (range > ATTEND_PARTS * chunk) chunk = (range + ATTEND_PARTS * step - 1) / (ATTEND_PARTS * step) * step;
     pl.chunk = (int)chunk;

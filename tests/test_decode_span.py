@@ -13,6 +13,16 @@ extern "C" void span(int length, int max_length, int window, int chunk, int *out
     const ann::AttendSpan s = ann::attend_span(length, max_length, window, chunk);
     out[0] = s.n, out[1] = s.lo, out[2] = s.start, out[3] = s.parts;
 }
+// of all lengths up to `longest`: the most LDS that a workgroup is to have, and how many plans keep scores there
+extern "C" void lds(int B, int heads, int G, int d, int elem_bytes, int longest, int64_t *out) {
+    out[0] = out[1] = 0;
+    for (int length = 1; length <= longest; ++length) {
+        const ann::AttendPlan p = ann::attend_plan(256, B, heads * G, heads, d, elem_bytes, length, 0, true, (size_t)1 << 30);
+        const int ve = ann::attend_ve(d);
+        const int64_t bytes = ann::attend_lds_bytes(elem_bytes, ve, ann::attend_head_tiles(elem_bytes, ve, G), G, p.keep);
+        out[0] = out[0] < bytes ? bytes : out[0], out[1] += p.keep > 0;
+    }
+}
 extern "C" int end(int n, int first, int chunk) { return ann::attend_end(n, first, chunk); }
 extern "C" void plan(int heads, int G, int d, int elem_bytes, int max_length, int window, int mass, int64_t *out) {
     const ann::AttendPlan p = ann::attend_plan(256, 1, heads * G, heads, d, elem_bytes, max_length, window, mass != 0, (size_t)1 << 30);
@@ -87,3 +97,16 @@ def test_launches_of_one_request(span):
                 refused += grid > most
                 assert mass or grid <= most
     assert 0 < refused < 20
+
+
+@pytest.mark.parametrize("elem_bytes", [2, 4])
+@pytest.mark.parametrize("B,heads", [(1, 1), (64, 8)])
+def test_no_workgroup_has_more_lds_than_there_is(span, elem_bytes, B, heads):
+    """Over all numbers of query heads that one workgroup may take and beyond, all sizes of a head, and all lengths whose scores may stay in LDS."""
+    out, kept = (ctypes.c_int64 * 2)(), 0
+    for G in range(1, 41):
+        for d in range(8, 257, 8):
+            span.lib.lds(B, heads, G, d, elem_bytes, 4400, out)
+            assert out[0] <= 160 * 1024, (G, d)
+            kept += out[1]
+    assert kept > 0

@@ -55,3 +55,13 @@ def test_attention_of_the_longest_context(dtype, with_mass):
     if with_mass:
         low, high = torch.aminmax(mass[0, 0, :n])
         assert abs(low.item() * n - 1) <= 2.0 ** -16 and abs(high.item() * n - 1) <= 2.0 ** -16 and not mass[0, 0, n:].any()
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("d", [136, 256])
+@pytest.mark.parametrize("G,heads,longest", [(32, 1, 192), (32, 1, 193), (32, 1, 250), (32, 1, 256), (32, 1, 257), (28, 32, 384), (28, 32, 400), (28, 32, 576),
+                                             (28, 32, 577), (25, 32, 600), (32, 32, 448)])
+def test_attention_weights_of_many_heads_beside_large_sums(dtype, d, G, heads, longest):
+    """Two tiles of query heads of d > 128 leave little of a compute unit's LDS for scores, which go to the workspace where they do not fit."""
+    lengths = [longest, 0, 1, 7, 33, 64, 65, 150] if heads > 1 else [longest, 200, 0]
+    attend(dtype, lengths, G * heads, heads, d, 16, mass=True, seed=longest)
