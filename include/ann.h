@@ -392,7 +392,8 @@ int ann_qk_norm_rotate(const void *qkv, int64_t token_stride, int64_t head_strid
  *   out         device [B, q_heads, d], contiguous;  lse  device float [B, q_heads], or NULL
  *   mass        NULL, or device float [B, heads, mass_slots], mass_slots >= width slots: the weight
  *               exp(x_j - lse) of slot j, summed over the query heads of a cache head, is added to mass[b, head, j]
- * An infinite value with a weight above 0 gives an infinity or a NaN.  Same inputs give bitwise-same outputs.  Uses the workspace of the current device (conventions at the top;
+ * An infinite value with a weight above 0 gives an infinity or a NaN; finite values, however large, do not (but for an out that itself
+ * rounds to beyond the type's largest).  Values of bf16 and fp32 below 2^-126 times the number of slots may count as 0.  Same inputs give bitwise-same outputs.  Uses the workspace of the current device (conventions at the top;
  * ann_set_workspace) for what the parts of a long context leave to be joined, and for scores if mass is given: the size below, where it is
  * there; with less, or beyond 1 GiB, a few requests at a time.  B = 0 returns ANN_OK at once. */
 int ann_paged_attention(const void *q, int64_t q_row, int64_t q_head, int32_t B, int32_t q_heads,

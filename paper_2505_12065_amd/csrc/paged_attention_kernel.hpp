@@ -80,6 +80,13 @@ template <> struct Words<4> { typedef u4 type; };
 // 2^12 times as large in the loop, which keeps what makes up a millionth of the sum of 2^17 slots.
 template <class T> constexpr int ATTEND_LIFT = std::is_same_v<T, F16> ? 12 : 0;
 
+// bf16 and fp32 have values up to the largest of the sums' 32 bits, and weights add up to as much as there are slots before they are divided by their sum: for the product with V they are
+// multiplied by this power of two, below 1 / n, and the rows stay so until they are divided.  (fp16: 65504 times 2^12 times 2^31 is far from it.)
+template <class T>
+__device__ __forceinline__ float attend_scale(int n) {
+    return std::is_same_v<T, F16> ? 1.f : __uint_as_float((uint32_t)(127 - (32 - __clz(n))) << 23);
+}
+
 // Eight weights as an operand of 16 bits and what that leaves, as another: the product with V then has 16 bits (bf16) or more of
 // them.  One part alone would be off by as much as the output's own rounding; the second product costs nothing here.
 template <class T>
@@ -135,11 +142,12 @@ __device__ __forceinline__ void attend_stats(const AttentionArgs &a, int64_t r, 
 __device__ __forceinline__ float attend_lse(float most, float total) {
     return total == 0.f ? -INFINITY : (most == -INFINITY ? 0.f : most) * 0.6931471805599453f + logf(total);
 }
-// Eight elements of head row r, a sum of its parts
+// Eight elements of head row r, a sum of its parts; n: the request's slots
 template <class T>
-__device__ __forceinline__ void attend_write(const AttentionArgs &a, int64_t r, int at, float (&y)[8], float most, float total) {
+__device__ __forceinline__ void attend_write(const AttentionArgs &a, int64_t r, int at, float (&y)[8], float most, float total, int n) {
+    const float by = total * attend_scale<T>(n);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = total == 0.f ? 0.f : y[j] / total;
+    for (int j = 0; j < 8; ++j) y[j] = total == 0.f ? 0.f : y[j] / by;
     Eight<T> e;
     e.set(y);
     e.store(static_cast<char *>(a.out) + (r * a.cache.d + at) * T::bytes);
@@ -166,7 +174,8 @@ __device__ __forceinline__ void attend_join_few(const AttentionArgs &a, int64_t 
         }
     };
     ask(first);
-    const int parts = max(1, attend_span(a, (int)(r / a.q_heads)).parts);
+    const AttendSpan span = attend_span(a, (int)(r / a.q_heads));
+    const int parts = max(1, span.parts);
     const float t = lane < parts ? own.x : -INFINITY, most = wave_max(t);
     // (a part without a score has a sum of 0, or NaN, and counts as it is)
     const float f = lane >= parts ? 0.f : t == -INFINITY ? 1.f : exp2_fast(t - most), total = wave_sum(lane < parts ? own.y * f : 0.f);
@@ -193,12 +202,13 @@ __device__ __forceinline__ void attend_join_few(const AttentionArgs &a, int64_t 
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[j] += o[j / 4][j % 4];
         }
-        attend_write<T>(a, r, 8 * lane, y, most, total);
+        attend_write<T>(a, r, 8 * lane, y, most, total, span.n);
     }
 }
 template <class T>
 __device__ __forceinline__ void attend_join(const AttentionArgs &a, int64_t r, float *lds) {
-    const int parts = max(1, attend_span(a, (int)(r / a.q_heads)).parts), per_row = a.cache.d / 8, tid = threadIdx.x, side = ATTEND_THREADS / per_row;
+    const AttendSpan span = attend_span(a, (int)(r / a.q_heads));
+    const int parts = max(1, span.parts), per_row = a.cache.d / 8, tid = threadIdx.x, side = ATTEND_THREADS / per_row;
     const float *from = a.partial + r * a.splits * a.cache.d + (tid % per_row) * 8;
     const float *st = a.stats + r * a.splits * 2;
     float most, total, y[8] = {};
@@ -226,7 +236,7 @@ __device__ __forceinline__ void attend_join(const AttentionArgs &a, int64_t r, f
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[j] += o[j / 4][j % 4];
         }
-        attend_write<T>(a, r, 8 * tid, y, most, total);
+        attend_write<T>(a, r, 8 * tid, y, most, total, span.n);
     }
 }
 
@@ -285,6 +295,7 @@ __global__ __launch_bounds__(ATTEND_THREADS, (MT > 1 && (VE == 16 || T::bytes ==
     const int n = span.n, lo = span.lo, start = span.start, first = start + part * a.chunk, end = attend_end(n, first, a.chunk);
     if (part >= max(span.parts, 1)) return;               // (the first part of nothing says so)
     const int64_t hq0 = (int64_t)b * a.q_heads + h * G + 16 * MT * hg;
+    const float scale = attend_scale<T>(n);
 
     // (LDS: what the waves' sums are written over afterwards)
     constexpr bool Q_LDS = attend_q_in_lds(VE);
@@ -449,6 +460,7 @@ __global__ __launch_bounds__(ATTEND_THREADS, (MT > 1 && (VE == 16 || T::bytes ==
                 for (int i = 0; i < 4; ++i) {
                     x[mt][t][i] = exp2_fast(x[mt][t][i] - lifted);
                     sum[mt] += x[mt][t][i];
+                    if (!std::is_same_v<T, F16>) x[mt][t][i] *= scale;
                 }
 #pragma unroll
             for (int c = 0; c < VE; ++c) o[mt][c] *= keep;
@@ -555,7 +567,7 @@ __global__ __launch_bounds__(ATTEND_THREADS, (MT > 1 && (VE == 16 || T::bytes ==
             reinterpret_cast<f4 *>(to)[0] = f4{y[0], y[1], y[2], y[3]};
             reinterpret_cast<f4 *>(to)[1] = f4{y[4], y[5], y[6], y[7]};
         } else {
-            const float f = total == 0.f ? 0.f : 1.f / total;
+            const float f = total == 0.f ? 0.f : 1.f / (total * scale);
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[j] = total == 0.f ? 0.f : y[j] * f;
             Eight<T> e;

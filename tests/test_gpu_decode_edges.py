@@ -65,3 +65,17 @@ def test_attention_weights_of_many_heads_beside_large_sums(dtype, d, G, heads, l
     """Two tiles of query heads of d > 128 leave little of a compute unit's LDS for scores, which go to the workspace where they do not fit."""
     lengths = [longest, 0, 1, 7, 33, 64, 65, 150] if heads > 1 else [longest, 200, 0]
     attend(dtype, lengths, G * heads, heads, d, 16, mass=True, seed=longest)
+
+
+@pytest.mark.parametrize("dtype,largest", [(F16, 6e4), (BF16, 3e38), (F32, 3e38)])
+@pytest.mark.parametrize("lengths,Hq,heads,d,page,window", [([300, 1, 17, 64, 0], 8, 2, 64, 16, 0), ([5000, 4, 700], 6, 2, 128, 16, 0), ([20_001, 90], 4, 4, 80, 64, 0),
+                                                            ([5000, 3000], 40, 2, 128, 16, 2000), ([2100], 4, 1, 256, 4, 0), ([900, 40, 0, 1, 2, 3, 4, 5], 64, 32, 16, 16, 0)])
+@pytest.mark.parametrize("same", [False, True])
+def test_attention_of_values_near_the_largest(dtype, largest, lengths, Hq, heads, d, page, window, same):
+    """Finite values whose sum over the slots, before it is divided, is beyond 32 bits: half the slots' of one sign, or all of one value."""
+    def edit(q, k, v, table, lens):
+        g = torch.Generator().manual_seed(5)
+        v[:] = largest if same else (torch.randint(0, 4, v.shape, generator=g).clamp(max=2) - 1) * largest
+        return q, k, v, table, lens
+    attend(dtype, lengths, Hq, heads, d, page, window=window, seed=41, edit=edit)
+    attend(dtype, lengths, Hq, heads, d, page, window=window, seed=42, edit=edit, mass=True)
