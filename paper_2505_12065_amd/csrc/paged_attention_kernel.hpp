@@ -240,6 +240,11 @@ __device__ __forceinline__ void attend_join(const AttentionArgs &a, int64_t r, f
     }
 }
 
+// Whether `weight` is slot key's: one without a row has 0, but where a head's scores hold a NaN, and is left alone then.
+__device__ __forceinline__ bool attend_counts(const AttentionArgs &a, int b, int key, float weight) {
+    return weight == weight || (unsigned)a.table[(int64_t)b * a.width + (key >> a.cache.slots_log)] < (unsigned)a.cache.pages;
+}
+
 // By a workgroup: the weights of slots start + j0 .. of a cache head, ATTEND_PIECE of them, summed over its query heads in their order and added to mass.
 constexpr int ATTEND_PIECE = 4 * ATTEND_THREADS;
 __device__ __forceinline__ void attend_add_mass(const AttentionArgs &a, int b, int h, const AttendSpan &span, int j0, float *lds) {
@@ -269,7 +274,7 @@ __device__ __forceinline__ void attend_add_mass(const AttentionArgs &a, int b, i
     float *to = a.mass + ((int64_t)b * a.cache.heads + h) * a.mass_slots + span.start + j;
 #pragma unroll
     for (int c = 0; c < 4; ++c)
-        if (j + c >= from && j + c < count) to[c] += w[c];
+        if (j + c >= from && j + c < count && attend_counts(a, b, span.start + j + c, w[c])) to[c] += w[c];
 }
 
 // FINE: pages of less than 16 slots, looked up for every row and not for a tile.  FULL: d is 16 VE.  ONCE: keys and values are more than the
@@ -595,7 +600,7 @@ __global__ __launch_bounds__(ATTEND_THREADS, (MT > 1 && (VE == 16 || T::bytes ==
     for (int j = lo + threadIdx.x; j < n; j += ATTEND_THREADS) {
         float w = 0.f;
         for (int r = 0; r < rows; ++r) w += exp2_fast(s_x[r * a.keep + j - start] - s_o[2 * r]) * s_o[2 * r + 1];
-        mass[j] += w;
+        if (attend_counts(a, b, j, w)) mass[j] += w;
     }
 }
 

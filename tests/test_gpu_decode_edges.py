@@ -79,3 +79,23 @@ def test_attention_of_values_near_the_largest(dtype, largest, lengths, Hq, heads
         return q, k, v, table, lens
     attend(dtype, lengths, Hq, heads, d, page, window=window, seed=41, edit=edit)
     attend(dtype, lengths, Hq, heads, d, page, window=window, seed=42, edit=edit, mass=True)
+
+
+@pytest.mark.parametrize("page", [2, 16])
+@pytest.mark.parametrize("length,B,heads", [(90, 2, 2), (3000, 2, 2), (300, 8, 32)])
+def test_weights_of_a_head_with_nan_leave_slots_without_a_row_alone(page, length, B, heads):
+    """One part, parts that are joined, and scores that stay on the chip."""
+    k, v, table = D.paged([length] * B, page, heads, 64, BF16, 3)
+    q = D.rows(B, 2 * heads, 64, dtype=BF16, seed=4)
+    q[1, 1, 3] = float("nan")                             # a query head of the first cache head of the second request
+    table[:, 1] = -1
+    slots = table.shape[1] * page
+    before = torch.rand(B, heads, slots, generator=torch.Generator().manual_seed(1))
+    mass = dev(before)
+    ann.ann_paged_attention(dev(q), dev(k), dev(v), dev(table), torch.full((B,), length, dtype=torch.int32, device=DEV), mass=mass)
+    mass = mass.cpu()
+    j = torch.arange(slots)
+    there = (j < length) & ((j < page) | (j >= 2 * page))
+    assert torch.equal(mass[:, :, ~there], before[:, :, ~there])
+    assert torch.isnan(mass[1, 0, there]).all() and torch.isfinite(mass[0]).all() and torch.isfinite(mass[1, 1:]).all() and torch.isfinite(mass[2:]).all()
+    assert (mass[0][:, there] >= before[0][:, there]).all()
