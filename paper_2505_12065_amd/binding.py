@@ -517,6 +517,14 @@ def _strides(t: torch.Tensor):
     return [s if n > 1 else 0 for s, n in zip(t.stride()[:-1], t.shape)]
 
 
+def _int32(x, name: str) -> int:
+    """x as an int that the C call takes as it is (ctypes keeps the low 32 bits of a larger one, without a word)."""
+    x = int(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError(f"{name} = {x} does not fit 32 bits")
+    return x
+
+
 def _cache(k_cache: torch.Tensor, v_cache: torch.Tensor) -> PagedCache:
     for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
         if t.dim() != 4 or not t.is_cuda or t.dtype not in _DTYPES or (t.shape[3] > 1 and t.stride(3) != 1):
@@ -584,15 +592,16 @@ def ann_paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.T
     lse = torch.empty(B, q_heads, dtype=torch.float32, device=q.device) if lse is None else _array(lse, "lse", torch.float32, (B, q_heads))
     _same_device(k_cache, q, page_table, lengths, mass, out, lse)
     _call(q.device, stream, lib().ann_paged_attention, q.data_ptr(), *_strides(q), B, q_heads, ctypes.byref(cache),
-          page_table.data_ptr(), width, lengths.data_ptr(), width * cache.slots if max_length is None else int(max_length),
-          d ** -0.5 if scale is None else float(scale), int(window), out.data_ptr(), lse.data_ptr(),
+          page_table.data_ptr(), width, lengths.data_ptr(), width * cache.slots if max_length is None else _int32(max_length, "max_length"),
+          d ** -0.5 if scale is None else float(scale), _int32(window, "window"), out.data_ptr(), lse.data_ptr(),
           0 if mass is None else mass.data_ptr(), 0 if mass is None else mass.shape[2])
     return out, lse
 
 
 def ann_paged_attention_workspace_bytes(B: int, q_heads: int, heads: int, d: int, dtype: torch.dtype, max_length: int,
                                         with_mass: bool = False) -> int:
-    return int(lib().ann_paged_attention_workspace_bytes(B, q_heads, heads, d, _DTYPES[dtype], max_length, 1 if with_mass else 0))
+    sizes = [_int32(x, name) for x, name in ((B, "B"), (q_heads, "q_heads"), (heads, "heads"), (d, "d"))]
+    return int(lib().ann_paged_attention_workspace_bytes(*sizes, _DTYPES[dtype], _int32(max_length, "max_length"), 1 if with_mass else 0))
 
 
 def ann_cache_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor,
@@ -607,7 +616,7 @@ def ann_cache_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: to
             return usual
     cache = _cache(k_cache, v_cache)
     _array(page_table, "page_table", torch.int32, (-1, -1))
-    B, device, budget = page_table.shape[0], k_cache.device, int(budget)
+    B, device, budget = page_table.shape[0], k_cache.device, _int32(budget, "budget")
     _array(lengths, "lengths", torch.int32, (B,)), _array(mass, "mass", torch.float32, (B, cache.heads, -1))
     _array(new_page_table, "new_page_table", torch.int32, (B, -1))
     _same_device(k_cache, page_table, lengths, mass, new_page_table)
@@ -616,7 +625,7 @@ def ann_cache_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: to
     new_lengths = torch.empty(B, dtype=torch.int32, device=device)
     new_mass = torch.empty(B, cache.heads, new_slots, dtype=torch.float32, device=device)
     _call(device, stream, lib().ann_cache_evict, ctypes.byref(cache), page_table.data_ptr(), page_table.shape[1], lengths.data_ptr(), B,
-          mass.data_ptr(), mass.shape[2], new_page_table.data_ptr(), new_page_table.shape[1], budget, int(first), int(recent),
+          mass.data_ptr(), mass.shape[2], new_page_table.data_ptr(), new_page_table.shape[1], budget, _int32(first, "first"), _int32(recent, "recent"),
           kept.data_ptr(), new_lengths.data_ptr(), new_mass.data_ptr(), new_slots)
     return kept, new_lengths, new_mass
 

@@ -99,3 +99,16 @@ def test_weights_of_a_head_with_nan_leave_slots_without_a_row_alone(page, length
     assert torch.equal(mass[:, :, ~there], before[:, :, ~there])
     assert torch.isnan(mass[1, 0, there]).all() and torch.isfinite(mass[0]).all() and torch.isfinite(mass[1, 1:]).all() and torch.isfinite(mass[2:]).all()
     assert (mass[0][:, there] >= before[0][:, there]).all()
+
+
+def test_whole_numbers_beyond_32_bits_are_refused():
+    """Not taken for what is left of them in 32 bits."""
+    k = torch.zeros(4, 2, 16, 64, dtype=BF16, device=DEV)
+    q, table = torch.zeros(3, 4, 64, dtype=BF16, device=DEV), torch.zeros(3, 2, dtype=torch.int32, device=DEV)
+    n, mass = torch.zeros(3, dtype=torch.int32, device=DEV), torch.zeros(3, 2, 32, device=DEV)
+    for kw in (dict(window=2 ** 32 + 1), dict(window=2 ** 32), dict(window=2 ** 31), dict(max_length=2 ** 32 + 8), dict(max_length=-2 ** 32 + 8)):
+        with pytest.raises(ValueError):
+            ann.ann_paged_attention(q, k, k, table, n, **kw)
+    for budget, kw in ((2 ** 32 + 8, {}), (-2 ** 32 + 8, {}), (8, dict(first=2 ** 32 + 1)), (8, dict(recent=2 ** 32)), (8, dict(first=-2 ** 32))):
+        with pytest.raises(ValueError):
+            ann.ann_cache_evict(k, k, table, n, mass, table, budget, **kw)
