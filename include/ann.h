@@ -433,6 +433,8 @@ int ann_cache_evict(const ann_paged_cache *cache, const int32_t *page_table, int
  *     bit v % 32 of masks[mask_rows[b], v / 32] is 0:  l = -inf
  *   logits, out     device [B, V] of dtype; strides row_stride, out_stride >= V; out may be logits
  *   tokens          device int32 [B, T], T <= ANN_HISTORY_MAX; ids outside [0, V) are skipped
+ *                   the order matters only in what lies before prompt_lengths[b]: put there all that the request did not choose itself, retrieved
+ *                   passages among it, wherever they came in (their words are what an answer repeats), and behind it what it did
  *   lengths, prompt_lengths  device int32 [B]; count as in [0, T];  repetition, presence, frequency  device float [B]
  *   bias_tokens, bias_values device int32 / float [B, K], K <= ANN_BIAS_MAX; K = 0: NULL.  Ids outside [0, V) are skipped
  *   masks           device uint32 [n_masks, ceil(V / 32)];  mask_rows  device int32 [B], outside [0, n_masks): no mask;

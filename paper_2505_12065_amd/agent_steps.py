@@ -55,7 +55,10 @@ class Agents:
         self.pages: List[List[int]] = [[] for _ in range(requests)]
         self.slots_used, self.position = [0] * requests, [0] * requests
         self.tokens = torch.zeros(requests, 8192, dtype=torch.int32, device=device)
-        self.told, self.prompt, self.asked = [0] * requests, len(prompt) + len(questions[0]), [0] * requests
+        self.told, self.asked = [0] * requests, [0] * requests
+        # the same tokens for the rules on logits, those that a request was given (prompt, question, passages) before those that it chose: penalties are for the latter,
+        # and the words of a passage are what an answer should repeat
+        self.history, self.given = torch.zeros_like(self.tokens), [0] * requests
         # what a state allows: row 0 anything, row 1 no further search; a token is a bit
         allowed = torch.ones(2, (vocab + 31) // 32 * 32, dtype=torch.int64)
         allowed[:, PAD], allowed[1, SEARCH] = 0, 0
@@ -68,8 +71,8 @@ class Agents:
             self.pages[b] = list(self.pages[0])
             for p in self.pages[b]:
                 self.used[p] += 1
-            self.slots_used[b], self.position[b], self.told[b] = self.slots_used[0], self.position[0], self.told[0]
-            self.tokens[b, :shared] = self.tokens[0, :shared]
+            self.slots_used[b], self.position[b], self.told[b], self.given[b] = self.slots_used[0], self.position[0], self.told[0], self.given[0]
+            self.tokens[b, :shared], self.history[b, :shared] = self.tokens[0, :shared], self.history[0, :shared]
             for m in self.mass:
                 m[b] = m[0]
         for tokens in [[token] * requests for token in prompt[shared:]] + [list(t) for t in zip(*questions)]:
@@ -105,8 +108,8 @@ class Agents:
             self.pages[b], self.slots_used[b] = pages, min(self.slots_used[b], self.budget)
         return kept
 
-    def step(self, next_tokens: List[int], rows=None):
-        """One new token of each of these requests (all, unless given): (logits [requests, vocab], last hidden state)."""
+    def step(self, next_tokens: List[int], rows=None, chosen=()):
+        """One new token of each of these requests (all, unless given), which those in `chosen` chose themselves: (logits [requests, vocab], last hidden state)."""
         rows = list(range(self.B)) if rows is None else rows
         full = [b for b in rows if self.slots_used[b] == self.limit]
         if full:
@@ -115,7 +118,11 @@ class Agents:
             if self.slots_used[b] % self.page == 0:       # a page of its own (one that is shared is full)
                 self.pages[b] += self._take(1)
             self.slots_used[b] += 1
-            self.tokens[b, self.told[b]] = token
+            self.tokens[b, self.told[b]] = self.history[b, self.told[b]] = token
+            if b not in chosen:                           # (changes places with the first that was chosen: their order does not matter)
+                self.history[b, self.told[b]] = self.history[b, self.given[b]]
+                self.history[b, self.given[b]] = token
+                self.given[b] += 1
             self.told[b] += 1
         slots = self._ints([self.pages[b][(self.slots_used[b] - 1) // self.page] * self.page + (self.slots_used[b] - 1) % self.page for b in rows])
         positions, lengths = self._ints([self.position[b] for b in rows]), self._ints([self.slots_used[b] for b in rows])
@@ -137,10 +144,10 @@ class Agents:
     def choose(self) -> List[int]:
         """The next token of every request by the rules of its state."""
         B = self.B
-        told, prompts = self._ints(self.told), self._ints([self.prompt] * B)
+        told, given = self._ints(self.told), self._ints(self.given)
         rates = [torch.full((B,), r, device=self.device) for r in (1.1, 0.2, 0.05)]
         bias = self._ints([[SEARCH, ANSWER]] * B), torch.tensor([[2.0, 1.0 * a] for a in self.asked], device=self.device)
-        logits = ann.ann_logit_rules(self.logits, self.tokens, told, prompts, *rates, bias_tokens=bias[0], bias_values=bias[1],
+        logits = ann.ann_logit_rules(self.logits, self.history, told, given, *rates, bias_tokens=bias[0], bias_values=bias[1],
                                      masks=self.masks, mask_rows=self._ints([0 if a < self.searches else 1 for a in self.asked]))
         return logits.float().argmax(1).tolist()
 
@@ -152,6 +159,7 @@ class Agents:
         for _ in range(steps):
             tokens = self.choose()
             asking = [b for b in range(self.B) if not pending[b] and tokens[b] == SEARCH]
+            chosen = [b for b in range(self.B) if not pending[b]]
             tokens = [pending[b].pop(0) if pending[b] else tokens[b] for b in range(self.B)]
             if asking:
                 query = torch.nn.functional.normalize(self.hidden[asking], dim=1).to(torch.float16)
@@ -162,7 +170,7 @@ class Agents:
                     pending[b] = self.passage_tokens[found].flatten().tolist()
             for b in range(self.B):
                 said[b].append(tokens[b])
-            self.logits, self.hidden = self.step(tokens)
+            self.logits, self.hidden = self.step(tokens, chosen=chosen)
         return said, given
 
 

@@ -636,7 +636,7 @@ def ann_logit_rules(logits: torch.Tensor, tokens: torch.Tensor, lengths: torch.T
                     masks: Optional[torch.Tensor] = None, mask_rows: Optional[torch.Tensor] = None, out=None,
                     stream=None) -> torch.Tensor:
     """Penalties for repeated tokens, biases and grammar masks on logits [B, V] (fp16, bf16 or fp32).  tokens int32 [B, T], of which
-    lengths[b] count, the first prompt_lengths[b] of them as the prompt; repetition, presence, frequency float32 [B]; bias_tokens int32
+    lengths[b] count, the first prompt_lengths[b] of them as given (prompt and retrieved passages) and not chosen; repetition, presence, frequency float32 [B]; bias_tokens int32
     and bias_values float32 [B, K]; masks int32 [M, ceil(V / 32)], a bit for each token, 1: allowed, and mask_rows int32 [B] into it,
     -1: no mask.  out may be logits.  Returns out."""
     if out is None and stream is None:
