@@ -1,10 +1,13 @@
-"""The operators over a paged cache at the ends of their ranges, against their definitions in 64 bits."""
+"""The operators over a paged cache at the ends of their ranges, against their definitions in 64 bits, and ways to call them that take another path."""
+import math
+
+import numpy as np
 import pytest
 import torch
 
 import decode as D                                        # (beside this file)
 import paper_2505_12065_amd as ann
-from test_gpu_decode import attend, close, dev            # noqa: F401
+from test_gpu_decode import all_four, attend, dev
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -112,3 +115,135 @@ def test_whole_numbers_beyond_32_bits_are_refused():
     for budget, kw in ((2 ** 32 + 8, {}), (-2 ** 32 + 8, {}), (8, dict(first=2 ** 32 + 1)), (8, dict(recent=2 ** 32)), (8, dict(first=-2 ** 32))):
         with pytest.raises(ValueError):
             ann.ann_cache_evict(k, k, table, n, mass, table, budget, **kw)
+
+
+@pytest.mark.parametrize("most", [4095, 4096, 4097, 8191, 8192, 8193, 12_001, 16_383, 16_384, 16_385, 32_767, 32_768, 32_769])
+@pytest.mark.parametrize("budget,first,recent", [(700, 3, 40), (4000, 0, 0)])
+def test_evict_on_both_sides_of_what_a_thread_holds(most, budget, first, recent):
+    """Rows of as many slots as fit the ranks that a thread holds, one more and one less, and shorter requests among them."""
+    heads, d, page, lengths = 3, 64, 16, [most, most - 1, most * 3 // 5]
+    g = torch.Generator().manual_seed(most + budget)
+    B, new_width = 3, -(-budget // page)
+    k, v, table = D.paged(lengths, page, heads, d, BF16, most, unused=9.0, spare=B * new_width)
+    free = [p for p in range(k.shape[0]) if p not in set(table.flatten().tolist())]
+    new_table = torch.tensor(free[:B * new_width], dtype=torch.int32).view(B, new_width)
+    mass = torch.randn(B, heads, most, generator=g).pow(3)
+    mass[:, 1] = (mass[:, 1] * 2).round() / 2             # equal ones by the hundred
+    mass[:, 2, ::5] = 0.25
+    mass[0, 0, 3::7], mass[0, 0, 4::11], mass[0, 2, 2::9] = math.nan, math.inf, -math.inf
+    mass[1, 2] = math.nan
+    mass[2, 2] = 1.0
+    want, new = D.evict(mass.numpy(), lengths, most, budget, first, recent)
+    dk, dv = dev(k), dev(v)
+    kept, got_new, got_mass = ann.ann_cache_evict(dk, dv, dev(table), torch.tensor(lengths, dtype=torch.int32, device=DEV), dev(mass), dev(new_table), budget,
+                                                  first=first, recent=recent)
+    assert np.array_equal(kept.cpu().numpy(), want) and np.array_equal(got_new.cpu().numpy(), new)
+    for b in range(B):
+        i = torch.arange(int(new[b]))
+        for h in range(heads):
+            j = torch.from_numpy(want[b, h, :int(new[b])]).long()
+            assert np.array_equal(got_mass[b, h, :len(i)].cpu().numpy(), mass[b, h, j].numpy(), equal_nan=True)
+            for got, source in ((dk, k), (dv, v)):
+                assert torch.equal(got[new_table[b].long()[i // page].to(DEV), h, (i % page).to(DEV)].cpu(), source[table[b].long()[j // page], h, j % page])
+
+
+def test_streams_that_are_named():
+    """stream= of all four, a Stream or its handle, instead of the current one."""
+    want = [t.clone() for t in all_four()()]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream):
+        call = all_four(stream)
+        torch.cuda.synchronize()                          # (its inputs were made on the current one)
+        with torch.cuda.stream(side):                     # (what torch itself does inside)
+            got = call()
+        side.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    # the operators alone on `side`, torch's own work on the current stream
+    k, v, table = (dev(t) for t in D.paged([300, 40], 16, 2, 64, BF16, 21, unused=0.0))
+    q, n = dev(D.rows(2, 8, 64, dtype=BF16, seed=5)), torch.tensor([300, 40], dtype=torch.int32, device=DEV)
+    plain = ann.ann_paged_attention(q, k, v, table, n)
+    torch.cuda.synchronize()
+    named = ann.ann_paged_attention(q, k, v, table, n, stream=side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(plain, named))
+
+
+@pytest.mark.parametrize("lengths", [[300, 0, 33], [5000, 1, 0]])
+@pytest.mark.parametrize("with_mass", [False, True])
+def test_outputs_that_are_given_or_not_wanted(lengths, with_mass):
+    k, v, table = (dev(t) for t in D.paged(lengths, 16, 2, 64, F16, 8))
+    q, n = dev(D.rows(3, 8, 64, dtype=F16, seed=9)), torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    masses = [torch.zeros(3, 2, table.shape[1] * 16, device=DEV) if with_mass else None for _ in range(3)]
+    want = ann.ann_paged_attention(q, k, v, table, n, mass=masses[0])
+    out, lse = torch.full_like(want[0], 7), torch.full_like(want[1], 7)
+    got = ann.ann_paged_attention(q, k, v, table, n, out=out, lse=lse, mass=masses[1])
+    assert got[0] is out and got[1] is lse and torch.equal(out, want[0]) and torch.equal(lse, want[1])
+    out = torch.full_like(out, 7)
+    b = ann.binding
+    cache = b._cache(k, v)
+    rc = b.lib().ann_paged_attention(q.data_ptr(), 512, 64, 3, 8, cache, table.data_ptr(), table.shape[1], n.data_ptr(), table.shape[1] * 16, 0.125, 0,
+                                     out.data_ptr(), None, masses[2].data_ptr() if with_mass else None, table.shape[1] * 16, torch.cuda.current_stream().cuda_stream)
+    assert rc == 0 and torch.equal(out, want[0])
+    assert not with_mass or all(torch.equal(m, masses[0]) for m in masses)
+    for bad in (dict(out=out.float()), dict(out=out[:2]), dict(lse=lse.half()), dict(lse=lse[:, :4]), dict(out=out.cpu())):
+        with pytest.raises(ValueError):
+            ann.ann_paged_attention(q, k, v, table, n, **bad)
+
+
+@pytest.mark.parametrize("with_mass", [False, True])
+@pytest.mark.parametrize("own", [False, True])
+def test_captured_with_less_workspace_than_is_wanted(with_mass, own):
+    """The library's buffer may not grow while a stream is captured, a caller's never does: the graph takes fewer requests at a time, with the same bits."""
+    lengths = [3000, 10, 2000, 0, 2999, 1500, 700]
+    k, v, table = D.paged(lengths, 16, 2, 64, F16, 2)
+    args = dev(D.rows(7, 8, 64, dtype=F16, seed=4)), dev(k), dev(v), dev(table), torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    slots = table.shape[1] * 16
+    want = ann.ann_paged_attention(*args, mass=None)
+    mass = torch.zeros(7, 2, slots, device=DEV) if with_mass else None
+    if with_mass:
+        want = (*ann.ann_paged_attention(*args, mass=mass), mass.clone())
+    one, whole = (ann.ann_paged_attention_workspace_bytes(B, 8, 2, 64, F16, slots, with_mass) for B in (1, 7))
+    assert 1.3 * one < whole
+    torch.cuda.synchronize()
+    ann.ann_release_workspace()
+    if own:                                               # (a call of one request, so that there is a little; it grows by a quarter more than that)
+        ann.ann_paged_attention(args[0][:1], args[1], args[2], args[3][:1], args[4][:1], mass=None if mass is None else torch.zeros_like(mass[:1]))
+    else:
+        buffer = torch.empty(one, dtype=torch.uint8, device=DEV)            # (the library keeps its address alone)
+        ann.ann_set_workspace(buffer)
+    torch.cuda.synchronize()
+    try:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            if with_mass:
+                mass.zero_()
+            got = ann.ann_paged_attention(*args, mass=mass)
+        got = (*got, mass) if with_mass else got
+        for _ in range(4):
+            for t in got:
+                t.fill_(3)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+            torch.randn(1000, 1000, device=DEV).sum().item()
+    finally:
+        torch.cuda.synchronize()
+        ann.ann_set_workspace(None)
+
+
+@pytest.mark.parametrize("dtype,bits", [(F32, 0), (F16, 2.0 ** -22), (BF16, 2.0 ** -17)])
+def test_bits_of_a_weight(dtype, bits):
+    """An output that is one weight: its exponent t log2 e is off by two roundings, |t| <= 3 times 2 U, the power of two, the sum, its reciprocal and the product
+    by 1 to 2 U each; 16-bit types have the weight in two parts, which are off by `bits`, and round the output.  An fp32 weight in two such parts would be seen."""
+    B, d, g = 256, 8, torch.Generator().manual_seed(7)
+    t = (3 * torch.rand(B, generator=g)).to(dtype)
+    q, k, v = torch.zeros(B, 1, d, dtype=dtype), torch.zeros(B, 1, 16, d, dtype=dtype), torch.zeros(B, 1, 16, d, dtype=dtype)
+    q[:, 0, 0], k[:, 0, 1, 0], v[:, 0, 1] = 1, -t, 1
+    table, n = torch.arange(B, dtype=torch.int32).view(B, 1), torch.full((B,), 2, dtype=torch.int32)
+    out, lse = ann.ann_paged_attention(dev(q), dev(k), dev(v), dev(table), dev(n), scale=1.0)
+    w = torch.exp(-t.double())
+    want = (w / (1 + w))[:, None, None]
+    off = ((out.double().cpu() - want) / want).abs().max().item()
+    assert off <= 20 * D.U + bits + (D.HALF_ULP[dtype] * 1.01 if dtype != F32 else 0), off
+    assert (lse[:, 0].double().cpu() - torch.log1p(w)).abs().max() <= 20 * D.U
