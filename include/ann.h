@@ -417,7 +417,7 @@ int64_t ann_paged_attention_workspace_bytes(int32_t B, int32_t q_heads, int32_t 
  *               still reads; rows that would go to an empty page are dropped
  *   budget      1 <= budget <= min(new_width slots, new_mass_slots); first, recent >= 0, first + recent <= budget
  *   kept        device int32 [B, heads, budget]: the slots, ascending, -1 behind the last (written)
- *   new_lengths device int32 [B]: min(n, budget) (written)
+ *   new_lengths device int32 [B]: min(n, budget) (written; not lengths itself, which workgroups go on reading, nor new_mass mass)
  *   new_mass    device float [B, heads, new_mass_slots]: the mass of the kept slots, 0 behind them (written)
  * No workspace.  B = 0 returns ANN_OK at once. */
 int ann_cache_evict(const ann_paged_cache *cache, const int32_t *page_table, int32_t width, const int32_t *lengths, int32_t B,
@@ -431,7 +431,7 @@ int ann_cache_evict(const ann_paged_cache *cache, const int32_t *page_table, int
  *     v c > 0 times among those from prompt_lengths[b] on:  l = l - frequency[b] c - presence[b]
  *     v = bias_tokens[b, i]:  l = l + bias_values[b, i]  (the last such i)
  *     bit v % 32 of masks[mask_rows[b], v / 32] is 0:  l = -inf
- *   logits, out     device [B, V] of dtype; strides row_stride, out_stride >= V; out may be logits
+ *   logits, out     device [B, V] of dtype; strides row_stride, out_stride >= V; out may be logits, with its stride
  *   tokens          device int32 [B, T], T <= ANN_HISTORY_MAX; ids outside [0, V) are skipped
  *                   the order matters only in what lies before prompt_lengths[b]: put there all that the request did not choose itself, retrieved
  *                   passages among it, wherever they came in (their words are what an answer repeats), and behind it what it did

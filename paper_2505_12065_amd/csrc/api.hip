@@ -540,6 +540,7 @@ int ann_cache_evict(const ann_paged_cache *cache, const int32_t *page_table, int
         return fail(ANN_ERR_ALIGNMENT, "tables, lengths, masses and kept must be 4-byte aligned");
     if ((int64_t)B * cache->heads > GRID_MAX / 4 || (int64_t)B * cache->heads * (((int64_t)budget + 3) / 4) > GRID_MAX * 2)
         return fail(ANN_ERR_INVALID, "%d requests of %d heads with a budget of %d are too many for a call", B, cache->heads, budget);
+    if (new_lengths == lengths || new_mass == mass) return fail(ANN_ERR_INVALID, "new_lengths and new_mass may not be what is read: lengths, mass");
     a.table = page_table; a.width = width; a.lengths = lengths; a.mass = mass; a.mass_slots = mass_slots;
     a.most = (int)(mass_slots < (int64_t)width * cache->slots ? mass_slots : (int64_t)width * cache->slots);
     a.new_table = new_page_table; a.new_width = new_width; a.budget = budget; a.first = first; a.recent = recent;
@@ -564,6 +565,7 @@ int ann_logit_rules(const void *logits, int64_t row_stride, int32_t B, int32_t V
     if (n_masks < 0) return fail(ANN_ERR_INVALID, "n_masks = %d out of range", n_masks);
     if (row_stride < V || out_stride < V || row_stride > INT64_MAX >> 34 || out_stride > INT64_MAX >> 34)
         return fail(ANN_ERR_INVALID, "strides of logits or out out of range");
+    if (out == logits && B > 1 && out_stride != row_stride) return fail(ANN_ERR_INVALID, "out may be logits only with its strides");
     const uintptr_t odd = (uintptr_t)elem_bytes(dtype) - 1;
     if ((reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(out)) & odd)
         return fail(ANN_ERR_ALIGNMENT, "logits and out must be aligned to their elements");
