@@ -23,9 +23,11 @@
  *     1.25 GiB at most for the flat search).  A buffer that a captured graph may hold
  *     is not freed then but kept until ann_release_workspace, so the graph can be replayed.
  *   - One workspace per device: calls that use it (the flat search over more rows than
- *     it says below, the graph search with ef > 512, the non-stall graph search) are safe
+ *     it says below, the graph search with ef > 512, the non-stall graph search, ann_paged_attention
+ *     where a context is divided into parts or weights are kept for their sum) are safe
  *     one after the other on one stream, or on several streams if the caller orders them;
- *     two of them running at once on one device race on the workspace.  The plain
+ *     two of them running at once on one device race on the workspace, a decode step beside a
+ *     search on another stream among them.  The plain
  *     graph search with ef <= 512 uses no workspace and may overlap anything, as
  *     may a flat search over so few rows that it uses none.
  *   - corpus  [N, d] row-major, contiguous, 16-byte aligned base.
@@ -273,7 +275,7 @@ int64_t ann_flat_workspace_bytes(int64_t N, int32_t d, int32_t dtype, int32_t B,
 
 /* Use a caller-owned device buffer as the workspace of the current device (so that, e.g., the
  * caller's allocator owns the memory and no entry point ever allocates): every call that needs
- * workspace (ann_flat_workspace_bytes, ann_graph_nonstall_workspace_bytes) then runs in it.  A flat
+ * workspace (ann_flat_workspace_bytes, ann_graph_nonstall_workspace_bytes, ann_paged_attention_workspace_bytes) then runs in it.  A flat
  * search that does not fit `bytes` at once takes the corpus in parts, or fewer slabs, or (up to 64
  * queries of 16 bits) the kernel that needs less, if its own needs parts that take longer; one that would need parts of fewer than 8192 rows, or
  * less than a quarter of its slabs, and a graph search that needs more than `bytes`, fail with
@@ -373,7 +375,7 @@ typedef struct ann_paged_cache {
  *               is zero and nothing is put into the cache.
  *   slots       device int32 [T].  A token whose slot is not one of the cache's is not put there.  Two tokens
  *               with one slot: either's row is left, or a mixture.
- * T = 0 returns ANN_OK at once.  No workspace. */
+ * T at most 2^22, q_heads and heads 65536.  T = 0 returns ANN_OK at once.  No workspace. */
 int ann_qk_norm_rotate(const void *qkv, int64_t token_stride, int64_t head_stride, int32_t T, int32_t q_heads,
                        const void *q_weight, const void *k_weight, float eps,
                        const int32_t *positions, const float *cos_sin, int32_t max_positions, int32_t rot,
@@ -383,19 +385,23 @@ int ann_qk_norm_rotate(const void *qkv, int64_t token_stride, int64_t head_strid
  * values of cache head h / (q_heads / heads):
  *     x_j = scale <q, k_j>,  lse = log sum_j exp(x_j),  out = sum_j exp(x_j - lse) v_j
  * over the slots j < n = lengths[b] whose page is not empty, and of these, with window > 0, the last `window`
- * only (j >= n - window).  A request for which nothing is left gives out = 0, lse = -inf.  Sums, the softmax and its
- * statistics are binary32; out is rounded once.
+ * only (j >= n - window).  A request for which nothing is left gives out = 0, lse = -inf.  Scores, sums,
+ * weights and statistics are binary32, but for the product with V 16-bit types have a weight in two parts of their own bits, which is off by at most
+ * 2^-17 of it (bf16), or 2^-22 of it or 2^-37 of the largest (fp16); out is rounded once.
  *   q           device [B, q_heads, d] of the cache's type; strides q_row, q_head (multiples of 16 bytes)
  *   page_table  device int32 [B, width], rows one after the other; width >= 1
  *   lengths     device int32 [B]; counts as no more than max_length (1 <= max_length <= width slots), and as 0 if negative
- *   max_length  what the work is divided by: the largest length, where the host knows it
+ *   max_length  what the work is divided by, since no length is read on the host: the largest length, or a bound on it as close as the host knows.  In
+ *               graphs it is what the graph is captured with.  Too large a bound costs parts that are too large or too many: one request of 1500 slots takes
+ *               24 us instead of 9 if told 131072, 64 of up to 1000 with mass 60 instead of 41 if told 32768 (8 cache heads, 32 query heads of 128)
  *   out         device [B, q_heads, d], contiguous;  lse  device float [B, q_heads], or NULL
  *   mass        NULL, or device float [B, heads, mass_slots], mass_slots >= width slots: the weight
  *               exp(x_j - lse) of slot j, summed over the query heads of a cache head, is added to mass[b, head, j]
  * An infinite value with a weight above 0 gives an infinity or a NaN; finite values, however large, do not (but for an out that itself
- * rounds to beyond the type's largest).  Values of bf16 and fp32 below 2^-126 times the number of slots may count as 0.  Same inputs give bitwise-same outputs.  Uses the workspace of the current device (conventions at the top;
- * ann_set_workspace) for what the parts of a long context leave to be joined, and for scores if mass is given: the size below, where it is
- * there; with less, or beyond 1 GiB, a few requests at a time.  B = 0 returns ANN_OK at once. */
+ * rounds to beyond the type's largest).  Values of bf16 and fp32 below 2^-126 times the number of slots may count as 0.  Same inputs
+ * give bitwise-same outputs.  Uses the workspace of the current device (conventions at the top; ann_set_workspace) for what the parts of a
+ * long context leave to be joined, and for scores if mass is given: the size below, where it is there; with less, or beyond 1 GiB, a few
+ * requests at a time.  q_heads at most 8192, B q_heads 2^22, width slots 2^31 - 65537.  B = 0 returns ANN_OK at once. */
 int ann_paged_attention(const void *q, int64_t q_row, int64_t q_head, int32_t B, int32_t q_heads,
                         const ann_paged_cache *cache, const int32_t *page_table, int32_t width,
                         const int32_t *lengths, int32_t max_length, float scale, int32_t window,
@@ -419,7 +425,7 @@ int64_t ann_paged_attention_workspace_bytes(int32_t B, int32_t q_heads, int32_t 
  *   kept        device int32 [B, heads, budget]: the slots, ascending, -1 behind the last (written)
  *   new_lengths device int32 [B]: min(n, budget) (written; not lengths itself, which workgroups go on reading, nor new_mass mass)
  *   new_mass    device float [B, heads, new_mass_slots]: the mass of the kept slots, 0 behind them (written)
- * No workspace.  B = 0 returns ANN_OK at once. */
+ * B heads at most 2^20, B heads ceil(budget / 4) 2^23.  No workspace.  B = 0 returns ANN_OK at once. */
 int ann_cache_evict(const ann_paged_cache *cache, const int32_t *page_table, int32_t width, const int32_t *lengths, int32_t B,
                     const float *mass, int64_t mass_slots, const int32_t *new_page_table, int32_t new_width,
                     int32_t budget, int32_t first, int32_t recent,
@@ -432,14 +438,14 @@ int ann_cache_evict(const ann_paged_cache *cache, const int32_t *page_table, int
  *     v = bias_tokens[b, i]:  l = l + bias_values[b, i]  (the last such i)
  *     bit v % 32 of masks[mask_rows[b], v / 32] is 0:  l = -inf
  *   logits, out     device [B, V] of dtype; strides row_stride, out_stride >= V; out may be logits, with its stride
- *   tokens          device int32 [B, T], T <= ANN_HISTORY_MAX; ids outside [0, V) are skipped
- *                   the order matters only in what lies before prompt_lengths[b]: put there all that the request did not choose itself, retrieved
+ *   tokens          device int32 [B, T], T <= ANN_HISTORY_MAX; ids outside [0, V) are skipped.  Their
+ *                   order matters only in what lies before prompt_lengths[b]: put there all that the request did not choose itself, retrieved
  *                   passages among it, wherever they came in (their words are what an answer repeats), and behind it what it did
  *   lengths, prompt_lengths  device int32 [B]; count as in [0, T];  repetition, presence, frequency  device float [B]
  *   bias_tokens, bias_values device int32 / float [B, K], K <= ANN_BIAS_MAX; K = 0: NULL.  Ids outside [0, V) are skipped
  *   masks           device uint32 [n_masks, ceil(V / 32)];  mask_rows  device int32 [B], outside [0, n_masks): no mask;
  *                   both NULL with n_masks = 0
- * No workspace.  B = 0 returns ANN_OK at once. */
+ * B ceil(V / 1024) at most 2^22.  No workspace.  B = 0 returns ANN_OK at once. */
 #define ANN_HISTORY_MAX 16777215
 #define ANN_BIAS_MAX    4096
 int ann_logit_rules(const void *logits, int64_t row_stride, int32_t B, int32_t V, int32_t dtype,

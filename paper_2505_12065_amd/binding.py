@@ -574,8 +574,10 @@ def ann_paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.T
                         lengths: torch.Tensor, *, scale: Optional[float] = None, window: int = 0, max_length: Optional[int] = None,
                         mass: Optional[torch.Tensor] = None, out=None, lse=None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Attention of one new token per request over its paged cache.  q [B, query heads, d], page_table int32 [B, pages of a
-    request], lengths int32 [B]; scale 1 / sqrt(d) unless given; max_length: the largest length, where it is known.  mass
-    float32 [B, heads, slots]: the weight of every slot is added to it.  Returns (out [B, query heads, d], lse float32 [B, query heads])."""
+    request], lengths int32 [B]; scale 1 / sqrt(d) unless given; max_length: the largest length, or a bound as close as
+    is known, which decides how the work is divided (else all that the page table holds, which costs time where contexts are much shorter).  mass
+    float32 [B, heads, slots]: the weight of every slot is added to it.  Long contexts and weights use the device's one workspace, as some searches do: such
+    calls on several streams have to be ordered (ann_set_workspace).  Returns (out [B, query heads, d], lse float32 [B, query heads])."""
     if out is None and lse is None and stream is None:
         usual = _usual("attend", q, k_cache, v_cache, page_table, lengths, scale, window, max_length, mass)
         if usual is not None:
