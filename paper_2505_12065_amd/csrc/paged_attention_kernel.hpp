@@ -10,8 +10,8 @@
 //
 // Bound by reading K and V once: G = q_heads / heads query heads make G multiply-adds of a 16-bit element, a tenth of what the matrix cores do in the
 // time even where 15 of 16 columns are empty (G = 1).  So the loop asks for V of these slots and K of the next before it needs either, 16 KB a wave at d = 128, three
-// workgroups to a compute unit.  64 requests of 9216 slots, 8 cache heads of 128, bf16 (2.4 GB): 390 us, 6.2 TB/s, which is what a loop of loads reads; G = 1: 6.35,
-// d = 256: 6.1, fp32: 6.2, pages of 8 slots 5.7, of one 4.2 (a look-up for each row).  One request of 131072 slots (0.54 GB): 103 us a call.
+// workgroups to a compute unit.  64 requests of 9216 slots, 8 cache heads of 128, bf16 (2.4 GB): 376 to 390 us, 6.4 to 6.2 TB/s, which is what a loop of loads reads; G = 1: 6.6,
+// d = 256: 6.3, fp32: 6.4, pages of 8 slots 5.7, of one 5.4 (a look-up for each row).  One request of 131072 slots (0.54 GB): 103 to 107 us a call.
 #pragma once
 
 #include <type_traits>
@@ -604,8 +604,8 @@ __global__ __launch_bounds__(ATTEND_THREADS, (MT > 1 && (VE == 16 || T::bytes ==
     }
 }
 
-// What the parts of a context left, joined by a launch of its own: the workgroup that is done last could do it, but only behind fences that write back an XCD's
-// whole L2 (one request of 1500 slots: 16.9 us against 10.2).  The first workgroups take query heads: a wave to a head if there are few parts (FEW), else a
+// What the parts of a context left, joined by a launch of its own: the workgroup that is done last was slower at it behind __threadfence, which writes back an XCD's
+// whole L2 (one request of 1500 slots: 16.9 us against 10.2); stores and loads at agent scope, which pass the L2 by, were not tried.  The first workgroups take query heads: a wave to a head if there are few parts (FEW), else a
 // workgroup to a head; none do where there is one part only.  Those behind them (scores given) take a piece of the slots of a cache head each.
 template <class T, bool FEW>
 __global__ __launch_bounds__(ATTEND_THREADS) void paged_attention_join_kernel(AttentionArgs a) {
