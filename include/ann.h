@@ -455,6 +455,83 @@ int ann_logit_rules(const void *logits, int64_t row_stride, int32_t B, int32_t V
                     const uint32_t *masks, int32_t n_masks, const int32_t *mask_rows,
                     void *out, int64_t out_stride, void *stream);
 
+/*
+ * ---- Many tokens at once: prompts and passages into a paged cache, and contexts in common ---------
+ *
+ * What a retrieval returns, or a prompt, is taken in at once: ann_rotate_append puts the new tokens of several requests into their caches,
+ * ann_chunk_attention attends from them.  Agents that share a context go on from it together with ann_shared_attention.
+ * The tokens of a batch are packed, request b's being starts[b] to starts[b + 1] - 1 (n of them); starts is a device int32 array [B + 1] that ascends, within [0, T].  Rows of tokens that are
+ * no request's are not written.  lengths[b] counts the slots of request b with its new tokens, which are the last: token i of n has slot lengths[b] - n + i.  The conventions and the paged cache are those
+ * of the section above.
+ */
+
+/* How the frequencies of a rotation are scaled for contexts longer than those a model was trained with.  With f_i = base^(-2 i / rot), i < rot / 2: */
+#define ANN_ROTATION_NONE   0  /* f_i */
+#define ANN_ROTATION_LINEAR 1  /* f_i / factor */
+#define ANN_ROTATION_BASE   2  /* f_i of the base  base factor^(rot / (rot - 2)) */
+#define ANN_ROTATION_RAMP   3  /* f_i ((1 - g_i) + g_i / factor), g_i = (i - a) / (b - a) held to [0, 1], where i(r) = rot ln(original / (2 pi r)) / (2 ln base) is the pair that turns r times in
+                                  the original context, a = max(floor(i(high)), 0), b = min(ceil(i(low)), rot - 1), a + 0.001 if that is not above a; amplitude 0.1 ln(factor) + 1 */
+#define ANN_ROTATION_SMOOTH 4  /* with r = original f_i / (2 pi) turns: f_i / factor if r < low, f_i if r > high, else f_i ((1 - u) / factor + u), u = (r - low) / (high - low) */
+
+/* The rot / 2 frequencies, in radians for each position, and the amplitude (1 but for ANN_ROTATION_RAMP) that ann_rotate_append takes, in binary64.  On the host; needs no device.
+ *   rot a multiple of 16 in [16, ANN_HEAD_MAX]; base > 1; factor >= 1 (ignored by ANN_ROTATION_NONE)
+ *   original, low, high  the original context's length (at least 1) and 0 < low < high turns in it, for ANN_ROTATION_RAMP (usually 1 and 32) and ANN_ROTATION_SMOOTH (1 and 4)
+ *   frequencies, amplitude  host pointers (written) */
+int ann_rotation_frequencies(int32_t rot, double base, int32_t scaling, double factor, int32_t original, double low, double high,
+                             double *frequencies, double *amplitude);
+
+/* The rotation of queries and keys by position, and the write of keys and values behind what each request holds in its cache, in one pass.  For a token at position p and the pair (a, b) of
+ * elements i and rot / 2 + i, or 2 i and 2 i + 1 if `interleaved`, of every query and key head:
+ *     (a, b) becomes amplitude (a c - b s, b c + a s),   c, s = cos, sin(p frequencies[i]),   i < rot / 2;
+ * elements from rot on keep their bits.  The angle is taken in binary64, the rest in binary32 and rounded once.
+ *   qkv          device, [T, q_heads + 2 heads, d]: query heads, the cache's heads of keys, as many of values; strides token_stride, head_stride (multiples of 16 bytes)
+ *   lengths, page_table  device int32 [B], [B, width]: a token's keys and values go to its slot; one that is not in the table, or whose page is empty, is dropped
+ *   positions    device int32 [T], or NULL: a token's position is its slot.  A token of a negative position is padding: its row of q is zero and nothing is put into the cache
+ *   frequencies  device double [rot / 2]; rot a multiple of 16 in [0, d] (0: nothing is rotated; NULL)
+ *   q            device, [T, q_heads, d]
+ * T at most 2^22, B, q_heads and heads 65536, width slots 2^31 - 65537.  Two tokens with one slot of one page: either's row is left, or a mixture.  T = 0 returns ANN_OK at once.  No workspace. */
+int ann_rotate_append(const void *qkv, int64_t token_stride, int64_t head_stride, int32_t T, int32_t q_heads,
+                      const int32_t *starts, int32_t B, const int32_t *lengths, const int32_t *page_table, int32_t width,
+                      const int32_t *positions, const double *frequencies, int32_t rot, float amplitude, int32_t interleaved,
+                      const ann_paged_cache *cache, void *q, void *stream);
+
+/* Attention of the new tokens of every request, a passage's or a prompt's, over its paged cache, which holds them: ann_paged_attention with as many queries of a request as it has new
+ * tokens.  The token in slot i attends to the slots j <= i whose page is not empty and, with window > 0, of these to j > i - window: x_j, lse and out are those of ann_paged_attention.  A token
+ * without a slot, or for which nothing is left, gives out = 0, lse = -inf.  Scores, sums and statistics are binary32; weights of 16-bit types are rounded to the type for the
+ * product with V (each is off by at most half a unit in its last place; fp16: or 2^-32 of the largest), out is rounded once.
+ *   q           device [T, q_heads, d] of the cache's type; strides q_row, q_head (multiples of 16 bytes)
+ *   lengths     device int32 [B], with the new tokens; as 0 if negative.  A token has its slot only if that is in [0, max_length), 1 <= max_length <= width slots
+ *   max_length  what the work is divided by, as no length is read on the host: the largest length, or a bound as close as the host knows
+ *   out         device [T, q_heads, d], contiguous;  lse  device float [T, q_heads], or NULL
+ * Values that a token does not attend to do not matter to it, NaN and infinities among them; a value that is one of these and has a weight gives one.  Same inputs and workspace give bitwise-same
+ * outputs.  Where there are few tokens, contexts are divided into parts that are joined in the workspace of the current device; with less than the size below they are divided
+ * less, or not at all.  q_heads at most 8192, T q_heads 2^26, T 2^22, B 65536, width slots 2^31 - 65537.  T = 0 returns ANN_OK at once. */
+int ann_chunk_attention(const void *q, int64_t q_row, int64_t q_head, int32_t T, int32_t q_heads, const int32_t *starts, int32_t B,
+                        const ann_paged_cache *cache, const int32_t *page_table, int32_t width,
+                        const int32_t *lengths, int32_t max_length, float scale, int32_t window,
+                        void *out, float *lse, void *stream);
+
+/* Bytes of workspace that ann_chunk_attention uses at these sizes where it has them. */
+int64_t ann_chunk_attention_workspace_bytes(int32_t T, int32_t B, int32_t q_heads, int32_t heads, int32_t d, int32_t dtype, int32_t max_length, int32_t window);
+
+/* Attention of one new token per request, as ann_paged_attention without window and weights, where groups of requests have their leading slots in common (one prompt, one set of
+ * documents): these are read once for a group and not once for each of its requests.
+ *   group_starts  device int32 [groups + 1], ascending, within [0, B]: the requests of group g are group_starts[g] to group_starts[g + 1] - 1; the others are in none
+ *   shared        device int32 [groups]: the first shared[g] slots of the group's requests are the same slots of the same pages (they are read by the page table of the group's first request).
+ *                 It counts as no more than max_shared, as 0 if negative, and for a request as no more than its length
+ *   lengths       device int32 [B]; the slots of request b from the shared ones on are its own, of which no more than max_own count; as 0 if negative
+ *   max_shared, max_own  what the work is divided by: the largest numbers of shared and of own slots, or bounds as close as the host knows.  0 <= max_shared <= width slots, 1 <= max_own <= width slots
+ * 16-bit types: weights are rounded to the type for the product with V, as in ann_chunk_attention.  Otherwise, and for q, page_table, out and lse, as in ann_paged_attention.
+ * Same inputs and workspace give bitwise-same outputs.  Uses the workspace of the current device; with less than the size below
+ * nothing is shared.  groups in [1, 65536], B at most 65536, q_heads 8192, B q_heads 2^22, width slots 2^31 - 65537.  B = 0 returns ANN_OK at once. */
+int ann_shared_attention(const void *q, int64_t q_row, int64_t q_head, int32_t B, int32_t q_heads,
+                         const ann_paged_cache *cache, const int32_t *page_table, int32_t width, const int32_t *lengths,
+                         const int32_t *group_starts, const int32_t *shared, int32_t groups, int32_t max_shared, int32_t max_own, float scale,
+                         void *out, float *lse, void *stream);
+
+/* Bytes of workspace that ann_shared_attention uses at these sizes where it has them. */
+int64_t ann_shared_attention_workspace_bytes(int32_t B, int32_t groups, int32_t q_heads, int32_t heads, int32_t d, int32_t dtype, int32_t max_shared, int32_t max_own);
+
 /* Measurement support (no paper passage): the dense fp16 MFMA rate the current device sustains
  * on register-resident operands, in TFLOP/s, on the default stream (synchronises it).  With
  * random_operands != 0 the operands are random fp16 values that change from one MFMA to the

@@ -23,6 +23,8 @@ ANN_K_MAX, ANN_EF_MAX, ANN_R_MAX, ANN_D_MAX = 16, 16384, 256, 4096
 ANN_ENTRIES_MAX = 32
 ANN_PAGE_MAX, ANN_HEAD_MAX, ANN_HISTORY_MAX, ANN_BIAS_MAX = 1024, 256, 16777215, 4096
 
+ROTATIONS = {"none": 0, "linear": 1, "base": 2, "ramp": 3, "smooth": 4}      # ANN_ROTATION_* of include/ann.h
+
 _DTYPES = {torch.float16: ANN_F16, torch.bfloat16: ANN_BF16, torch.float32: ANN_F32}
 
 EXPORTS = ("ann_version", "ann_last_error", "ann_flat_search_typed", "ann_flat_search",
@@ -33,7 +35,9 @@ EXPORTS = ("ann_version", "ann_last_error", "ann_flat_search_typed", "ann_flat_s
            "ann_measure_mfma_rate", "ann_priority_order", "ann_flat_search_static",
            "ann_graph_search_multi_typed", "ann_timing_read_each",
            "ann_set_workspace", "ann_flat_search_after_typed",
-           "ann_qk_norm_rotate", "ann_paged_attention", "ann_paged_attention_workspace_bytes", "ann_cache_evict", "ann_logit_rules")
+           "ann_qk_norm_rotate", "ann_paged_attention", "ann_paged_attention_workspace_bytes", "ann_cache_evict", "ann_logit_rules",
+           "ann_rotation_frequencies", "ann_rotate_append", "ann_chunk_attention", "ann_chunk_attention_workspace_bytes",
+           "ann_shared_attention", "ann_shared_attention_workspace_bytes")
 
 
 class PagedCache(ctypes.Structure):
@@ -96,9 +100,18 @@ def lib() -> ctypes.CDLL:
         L.ann_paged_attention_workspace_bytes.restype = i64
         L.ann_cache_evict.argtypes = [cache, vp, i32, vp, i32, vp, i64, vp, i32, i32, i32, i32, vp, vp, vp, i64, vp]
         L.ann_logit_rules.argtypes = [vp, i64, i32, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, i32, vp, i32, vp, vp, i64, vp]
+        f64 = c.c_double
+        L.ann_rotation_frequencies.argtypes = [i32, f64, i32, f64, i32, f64, f64, vp, vp]
+        L.ann_rotate_append.argtypes = [vp, i64, i64, i32, i32, vp, i32, vp, vp, i32, vp, vp, i32, f32, i32, cache, vp, vp]
+        L.ann_chunk_attention.argtypes = [vp, i64, i64, i32, i32, vp, i32, cache, vp, i32, vp, i32, f32, i32, vp, vp, vp]
+        L.ann_chunk_attention_workspace_bytes.argtypes = [i32] * 8
+        L.ann_chunk_attention_workspace_bytes.restype = i64
+        L.ann_shared_attention.argtypes = [vp, i64, i64, i32, i32, cache, vp, i32, vp, vp, vp, i32, i32, i32, f32, vp, vp, vp]
+        L.ann_shared_attention_workspace_bytes.argtypes = [i32] * 8
+        L.ann_shared_attention_workspace_bytes.restype = i64
         for name in EXPORTS:
             if name not in ("ann_last_error", "ann_flat_workspace_bytes", "ann_graph_nonstall_workspace_bytes",
-                            "ann_paged_attention_workspace_bytes"):
+                            "ann_paged_attention_workspace_bytes", "ann_chunk_attention_workspace_bytes", "ann_shared_attention_workspace_bytes"):
                 getattr(L, name).restype = c.c_int
         _lib = L
         _load_marshal(L)
@@ -125,6 +138,7 @@ def _load_marshal(L: ctypes.CDLL) -> None:
     module.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in
                   (L.ann_flat_search_typed, L.ann_flat_search_after_typed, L.ann_graph_search_typed, L.ann_graph_search_entries_typed,
                    L.ann_graph_search_nonstall_typed, L.ann_gather_ids, L.ann_priority_order)))
+    module.bind_many(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.ann_rotate_append, L.ann_chunk_attention, L.ann_shared_attention)))
     module.bind_decode(*(ctypes.cast(f, ctypes.c_void_p).value for f in
                          (L.ann_qk_norm_rotate, L.ann_paged_attention, L.ann_cache_evict, L.ann_logit_rules)))
     _marshal = module
@@ -672,3 +686,117 @@ def ann_logit_rules(logits: torch.Tensor, tokens: torch.Tensor, lengths: torch.T
           presence.data_ptr(), frequency.data_ptr(), bias_tokens.data_ptr() if K else 0, bias_values.data_ptr() if K else 0, K,
           masks.data_ptr() if M else 0, M, mask_rows.data_ptr() if M else 0, out.data_ptr(), out.stride(0) if B > 1 else V)
     return out
+
+
+# ---- many tokens at once ---------------------------------------------------------------------
+
+def ann_rotation_frequencies(rot: int, base: float = 10_000.0, *, scaling: str = "none", factor: float = 1.0, original: int = 0,
+                             low: float = 1.0, high: float = 32.0, device=None) -> Tuple[torch.Tensor, float]:
+    """(frequencies float64 [rot / 2], amplitude) of a rotation, as ann_rotate_append takes them; scaling for contexts longer than the
+    `original` length: "none", "linear", "base", "ramp" (by the pair's number, between those that turn `high` and `low` times in the original context) or "smooth" (by
+    the turns themselves).  On the CPU unless a device is given."""
+    if scaling not in ROTATIONS:
+        raise ValueError(f"scaling must be one of {list(ROTATIONS)}")
+    frequencies, amplitude = torch.empty(max(0, _int32(rot, "rot") // 2), dtype=torch.float64), ctypes.c_double(1.0)
+    _check(lib().ann_rotation_frequencies(rot, float(base), ROTATIONS[scaling], float(factor), _int32(original, "original"), float(low), float(high),
+                                          frequencies.data_ptr(), ctypes.byref(amplitude)))
+    return (frequencies if device is None else frequencies.to(device)), amplitude.value
+
+
+def ann_rotate_append(qkv: torch.Tensor, starts: torch.Tensor, lengths: torch.Tensor, page_table: torch.Tensor, frequencies: Optional[torch.Tensor],
+                      k_cache: torch.Tensor, v_cache: torch.Tensor, *, positions: Optional[torch.Tensor] = None, amplitude: float = 1.0,
+                      interleaved: bool = False, q=None, stream=None) -> torch.Tensor:
+    """The rotation of queries and keys by position and the write of keys and values behind what each request holds in the paged cache
+    [pages, heads, slots, d].  qkv is [T, query heads + 2 heads, d], request b's tokens being starts[b] to starts[b + 1] - 1 (int32 [B + 1]) and the last of the
+    lengths[b] slots that it then has; page_table int32 [B, pages of a request]; frequencies float64 [rot / 2] on the device (None: nothing is rotated); positions int32 [T]
+    where they are not the slots.  Returns the queries [T, query heads, d]; rows of tokens that are no request's are left as they were."""
+    if q is None and stream is None:
+        usual = _usual("append", qkv, starts, lengths, page_table, frequencies, k_cache, v_cache, positions, amplitude, interleaved)
+        if usual is not None:
+            return usual[0]
+    cache = _cache(k_cache, v_cache)
+    dtype, heads, d = k_cache.dtype, cache.heads, cache.d
+    _rows(qkv, "qkv", dtype, (-1, -1, d))
+    T, q_heads = qkv.shape[0], qkv.shape[1] - 2 * heads
+    if q_heads < 1:
+        raise ValueError("qkv must have query heads and the cache's heads twice")
+    B = _array(lengths, "lengths", torch.int32, (-1,)).shape[0]
+    _array(starts, "starts", torch.int32, (B + 1,)), _array(page_table, "page_table", torch.int32, (B, -1))
+    if positions is not None:
+        _array(positions, "positions", torch.int32, (T,))
+    if frequencies is not None:
+        _array(frequencies, "frequencies", torch.float64, (-1,))
+    if q is None:
+        q = torch.empty(T, q_heads, d, dtype=dtype, device=qkv.device)
+    _array(q, "q", dtype, (T, q_heads, d))
+    _same_device(k_cache, qkv, starts, lengths, page_table, frequencies, positions, q)
+    _call(qkv.device, stream, lib().ann_rotate_append, qkv.data_ptr(), *_strides(qkv), T, q_heads, starts.data_ptr(), B, lengths.data_ptr(),
+          page_table.data_ptr(), page_table.shape[1], 0 if positions is None else positions.data_ptr(), 0 if frequencies is None else frequencies.data_ptr(),
+          0 if frequencies is None else 2 * frequencies.shape[0], float(amplitude), 1 if interleaved else 0, ctypes.byref(cache), q.data_ptr())
+    return q
+
+
+def ann_chunk_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor,
+                        starts: torch.Tensor, *, scale: Optional[float] = None, window: int = 0, max_length: Optional[int] = None, out=None, lse=None,
+                        stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Attention of every request's new tokens over its paged cache, each up to its own slot.  q [T, query heads, d], request b's tokens being starts[b] to
+    starts[b + 1] - 1 (int32 [B + 1]) and the last of its lengths[b] slots; page_table int32 [B, pages of a request]; scale 1 / sqrt(d) unless given; max_length: the
+    largest length, or a bound as close as is known (else all that the page table holds).  Few tokens of long contexts use the device's one workspace, as some searches do: such calls on
+    several streams have to be ordered (ann_set_workspace).  Returns (out [T, query heads, d], lse float32 [T, query heads]); rows of tokens that are no request's are left
+    as they were."""
+    if out is None and lse is None and stream is None:
+        usual = _usual("chunk", q, k_cache, v_cache, page_table, lengths, starts, scale, window, max_length)
+        if usual is not None:
+            return usual
+    cache = _cache(k_cache, v_cache)
+    d = cache.d
+    _rows(q, "q", k_cache.dtype, (-1, -1, d))
+    T, q_heads = q.shape[:2]
+    B = _array(lengths, "lengths", torch.int32, (-1,)).shape[0]
+    _array(page_table, "page_table", torch.int32, (B, -1)), _array(starts, "starts", torch.int32, (B + 1,))
+    width = page_table.shape[1]
+    out = torch.empty(T, q_heads, d, dtype=q.dtype, device=q.device) if out is None else _array(out, "out", q.dtype, (T, q_heads, d))
+    lse = torch.empty(T, q_heads, dtype=torch.float32, device=q.device) if lse is None else _array(lse, "lse", torch.float32, (T, q_heads))
+    _same_device(k_cache, q, page_table, lengths, starts, out, lse)
+    _call(q.device, stream, lib().ann_chunk_attention, q.data_ptr(), *_strides(q), T, q_heads, starts.data_ptr(), B, ctypes.byref(cache), page_table.data_ptr(),
+          width, lengths.data_ptr(), width * cache.slots if max_length is None else _int32(max_length, "max_length"), d ** -0.5 if scale is None else float(scale),
+          _int32(window, "window"), out.data_ptr(), lse.data_ptr())
+    return out, lse
+
+
+def ann_chunk_attention_workspace_bytes(T: int, B: int, q_heads: int, heads: int, d: int, dtype: torch.dtype, max_length: int, window: int = 0) -> int:
+    sizes = [_int32(x, name) for x, name in ((T, "T"), (B, "B"), (q_heads, "q_heads"), (heads, "heads"), (d, "d"))]
+    return int(lib().ann_chunk_attention_workspace_bytes(*sizes, _DTYPES[dtype], _int32(max_length, "max_length"), _int32(window, "window")))
+
+
+def ann_shared_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor,
+                         group_starts: torch.Tensor, shared: torch.Tensor, *, max_shared: Optional[int] = None, max_own: Optional[int] = None,
+                         scale: Optional[float] = None, out=None, lse=None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Attention of one new token per request over its paged cache, where the requests group_starts[g] to group_starts[g + 1] - 1 (int32 [groups + 1]) have their first shared[g] (int32
+    [groups]) slots in common, which are then read once for the group.  q [B, query heads, d], page_table int32 [B, pages of a request], lengths int32 [B]; max_shared and max_own: the
+    largest numbers of shared and of own slots, or bounds as close as are known (else all that the page table holds).  Uses the device's one workspace: such calls on several
+    streams have to be ordered (ann_set_workspace).  Returns (out [B, query heads, d], lse float32 [B, query heads])."""
+    if out is None and lse is None and stream is None:
+        usual = _usual("shared", q, k_cache, v_cache, page_table, lengths, group_starts, shared, max_shared, max_own, scale)
+        if usual is not None:
+            return usual
+    cache = _cache(k_cache, v_cache)
+    d = cache.d
+    _rows(q, "q", k_cache.dtype, (-1, -1, d))
+    B, q_heads = q.shape[:2]
+    _array(page_table, "page_table", torch.int32, (B, -1)), _array(lengths, "lengths", torch.int32, (B,))
+    groups = _array(shared, "shared", torch.int32, (-1,)).shape[0]
+    _array(group_starts, "group_starts", torch.int32, (groups + 1,))
+    width = page_table.shape[1]
+    out = torch.empty(B, q_heads, d, dtype=q.dtype, device=q.device) if out is None else _array(out, "out", q.dtype, (B, q_heads, d))
+    lse = torch.empty(B, q_heads, dtype=torch.float32, device=q.device) if lse is None else _array(lse, "lse", torch.float32, (B, q_heads))
+    _same_device(k_cache, q, page_table, lengths, group_starts, shared, out, lse)
+    bounds = [width * cache.slots if x is None else _int32(x, name) for x, name in ((max_shared, "max_shared"), (max_own, "max_own"))]
+    _call(q.device, stream, lib().ann_shared_attention, q.data_ptr(), *_strides(q), B, q_heads, ctypes.byref(cache), page_table.data_ptr(), width,
+          lengths.data_ptr(), group_starts.data_ptr(), shared.data_ptr(), groups, *bounds, d ** -0.5 if scale is None else float(scale), out.data_ptr(), lse.data_ptr())
+    return out, lse
+
+
+def ann_shared_attention_workspace_bytes(B: int, groups: int, q_heads: int, heads: int, d: int, dtype: torch.dtype, max_shared: int, max_own: int) -> int:
+    sizes = [_int32(x, name) for x, name in ((B, "B"), (groups, "groups"), (q_heads, "q_heads"), (heads, "heads"), (d, "d"))]
+    return int(lib().ann_shared_attention_workspace_bytes(*sizes, _DTYPES[dtype], _int32(max_shared, "max_shared"), _int32(max_own, "max_own")))

@@ -520,6 +520,115 @@ int ann_paged_attention(const void *q, int64_t q_row, int64_t q_head, int32_t B,
     return ANN_OK;
 }
 
+int ann_rotation_frequencies(int32_t rot, double base, int32_t scaling, double factor, int32_t original, double low, double high,
+                             double *frequencies, double *amplitude) {
+    if (null_in({frequencies, amplitude})) return fail(ANN_ERR_INVALID, "null pointer argument");
+    if (rot < 16 || rot > ANN_HEAD_MAX || rot % 16) return fail(ANN_ERR_INVALID, "rot = %d: a multiple of 16 in [16, %d] is wanted", rot, ANN_HEAD_MAX);
+    if (scaling < ANN_ROTATION_NONE || scaling > ANN_ROTATION_SMOOTH) return fail(ANN_ERR_INVALID, "unknown scaling %d", scaling);
+    if (!(base > 1.0) || !(base < INFINITY)) return fail(ANN_ERR_INVALID, "base = %g: a number above 1 is wanted", base);
+    if (scaling != ANN_ROTATION_NONE && (!(factor >= 1.0) || !(factor < INFINITY))) return fail(ANN_ERR_INVALID, "factor = %g: a number from 1 on is wanted", factor);
+    if (scaling >= ANN_ROTATION_RAMP && (original < 1 || !(low > 0.0) || !(high > low) || !(high < INFINITY)))
+        return fail(ANN_ERR_INVALID, "original = %d, low = %g, high = %g: a length of at least 1 and 0 < low < high are wanted", original, low, high);
+    rotation_frequencies(rot, base, scaling, factor, original, low, high, frequencies, amplitude);
+    return ANN_OK;
+}
+
+int ann_rotate_append(const void *qkv, int64_t token_stride, int64_t head_stride, int32_t T, int32_t q_heads,
+                      const int32_t *starts, int32_t B, const int32_t *lengths, const int32_t *page_table, int32_t width,
+                      const int32_t *positions, const double *frequencies, int32_t rot, float amplitude, int32_t interleaved,
+                      const ann_paged_cache *cache, void *q, void *stream) {
+    if (T == 0) return ANN_OK;
+    AppendArgs a{};
+    if (int rc = check_cache(cache, &a.cache)) return rc;
+    if (null_in({qkv, starts, lengths, page_table, q}) || (rot > 0 && !frequencies)) return fail(ANN_ERR_INVALID, "null pointer argument");
+    if (T < 1 || T > GRID_MAX) return fail(ANN_ERR_INVALID, "T = %d out of range [0, %lld]", T, (long long)GRID_MAX);
+    if (B < 1 || B > 65536) return fail(ANN_ERR_INVALID, "B = %d out of range [1, 65536]", B);
+    if (q_heads < 1 || q_heads > 65536 || cache->heads > 65536)
+        return fail(ANN_ERR_INVALID, "%d query heads and %d heads of the cache", q_heads, cache->heads);
+    if (width < 1 || (int64_t)width * cache->slots > INT32_MAX - 65536) return fail(ANN_ERR_INVALID, "width = %d out of range", width);
+    if (rot < 0 || rot > cache->d || rot % 16) return fail(ANN_ERR_INVALID, "rot = %d: a multiple of 16 up to d is wanted", rot);
+    if (!(fabsf(amplitude) < INFINITY)) return fail(ANN_ERR_INVALID, "amplitude is not a finite number");
+    const int e = elem_bytes(cache->dtype);
+    if (int rc = check_rows("qkv", token_stride, head_stride, e)) return rc;
+    if (off16(qkv) || off16(q)) return fail(ANN_ERR_ALIGNMENT, "qkv and q must be 16-byte aligned");
+    if (off4({starts, lengths, page_table, positions})) return fail(ANN_ERR_ALIGNMENT, "starts, lengths, page_table and positions must be 4-byte aligned");
+    if (reinterpret_cast<uintptr_t>(frequencies) & 7) return fail(ANN_ERR_ALIGNMENT, "frequencies must be 8-byte aligned");
+    a.qkv = qkv; a.token = token_stride * e; a.head = head_stride * e; a.tokens = T; a.q_heads = q_heads;
+    a.starts = starts; a.requests = B; a.lengths = lengths; a.table = page_table; a.width = width;
+    a.positions = positions; a.frequencies = frequencies; a.rot = rot; a.amplitude = amplitude; a.interleaved = interleaved != 0; a.q = q;
+    return check_launch("rotate_append_kernel", launch_rotate_append(cache->dtype, a, static_cast<hipStream_t>(stream)));
+}
+
+// What both attentions of many rows check alike, and what they take from it.
+static int check_attention(const void *q, int64_t q_row, int64_t q_head, int32_t q_heads, const ann_paged_cache *cache, const int32_t *page_table, int32_t width,
+                           const int32_t *lengths, float scale, const void *out, const float *lse, ChunkArgs *a) {
+    if (int rc = check_cache(cache, &a->cache)) return rc;
+    if (null_in({q, page_table, lengths, out})) return fail(ANN_ERR_INVALID, "null pointer argument");
+    if (q_heads < 1 || q_heads > 8192 || q_heads % cache->heads)
+        return fail(ANN_ERR_INVALID, "%d query heads: a multiple of the cache's %d, at most 8192, is wanted", q_heads, cache->heads);
+    if (width < 1 || (int64_t)width * cache->slots > INT32_MAX - 65536) return fail(ANN_ERR_INVALID, "width = %d out of range", width);
+    if (!(fabsf(scale) < INFINITY)) return fail(ANN_ERR_INVALID, "scale is not a finite number");
+    const int e = elem_bytes(cache->dtype);
+    if (int rc = check_rows("q", q_row, q_head, e)) return rc;
+    if (off16(q) || off16(out)) return fail(ANN_ERR_ALIGNMENT, "q and out must be 16-byte aligned");
+    if (off4({page_table, lengths, lse})) return fail(ANN_ERR_ALIGNMENT, "page_table, lengths and lse must be 4-byte aligned");
+    a->q = q; a->q_row = q_row * e; a->q_head = q_head * e; a->q_heads = q_heads;
+    a->table = page_table; a->width = width; a->lengths = lengths; a->scale = scale * 1.4426950408889634f;
+    return ANN_OK;
+}
+
+int64_t ann_chunk_attention_workspace_bytes(int32_t T, int32_t B, int32_t q_heads, int32_t heads, int32_t d, int32_t dtype, int32_t max_length, int32_t window) {
+    if (T < 1 || T > GRID_MAX || B < 1 || B > 65536 || heads < 1 || q_heads < heads || q_heads > 8192 || q_heads % heads || d < 8 || d > ANN_HEAD_MAX || max_length < 1 || window < 0)
+        return ANN_ERR_INVALID;
+    if (check_dtype(dtype) != ANN_OK) return ANN_ERR_INVALID;
+    return 0;
+}
+
+int ann_chunk_attention(const void *q, int64_t q_row, int64_t q_head, int32_t T, int32_t q_heads, const int32_t *starts, int32_t B,
+                        const ann_paged_cache *cache, const int32_t *page_table, int32_t width,
+                        const int32_t *lengths, int32_t max_length, float scale, int32_t window,
+                        void *out, float *lse, void *stream) {
+    if (T == 0) return ANN_OK;
+    ChunkArgs a{};
+    if (int rc = check_attention(q, q_row, q_head, q_heads, cache, page_table, width, lengths, scale, out, lse, &a)) return rc;
+    if (!starts) return fail(ANN_ERR_INVALID, "null pointer argument");
+    if (off4({starts})) return fail(ANN_ERR_ALIGNMENT, "starts must be 4-byte aligned");
+    if (T < 1 || T > GRID_MAX || (int64_t)T * q_heads > CHUNK_ROWS_MAX) return fail(ANN_ERR_INVALID, "%d tokens of %d heads are out of range", T, q_heads);
+    if (B < 1 || B > 65536) return fail(ANN_ERR_INVALID, "B = %d out of range [1, 65536]", B);
+    if (max_length < 1 || max_length > width * cache->slots) return fail(ANN_ERR_INVALID, "max_length = %d out of range [1, width slots]", max_length);
+    if (window < 0) return fail(ANN_ERR_INVALID, "window = %d out of range", window);
+    a.tokens = T; a.starts = starts; a.requests = B; a.max_length = max_length; a.window = window; a.out = out; a.lse = lse;
+    return check_launch("chunk_attention_kernel", (cache->dtype == ANN_F16 ? launch_chunk_attention_f16 : cache->dtype == ANN_BF16 ? launch_chunk_attention_bf16
+                                                   : launch_chunk_attention_f32)(a, static_cast<hipStream_t>(stream)));
+}
+
+int64_t ann_shared_attention_workspace_bytes(int32_t B, int32_t groups, int32_t q_heads, int32_t heads, int32_t d, int32_t dtype, int32_t max_shared, int32_t max_own) {
+    if (B < 1 || B > 65536 || groups < 1 || groups > 65536 || heads < 1 || q_heads < heads || q_heads > 8192 || q_heads % heads || d < 8 || d > ANN_HEAD_MAX || max_shared < 0 || max_own < 1)
+        return ANN_ERR_INVALID;
+    if (check_dtype(dtype) != ANN_OK) return ANN_ERR_INVALID;
+    return 0;
+}
+
+int ann_shared_attention(const void *q, int64_t q_row, int64_t q_head, int32_t B, int32_t q_heads,
+                         const ann_paged_cache *cache, const int32_t *page_table, int32_t width, const int32_t *lengths,
+                         const int32_t *group_starts, const int32_t *shared, int32_t groups, int32_t max_shared, int32_t max_own, float scale,
+                         void *out, float *lse, void *stream) {
+    if (B == 0) return ANN_OK;
+    ChunkArgs a{};
+    if (int rc = check_attention(q, q_row, q_head, q_heads, cache, page_table, width, lengths, scale, out, lse, &a)) return rc;
+    if (null_in({group_starts, shared})) return fail(ANN_ERR_INVALID, "null pointer argument");
+    if (off4({group_starts, shared})) return fail(ANN_ERR_ALIGNMENT, "group_starts and shared must be 4-byte aligned");
+    if (B < 1 || B > 65536 || groups < 1 || groups > 65536) return fail(ANN_ERR_INVALID, "B = %d or groups = %d out of range [1, 65536]", B, groups);
+    if ((int64_t)B * q_heads > GRID_MAX) return fail(ANN_ERR_INVALID, "%d requests of %d heads are too many for a call", B, q_heads);
+    const int32_t most = width * cache->slots;
+    if (max_shared < 0 || max_shared > most || max_own < 1 || max_own > most)
+        return fail(ANN_ERR_INVALID, "max_shared = %d or max_own = %d out of range", max_shared, max_own);
+    a.tokens = a.requests = B; a.max_length = most; a.out = out; a.lse = lse;
+    a.group_starts = group_starts; a.shared = shared; a.groups = groups; a.max_shared = max_shared; a.max_own = max_own;
+    return check_launch("chunk_attention_kernel", (cache->dtype == ANN_F16 ? launch_chunk_attention_f16 : cache->dtype == ANN_BF16 ? launch_chunk_attention_bf16
+                                                   : launch_chunk_attention_f32)(a, static_cast<hipStream_t>(stream)));
+}
+
 int ann_cache_evict(const ann_paged_cache *cache, const int32_t *page_table, int32_t width, const int32_t *lengths, int32_t B,
                     const float *mass, int64_t mass_slots, const int32_t *new_page_table, int32_t new_width,
                     int32_t budget, int32_t first, int32_t recent,

@@ -1,0 +1,8 @@
+// Attention of many rows over paged caches of BF16 elements.
+#include "chunk_attention_kernel.hpp"
+
+namespace ann {
+
+hipError_t launch_chunk_attention_bf16(const ChunkArgs &a, hipStream_t stream) { return launch_chunk<BF16>(a, stream); }
+
+}  // namespace ann

@@ -160,6 +160,46 @@ struct EvictArgs {
 };
 hipError_t launch_cache_evict(int dtype, const EvictArgs &args, int B, hipStream_t stream);
 
+// ---- many tokens at once -------------------------------------------------------------------------
+struct AppendArgs {
+    const void *qkv;
+    int64_t token, head;
+    int tokens, q_heads;
+    const int32_t *starts;
+    int requests;
+    const int32_t *lengths, *table;
+    int width;
+    const int32_t *positions;
+    const double *frequencies;
+    int rot;
+    float amplitude;
+    int interleaved;
+    Paged cache;
+    void *q;
+};
+hipError_t launch_rotate_append(int dtype, const AppendArgs &args, hipStream_t stream);
+
+struct ChunkArgs {
+    const void *q;
+    int64_t q_row, q_head;
+    int tokens, q_heads;
+    const int32_t *starts;    // null: one token of each request
+    int requests;
+    Paged cache;
+    const int32_t *table;
+    int width;
+    const int32_t *lengths;
+    int max_length, window;
+    float scale;              // times log2 e
+    const int32_t *group_starts, *shared;   // null: nothing is shared
+    int groups, max_shared, max_own;
+    void *out;
+    float *lse;
+};
+hipError_t launch_chunk_attention_f16(const ChunkArgs &args, hipStream_t stream);
+hipError_t launch_chunk_attention_bf16(const ChunkArgs &args, hipStream_t stream);
+hipError_t launch_chunk_attention_f32(const ChunkArgs &args, hipStream_t stream);
+
 struct RulesArgs {
     const void *logits;
     int64_t row;              // in elements

@@ -32,6 +32,9 @@ decltype(&ann_qk_norm_rotate) qk_norm_rotate;
 decltype(&ann_paged_attention) paged_attention;
 decltype(&ann_cache_evict) cache_evict;
 decltype(&ann_logit_rules) logit_rules;
+decltype(&ann_rotate_append) rotate_append;
+decltype(&ann_chunk_attention) chunk_attention;
+decltype(&ann_shared_attention) shared_attention;
 
 struct OtherForm {};                                      // the call is not of the usual form
 
@@ -377,6 +380,97 @@ PyObject *rules(PyObject *, PyObject *const *args, Py_ssize_t n) {
     });
 }
 
+// ---- many tokens at once
+
+// qkv, starts, lengths, page_table, frequencies or None, k_cache, v_cache, positions or None, amplitude, interleaved, device, stream
+PyObject *append(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    return usual<12>(args, n, [](PyObject *const *a) {
+        const int64_t device = integer(a[10], 0, INT32_MAX);
+        const ann_paged_cache c = cache_of(a[5], a[6], device);
+        const at::ScalarType type = tensor(a[5]).scalar_type();
+        const at::Tensor &qkv = rows_on_device(a[0], device, type, 3);
+        const int32_t T = count(qkv.size(0)), q_heads = count(qkv.size(1)) - 2 * c.heads;
+        if (qkv.size(2) != c.d || c.heads > 65536 || q_heads < 1) throw OtherForm();
+        const at::Tensor &lengths = array_on_device(a[2], device, at::kInt, {-1});
+        const int32_t B = count(lengths.size(0));
+        const at::Tensor &starts = array_on_device(a[1], device, at::kInt, {(int64_t)B + 1}), &table = array_on_device(a[3], device, at::kInt, {B, -1});
+        const at::Tensor *turns = a[4] == Py_None ? nullptr : &array_on_device(a[4], device, at::kDouble, {-1}),
+                         *positions = a[7] == Py_None ? nullptr : &array_on_device(a[7], device, at::kInt, {T});
+        if (turns && turns->size(0) > 65536) throw OtherForm();
+        const double amplitude = number(a[8]);
+        if (!PyBool_Check(a[9])) throw OtherForm();
+        void *stream = stream_of(a[11]);
+        const at::Tensor q = empty({T, q_heads, c.d}, type, qkv);
+        return answer(without_gil(rotate_append, (const void *)qkv.data_ptr(), step_of(qkv, 0), step_of(qkv, 1), T, q_heads, (const int32_t *)ints(starts), B,
+                                  (const int32_t *)ints(lengths), (const int32_t *)ints(table), count(table.size(1)),
+                                  positions ? (const int32_t *)ints(*positions) : nullptr, turns ? static_cast<const double *>(turns->data_ptr()) : nullptr,
+                                  turns ? (int32_t)(2 * turns->size(0)) : 0, (float)amplitude, (int32_t)(a[9] == Py_True), &c, q.data_ptr(), stream), {&q});
+    });
+}
+
+// q, k_cache, v_cache, page_table, lengths, starts, scale or None, window, max_length or None, device, stream
+PyObject *chunk(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    return usual<11>(args, n, [](PyObject *const *a) {
+        const int64_t device = integer(a[9], 0, INT32_MAX);
+        const ann_paged_cache c = cache_of(a[1], a[2], device);
+        const at::ScalarType type = tensor(a[1]).scalar_type();
+        const at::Tensor &q = rows_on_device(a[0], device, type, 3);
+        const int32_t T = count(q.size(0)), q_heads = count(q.size(1));
+        if (q.size(2) != c.d) throw OtherForm();
+        const at::Tensor &lengths = array_on_device(a[4], device, at::kInt, {-1});
+        const int32_t B = count(lengths.size(0));
+        const at::Tensor &table = array_on_device(a[3], device, at::kInt, {B, -1}), &starts = array_on_device(a[5], device, at::kInt, {(int64_t)B + 1});
+        const double scale = a[6] == Py_None ? 1.0 / std::sqrt((double)c.d) : number(a[6]);
+        const int32_t window = int32(a[7]), width = count(table.size(1)),
+                      most = a[8] == Py_None ? (int32_t)std::min<int64_t>(INT32_MAX, (int64_t)width * c.slots) : int32(a[8]);
+        void *stream = stream_of(a[10]);
+        const at::Tensor out = empty({T, q_heads, c.d}, type, q), lse = empty({T, q_heads}, at::kFloat, q);
+        return answer(without_gil(chunk_attention, (const void *)q.data_ptr(), step_of(q, 0), step_of(q, 1), T, q_heads, (const int32_t *)ints(starts), B, &c,
+                                  (const int32_t *)ints(table), width, (const int32_t *)ints(lengths), most, (float)scale, window, out.data_ptr(), floats(lse),
+                                  stream), {&out, &lse});
+    });
+}
+
+// q, k_cache, v_cache, page_table, lengths, group_starts, shared, max_shared or None, max_own or None, scale or None, device, stream
+PyObject *shared(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    return usual<12>(args, n, [](PyObject *const *a) {
+        const int64_t device = integer(a[10], 0, INT32_MAX);
+        const ann_paged_cache c = cache_of(a[1], a[2], device);
+        const at::ScalarType type = tensor(a[1]).scalar_type();
+        const at::Tensor &q = rows_on_device(a[0], device, type, 3);
+        const int32_t B = count(q.size(0)), q_heads = count(q.size(1));
+        if (q.size(2) != c.d) throw OtherForm();
+        const at::Tensor &table = array_on_device(a[3], device, at::kInt, {B, -1}), &lengths = array_on_device(a[4], device, at::kInt, {B}),
+                         &common = array_on_device(a[6], device, at::kInt, {-1});
+        const int32_t groups = count(common.size(0)), width = count(table.size(1)), all = (int32_t)std::min<int64_t>(INT32_MAX, (int64_t)width * c.slots);
+        const at::Tensor &starts = array_on_device(a[5], device, at::kInt, {(int64_t)groups + 1});
+        const int32_t most_shared = a[7] == Py_None ? all : int32(a[7]), most_own = a[8] == Py_None ? all : int32(a[8]);
+        const double scale = a[9] == Py_None ? 1.0 / std::sqrt((double)c.d) : number(a[9]);
+        void *stream = stream_of(a[11]);
+        const at::Tensor out = empty({B, q_heads, c.d}, type, q), lse = empty({B, q_heads}, at::kFloat, q);
+        return answer(without_gil(shared_attention, (const void *)q.data_ptr(), step_of(q, 0), step_of(q, 1), B, q_heads, &c, (const int32_t *)ints(table), width,
+                                  (const int32_t *)ints(lengths), (const int32_t *)ints(starts), (const int32_t *)ints(common), groups, most_shared, most_own,
+                                  (float)scale, out.data_ptr(), floats(lse), stream), {&out, &lse});
+    });
+}
+
+// addresses of the three, in the order of their declarations above
+PyObject *bind_many(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    void *p[3];
+    if (n != 3) {
+        PyErr_SetString(PyExc_TypeError, "bind_many takes 3 addresses");
+        return nullptr;
+    }
+    for (int i = 0; i < 3; ++i) {
+        p[i] = PyLong_AsVoidPtr(args[i]);
+        if (PyErr_Occurred()) return nullptr;
+    }
+    rotate_append = reinterpret_cast<decltype(rotate_append)>(p[0]);
+    chunk_attention = reinterpret_cast<decltype(chunk_attention)>(p[1]);
+    shared_attention = reinterpret_cast<decltype(shared_attention)>(p[2]);
+    Py_RETURN_NONE;
+}
+
 // addresses of the four, in the order of their declarations above
 PyObject *bind_decode(PyObject *, PyObject *const *args, Py_ssize_t n) {
     void *p[4];
@@ -418,7 +512,8 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {
 
 #define ENTRY(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(bind), ENTRY(flat), ENTRY(graph), ENTRY(graph_entries), ENTRY(nonstall), ENTRY(gather), ENTRY(order),
-                         ENTRY(bind_decode), ENTRY(rotate), ENTRY(attend), ENTRY(evict), ENTRY(rules), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(bind_decode), ENTRY(rotate), ENTRY(attend), ENTRY(evict), ENTRY(rules),
+                         ENTRY(bind_many), ENTRY(append), ENTRY(chunk), ENTRY(shared), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

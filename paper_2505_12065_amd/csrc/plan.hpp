@@ -1121,4 +1121,35 @@ inline int rotate_rows(int T, int heads, int groups) {
     return T < 512 ? 1 : (rows + parts - 1) / parts;
 }
 
+// ---- many tokens at once ------------------------------------------------------------------------------------
+constexpr int64_t CHUNK_ROWS_MAX = 1 << 26;               // query heads of all tokens
+
+// Frequencies of a rotation; scaling: an ANN_ROTATION_* code.
+inline void rotation_frequencies(int rot, double base, int scaling, double factor, int original, double low, double high, double *frequencies, double *amplitude) {
+    const double two_pi = 6.283185307179586;
+    if (scaling == ANN_ROTATION_BASE) base *= pow(factor, rot / (rot - 2.0));
+    // the pair that turns r times in the original context
+    auto pair_of = [&](double r) { return rot * log(original / (two_pi * r)) / (2.0 * log(base)); };
+    double a = 0.0, b = 1.0;
+    if (scaling == ANN_ROTATION_RAMP) {
+        a = fmax(floor(pair_of(high)), 0.0);
+        b = fmin(ceil(pair_of(low)), rot - 1.0);
+        if (!(b > a)) b = a + 0.001;
+    }
+    *amplitude = scaling == ANN_ROTATION_RAMP ? 0.1 * log(factor) + 1.0 : 1.0;
+    for (int i = 0; i < rot / 2; ++i) {
+        double f = pow(base, -2.0 * i / rot);
+        if (scaling == ANN_ROTATION_LINEAR) f /= factor;
+        if (scaling == ANN_ROTATION_RAMP) {
+            const double g = fmin(fmax((i - a) / (b - a), 0.0), 1.0);
+            f *= (1.0 - g) + g / factor;
+        }
+        if (scaling == ANN_ROTATION_SMOOTH) {
+            const double u = fmin(fmax((original * f / two_pi - low) / (high - low), 0.0), 1.0);
+            f *= (1.0 - u) / factor + u;
+        }
+        frequencies[i] = f;
+    }
+}
+
 }  // namespace ann
