@@ -3,6 +3,6 @@
 
 namespace ann {
 
-hipError_t launch_chunk_attention_bf16(const ChunkArgs &a, hipStream_t stream) { return launch_chunk<BF16>(a, stream); }
+hipError_t launch_chunk_attention_bf16(const ChunkArgs &a, const ChunkPlan &pl, hipStream_t stream) { return launch_chunk<BF16>(a, pl, stream); }
 
 }  // namespace ann

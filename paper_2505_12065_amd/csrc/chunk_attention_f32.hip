@@ -3,6 +3,6 @@
 
 namespace ann {
 
-hipError_t launch_chunk_attention_f32(const ChunkArgs &a, hipStream_t stream) { return launch_chunk<F32>(a, stream); }
+hipError_t launch_chunk_attention_f32(const ChunkArgs &a, const ChunkPlan &pl, hipStream_t stream) { return launch_chunk<F32>(a, pl, stream); }
 
 }  // namespace ann

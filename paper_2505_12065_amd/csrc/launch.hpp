@@ -179,11 +179,13 @@ struct AppendArgs {
 };
 hipError_t launch_rotate_append(int dtype, const AppendArgs &args, hipStream_t stream);
 
+// Attention of many rows.  A launch goes through the slots that new tokens attend to, those that groups have in common, or those that are a request's own.
+enum { CHUNK_NEW, CHUNK_COMMON, CHUNK_OWN };
 struct ChunkArgs {
     const void *q;
     int64_t q_row, q_head;
     int tokens, q_heads;
-    const int32_t *starts;    // null: one token of each request
+    const int32_t *starts;
     int requests;
     Paged cache;
     const int32_t *table;
@@ -191,14 +193,19 @@ struct ChunkArgs {
     const int32_t *lengths;
     int max_length, window;
     float scale;              // times log2 e
-    const int32_t *group_starts, *shared;   // null: nothing is shared
+    const int32_t *group_starts, *shared;   // null: new tokens
     int groups, max_shared, max_own;
     void *out;
     float *lse;
+    float lift;               // weights are 2^lift times as large until they are divided
+    int splits;               // parts of a row, of both launches
+    float *partial, *stats;   // [rows, splits, d], [rows, splits, 2] (largest exponent, sum) if there are more than one
+    int mode, tiles, chunk, part0;          // of a launch: tiles of rows of a cache head, slots of a part, its first part's number
 };
-hipError_t launch_chunk_attention_f16(const ChunkArgs &args, hipStream_t stream);
-hipError_t launch_chunk_attention_bf16(const ChunkArgs &args, hipStream_t stream);
-hipError_t launch_chunk_attention_f32(const ChunkArgs &args, hipStream_t stream);
+struct ChunkJoin { int chunk, first_parts, own_chunk, rows; };
+hipError_t launch_chunk_attention_f16(const ChunkArgs &args, const ChunkPlan &pl, hipStream_t stream);
+hipError_t launch_chunk_attention_bf16(const ChunkArgs &args, const ChunkPlan &pl, hipStream_t stream);
+hipError_t launch_chunk_attention_f32(const ChunkArgs &args, const ChunkPlan &pl, hipStream_t stream);
 
 struct RulesArgs {
     const void *logits;

@@ -1123,6 +1123,85 @@ inline int rotate_rows(int T, int heads, int groups) {
 
 // ---- many tokens at once ------------------------------------------------------------------------------------
 constexpr int64_t CHUNK_ROWS_MAX = 1 << 26;               // query heads of all tokens
+constexpr int64_t CHUNK_GRID = (1 << 24) - 1;             // workgroups of a launch, which has fewer than 2^32 threads
+constexpr size_t CHUNK_WS_MAX = (size_t)256 << 20;        // of workspace
+// Shapes of a workgroup.  FEW: 32 rows, whose slots its waves share out; MORE: 32 rows to a wave, MANY: 64.
+enum { CHUNK_FEW, CHUNK_MORE, CHUNK_MANY };
+constexpr int chunk_class(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+constexpr int chunk_most(int elem_bytes, int dp) { return elem_bytes == 2 && dp <= 128 ? 2 : 1; }     // row tiles of a wave, as registers allow
+constexpr int chunk_slots(int row_bytes, bool split) { return split || row_bytes > 256 ? 32 : 64; }   // slots of a tile
+constexpr int chunk_waves(int row_bytes, bool split) { return !split || row_bytes <= 256 ? 4 : row_bytes == 512 ? 2 : 1; }
+constexpr int chunk_per_simd(int elem_bytes, int dp) { return elem_bytes == 4 || dp == 256 ? 1 : 2; } // waves
+constexpr int chunk_rows(int elem_bytes, int dp, int shape) { return shape == CHUNK_FEW ? 32 : shape == CHUNK_MANY && chunk_most(elem_bytes, dp) == 2 ? 256 : 128; }
+
+// One launch: tiles of `rows` rows of a cache head, `parts` parts of `chunk` slots of each.
+struct ChunkPass { int shape = CHUNK_FEW, rows = 32, tiles = 0, parts = 0, chunk = 0; };
+struct ChunkPlan {
+    ChunkPass first, own;        // of new tokens, or of slots in common; of own slots
+    int splits = 1;
+    size_t bytes = 0;            // of workspace
+};
+inline ChunkPass chunk_pass_plan(int cus, int elem_bytes, int d, int heads, int64_t rows, int64_t sequences, int64_t range, int most_parts) {
+    ChunkPass p;
+    const int dp = chunk_class(d);
+    const int64_t mean = rows / (sequences > 0 ? sequences : 1);
+    p.shape = mean <= 32 ? CHUNK_FEW : mean <= 128 ? CHUNK_MORE : CHUNK_MANY;
+    p.rows = chunk_rows(elem_bytes, dp, p.shape);
+    p.tiles = (int)(rows / p.rows + sequences);
+    const int64_t units = (mean + p.rows - 1) / p.rows * sequences * heads, step = 256;
+    const int64_t fill = 2 * (int64_t)cus;
+    int64_t parts = units >= fill ? 1 : fill / units;
+    int64_t chunk = (range + parts - 1) / parts;
+    chunk = (chunk + step - 1) / step * step;
+    parts = (range + chunk - 1) / chunk;
+    if (parts > most_parts) {
+        chunk = ((range + most_parts - 1) / most_parts + 31) / 32 * 32;
+        parts = (range + chunk - 1) / chunk;
+    }
+    p.parts = parts < 1 ? 1 : (int)parts;
+    p.chunk = (int)chunk;
+    return p;
+}
+inline size_t chunk_bytes(int64_t rows, int64_t d, int64_t splits) { return splits > 1 ? (size_t)rows * splits * (d + 2) * 4 : 0; }
+// Parts that `most` bytes hold.
+inline int64_t chunk_parts_in(int64_t rows, int64_t d, size_t most) { return (int64_t)(most / ((size_t)rows * (d + 2) * 4)); }
+inline ChunkPlan chunk_plan(int cus, int elem_bytes, int d, int q_heads, int heads, int64_t T, int64_t B, int64_t max_length, int64_t window, size_t most) {
+    ChunkPlan pl;
+    const int G = q_heads / heads;
+    // (what a tile of rows attends to may begin 31 slots before its first row's window, and ends with its last row's)
+    const int64_t range = window > 0 && window + 256 + 31 < max_length ? window + 256 + 31 : max_length + 0;
+    int64_t parts = chunk_parts_in(T * q_heads, d, most);
+    pl.first = chunk_pass_plan(cus, elem_bytes, d, heads, T * G, B, range, (int)(parts < 1 ? 1 : parts > 256 ? 256 : parts));
+    pl.splits = pl.first.parts;
+    pl.bytes = chunk_bytes(T * q_heads, d, pl.splits);
+    return pl;
+}
+// Nothing in common (max_shared 0, or no room for the parts of both): all slots are the requests' own.
+inline ChunkPlan shared_plan(int cus, int elem_bytes, int d, int q_heads, int heads, int64_t B, int64_t groups, int64_t max_shared, int64_t max_own, size_t most) {
+    ChunkPlan pl;
+    const int G = q_heads / heads;
+    int64_t parts = chunk_parts_in(B * q_heads, d, most);
+    parts = parts > 256 ? 256 : parts;
+    const bool both = max_shared > 0 && parts >= 2;
+    if (both) {
+        pl.first = chunk_pass_plan(cus, elem_bytes, d, heads, B * G, groups < B ? groups : B, max_shared, (int)(parts + 1) / 2);
+        pl.first.tiles = (int)(B * G / pl.first.rows + groups);
+        parts -= pl.first.parts;
+    }
+    const int64_t own = both ? max_own : max_own + max_shared;
+    pl.own = chunk_pass_plan(cus, elem_bytes, d, heads, B * G, B, own + 31, (int)(parts < 1 ? 1 : parts));
+    pl.own.tiles = (int)(B * ((G + pl.own.rows - 1) / pl.own.rows));
+    pl.splits = pl.first.parts + pl.own.parts;
+    pl.bytes = chunk_bytes(B * q_heads, d, pl.splits);
+    return pl;
+}
+// Weights of the product with V.  fp16 has no numbers below 2^-24, and 65504 is its largest: 2^7 times as large they may still be 2^8 times that.  bf16 and fp32 have values up to the largest of the sums' 32
+// bits: as much smaller as there are slots to sum, and by the 2^8.
+inline float chunk_lift(int dtype, int64_t slots) {
+    int bits = 0;
+    while (slots >> bits) ++bits;
+    return dtype == ANN_F16 ? 7.f : -(float)(bits + 8);
+}
 
 // Frequencies of a rotation; scaling: an ANN_ROTATION_* code.
 inline void rotation_frequencies(int rot, double base, int scaling, double factor, int original, double low, double high, double *frequencies, double *amplitude) {
