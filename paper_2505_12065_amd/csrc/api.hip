@@ -312,6 +312,37 @@ int check_rows(const char *what, int64_t row, int64_t head, int e) {
     return ANN_OK;
 }
 
+int units_of_device() {
+    std::lock_guard<std::mutex> lock(g_mu);
+    DeviceState *st = nullptr;
+    return device_state(&st) == ANN_OK ? st->cus : 256;
+}
+
+// Launches an attention by the plan that `plan` makes for the bytes that are there.
+template <class Plan>
+int run_attention(ChunkArgs a, int dtype, Plan &&plan, hipStream_t stream) {
+    std::lock_guard<std::mutex> lock(g_mu);
+    DeviceState *st = nullptr;
+    if (int rc = device_state(&st)) return rc;
+    ChunkPlan pl = plan(st->cus, CHUNK_WS_MAX);
+    // a buffer that a caller gave, or that a graph may not let grow, takes fewer parts
+    if (pl.bytes && !at_hand(st, st->ws, pl.bytes, stream)) pl = plan(st->cus, st->user_ws ? st->user_bytes : st->ws.bytes);
+    for (const ChunkPass *p : {&pl.first, &pl.own})
+        if ((int64_t)p->tiles * p->parts * a.cache.heads > CHUNK_GRID) return fail(ANN_ERR_INVALID, "%d tokens of %d heads and %d requests are too many for a call", a.tokens, a.q_heads, a.requests);
+    void *ws = nullptr;
+    if (pl.bytes)
+        if (int rc = workspace_for(st, &st->ws, pl.bytes, stream, &ws)) return rc;
+    a.splits = pl.splits;
+    a.partial = static_cast<float *>(ws);
+    a.stats = a.partial + (size_t)a.tokens * a.q_heads * pl.splits * a.cache.d;
+    if (a.group_starts && pl.first.parts == 0) {          // (the slots in common are everyone's own)
+        a.max_own = (int)((int64_t)a.max_shared + a.max_own < INT_MAX ? a.max_shared + a.max_own : INT_MAX);
+        a.max_shared = 0;
+    }
+    return check_launch("chunk_attention_kernel", (dtype == ANN_F16 ? launch_chunk_attention_f16 : dtype == ANN_BF16 ? launch_chunk_attention_bf16
+                                                   : launch_chunk_attention_f32)(a, pl, stream));
+}
+
 }  // namespace
 
 extern "C" {
@@ -575,37 +606,6 @@ static int check_attention(const void *q, int64_t q_row, int64_t q_head, int32_t
     a->q = q; a->q_row = q_row * e; a->q_head = q_head * e; a->q_heads = q_heads;
     a->table = page_table; a->width = width; a->lengths = lengths; a->scale = scale * 1.4426950408889634f;
     return ANN_OK;
-}
-
-static int units_of_device() {
-    std::lock_guard<std::mutex> lock(g_mu);
-    DeviceState *st = nullptr;
-    return device_state(&st) == ANN_OK ? st->cus : 256;
-}
-
-// Launches an attention by the plan that `plan` makes for the bytes that are there.
-template <class Plan>
-static int run_attention(ChunkArgs a, int dtype, Plan &&plan, hipStream_t stream) {
-    std::lock_guard<std::mutex> lock(g_mu);
-    DeviceState *st = nullptr;
-    if (int rc = device_state(&st)) return rc;
-    ChunkPlan pl = plan(st->cus, CHUNK_WS_MAX);
-    // a buffer that a caller gave, or that a graph may not let grow, takes fewer parts
-    if (pl.bytes && !at_hand(st, st->ws, pl.bytes, stream)) pl = plan(st->cus, st->user_ws ? st->user_bytes : st->ws.bytes);
-    for (const ChunkPass *p : {&pl.first, &pl.own})
-        if ((int64_t)p->tiles * p->parts * a.cache.heads > CHUNK_GRID) return fail(ANN_ERR_INVALID, "%d tokens of %d heads and %d requests are too many for a call", a.tokens, a.q_heads, a.requests);
-    void *ws = nullptr;
-    if (pl.bytes)
-        if (int rc = workspace_for(st, &st->ws, pl.bytes, stream, &ws)) return rc;
-    a.splits = pl.splits;
-    a.partial = static_cast<float *>(ws);
-    a.stats = a.partial + (size_t)a.tokens * a.q_heads * pl.splits * a.cache.d;
-    if (a.group_starts && pl.first.parts == 0) {          // (the slots in common are everyone's own)
-        a.max_own = (int)((int64_t)a.max_shared + a.max_own < INT_MAX ? a.max_shared + a.max_own : INT_MAX);
-        a.max_shared = 0;
-    }
-    return check_launch("chunk_attention_kernel", (dtype == ANN_F16 ? launch_chunk_attention_f16 : dtype == ANN_BF16 ? launch_chunk_attention_bf16
-                                                   : launch_chunk_attention_f32)(a, pl, stream));
 }
 
 int64_t ann_chunk_attention_workspace_bytes(int32_t T, int32_t B, int32_t q_heads, int32_t heads, int32_t d, int32_t dtype, int32_t max_length, int32_t window) {

@@ -423,7 +423,7 @@ __global__ __launch_bounds__((ChunkShape<T, DP, NR, SPLIT>::THREADS), (ChunkShap
                 constexpr bool EXACT = decltype(exact)::value;
 #pragma unroll
                 for (int c = 0; c < NC; ++c) {
-#pragma unroll
+#pragma unroll 1
                     for (int what = 0; what < (EXACT ? 4 : 1); ++what) {
                         f16v count[NR];
 #pragma unroll
