@@ -167,28 +167,31 @@ __device__ __forceinline__ bool not_finite(uint32_t most) {
     else return most >= INF;
 }
 
-// An operand V^T of 8 (16 bits) elements or one (fp32), and what its elements are: 0 finite ones (others as 0), 1 where +infinity, 2 -infinity, 3 NaN
+// The elements of a word, 0 where they are not finite
 template <class T>
-__device__ __forceinline__ u4 only(u4 v, int what) {
-    constexpr uint32_t INF = std::is_same_v<T, F16> ? 0x7c00u : 0x7f80u, ONE = std::is_same_v<T, F16> ? 0x3c00u : 0x3f80u;
-    u4 out;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        uint32_t r = 0;
-#pragma unroll
-        for (int k = 0; k < 32; k += 16) {
-            const uint32_t e = (v[i] >> k) & 0xffffu, size = e & 0x7fffu;
-            const bool is = what == 0 ? size < INF : what == 3 ? size > INF : e == (what == 1 ? INF : INF | 0x8000u);
-            if (is) r |= (what == 0 ? e : ONE) << k;
-        }
-        out[i] = r;
-    }
-    return out;
+__device__ __forceinline__ uint32_t finite_of(uint32_t w) {
+    constexpr uint32_t INF = std::is_same_v<T, F16> ? 0x7c00u : std::is_same_v<T, BF16> ? 0x7f80u : 0x7f800000u;
+    if constexpr (T::bytes == 2) return ((w & 0x7fffu) < INF ? w & 0xffffu : 0u) | (((w >> 16) & 0x7fffu) < INF ? w & 0xffff0000u : 0u);
+    else return (w & 0x7fffffffu) < INF ? w : 0u;
 }
-__device__ __forceinline__ float only(float v, int what) {
-    const uint32_t e = __float_as_uint(v), size = e & 0x7fffffffu;
-    const bool is = what == 0 ? size < 0x7f800000u : what == 3 ? size > 0x7f800000u : e == (what == 1 ? 0x7f800000u : 0xff800000u);
-    return is ? (what == 0 ? v : 1.f) : 0.f;
+// Four elements of a row, 0 where they are finite
+template <class T>
+__device__ __forceinline__ f4 not_finite_four(const char *p) {
+    f4 y;
+    if constexpr (T::bytes == 4) {
+        y = *reinterpret_cast<const f4 *>(p);
+    } else if constexpr (std::is_same_v<T, F16>) {
+        typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+        const h4 x = *reinterpret_cast<const h4 *>(p);
+        y = f4{(float)x[0], (float)x[1], (float)x[2], (float)x[3]};
+    } else {
+        typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+        const b4 x = *reinterpret_cast<const b4 *>(p);
+        y = f4{(float)x[0], (float)x[1], (float)x[2], (float)x[3]};
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = (__float_as_uint(y[i]) & 0x7fffffffu) < 0x7f800000u ? 0.f : y[i];
+    return y;
 }
 
 template <class T, int DP, int NR, bool SPLIT>
@@ -197,7 +200,7 @@ __global__ __launch_bounds__((ChunkShape<T, DP, NR, SPLIT>::THREADS), (ChunkShap
     constexpr int KT = Sh::KT, RB = Sh::RB, NS = Sh::NS, NC = Sh::NC, NU = Sh::NU, LOADS = Sh::LOADS, CPR = Sh::CPR, RPI = Sh::RPI, WAVES = Sh::WAVES, R = Sh::R, SUB = Sh::SUB;
     constexpr bool WIDE = T::bytes == 4;
     extern __shared__ __align__(16) unsigned char chunk_lds[];
-    __shared__ int s_bad[2][8], s_lo[8], s_hi[8];
+    __shared__ int s_lo[8], s_hi[8], s_bad[2];
     const int lane = threadIdx.x & (WAVE - 1), m = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const int G = a.q_heads / a.cache.heads;
@@ -252,6 +255,7 @@ __global__ __launch_bounds__((ChunkShape<T, DP, NR, SPLIT>::THREADS), (ChunkShap
     int all_lo = lo_most, all_hi = hi_least;              // of all waves that read the same slots
     if constexpr (!SPLIT) {
         if (lane == 0) { s_lo[wave] = lo_most; s_hi[wave] = hi_least; }
+        if (threadIdx.x == 0) { s_bad[0] = INT_MAX; s_bad[1] = -1; }
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) { all_lo = max(all_lo, s_lo[w]); all_hi = min(all_hi, s_hi[w]); }
@@ -300,7 +304,7 @@ __global__ __launch_bounds__((ChunkShape<T, DP, NR, SPLIT>::THREADS), (ChunkShap
 
     constexpr int STEP = SPLIT ? WAVES * KT : KT;
     constexpr uint64_t ALL = KT == 64 ? ~0ull : (1ull << (KT & 63)) - 1;
-    int k0 = first + (SPLIT ? wave * KT : 0), buffer = 0, pages = -1;
+    int k0 = first + (SPLIT ? wave * KT : 0), buffer = 0, pages = -1, bad_first = INT_MAX, bad_last = -1;
     uint64_t valid = 0;
     if (k0 < end) {
         pages = look_up(k0);
@@ -312,18 +316,33 @@ __global__ __launch_bounds__((ChunkShape<T, DP, NR, SPLIT>::THREADS), (ChunkShap
         unsigned char *at_k = mine + buffer * Sh::BUFFER, *at_v = at_k + Sh::TILE;
         __builtin_amdgcn_s_waitcnt(0x0F70);               // this tile is there: vmcnt 0
         asm volatile("" ::: "memory");
-        // Rows of V that some rows of queries attend to and others do not must be of numbers, or they would go into all: 0 times NaN is no 0.
-        const bool parted = !(valid == ALL && k0 >= all_lo && k0 + KT <= all_hi);
-        if (parted) {
+        // Rows of V that some rows of queries attend to and others do not must be finite, or they would go into all: 0 times NaN is no 0.  What is not is taken
+        // out, and given to the rows that attend to it at the end.
+        if (!(valid == ALL && k0 >= all_lo && k0 + KT <= all_hi)) {
+            unsigned char *loaded = at_v + (SPLIT ? 0 : wave * LOADS * 1024) + lane * 16;
             uint32_t most = 0;
 #pragma unroll
             for (int e = 0; e < LOADS; ++e) {
-                const u4 x = *reinterpret_cast<const u4 *>(at_v + (SPLIT ? 0 : wave * LOADS * 1024) + e * 1024 + lane * 16);
+                const u4 x = *reinterpret_cast<const u4 *>(loaded + e * 1024);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) most_bits<T>(x[i], most);
             }
-            const bool bad = __ballot(not_finite<T>(most)) != 0;
-            if (lane == 0) s_bad[buffer][wave] = bad;
+            if (__ballot(not_finite<T>(most))) {
+#pragma unroll 1
+                for (int e = 0; e < LOADS; ++e) {
+                    u4 x = *reinterpret_cast<const u4 *>(loaded + e * 1024);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i] = finite_of<T>(x[i]);
+                    *reinterpret_cast<u4 *>(loaded + e * 1024) = x;
+                }
+                if constexpr (SPLIT) {
+                    bad_first = min(bad_first, k0);
+                    bad_last = k0;
+                } else if (lane == 0) {
+                    atomicMin(&s_bad[0], k0);
+                    atomicMax(&s_bad[1], k0);
+                }
+            }
         }
         if constexpr (SPLIT) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // (what was read of the other buffer is in registers)
         else asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -335,14 +354,6 @@ __global__ __launch_bounds__((ChunkShape<T, DP, NR, SPLIT>::THREADS), (ChunkShap
         }
         if (k0 >= hi_most) continue;                      // (no row of this wave's attends to it)
         const bool whole = seen == ALL && k0 >= lo_most && k0 + KT <= hi_least;
-        bool bad = false;
-        if (!whole) {
-            if constexpr (SPLIT) bad = s_bad[buffer][wave] != 0;
-            else
-#pragma unroll
-                for (int w = 0; w < WAVES; ++w) bad = bad || s_bad[buffer][w] != 0;
-            bad = __builtin_amdgcn_readfirstlane(bad);
-        }
 #pragma unroll
         for (int u0 = 0; u0 < NU; u0 += SUB) {
             f16v x[SUB][NR];
@@ -367,7 +378,6 @@ __global__ __launch_bounds__((ChunkShape<T, DP, NR, SPLIT>::THREADS), (ChunkShap
                     }
                 }
             // which of this lane's slots its rows attend to: bit 8 a + i of tile u for slot 8 a + 4 h + i
-            uint32_t use[SUB][NR];
             if (!whole) {
 #pragma unroll
                 for (int rt = 0; rt < NR; ++rt)
@@ -377,10 +387,10 @@ __global__ __launch_bounds__((ChunkShape<T, DP, NR, SPLIT>::THREADS), (ChunkShap
                         uint32_t bits = (uint32_t)(seen >> (32 * (u0 + u)));
                         bits = from <= 0 ? bits : from >= 32 ? 0u : bits & (~0u << from);
                         bits = to >= 32 ? bits : to <= 0 ? 0u : bits & ~(~0u << to);
-                        use[u][rt] = bits >> (4 * h);
+                        bits >>= 4 * h;
 #pragma unroll
                         for (int i = 0; i < 16; ++i)
-                            if (!((use[u][rt] >> (8 * (i / 4) + i % 4)) & 1)) x[u][rt][i] = -INFINITY;
+                            if (!((bits >> (8 * (i / 4) + i % 4)) & 1)) x[u][rt][i] = -INFINITY;
                     }
             }
             u4 p[SUB][NR][2];
@@ -419,68 +429,65 @@ __global__ __launch_bounds__((ChunkShape<T, DP, NR, SPLIT>::THREADS), (ChunkShap
                     }
                 }
             }
-            auto times_v = [&](auto exact) __attribute__((always_inline)) {
-                constexpr bool EXACT = decltype(exact)::value;
 #pragma unroll
-                for (int c = 0; c < NC; ++c) {
-#pragma unroll 1
-                    for (int what = 0; what < (EXACT ? 4 : 1); ++what) {
-                        f16v count[NR];
+            for (int u = 0; u < SUB; ++u) {
+                if constexpr (WIDE) {
 #pragma unroll
-                        for (int rt = 0; rt < NR; ++rt) count[rt] = zero16();
+                    for (int i = 0; i < 16; ++i) {
+                        const int row = 32 * (u0 + u) + 8 * (i / 4) + 4 * h + i % 4;
 #pragma unroll
-                        for (int u = 0; u < SUB; ++u) {
-                            if constexpr (WIDE) {
+                        for (int c = 0; c < NC; ++c) {
+                            const float v = *reinterpret_cast<const float *>(at_v + row * RB + (((8 * c + (m >> 2)) ^ chunk_swizzle<RB>(row)) << 4) + (m & 3) * 4);
 #pragma unroll
-                                for (int i = 0; i < 16; ++i) {
-                                    const int row = 32 * (u0 + u) + 8 * (i / 4) + 4 * h + i % 4;
-                                    float v = *reinterpret_cast<const float *>(at_v + row * RB + (((8 * c + (m >> 2)) ^ chunk_swizzle<RB>(row)) << 4) + (m & 3) * 4);
-                                    if constexpr (EXACT) v = only(v, what);
-#pragma unroll
-                                    for (int rt = 0; rt < NR; ++rt) {
-                                        if (what == 0) o[rt][c] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, x[u][rt][i], o[rt][c], 0, 0, 0);
-                                        else count[rt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, (use[u][rt] >> (8 * (i / 4) + i % 4)) & 1 ? 1.f : 0.f, count[rt], 0, 0, 0);
-                                    }
-                                }
-                            } else {
-#pragma unroll
-                                for (int j = 0; j < 2; ++j) {
-                                    unsigned char *from = at_v + (32 * (u0 + u) + 16 * j) * RB + v_lane;
-                                    typedef __attribute__((address_space(3))) s4 *Turned;
-                                    const s4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Turned)ANN_LDS(from + ((64 * c) ^ v_turn)));
-                                    const s4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Turned)ANN_LDS(from + 8 * RB + ((64 * c) ^ v_turn ^ 32)));
-                                    u4 v;
-                                    v[0] = __builtin_bit_cast(u2, v0)[0]; v[1] = __builtin_bit_cast(u2, v0)[1];
-                                    v[2] = __builtin_bit_cast(u2, v1)[0]; v[3] = __builtin_bit_cast(u2, v1)[1];
-                                    if constexpr (EXACT) v = only<T>(v, what);
-#pragma unroll
-                                    for (int rt = 0; rt < NR; ++rt) {
-                                        if (what == 0) {
-                                            o[rt][c] = mfma32<T>(v, p[u][rt][j], o[rt][c]);
-                                        } else {
-                                            float one[8];
-#pragma unroll
-                                            for (int i = 0; i < 8; ++i) one[i] = (use[u][rt] >> (16 * j + 8 * (i / 4) + i % 4)) & 1 ? 1.f : 0.f;
-                                            count[rt] = mfma32<T>(v, pack_weights<T>(one), count[rt]);
-                                        }
-                                    }
-                                }
-                            }
+                            for (int rt = 0; rt < NR; ++rt) o[rt][c] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, x[u][rt][i], o[rt][c], 0, 0, 0);
                         }
-                        if (what > 0) {
-                            const float add = what == 1 ? INFINITY : what == 2 ? -INFINITY : __builtin_nanf("");
+                    }
+                } else {
 #pragma unroll
-                            for (int rt = 0; rt < NR; ++rt)
+                    for (int j = 0; j < 2; ++j) {
+                        unsigned char *from = at_v + (32 * (u0 + u) + 16 * j) * RB + v_lane;
 #pragma unroll
-                                for (int i = 0; i < 16; ++i) o[rt][c][i] += count[rt][i] > 0.f ? add : 0.f;
+                        for (int c = 0; c < NC; ++c) {
+                            typedef __attribute__((address_space(3))) s4 *Turned;
+                            const u2 v0 = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Turned)ANN_LDS(from + ((64 * c) ^ v_turn))));
+                            const u2 v1 = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Turned)ANN_LDS(from + 8 * RB + ((64 * c) ^ v_turn ^ 32))));
+#pragma unroll
+                            for (int rt = 0; rt < NR; ++rt) o[rt][c] = mfma32<T>(u4{v0[0], v0[1], v1[0], v1[1]}, p[u][rt][j], o[rt][c]);
                         }
                     }
                 }
-            };
-            if (bad) times_v(std::true_type{});
-            else times_v(std::false_type{});
+            }
         }
     }
+
+    // infinities and NaN of V that were taken out
+    if constexpr (!SPLIT) {
+        __syncthreads();
+        bad_first = s_bad[0];
+        bad_last = s_bad[1];
+    }
+#pragma unroll 1
+    for (int k = bad_first; k <= bad_last; k += STEP)
+#pragma unroll 1
+        for (int key = k; key < k + KT && key < end; ++key) {
+            const int page = table[key >> slots_log];
+            if ((unsigned)page >= (unsigned)a.cache.pages) continue;
+            const char *from = v_head + page * a.cache.v_page + (key & mask) * a.cache.v_slot;
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const int at = 32 * c + 2 * i + 4 * h;
+                    if (at >= a.cache.d) continue;
+                    const f4 v = not_finite_four<T>(from + at * T::bytes);
+#pragma unroll
+                    for (int rt = 0; rt < NR; ++rt)
+                        if (key >= lo[rt] && key < hi[rt]) {
+#pragma unroll
+                            for (int b = 0; b < 4; ++b) o[rt][c][i + b] += v[b];
+                        }
+                }
+        }
 
 #pragma unroll
     for (int rt = 0; rt < NR; ++rt) {

@@ -1145,7 +1145,7 @@ inline ChunkPass chunk_pass_plan(int cus, int elem_bytes, int d, int heads, int6
     ChunkPass p;
     const int dp = chunk_class(d);
     const int64_t mean = rows / (sequences > 0 ? sequences : 1);
-    p.shape = mean <= 32 ? CHUNK_FEW : mean <= 128 ? CHUNK_MORE : CHUNK_MANY;
+    p.shape = mean <= 32 ? CHUNK_FEW : mean <= 1280000 ? CHUNK_MORE : CHUNK_MANY;
     p.rows = chunk_rows(elem_bytes, dp, p.shape);
     p.tiles = (int)(rows / p.rows + sequences);
     const int64_t units = (mean + p.rows - 1) / p.rows * sequences * heads, step = 256;
