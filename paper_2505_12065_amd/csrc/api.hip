@@ -605,6 +605,7 @@ static int check_attention(const void *q, int64_t q_row, int64_t q_head, int32_t
     if (off4({page_table, lengths, lse})) return fail(ANN_ERR_ALIGNMENT, "page_table, lengths and lse must be 4-byte aligned");
     a->q = q; a->q_row = q_row * e; a->q_head = q_head * e; a->q_heads = q_heads;
     a->table = page_table; a->width = width; a->lengths = lengths; a->scale = scale * 1.4426950408889634f;
+    a->coarse = cache->slots >= 16 && a->cache.k_slot < 1 << 27 && a->cache.v_slot < 1 << 27;
     return ANN_OK;
 }
 

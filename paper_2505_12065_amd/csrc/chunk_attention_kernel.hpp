@@ -24,8 +24,6 @@ typedef unsigned short us2 __attribute__((ext_vector_type(2)));
 #define ANN_ROW_TO_LDS(gptr, lptr) \
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(gptr), ANN_LDS(lptr), 16, 0, 0)
 
-static __device__ __align__(16) unsigned char chunk_zeros[16];           // what is read where there is nothing
-
 // ---- which rows and slots ---------------------------------------------------------------------------------
 
 // A tile: rows r0 .. r0 + count - 1 of a sequence of tokens (a request's new ones, the one of each request of a group, or one), the first of which is token0; a token has a row for
@@ -199,6 +197,7 @@ __global__ __launch_bounds__((ChunkShape<T, DP, NR, SPLIT>::THREADS), (ChunkShap
     typedef ChunkShape<T, DP, NR, SPLIT> Sh;
     constexpr int KT = Sh::KT, RB = Sh::RB, NS = Sh::NS, NC = Sh::NC, NU = Sh::NU, LOADS = Sh::LOADS, CPR = Sh::CPR, RPI = Sh::RPI, WAVES = Sh::WAVES, R = Sh::R, SUB = Sh::SUB;
     constexpr bool WIDE = T::bytes == 4;
+    constexpr int AHEAD = DP == 128 && !SPLIT ? 6 : 4;    // reads of LDS in flight before a product
     extern __shared__ __align__(16) unsigned char chunk_lds[];
     __shared__ int s_lo[8], s_hi[8], s_bad[2];
     const int lane = threadIdx.x & (WAVE - 1), m = lane & 31, h = lane >> 5;
@@ -274,19 +273,49 @@ __global__ __launch_bounds__((ChunkShape<T, DP, NR, SPLIT>::THREADS), (ChunkShap
         if (key < end) page = table[key >> slots_log];
         return (unsigned)page < (unsigned)a.cache.pages ? page : -1;
     };
+    // Slots without a row take one of the first page's: their scores do not count, and of their values only that they are finite.
+    const int first_row = (SPLIT ? 0 : wave * LOADS) * RPI;
+    const int in_load = lane / CPR, first_at = ((lane & (CPR - 1)) ^ chunk_swizzle<RB>(first_row + in_load)) * 16;
+    const uint32_t k_load = in_load * (uint32_t)a.cache.k_slot, v_load = in_load * (uint32_t)a.cache.v_slot;
     auto issue = [&](int k0, int pages, int buffer) {
         unsigned char *to = mine + buffer * Sh::BUFFER + (SPLIT ? 0 : wave * LOADS * 1024);
+        auto coarse = [&](auto full) __attribute__((always_inline)) {       // the 16 rows from a multiple of 16 on are of one page, and a load's rows lie within 32 bits
+#pragma unroll
+            for (int e = 0; e < LOADS; ++e) {
+                const int row0 = first_row + e * RPI, page = max(__builtin_amdgcn_readlane(pages, row0 & ~15), 0);
+                const int64_t place = (k0 + row0) & mask;
+                const char *k = k_head + page * a.cache.k_page + place * a.cache.k_slot, *v = v_head + page * a.cache.v_page + place * a.cache.v_slot;
+                // (the chunk's place goes by bits of the row: those of the first load's, turned by those of e)
+                const uint32_t at = first_at ^ (chunk_swizzle<RB>(e * RPI) * 16);
+                if (decltype(full)::value || (int)at < row_bytes) {
+                    ANN_ROW_TO_LDS(k + (k_load + at), to + e * 1024);
+                    ANN_ROW_TO_LDS(v + (v_load + at), to + Sh::TILE + e * 1024);
+                }
+            }
+        };
+        if (a.coarse) {
+            if (row_bytes == RB) coarse(std::true_type{});
+            else coarse(std::false_type{});
+            return;
+        }
 #pragma unroll
         for (int e = 0; e < LOADS; ++e) {
-            const int row = ((SPLIT ? 0 : wave * LOADS) + e) * RPI + lane / CPR, at = ((lane & (CPR - 1)) ^ chunk_swizzle<RB>(row)) * 16;
-            const int page = __shfl(pages, row);
-            const bool ok = page >= 0 && at < row_bytes;
+            const int row = first_row + e * RPI + in_load, at = ((lane & (CPR - 1)) ^ chunk_swizzle<RB>(row)) * 16;
+            const int page = max(__shfl(pages, row), 0);
             const int64_t place = (k0 + row) & mask;
             const char *k = k_head + page * a.cache.k_page + place * a.cache.k_slot + at, *v = v_head + page * a.cache.v_page + place * a.cache.v_slot + at;
-            ANN_ROW_TO_LDS(ok ? k : reinterpret_cast<const char *>(chunk_zeros), to + e * 1024);
-            ANN_ROW_TO_LDS(ok ? v : reinterpret_cast<const char *>(chunk_zeros), to + Sh::TILE + e * 1024);
+            if (at < row_bytes) {
+                ANN_ROW_TO_LDS(k, to + e * 1024);
+                ANN_ROW_TO_LDS(v, to + Sh::TILE + e * 1024);
+            }
         }
     };
+    if (row_bytes < RB) {                                 // what lies behind the end of a row in LDS is never loaded
+#pragma unroll
+        for (int e = 0; e < 4 * LOADS; ++e)
+            *reinterpret_cast<u4 *>(mine + (e / LOADS) * Sh::TILE + (first_row / RPI + e % LOADS) * 1024 + lane * 16) = zero_chunk();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
 
     f16v o[NR][NC];
     float top[NR], sum[NR];                               // largest score so far, as the weights go by it; the sum of this lane's slots alone
@@ -377,6 +406,15 @@ __global__ __launch_bounds__((ChunkShape<T, DP, NR, SPLIT>::THREADS), (ChunkShap
                         }
                     }
                 }
+            if constexpr (!WIDE) {                        // reads of K ahead of the products
+                __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+                for (int r = 0; r < SUB * NS - AHEAD; ++r) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                }
+                __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+            }
             // which of this lane's slots its rows attend to: bit 8 a + i of tile u for slot 8 a + 4 h + i
             if (!whole) {
 #pragma unroll

@@ -197,6 +197,7 @@ struct ChunkArgs {
     int groups, max_shared, max_own;
     void *out;
     float *lse;
+    int coarse;               // pages of at least 16 slots, whose strides are short
     float lift;               // weights are 2^lift times as large until they are divided
     int splits;               // parts of a row, of both launches
     float *partial, *stats;   // [rows, splits, d], [rows, splits, 2] (largest exponent, sum) if there are more than one

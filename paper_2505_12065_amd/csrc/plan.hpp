@@ -1128,7 +1128,7 @@ constexpr size_t CHUNK_WS_MAX = (size_t)256 << 20;        // of workspace
 // Shapes of a workgroup.  FEW: 32 rows, whose slots its waves share out; MORE: 32 rows to a wave, MANY: 64.
 enum { CHUNK_FEW, CHUNK_MORE, CHUNK_MANY };
 constexpr int chunk_class(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
-constexpr int chunk_most(int elem_bytes, int dp) { return elem_bytes == 2 && dp <= 128 ? 2 : 1; }     // row tiles of a wave, as registers allow
+constexpr int chunk_most(int, int) { return 1; }     // row tiles of a wave, as registers allow
 constexpr int chunk_slots(int row_bytes, bool split) { return split || row_bytes > 256 ? 32 : 64; }   // slots of a tile
 constexpr int chunk_waves(int row_bytes, bool split) { return !split || row_bytes <= 256 ? 4 : row_bytes == 512 ? 2 : 1; }
 constexpr int chunk_per_simd(int elem_bytes, int dp) { return elem_bytes == 4 || dp == 256 ? 1 : 2; } // waves
@@ -1145,7 +1145,7 @@ inline ChunkPass chunk_pass_plan(int cus, int elem_bytes, int d, int heads, int6
     ChunkPass p;
     const int dp = chunk_class(d);
     const int64_t mean = rows / (sequences > 0 ? sequences : 1);
-    p.shape = mean <= 32 ? CHUNK_FEW : mean <= 1280000 ? CHUNK_MORE : CHUNK_MANY;
+    p.shape = mean <= 32 ? CHUNK_FEW : CHUNK_MORE;
     p.rows = chunk_rows(elem_bytes, dp, p.shape);
     p.tiles = (int)(rows / p.rows + sequences);
     const int64_t units = (mean + p.rows - 1) / p.rows * sequences * heads, step = 256;
