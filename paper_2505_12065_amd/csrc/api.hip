@@ -327,15 +327,14 @@ int run_attention(ChunkArgs a, int dtype, Plan &&plan, hipStream_t stream) {
     ChunkPlan pl = plan(st->cus, CHUNK_WS_MAX);
     // a buffer that a caller gave, or that a graph may not let grow, takes fewer parts
     if (pl.bytes && !at_hand(st, st->ws, pl.bytes, stream)) pl = plan(st->cus, st->user_ws ? st->user_bytes : st->ws.bytes);
-    for (const ChunkPass *p : {&pl.first, &pl.own})
-        if ((int64_t)p->tiles * p->parts * a.cache.heads > CHUNK_GRID) return fail(ANN_ERR_INVALID, "%d tokens of %d heads and %d requests are too many for a call", a.tokens, a.q_heads, a.requests);
+    if (((int64_t)pl.first.items + pl.own.items) * a.cache.heads > CHUNK_GRID) return fail(ANN_ERR_INVALID, "%d tokens of %d heads and %d requests are too many for a call", a.tokens, a.q_heads, a.requests);
     void *ws = nullptr;
     if (pl.bytes)
         if (int rc = workspace_for(st, &st->ws, pl.bytes, stream, &ws)) return rc;
     a.splits = pl.splits;
     a.partial = static_cast<float *>(ws);
     a.stats = a.partial + (size_t)a.tokens * a.q_heads * pl.splits * a.cache.d;
-    if (a.group_starts && pl.first.parts == 0) {          // (the slots in common are everyone's own)
+    if (pl.first.mode == CHUNK_OWN) {                     // (the slots in common are everyone's own)
         a.max_own = (int)((int64_t)a.max_shared + a.max_own < INT_MAX ? a.max_shared + a.max_own : INT_MAX);
         a.max_shared = 0;
     }

@@ -179,8 +179,6 @@ struct AppendArgs {
 };
 hipError_t launch_rotate_append(int dtype, const AppendArgs &args, hipStream_t stream);
 
-// Attention of many rows.  A launch goes through the slots that new tokens attend to, those that groups have in common, or those that are a request's own.
-enum { CHUNK_NEW, CHUNK_COMMON, CHUNK_OWN };
 struct ChunkArgs {
     const void *q;
     int64_t q_row, q_head;
@@ -199,11 +197,9 @@ struct ChunkArgs {
     float *lse;
     int coarse;               // pages of at least 16 slots, whose strides are short
     float lift;               // weights are 2^lift times as large until they are divided
-    int splits;               // parts of a row, of both launches
+    int splits;               // parts that a row may have, of both passes
     float *partial, *stats;   // [rows, splits, d], [rows, splits, 2] (largest exponent, sum) if there are more than one
-    int mode, tiles, chunk, part0;          // of a launch: tiles of rows of a cache head, slots of a part, its first part's number
 };
-struct ChunkJoin { int chunk, first_parts, own_chunk, rows; };
 hipError_t launch_chunk_attention_f16(const ChunkArgs &args, const ChunkPlan &pl, hipStream_t stream);
 hipError_t launch_chunk_attention_bf16(const ChunkArgs &args, const ChunkPlan &pl, hipStream_t stream);
 hipError_t launch_chunk_attention_f32(const ChunkArgs &args, const ChunkPlan &pl, hipStream_t stream);

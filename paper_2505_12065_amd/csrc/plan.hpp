@@ -1125,41 +1125,58 @@ inline int rotate_rows(int T, int heads, int groups) {
 constexpr int64_t CHUNK_ROWS_MAX = 1 << 26;               // query heads of all tokens
 constexpr int64_t CHUNK_GRID = (1 << 24) - 1;             // workgroups of a launch, which has fewer than 2^32 threads
 constexpr size_t CHUNK_WS_MAX = (size_t)256 << 20;        // of workspace
-// Shapes of a workgroup.  FEW: 32 rows, whose slots its waves share out; MORE: 32 rows to a wave, MANY: 64.
-enum { CHUNK_FEW, CHUNK_MORE, CHUNK_MANY };
+// Shapes of a workgroup.  FEW: 32 rows, whose slots its waves share out; MORE: 32 rows to each of four waves.
+enum { CHUNK_FEW, CHUNK_MORE };
+constexpr int chunk_rows(bool few) { return few ? 32 : 128; }
 constexpr int chunk_class(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
-constexpr int chunk_most(int, int) { return 1; }     // row tiles of a wave, as registers allow
-constexpr int chunk_slots(int row_bytes, bool split) { return split || row_bytes > 256 ? 32 : 64; }   // slots of a tile
-constexpr int chunk_waves(int row_bytes, bool split) { return !split || row_bytes <= 256 ? 4 : row_bytes == 512 ? 2 : 1; }
-constexpr int chunk_per_simd(int elem_bytes, int dp) { return elem_bytes == 4 || dp == 256 ? 1 : 2; } // waves
-constexpr int chunk_rows(int elem_bytes, int dp, int shape) { return shape == CHUNK_FEW ? 32 : shape == CHUNK_MANY && chunk_most(elem_bytes, dp) == 2 ? 256 : 128; }
+constexpr int chunk_slots(int row_bytes, bool few) { return few || row_bytes > 256 ? 32 : 64; }       // slots of a tile
+constexpr int CHUNK_WAVES = 4;
+constexpr int chunk_slot_waves(int row_bytes) { return row_bytes > 512 ? 2 : CHUNK_WAVES; }            // FEW: waves that take slots, as LDS allows
+constexpr int chunk_per_simd(int elem_bytes, int dp) { return elem_bytes == 4 || dp == 256 ? 1 : 2; } // waves, as registers allow
 
-// One launch: tiles of `rows` rows of a cache head, `parts` parts of `chunk` slots of each.
-struct ChunkPass { int shape = CHUNK_FEW, rows = 32, tiles = 0, parts = 0, chunk = 0; };
+// A pass goes through the slots that new tokens attend to, those that groups have in common, or those that are a request's own.
+enum { CHUNK_NEW, CHUNK_COMMON, CHUNK_OWN };
+struct ChunkPass {
+    int mode = CHUNK_NEW, shape = CHUNK_FEW, rows = 32;   // rows of a tile
+    int items = 0;               // tiles and parts of a cache head that there may be
+    int fill = 1;                // workgroups of a cache head that fill the card
+    int most_parts = 1, least = 64, part0 = 0;            // parts of a row at most; slots of a part at least; number of a row's first part
+    int tiles = 0, chunk = 0;    // of more than 64 sequences: tiles that there may be, slots of a part
+};
 struct ChunkPlan {
-    ChunkPass first, own;        // of new tokens, or of slots in common; of own slots
+    ChunkPass first, own;        // new tokens or slots in common; own slots
     int splits = 1;
     size_t bytes = 0;            // of workspace
 };
-inline ChunkPass chunk_pass_plan(int cus, int elem_bytes, int d, int heads, int64_t rows, int64_t sequences, int64_t range, int most_parts) {
+constexpr int64_t CHUNK_PARTS = 64;                       // of a row in a pass
+// Sequences of `rows` rows in all, whose tiles go through `range` slots at most.
+inline ChunkPass chunk_pass(int mode, int cus, int elem_bytes, int d, int heads, int64_t rows, int64_t sequences, int64_t range, int64_t most_parts) {
     ChunkPass p;
     const int dp = chunk_class(d);
-    const int64_t mean = rows / (sequences > 0 ? sequences : 1);
-    p.shape = mean <= 32 ? CHUNK_FEW : CHUNK_MORE;
-    p.rows = chunk_rows(elem_bytes, dp, p.shape);
-    p.tiles = (int)(rows / p.rows + sequences);
-    const int64_t units = (mean + p.rows - 1) / p.rows * sequences * heads, step = 256;
-    const int64_t fill = 2 * (int64_t)cus;
-    int64_t parts = units >= fill ? 1 : fill / units;
-    int64_t chunk = (range + parts - 1) / parts;
-    chunk = (chunk + step - 1) / step * step;
-    parts = (range + chunk - 1) / chunk;
-    if (parts > most_parts) {
-        chunk = ((range + most_parts - 1) / most_parts + 31) / 32 * 32;
-        parts = (range + chunk - 1) / chunk;
+    p.mode = mode;
+    p.shape = mode == CHUNK_OWN || rows <= 32 * sequences ? CHUNK_FEW : CHUNK_MORE;
+    p.rows = chunk_rows(p.shape == CHUNK_FEW);
+    p.fill = cus * chunk_per_simd(elem_bytes, dp) / heads;
+    if (p.fill < 1) p.fill = 1;
+    p.least = elem_bytes == 4 ? 64 : p.shape == CHUNK_FEW ? 128 : 256;
+    const int64_t tiles = mode == CHUNK_OWN ? sequences * ((rows / sequences + p.rows - 1) / p.rows) : rows / p.rows + sequences;
+    // nothing is divided where tiles alone keep the card busy
+    const int64_t busy = rows / p.rows;
+    int64_t parts = (range + p.least - 1) / p.least;
+    if (parts > most_parts) parts = most_parts;
+    if (parts > CHUNK_PARTS) parts = CHUNK_PARTS;
+    if (busy >= 2 * p.fill || parts < 1) parts = 1;
+    p.tiles = (int)tiles;
+    if (sequences <= 64) {
+        p.most_parts = (int)parts;
+        p.items = (int)(parts > 1 && tiles < 2 * p.fill + sequences ? 2 * p.fill + sequences : tiles);
+    } else {
+        const int64_t mean = (rows / sequences + p.rows - 1) / p.rows * sequences, wanted = mean >= p.fill ? 1 : p.fill / (mean < 1 ? 1 : mean);
+        if (parts > wanted) parts = wanted;
+        p.chunk = (int)(((range + parts - 1) / parts + 63) / 64 * 64);
+        p.most_parts = (int)((range + p.chunk - 1) / p.chunk);
+        p.items = (int)(tiles * p.most_parts);
     }
-    p.parts = parts < 1 ? 1 : (int)parts;
-    p.chunk = (int)chunk;
     return p;
 }
 inline size_t chunk_bytes(int64_t rows, int64_t d, int64_t splits) { return splits > 1 ? (size_t)rows * splits * (d + 2) * 4 : 0; }
@@ -1168,30 +1185,26 @@ inline int64_t chunk_parts_in(int64_t rows, int64_t d, size_t most) { return (in
 inline ChunkPlan chunk_plan(int cus, int elem_bytes, int d, int q_heads, int heads, int64_t T, int64_t B, int64_t max_length, int64_t window, size_t most) {
     ChunkPlan pl;
     const int G = q_heads / heads;
-    // (what a tile of rows attends to may begin 31 slots before its first row's window, and ends with its last row's)
-    const int64_t range = window > 0 && window + 256 + 31 < max_length ? window + 256 + 31 : max_length + 0;
-    int64_t parts = chunk_parts_in(T * q_heads, d, most);
-    pl.first = chunk_pass_plan(cus, elem_bytes, d, heads, T * G, B, range, (int)(parts < 1 ? 1 : parts > 256 ? 256 : parts));
-    pl.splits = pl.first.parts;
+    // (a tile of rows may begin 31 slots before its first row's window, and ends with its last row's)
+    const int64_t range = window > 0 && window + 160 < max_length ? window + 160 : max_length;
+    pl.first = chunk_pass(CHUNK_NEW, cus, elem_bytes, d, heads, T * G, B, range, chunk_parts_in(T * q_heads, d, most));
+    pl.splits = pl.first.most_parts;
     pl.bytes = chunk_bytes(T * q_heads, d, pl.splits);
     return pl;
 }
-// Nothing in common (max_shared 0, or no room for the parts of both): all slots are the requests' own.
+// Nothing in common (max_shared 0, or no room for the parts of both): all slots are the requests' own, a pass without another.
 inline ChunkPlan shared_plan(int cus, int elem_bytes, int d, int q_heads, int heads, int64_t B, int64_t groups, int64_t max_shared, int64_t max_own, size_t most) {
     ChunkPlan pl;
-    const int G = q_heads / heads;
-    int64_t parts = chunk_parts_in(B * q_heads, d, most);
-    parts = parts > 256 ? 256 : parts;
-    const bool both = max_shared > 0 && parts >= 2;
-    if (both) {
-        pl.first = chunk_pass_plan(cus, elem_bytes, d, heads, B * G, groups < B ? groups : B, max_shared, (int)(parts + 1) / 2);
-        pl.first.tiles = (int)(B * G / pl.first.rows + groups);
-        parts -= pl.first.parts;
+    const int64_t G = q_heads / heads, parts = chunk_parts_in(B * q_heads, d, most);
+    if (max_shared < 1 || parts < 2) {
+        pl.first = chunk_pass(CHUNK_OWN, cus, elem_bytes, d, heads, B * G, B, max_shared + max_own + 31, parts);
+        pl.splits = pl.first.most_parts;
+    } else {
+        pl.own = chunk_pass(CHUNK_OWN, cus, elem_bytes, d, heads, B * G, B, max_own + 31, parts / 2);
+        pl.first = chunk_pass(CHUNK_COMMON, cus, elem_bytes, d, heads, B * G, groups, max_shared, parts - pl.own.most_parts);
+        pl.own.part0 = pl.first.most_parts;
+        pl.splits = pl.first.most_parts + pl.own.most_parts;
     }
-    const int64_t own = both ? max_own : max_own + max_shared;
-    pl.own = chunk_pass_plan(cus, elem_bytes, d, heads, B * G, B, own + 31, (int)(parts < 1 ? 1 : parts));
-    pl.own.tiles = (int)(B * ((G + pl.own.rows - 1) / pl.own.rows));
-    pl.splits = pl.first.parts + pl.own.parts;
     pl.bytes = chunk_bytes(B * q_heads, d, pl.splits);
     return pl;
 }
