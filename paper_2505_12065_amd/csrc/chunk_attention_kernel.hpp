@@ -13,6 +13,7 @@
 #include "chunk_rows.hpp"
 #include "launch.hpp"
 #include "paged.hpp"
+#include "paged_attention_kernel.hpp"
 
 namespace ann {
 
@@ -23,8 +24,6 @@ typedef unsigned short us2 __attribute__((ext_vector_type(2)));
 #define ANN_LDS(p) ((__attribute__((address_space(3))) void *)(p))
 #define ANN_ROW_TO_LDS(gptr, lptr) \
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(gptr), ANN_LDS(lptr), 16, 0, 0)
-
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 template <class T>
 __device__ __forceinline__ void store_four(char *to, f4 y);
@@ -55,21 +54,14 @@ __device__ __forceinline__ void wait_outstanding() {
 
 // ---- the kernel ----------------------------------------------------------------------------------------------
 
-// FEW: the waves take slots of their own, of 32 rows; else 32 rows each of their own, of the same slots.
-template <class T, int DP_, bool FEW_>
+template <class T, int DP_>
 struct ChunkShape {
     static constexpr int DP = DP_, RB = DP * T::bytes;                  // largest d; bytes of a row in LDS
-    static constexpr bool FEW = FEW_;
-    static constexpr int KT = chunk_slots(RB, FEW), WAVES = CHUNK_WAVES, SLOT_WAVES = chunk_slot_waves(RB);    // FEW: waves that take slots, as LDS allows
-    static constexpr int R = chunk_rows(FEW);
+    static constexpr int KT = chunk_slots(RB), WAVES = CHUNK_WAVES;
     static constexpr int CPR = RB / 16, RPI = 64 / CPR;                 // chunks of a row, rows that a load brings
-    static constexpr int LOADS = KT * RB / 1024 / (FEW ? 1 : WAVES);    // of K, and of V, that a wave issues for a tile of slots
-    static constexpr int TILE = KT * RB;
-    static constexpr int BUFFERS = FEW ? 1 : 2;                         // FEW: K of the next tile is loaded while the weights meet V, V while K meets the queries
+    static constexpr int LOADS = KT * RB / 1024 / WAVES;                // of K, and of V, that a wave issues for a tile of slots
+    static constexpr int TILE = KT * RB, LDS = 4 * TILE;                // K and V, twice
     static constexpr int NS = RB / 32, NC = DP / 32, NU = KT / 32;      // steps of 32 bytes of a row; tiles of 32 elements; tiles of 32 slots
-    static constexpr int LD = DP + 4;                                   // floats of a row where the waves' sums are joined
-    static constexpr int LDS_TILES = BUFFERS * 2 * TILE * (FEW ? SLOT_WAVES : 1), LDS_JOIN = FEW ? WAVES * 32 * (LD + 2) * 4 : 0;
-    static constexpr int LDS = LDS_TILES > LDS_JOIN ? LDS_TILES : LDS_JOIN;
 };
 
 // Where chunk c of row r lies in its row: 16 rows that an operand is read of lie in 16 places of the 256 bytes that the banks hold, and so do four rows of 64 bytes that are turned.
@@ -146,28 +138,54 @@ __device__ __forceinline__ f4 not_finite_four(const char *p) {
     return y;
 }
 
-template <class T, int DP, bool FEW>
-__device__ __forceinline__ void chunk_body(const ChunkArgs &a, const ChunkPass &pass, int block, unsigned char *chunk_lds, int *s_scratch) {
-    typedef ChunkShape<T, DP, FEW> Sh;
+// Slots of one row of a deal, of token t, the i-th of its sequence
+__device__ __forceinline__ ChunkSpan chunk_row_span(const ChunkArgs &a, int mode, const ChunkDeal &deal, int t, int i) {
+    if (mode == CHUNK_NEW) return chunk_span(a, deal.length, deal.q.tokens - i);
+    return {deal.range.lo, mode == CHUNK_COMMON ? min(deal.range.hi, chunk_length(a, t)) : deal.range.hi};
+}
+// Four elements of row `in` of a deal: divided and written if the row has no other parts, else left for what joins them.
+template <class T>
+__device__ __forceinline__ void chunk_write(const ChunkArgs &a, const ChunkPass &pass, const ChunkDeal &deal, int head, int in, int at, f4 y, float most, float total) {
+    const int G = a.q_heads / a.cache.heads, r = deal.r0 + in;
+    const int64_t row = (int64_t)(deal.q.token0 + r / G) * a.q_heads + head * G + r % G;
+    if (a.splits > 1) {
+        const int64_t place = row * a.splits + pass.part0 + deal.part;
+        if (at == 0) *reinterpret_cast<f4 *>(a.stats + 4 * place) = f4{most, total, __int_as_float(deal.parts), __int_as_float(deal.grouped)};
+        if (!deal.alone) {
+            *reinterpret_cast<f4 *>(a.partial + place * a.cache.d + at) = y;
+            return;
+        }
+    }
+    const float by = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = total == 0.f ? 0.f : y[i] * by;
+    store_four<T>(static_cast<char *>(a.out) + (row * a.cache.d + at) * T::bytes, y);
+    if (at == 0 && a.lse) a.lse[row] = chunk_lse(most, total, a.lift);
+}
+
+// ---- 128 rows -------------------------------------------------------------------------------------------------
+
+template <class T, int DP>
+__global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(T::bytes, DP)) void chunk_attention_kernel(ChunkArgs a, ChunkPass pass) {
+    typedef ChunkShape<T, DP> Sh;
     constexpr int KT = Sh::KT, RB = Sh::RB, NS = Sh::NS, NC = Sh::NC, NU = Sh::NU, LOADS = Sh::LOADS, CPR = Sh::CPR, RPI = Sh::RPI, WAVES = Sh::WAVES;
     constexpr bool WIDE = T::bytes == 4;
-    constexpr int AHEAD = DP == 128 && !FEW ? 6 : 4;      // reads of LDS in flight before a product
-    int *s_lo = s_scratch, *s_hi = s_scratch + 4, *s_bad = s_scratch + 8;
+    constexpr int AHEAD = DP == 128 ? 6 : 4;              // reads of LDS in flight before a product
+    extern __shared__ __align__(16) unsigned char chunk_lds[];
+    __shared__ int s_lo[WAVES], s_hi[WAVES], s_bad[2];
     const int lane = threadIdx.x & (WAVE - 1), m = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-    const int G = a.q_heads / a.cache.heads, head = block % a.cache.heads;
-    const ChunkDeal deal = chunk_deal(a, pass, block / a.cache.heads, G);
+    const int G = a.q_heads / a.cache.heads, head = blockIdx.x % a.cache.heads;
+    const ChunkDeal deal = chunk_deal(a, pass, blockIdx.x / a.cache.heads, G);
     if (deal.count <= 0) return;
-    const ChunkSpan range = chunk_range(a, pass.mode, deal.sequence, deal.q, deal.r0 / G, (deal.r0 + deal.count - 1) / G);
-    if (deal.part >= chunk_parts(chunk_slots_of(range), deal.chunk)) return;
-    const int first = chunk_begin(range) + deal.part * deal.chunk, end = range.hi - first < deal.chunk ? range.hi : first + deal.chunk;
+    const int first = deal.first, end = deal.end;
 
     // this lane's row: its query and the slots that it attends to
     u4 q[NS];
     int lo = 0, hi = INT_MAX, hi_most = 0;
     const uint32_t flip = a.scale < 0.f ? (WIDE ? 0x80000000u : 0x80008000u) : 0u;
     const float scale = fmaxf(fabsf(a.scale), 1e-37f);    // (not 0: a score of -infinity stays one)
-    const int row0 = FEW ? 0 : wave * 32, row_bytes = a.cache.d * T::bytes;
+    const int row0 = wave * 32, row_bytes = a.cache.d * T::bytes;
     {
         const int in = row0 + m, r = deal.r0 + in, t = deal.q.token0 + r / G;
         const bool there = in < deal.count;
@@ -181,9 +199,7 @@ __device__ __forceinline__ void chunk_body(const ChunkArgs &a, const ChunkPass &
             for (int i = 0; i < 4; ++i) q[s][i] ^= flip;
         }
         if (there) {
-            ChunkSpan span = range;
-            if (pass.mode == CHUNK_NEW) span = chunk_span(a, chunk_length(a, deal.q.request), deal.q.tokens - r / G);
-            if (pass.mode == CHUNK_COMMON) span.hi = min(span.hi, chunk_length(a, t));
+            const ChunkSpan span = chunk_row_span(a, pass.mode, deal, t, r / G);
             lo = span.lo;
             hi = span.hi;
             hi_most = hi;
@@ -200,7 +216,7 @@ __device__ __forceinline__ void chunk_body(const ChunkArgs &a, const ChunkPass &
     hi_least = __builtin_amdgcn_readfirstlane(hi_least);
     hi_most = __builtin_amdgcn_readfirstlane(hi_most);
     int all_lo = lo_most, all_hi = hi_least;              // ... of all waves that read the same slots
-    if constexpr (!FEW) {
+    {
         if (lane == 0) { s_lo[wave] = lo_most; s_hi[wave] = hi_least; }
         if (threadIdx.x == 0) { s_bad[0] = INT_MAX; s_bad[1] = -1; }
         __syncthreads();
@@ -210,7 +226,7 @@ __device__ __forceinline__ void chunk_body(const ChunkArgs &a, const ChunkPass &
         all_hi = __builtin_amdgcn_readfirstlane(all_hi);
     }
 
-    unsigned char *mine = chunk_lds + (FEW ? wave * 2 * Sh::TILE : 0);
+    unsigned char *const mine = chunk_lds;
     const int32_t *table = a.table + (int64_t)deal.q.request * a.width;
     const int slots_log = a.cache.slots_log, mask = (1 << slots_log) - 1;
     const char *k_head = a.cache.k + head * a.cache.k_head, *v_head = a.cache.v + head * a.cache.v_head;
@@ -222,10 +238,8 @@ __device__ __forceinline__ void chunk_body(const ChunkArgs &a, const ChunkPass &
         return (unsigned)page < (unsigned)a.cache.pages ? page : -1;
     };
     // Slots without a row take one of the first page's: their scores do not count, and of their values only that they are finite.
-    const int first_row = (FEW ? 0 : wave * LOADS) * RPI, in_load = lane / CPR, first_at = ((lane & (CPR - 1)) ^ chunk_swizzle<RB>(first_row + in_load)) * 16;
-    // K, V or both of the tile of slots from k0 on
-    auto issue = [&](int k0, int pages, unsigned char *to, auto keys, auto values) __attribute__((always_inline)) {
-        constexpr bool K = decltype(keys)::value, V = decltype(values)::value;
+    const int first_row = wave * LOADS * RPI, in_load = lane / CPR, first_at = ((lane & (CPR - 1)) ^ chunk_swizzle<RB>(first_row + in_load)) * 16;
+    auto issue = [&](int k0, int pages, unsigned char *to) __attribute__((always_inline)) {
         to += first_row * RB;
         auto coarse = [&](auto full) __attribute__((always_inline)) {       // the 16 rows from a multiple of 16 on are of one page, and a load's rows lie within 32 bits
 #pragma unroll
@@ -236,8 +250,8 @@ __device__ __forceinline__ void chunk_body(const ChunkArgs &a, const ChunkPass &
                 // (the chunk's place goes by bits of the row: those of the first load's, turned by those of e)
                 const uint32_t at = first_at ^ (chunk_swizzle<RB>(e * RPI) * 16);
                 if (decltype(full)::value || (int)at < row_bytes) {
-                    if constexpr (K) ANN_ROW_TO_LDS(k + (in_load * (uint32_t)a.cache.k_slot + at), to + e * 1024);
-                    if constexpr (V) ANN_ROW_TO_LDS(v + (in_load * (uint32_t)a.cache.v_slot + at), to + Sh::TILE + e * 1024);
+                    ANN_ROW_TO_LDS(k + (in_load * (uint32_t)a.cache.k_slot + at), to + e * 1024);
+                    ANN_ROW_TO_LDS(v + (in_load * (uint32_t)a.cache.v_slot + at), to + Sh::TILE + e * 1024);
                 }
             }
         };
@@ -253,15 +267,14 @@ __device__ __forceinline__ void chunk_body(const ChunkArgs &a, const ChunkPass &
             const int64_t place = (k0 + row) & mask;
             const char *k = k_head + page * a.cache.k_page + place * a.cache.k_slot + at, *v = v_head + page * a.cache.v_page + place * a.cache.v_slot + at;
             if (at < row_bytes) {
-                if constexpr (K) ANN_ROW_TO_LDS(k, to + e * 1024);
-                if constexpr (V) ANN_ROW_TO_LDS(v, to + Sh::TILE + e * 1024);
+                ANN_ROW_TO_LDS(k, to + e * 1024);
+                ANN_ROW_TO_LDS(v, to + Sh::TILE + e * 1024);
             }
         }
     };
-    const bool loads = !FEW || wave < Sh::SLOT_WAVES;
-    if (row_bytes < RB && loads) {                        // what lies behind the end of a row in LDS is never loaded
+    if (row_bytes < RB) {                                 // what lies behind the end of a row in LDS is never loaded
 #pragma unroll
-        for (int b = 0; b < 2 * Sh::BUFFERS; ++b)
+        for (int b = 0; b < 4; ++b)
 #pragma unroll
             for (int e = 0; e < LOADS; ++e) *reinterpret_cast<u4 *>(mine + b * Sh::TILE + first_row * RB + e * 1024 + lane * 16) = zero_chunk();
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -275,7 +288,6 @@ __device__ __forceinline__ void chunk_body(const ChunkArgs &a, const ChunkPass &
     const int i16 = lane & 15, v_row = 4 * h + (i16 >> 2), v_lane = v_row * RB;
     const int v_turn = ((2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1)) ^ chunk_swizzle<RB>(v_row)) << 4 | (i16 & 1) << 3;
     constexpr uint64_t ALL = KT == 64 ? ~0ull : (1ull << (KT & 63)) - 1;
-    int bad_first = INT_MAX, bad_last = -1;
 
     auto scores = [&](unsigned char *at_k, int k0, uint64_t seen, f16v (&x)[NU]) __attribute__((always_inline)) {
 #pragma unroll
@@ -399,83 +411,43 @@ __device__ __forceinline__ void chunk_body(const ChunkArgs &a, const ChunkPass &
             for (int i = 0; i < 4; ++i) x[i] = finite_of<T>(x[i]);
             *reinterpret_cast<u4 *>(loaded + e * 1024) = x;
         }
-        if constexpr (FEW) {
-            bad_first = min(bad_first, k0);
-            bad_last = k0;
-        } else if (lane == 0) {
+        if (lane == 0) {
             atomicMin(&s_bad[0], k0);
             atomicMax(&s_bad[1], k0);
         }
     };
 
-    constexpr int STEP = FEW ? Sh::SLOT_WAVES * KT : KT;
-    constexpr std::true_type YES{};
-    constexpr std::false_type NO{};
-    int k0 = !loads ? end : first + (FEW ? wave * KT : 0);
-    if constexpr (FEW) {
-        uint64_t valid = 0;
-        int pages = -1, next = -1;                        // of this tile, of the next
-        if (k0 < end) {
-            pages = look_up(k0);
-            issue(k0, pages, mine, YES, NO);
-            next = look_up(k0 + STEP);
-            issue(k0, pages, mine, NO, YES);
-        }
-        for (; k0 < end; k0 += STEP) {
-            const bool more = k0 + STEP < end;
-            f16v x[NU];
-            u4 p[NU][2];
-            // K is there once no more than the loads of V are outstanding, which were issued behind it; V likewise
-            wait_outstanding<LOADS>();
-            valid = __ballot(pages >= 0) & ALL;
-            scores(mine, k0, valid, x);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            pages = next;
-            if (more) {
-                issue(k0 + STEP, pages, mine, YES, NO);
-                next = look_up(k0 + 2 * STEP);
-            }
-            weights(x, p);
-            if (more) wait_outstanding<LOADS>();
-            else wait_outstanding<0>();
-            if (!(valid == ALL && k0 >= lo_most && k0 + KT <= hi_least)) take_out(mine + Sh::TILE, k0);
-            times_v(mine + Sh::TILE, x, p);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            if (more) issue(k0 + STEP, pages, mine, NO, YES);
-        }
-    } else {
-        int pages = -1, buffer = 0;
-        uint64_t valid = 0;
-        if (k0 < end) {
-            pages = look_up(k0);
-            issue(k0, pages, mine, YES, YES);
-            valid = __ballot(pages >= 0) & ALL;
-            pages = look_up(k0 + STEP);
-        }
-        for (; k0 < end; k0 += STEP, buffer ^= 1) {
-            unsigned char *at_k = mine + buffer * 2 * Sh::TILE;
-            wait_outstanding<0>();
-            if (!(valid == ALL && k0 >= all_lo && k0 + KT <= all_hi)) take_out(at_k + Sh::TILE, k0);
-            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // all waves' loads are there, and nobody reads the other buffer any more
-            const uint64_t seen = valid;
-            if (k0 + STEP < end) {
-                issue(k0 + STEP, pages, mine + (buffer ^ 1) * 2 * Sh::TILE, YES, YES);
-                valid = __ballot(pages >= 0) & ALL;
-                pages = look_up(k0 + 2 * STEP);
-            }
-            if (k0 >= hi_most) continue;                  // (no row of this wave's attends to it)
-            f16v x[NU];
-            u4 p[NU][2];
-            scores(at_k, k0, seen, x);
-            weights(x, p);
-            times_v(at_k + Sh::TILE, x, p);
-        }
-        __syncthreads();
-        bad_first = s_bad[0];
-        bad_last = s_bad[1];
+    int k0 = first;
+    int pages = -1, buffer = 0;
+    uint64_t valid = 0;
+    if (k0 < end) {
+        pages = look_up(k0);
+        issue(k0, pages, mine);
+        valid = __ballot(pages >= 0) & ALL;
+        pages = look_up(k0 + KT);
     }
+    for (; k0 < end; k0 += KT, buffer ^= 1) {
+        unsigned char *at_k = mine + buffer * 2 * Sh::TILE;
+        wait_outstanding<0>();
+        if (!(valid == ALL && k0 >= all_lo && k0 + KT <= all_hi)) take_out(at_k + Sh::TILE, k0);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // all waves' loads are there, and nobody reads the other buffer any more
+        const uint64_t seen = valid;
+        if (k0 + KT < end) {
+            issue(k0 + KT, pages, mine + (buffer ^ 1) * 2 * Sh::TILE);
+            valid = __ballot(pages >= 0) & ALL;
+            pages = look_up(k0 + 2 * KT);
+        }
+        if (k0 >= hi_most) continue;                  // (no row of this wave's attends to it)
+        f16v x[NU];
+        u4 p[NU][2];
+        scores(at_k, k0, seen, x);
+        weights(x, p);
+        times_v(at_k + Sh::TILE, x, p);
+    }
+    __syncthreads();
+    const int bad_first = s_bad[0], bad_last = s_bad[1];
 #pragma unroll 1
-    for (int k = bad_first; k <= bad_last; k += STEP)
+    for (int k = bad_first; k <= bad_last; k += KT)
 #pragma unroll 1
         for (int key = k; key < k + KT && key < end; ++key) {
             const int page = table[key >> slots_log];
@@ -499,126 +471,380 @@ __device__ __forceinline__ void chunk_body(const ChunkArgs &a, const ChunkPass &
         sum = __uint_as_float(b0) + __uint_as_float(b1);
         top *= scale;                                     // an exponent of 2
     }
-    // four elements of a row: divided and written, or left for what joins the parts
-    auto write = [&](int in, int at, f4 y, float most, float total) {
-        const int r = deal.r0 + in;
-        const int64_t row = (int64_t)(deal.q.token0 + r / G) * a.q_heads + head * G + r % G;
-        if (a.splits > 1) {
-            const int64_t place = row * a.splits + pass.part0 + deal.part;
-            *reinterpret_cast<f4 *>(a.partial + place * a.cache.d + at) = y;
-            if (at == 0) {
-                a.stats[2 * place] = most;
-                a.stats[2 * place + 1] = total;
-            }
-        } else {
-            const float by = total == 0.f ? 0.f : 1.f / total;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] = total == 0.f ? 0.f : y[i] * by;
-            store_four<T>(static_cast<char *>(a.out) + (row * a.cache.d + at) * T::bytes, y);
-            if (at == 0 && a.lse) a.lse[row] = chunk_lse(most, total, a.lift);
-        }
-    };
-    if constexpr (!FEW) {
-        const int in = row0 + m;
-        if (in < deal.count) {
-#pragma unroll
-            for (int c = 0; c < NC; ++c)
-#pragma unroll
-                for (int i = 0; i < 16; i += 4) {
-                    const int at = 32 * c + 2 * i + 4 * h;
-                    if (at < a.cache.d) write(in, at, f4{o[c][i], o[c][i + 1], o[c][i + 2], o[c][i + 3]}, top, sum);
-                }
-        }
-    } else {
-        // the waves' sums, joined
-        constexpr int LD = Sh::LD;
-        float *s_o = reinterpret_cast<float *>(chunk_lds), *s_top = s_o + WAVES * 32 * LD, *s_sum = s_top + WAVES * 32;
-        __syncthreads();
-        if (h == 0) { s_top[wave * 32 + m] = top; s_sum[wave * 32 + m] = sum; }
-        __syncthreads();
-        float all = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) all = fmaxf(all, s_top[w * 32 + m]);
-        const float f = top == -INFINITY ? 1.f : exp2_fast(top - all);      // (a row without a score has zeros, or NaN)
+    const int in = row0 + m;
+    if (in < deal.count) {
 #pragma unroll
         for (int c = 0; c < NC; ++c)
 #pragma unroll
-            for (int i = 0; i < 16; i += 4)
-                *reinterpret_cast<f4 *>(s_o + (wave * 32 + m) * LD + 32 * c + 2 * i + 4 * h) = f4{o[c][i], o[c][i + 1], o[c][i + 2], o[c][i + 3]} * f;
-        __syncthreads();
-        const int per_row = a.cache.d / 4;
-        for (int i = threadIdx.x; i < deal.count * per_row; i += WAVES * WAVE) {
-            const int in = i / per_row, at = i % per_row * 4;
-            float most = -INFINITY, total = 0.f;
-            f4 y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) most = fmaxf(most, s_top[w * 32 + in]);
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) {
-                const float t = s_top[w * 32 + in];
-                total += s_sum[w * 32 + in] * (t == -INFINITY ? 1.f : exp2_fast(t - most));
-                y += *reinterpret_cast<const f4 *>(s_o + (w * 32 + in) * LD + at);
+            for (int i = 0; i < 16; i += 4) {
+                const int at = 32 * c + 2 * i + 4 * h;
+                if (at < a.cache.d) chunk_write<T>(a, pass, deal, head, in, at, f4{o[c][i], o[c][i + 1], o[c][i + 2], o[c][i + 3]}, top, sum);
             }
-            write(in, at, y, most, total);
+    }
+}
+
+// ---- few rows -------------------------------------------------------------------------------------------------
+//
+// Up to 16 MT rows: the waves share the slots out, K and V go from memory to registers, and the tiles are of 16 slots and 16 rows, as in paged_attention_kernel: reading K and V once bounds it.
+// Lane 16 g + m has the scores of row m and slots 4 g .. 4 g + 3 of a tile; weights are operands of two parts.  Both passes of groups go in one launch where both have few rows.
+template <class T, int VE, int MT, bool FINE>
+__global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE, MT)) void chunk_few_kernel(ChunkArgs a, ChunkPass first_pass, ChunkPass own_pass) {
+    typedef AttendShape<T, VE> Sh;
+    typedef typename Words<Sh::CW>::type VChunk;
+    constexpr int NT = Sh::NT, NS = Sh::NS, NU = Sh::NU, CE = Sh::CE, WAVES = CHUNK_WAVES, STEP = 16 * NT * WAVES, ROWS = 16 * MT, LD = attend_lds_row(VE);
+    extern __shared__ __align__(16) float few_lds[];
+    const int lane = threadIdx.x & (WAVE - 1), g = lane >> 4, m = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+    const int G = a.q_heads / a.cache.heads, head = blockIdx.x % a.cache.heads, item = blockIdx.x / a.cache.heads;
+    const bool is_own = item >= first_pass.items;
+    const ChunkPass &pass = is_own ? own_pass : first_pass;
+    const ChunkDeal deal = chunk_deal(a, pass, is_own ? item - first_pass.items : item, G);
+    if (deal.count <= 0) return;
+    const int first = deal.first, end = deal.end, row_bytes = a.cache.d * T::bytes;
+    const bool full = a.cache.d == 16 * VE;
+
+    float *s_top = few_lds, *s_sum = few_lds + WAVES * ROWS, *s_o = few_lds + 2 * WAVES * ROWS;
+    constexpr bool Q_LDS = attend_q_in_lds(VE);
+    u4 *s_q = reinterpret_cast<u4 *>(s_o), q[Q_LDS ? 1 : MT][Q_LDS ? 1 : NS];
+    int lo[MT], hi[MT], lo_most = 0, hi_least = INT_MAX;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        const int in = 16 * mt + m, r = deal.r0 + in, t = deal.q.token0 + r / G;
+        const bool there = in < deal.count;
+        const char *from = static_cast<const char *>(a.q) + t * a.q_row + (head * G + r % G) * a.q_head;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            const int at = (4 * s + g) * 16;
+            u4 x = zero_chunk();
+            if (there && at < row_bytes) x = load_chunk(from + at);
+            if constexpr (!Q_LDS) q[mt][s] = x;
+            else if ((mt * NS + s) % WAVES == wave) s_q[(mt * NS + s) * WAVE + lane] = x;
+        }
+        lo[mt] = 0;
+        hi[mt] = INT_MAX;
+        if (there) {
+            const ChunkSpan span = chunk_row_span(a, pass.mode, deal, t, r / G);
+            lo[mt] = span.lo;
+            hi[mt] = span.hi;
+        }
+        lo_most = max(lo_most, lo[mt]);
+        hi_least = min(hi_least, hi[mt]);
+    }
+#pragma unroll
+    for (int i = 1; i < 16; i *= 2) {
+        lo_most = max(lo_most, __shfl_xor(lo_most, i));
+        hi_least = min(hi_least, __shfl_xor(hi_least, i));
+    }
+    lo_most = __builtin_amdgcn_readfirstlane(lo_most);
+    hi_least = __builtin_amdgcn_readfirstlane(hi_least);
+
+    const int32_t *table = a.table + (int64_t)deal.q.request * a.width;
+    const int slots_log = a.cache.slots_log, mask = (1 << slots_log) - 1;
+    const char *k_head = a.cache.k + head * a.cache.k_head, *v_head = a.cache.v + head * a.cache.v_head;
+    auto row_page = [&](int key) {
+        int page = -1;
+        if (key < end) page = table[key >> slots_log];
+        return (unsigned)page < (unsigned)a.cache.pages ? page : -1;
+    };
+    // pages of tiles, looked up a step ahead; -1: none.  FINE: of the lane's row of K, and of its four rows of V
+    struct Pages { int k[NT], v[NT][FINE ? 4 : 1]; };
+    Pages page, page_next;
+    u4 kr[NT][NS];
+    auto pages_of = [&](int k0, Pages &out) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            if (!FINE) {
+                out.k[t] = __builtin_amdgcn_readfirstlane(row_page(k0 + 16 * t));
+                continue;
+            }
+            out.k[t] = row_page(k0 + 16 * t + m);
+#pragma unroll
+            for (int i = 0; i < (FINE ? 4 : 1); ++i) out.v[t][i] = row_page(k0 + 16 * t + 4 * g + i);
+        }
+    };
+    auto load_k = [&](int k0, const Pages &pg) __attribute__((always_inline)) {
+        auto load = [&](auto whole) __attribute__((always_inline)) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const int p = max(pg.k[t], 0);
+                const char *row = k_head + (int64_t)p * a.cache.k_page + ((k0 + 16 * t + m) & mask) * a.cache.k_slot;
+#pragma unroll
+                for (int s = 0; s < NS; ++s) {
+                    const int at = (4 * s + g) * 16;
+                    if (decltype(whole)::value || at < row_bytes) kr[t][s] = load_chunk(row + at);
+                    else kr[t][s] = zero_chunk();
+                }
+            }
+        };
+        if (full) load(std::true_type{});
+        else load(std::false_type{});
+    };
+
+    f4 o[MT][VE];
+    float top[MT], sum[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+        for (int c = 0; c < VE; ++c) o[mt][c] = f4{0.f, 0.f, 0.f, 0.f};
+        top[mt] = -INFINITY;
+        sum[mt] = 0.f;
+    }
+    int k0 = first + wave * 16 * NT, bad_first = INT_MAX, bad_last = -1;
+    if (k0 < end) {
+        pages_of(k0, page);
+        load_k(k0, page);
+    }
+    if constexpr (Q_LDS) __syncthreads();
+    for (; k0 < end; k0 += STEP) {
+        const bool more = k0 + STEP < end;
+        if (more) pages_of(k0 + STEP, page_next);
+        VChunk vr[NT][4][NU];
+        auto load_v = [&](auto whole) __attribute__((always_inline)) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int p = max(FINE ? page.v[t][FINE ? i : 0] : page.k[t], 0);
+                    const char *row = v_head + (int64_t)p * a.cache.v_page + ((k0 + 16 * t + 4 * g + i) & mask) * a.cache.v_slot;
+#pragma unroll
+                    for (int u = 0; u < NU; ++u) {
+                        const int at = (u * 16 + m) * CE;
+                        if (decltype(whole)::value || at < a.cache.d) vr[t][i][u] = *reinterpret_cast<const VChunk *>(row + at * T::bytes);
+                        else vr[t][i][u] = VChunk(0);
+                    }
+                }
+        };
+        if (full) load_v(std::true_type{});
+        else load_v(std::false_type{});
+        if constexpr (Q_LDS) asm volatile("" ::: "memory");                 // (the queries stay where they are)
+        f4 x[MT][NT];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                x[mt][t] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int s = 0; s < NS; ++s) x[mt][t] = scores_step<T>(kr[t][s], Q_LDS ? s_q[(mt * NS + s) * WAVE + lane] : q[Q_LDS ? 0 : mt][Q_LDS ? 0 : s], x[mt][t]);
+                x[mt][t] *= a.scale;
+            }
+        if (more) load_k(k0 + STEP, page_next);
+        bool whole = k0 >= lo_most && k0 + 16 * NT <= hi_least && k0 + 16 * NT <= end;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) whole = whole && page.k[t] >= 0;
+        if (FINE || !whole) {                             // slots that do not count, for all rows or for some: no score, and values that are numbers
+            uint32_t most = 0;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int key = k0 + 16 * t + 4 * g + i;
+                    const bool there = (FINE ? page.v[t][FINE ? i : 0] : page.k[t]) >= 0 && key < end;
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt)
+                        if (!there || key < lo[mt] || key >= hi[mt]) x[mt][t][i] = -INFINITY;
+#pragma unroll
+                    for (int u = 0; u < NU; ++u) {
+                        if (!there) vr[t][i][u] = VChunk(0);
+#pragma unroll
+                        for (int w = 0; w < Sh::CW; ++w) most_bits<T>(vr[t][i][u][w], most);
+                    }
+                }
+            // (infinities and NaN are given to the rows that attend to them at the end: 0 times NaN is no 0)
+            if (__ballot(not_finite<T>(most))) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int u = 0; u < NU; ++u)
+#pragma unroll
+                            for (int w = 0; w < Sh::CW; ++w) vr[t][i][u][w] = finite_of<T>(vr[t][i][u][w]);
+                bad_first = min(bad_first, k0);
+                bad_last = k0;
+            }
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {                 // x becomes the weights
+            float most = x[mt][0][0];
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) most = fmaxf(most, x[mt][t][i]);
+            const float now = fmaxf(top[mt], column_max(most)), keep = top[mt] == now ? 1.f : exp2_fast(top[mt] - now), off = (now == -INFINITY ? 0.f : now) - a.lift;
+            top[mt] = now;
+            sum[mt] *= keep;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    x[mt][t][i] = exp2_fast(x[mt][t][i] - off);
+                    sum[mt] += x[mt][t][i];
+                }
+#pragma unroll
+            for (int c = 0; c < VE; ++c) o[mt][c] *= keep;
+        }
+        if constexpr (T::bytes == 2) {
+#pragma unroll
+            for (int t = 0; t < NT; t += 2) {
+                u4 high[MT], low[MT];
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    const f4 x0 = x[mt][t], x1 = x[mt][t + 1];
+                    const float w[8] = {x0[0], x0[1], x0[2], x0[3], x1[0], x1[1], x1[2], x1[3]};
+                    split_weights<T>(w, high[mt], low[mt]);
+                }
+#pragma unroll
+                for (int u = 0; u < NU; ++u)
+#pragma unroll
+                    for (int c = 0; c < CE; ++c) {
+                        u4 v;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            v[k] = __builtin_amdgcn_perm(vr[t + k / 2][2 * (k & 1) + 1][u][c / 2], vr[t + k / 2][2 * (k & 1)][u][c / 2], c & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) {
+                            f4 &acc = o[mt][u * CE + c];
+                            acc = mfma16<T>(v, high[mt], acc);
+                            acc = mfma16<T>(v, low[mt], acc);
+                        }
+                    }
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int u = 0; u < NU; ++u)
+#pragma unroll
+                        for (int c = 0; c < CE; ++c)
+#pragma unroll
+                            for (int mt = 0; mt < MT; ++mt)
+                                o[mt][u * CE + c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[t][i][u][c]), x[mt][t][i], o[mt][u * CE + c], 0, 0, 0);
+        }
+        page = page_next;
+    }
+#pragma unroll 1
+    for (int k = bad_first; k <= bad_last; k += STEP)
+#pragma unroll 1
+        for (int key = k; key < k + 16 * NT && key < end; ++key) {
+            const int p = row_page(key);
+            if (p < 0) continue;
+            const char *from = v_head + (int64_t)p * a.cache.v_page + (key & mask) * a.cache.v_slot;
+#pragma unroll
+            for (int u = 0; u < NU; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int c = 0; c < CE; c += 4) {
+                        const int at = (u * 16 + 4 * g + i) * CE + c;
+                        if (at >= a.cache.d) continue;
+                        const f4 v = not_finite_four<T>(from + at * T::bytes);
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt)
+                            if (key >= lo[mt] && key < hi[mt]) {
+#pragma unroll
+                                for (int b = 0; b < 4; ++b) o[mt][u * CE + c + b][i] += v[b];
+                            }
+                    }
+        }
+
+    // the waves' sums, joined (of those that had a slot): lane 16 g + m holds elements CE (4 g + i) .. of every 16 CE, row 16 mt + m
+    const int used = min(WAVES, (max(end - first, 1) + 16 * NT - 1) / (16 * NT));
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        sum[mt] = column_sum(sum[mt]);
+        if (g == 0) {
+            s_top[wave * ROWS + 16 * mt + m] = top[mt];
+            s_sum[wave * ROWS + 16 * mt + m] = sum[mt];
         }
     }
-}
-
-// One pass, or two side by side: workgroups of either in turn, as long as there are both, so that a compute unit has some that wait for memory beside some that multiply.
-template <class T, int DP, bool FEW, bool BOTH>
-__global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(T::bytes, DP)) void chunk_attention_kernel(ChunkArgs a, ChunkPass first, ChunkPass own) {
-    extern __shared__ __align__(16) unsigned char chunk_lds[];
-    __shared__ int s_scratch[12];
-    int block = blockIdx.x;
-    if constexpr (BOTH) {
-        const int n0 = first.items * a.cache.heads, n1 = own.items * a.cache.heads, both = 2 * min(n0, n1);
-        const bool is_own = block < both ? block & 1 : n1 > n0;
-        block = block < both ? block >> 1 : block - both / 2;
-        if (is_own) return chunk_body<T, DP, true>(a, own, block, chunk_lds, s_scratch);
+    __syncthreads();
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        const int in = 16 * mt + m;
+        float all = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) all = fmaxf(all, s_top[w * ROWS + in]);
+        const float f = top[mt] == -INFINITY ? 1.f : exp2_fast(top[mt] - all);          // (a row without a score has zeros, or NaN)
+        if (in < deal.count && wave < used) {
+#pragma unroll
+            for (int u = 0; u < NU; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int c = 0; c < CE; c += 4) {
+                        const int at = (u * 16 + 4 * g + i) * CE + c, e = u * CE + c;
+                        *reinterpret_cast<f4 *>(s_o + (wave * deal.count + in) * LD + at) = f4{o[mt][e][i], o[mt][e + 1][i], o[mt][e + 2][i], o[mt][e + 3][i]} * f;
+                    }
+        }
     }
-    chunk_body<T, DP, FEW>(a, first, block, chunk_lds, s_scratch);
+    __syncthreads();
+    const int per_row = a.cache.d / 4;
+    for (int i = threadIdx.x; i < deal.count * per_row; i += WAVES * WAVE) {
+        const int in = i / per_row, at = i % per_row * 4;
+        float most = -INFINITY, total = 0.f;
+        f4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) most = fmaxf(most, s_top[w * ROWS + in]);
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float t = s_top[w * ROWS + in];
+            total += s_sum[w * ROWS + in] * (t == -INFINITY ? 1.f : exp2_fast(t - most));
+        }
+        for (int w = 0; w < used; ++w) y += *reinterpret_cast<const f4 *>(s_o + (w * deal.count + in) * LD + at);
+        chunk_write<T>(a, pass, deal, head, in, at, y, most, total);
+    }
 }
 
-// What the parts of a row left, joined by a wave: lanes share the parts out where a row takes fewer than there are.
+// What the parts of a row left, joined by a wave, whose lanes share the parts out where a row takes fewer than there are.  The first part of a pass says how many there are, and the one of own slots whether
+// the row is in a group.
 template <class T>
-__global__ __launch_bounds__(256) void chunk_join_kernel(ChunkArgs a, ChunkPass first, ChunkPass own) {
-    const int lane = threadIdx.x & (WAVE - 1), d = a.cache.d, G = a.q_heads / a.cache.heads;
+__global__ __launch_bounds__(256) void chunk_join_kernel(ChunkArgs a, int own_part0, bool new_tokens) {
+    const int lane = threadIdx.x & (WAVE - 1), d = a.cache.d;
     const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / WAVE;
     if (row >= (int64_t)a.tokens * a.q_heads) return;
-    const int t = (int)(row / a.q_heads), in_head = (int)(row % a.q_heads) % G;
-    int parts0 = 0, parts1 = 0;                           // of the two passes, or of the only one
-    if (first.mode == CHUNK_NEW) {
-        const PackedToken token = packed_token(a.starts, a.requests, a.tokens, t);
-        if (token.request < 0) return;
-        parts0 = chunk_parts_of(a, first, token.request, t, in_head, G);
-    } else if (first.mode == CHUNK_OWN) {
-        parts0 = chunk_parts_of(a, first, t, t, in_head, G);
+    const f4 *stats = reinterpret_cast<const f4 *>(a.stats) + row * a.splits;
+    // (of parts that are not there too, which are at most 128; what they hold is not looked at)
+    const f4 s0 = lane < a.splits ? stats[lane] : f4{0.f, 0.f, 0.f, 0.f}, s1 = lane + WAVE < a.splits ? stats[lane + WAVE] : f4{0.f, 0.f, 0.f, 0.f};
+    if (new_tokens && packed_token(a.starts, a.requests, a.tokens, (int)(row / a.q_heads)).request < 0) return;
+    auto word = [&](int s, int i) { return __builtin_amdgcn_readlane(__float_as_int(s < WAVE ? s0[i] : s1[i]), s & (WAVE - 1)); };
+    // (no more than there is room for, whatever the groups' starts are)
+    auto parts = [&](int s, int most) { return min(max(word(s, 2), 0), most); };
+    int parts0 = 0, parts1 = 0;
+    if (new_tokens) {
+        parts0 = parts(0, a.splits);
+        if (parts0 == 1) return;                          // (it is written)
     } else {
-        const int g = chunk_group(a, t);
-        if (g >= 0) parts0 = chunk_parts_of(a, first, g, t, in_head, G);
-        parts1 = chunk_parts_of(a, own, t, t, in_head, G);
+        parts1 = parts(own_part0, a.splits - own_part0);
+        if (own_part0 > 0 && word(own_part0, 3)) parts0 = parts(0, own_part0);
     }
-    const int n = parts0 + parts1;
-    auto place = [&](int s) { return row * a.splits + (s < parts0 ? s : own.part0 + s - parts0); };
-    const float2 *stats = reinterpret_cast<const float2 *>(a.stats);
-    float most = -INFINITY;
-    for (int s = lane; s < n; s += WAVE) most = fmaxf(most, stats[place(s)].x);
-#pragma unroll
-    for (int i = 1; i < WAVE; i *= 2) most = fmaxf(most, __shfl_xor(most, i));
+    auto there = [&](int s) { return s < parts0 || (s >= own_part0 && s < own_part0 + parts1); };
+    float most = fmaxf(there(lane) ? s0[0] : -INFINITY, there(lane + WAVE) ? s1[0] : -INFINITY);
+    most = wave_max(most);
+    // (a part without a score has a sum of 0, or NaN, and counts as it is)
+    const float f0 = !there(lane) ? 0.f : s0[0] == -INFINITY ? 1.f : exp2_fast(s0[0] - most), f1 = !there(lane + WAVE) ? 0.f : s1[0] == -INFINITY ? 1.f : exp2_fast(s1[0] - most);
+    const float total = wave_sum((there(lane) ? s0[1] * f0 : 0.f) + (there(lane + WAVE) ? s1[1] * f1 : 0.f));
     // lanes of a row: the power of two from d / 4 on
-    const int per = d <= 32 ? 8 : d <= 64 ? 16 : d <= 128 ? 32 : 64, at = 4 * (lane % per);
-    float total = 0.f;
+    const int per = d <= 32 ? 8 : d <= 64 ? 16 : d <= 128 ? 32 : 64, at = 4 * (lane % per), n = parts0 + parts1;
+    const float *from = a.partial + row * a.splits * d + at;
     f4 y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int s = lane / per; s < n; s += WAVE / per) {
-        const int64_t p = place(s);
-        const float2 st = stats[p];
-        const float f = st.x == -INFINITY ? 1.f : exp2_fast(st.x - most);
-        total += st.y * f;
-        if (at < d) y += *reinterpret_cast<const f4 *>(a.partial + p * d + at) * f;
+    constexpr int AHEAD = 8;
+    for (int i0 = 0; i0 < n; i0 += AHEAD * WAVE / per) {
+        f4 z[AHEAD];
+        float f[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int i = i0 + k * (WAVE / per) + lane / per, s = i < parts0 ? i : own_part0 + i - parts0;
+            const float g0 = __shfl(f0, s & (WAVE - 1)), g1 = __shfl(f1, s & (WAVE - 1));
+            const bool ok = i < n && at < d;
+            z[k] = ok ? *reinterpret_cast<const f4 *>(from + (int64_t)s * d) : f4{0.f, 0.f, 0.f, 0.f};
+            f[k] = !ok ? 0.f : s < WAVE ? g0 : g1;
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) y += z[k] * f[k];
     }
     for (int i = per; i < WAVE; i *= 2) {
-        total += __shfl_xor(total, i);
 #pragma unroll
         for (int j = 0; j < 4; ++j) y[j] += __shfl_xor(y[j], i);
     }
@@ -630,28 +856,42 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(ChunkArgs a, ChunkPass 
     if (lane == 0 && a.lse) a.lse[row] = chunk_lse(most, total, a.lift);
 }
 
-template <class T, int DP, bool FEW, bool BOTH>
-hipError_t chunk_launch(const ChunkArgs &a, const ChunkPlan &pl, hipStream_t stream) {
-    typedef ChunkShape<T, DP, FEW> Sh;
-    typedef ChunkShape<T, DP, true> Own;
-    constexpr int LDS = BOTH && Own::LDS > Sh::LDS ? Own::LDS : Sh::LDS;
+template <class T, int DP>
+hipError_t chunk_more(const ChunkArgs &a, const ChunkPass &pass, hipStream_t stream) {
     static size_t granted = 0;
-    if (hipError_t e = allow_big_lds(reinterpret_cast<const void *>(chunk_attention_kernel<T, DP, FEW, BOTH>), LDS, &granted)) return e;
-    const int64_t blocks = (int64_t)(pl.first.items + (BOTH ? pl.own.items : 0)) * a.cache.heads;
-    hipLaunchKernelGGL((chunk_attention_kernel<T, DP, FEW, BOTH>), dim3((unsigned)blocks), dim3(CHUNK_WAVES * WAVE), LDS, stream, a, pl.first, pl.own);
+    constexpr int bytes = ChunkShape<T, DP>::LDS;
+    if (hipError_t e = allow_big_lds(reinterpret_cast<const void *>(chunk_attention_kernel<T, DP>), bytes, &granted)) return e;
+    hipLaunchKernelGGL((chunk_attention_kernel<T, DP>), dim3((unsigned)((int64_t)pass.items * a.cache.heads)), dim3(CHUNK_WAVES * WAVE), bytes, stream, a, pass);
     return hipGetLastError();
 }
-template <class T, int DP>
+template <class T, int VE, int MT, bool FINE>
+hipError_t chunk_few(const ChunkArgs &a, const ChunkPass &first, const ChunkPass &own, hipStream_t stream) {
+    static size_t granted = 0;
+    const size_t bytes = attend_lds_bytes(T::bytes, VE, MT, 16 * MT, 0);
+    if (hipError_t e = allow_big_lds(reinterpret_cast<const void *>(chunk_few_kernel<T, VE, MT, FINE>), bytes, &granted)) return e;
+    hipLaunchKernelGGL((chunk_few_kernel<T, VE, MT, FINE>), dim3((unsigned)((int64_t)(first.items + own.items) * a.cache.heads)), dim3(CHUNK_WAVES * WAVE), bytes, stream, a, first, own);
+    return hipGetLastError();
+}
+template <class T, int VE>
+hipError_t chunk_few(const ChunkArgs &a, const ChunkPass &first, const ChunkPass &own, int rows, hipStream_t stream) {
+    const bool fine = a.cache.slots_log < 4;
+    if constexpr (chunk_few_rows(T::bytes, VE, 32) == 32)
+        if (rows == 32) return fine ? chunk_few<T, VE, 2, true>(a, first, own, stream) : chunk_few<T, VE, 2, false>(a, first, own, stream);
+    return fine ? chunk_few<T, VE, 1, true>(a, first, own, stream) : chunk_few<T, VE, 1, false>(a, first, own, stream);
+}
+template <class T, int VE>
 hipError_t chunk_launch(const ChunkArgs &a, const ChunkPlan &pl, hipStream_t stream) {
-    if (pl.own.items) return pl.first.shape == CHUNK_FEW ? chunk_launch<T, DP, true, true>(a, pl, stream) : chunk_launch<T, DP, false, true>(a, pl, stream);
-    return pl.first.shape == CHUNK_FEW ? chunk_launch<T, DP, true, false>(a, pl, stream) : chunk_launch<T, DP, false, false>(a, pl, stream);
+    if (pl.first.rows <= 32) return chunk_few<T, VE>(a, pl.first, pl.own, pl.first.rows, stream);
+    if (hipError_t e = chunk_more<T, 16 * VE>(a, pl.first, stream)) return e;
+    return pl.own.items ? chunk_few<T, VE>(a, ChunkPass{}, pl.own, pl.own.rows, stream) : hipSuccess;
 }
 template <class T>
 hipError_t launch_chunk(const ChunkArgs &a, const ChunkPlan &pl, hipStream_t stream) {
-    if (hipError_t e = a.cache.d <= 64 ? chunk_launch<T, 64>(a, pl, stream) : a.cache.d <= 128 ? chunk_launch<T, 128>(a, pl, stream) : chunk_launch<T, 256>(a, pl, stream)) return e;
+    const int ve = attend_ve(a.cache.d);
+    if (hipError_t e = ve == 4 ? chunk_launch<T, 4>(a, pl, stream) : ve == 8 ? chunk_launch<T, 8>(a, pl, stream) : chunk_launch<T, 16>(a, pl, stream)) return e;
     if (a.splits == 1) return hipSuccess;
     const int64_t rows = (int64_t)a.tokens * a.q_heads;
-    hipLaunchKernelGGL((chunk_join_kernel<T>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, a, pl.first, pl.own);
+    hipLaunchKernelGGL((chunk_join_kernel<T>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, a, pl.own.part0, pl.first.mode == CHUNK_NEW);
     return hipGetLastError();
 }
 

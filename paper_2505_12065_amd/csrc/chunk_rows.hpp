@@ -49,9 +49,8 @@ __device__ __forceinline__ ChunkSpan chunk_span(const ChunkArgs &a, int length, 
     if (slot < 0 || slot >= a.max_length) return {0, 0};
     return {a.window > 0 ? max(slot + 1 - a.window, 0) : 0, slot + 1};
 }
-// ... that tokens t0 to t1 of sequence i attend to, all of them together.  By whole waves.
-__device__ __forceinline__ ChunkSpan chunk_range(const ChunkArgs &a, int mode, int i, const ChunkSequence &q, int t0, int t1) {
-    const int length = chunk_length(a, q.request);
+// ... that tokens t0 to t1 of sequence i, of a request of `length` slots, attend to, all of them together.  By whole waves.
+__device__ __forceinline__ ChunkSpan chunk_range(const ChunkArgs &a, int mode, int i, const ChunkSequence &q, int length, int t0, int t1) {
     if (mode == CHUNK_NEW) {
         const int first = length - (q.tokens - t0), last = length - (q.tokens - t1);
         return {a.window > 0 ? max(first + 1 - a.window, 0) : 0, min(max(last + 1, 0), a.max_length)};
@@ -78,7 +77,7 @@ __device__ __forceinline__ ChunkLane chunk_lane(const ChunkArgs &a, const ChunkP
     if (lane < n) l.tiles = (int)((rows + p.rows - 1) / p.rows);
     // (the last tile has most, but for what a window leaves it)
     const int t0 = (int)(max(l.tiles - 1, 0) * (int64_t)p.rows / G), t1 = max(q.tokens - 1, 0);
-    const ChunkSpan range = chunk_range(a, p.mode, i, q, t0, t1);
+    const ChunkSpan range = chunk_range(a, p.mode, i, q, chunk_length(a, q.request), t0, t1);
     if (l.tiles > 0) l.slots = chunk_slots_of(range);
     if (l.tiles > 0 && p.mode == CHUNK_NEW && a.window > 0) l.slots = (int)max((int64_t)l.slots, min((int64_t)range.hi, (int64_t)a.window + p.rows + 32));
     if (p.most_parts == 1) return l;
@@ -98,12 +97,20 @@ __device__ __forceinline__ ChunkLane chunk_lane(const ChunkArgs &a, const ChunkP
     return l;
 }
 
-// What a workgroup does: part `part`, of `chunk` slots, of the tile that begins with row r0 of a sequence; count 0: nothing.
-struct ChunkDeal { ChunkSequence q; int sequence, r0, count, part, chunk; };
+// What a workgroup does: slots first .. end - 1 of the tile that begins with row r0 of a sequence, of whose range they are part `part`; count 0: nothing.
+struct ChunkDeal {
+    ChunkSequence q;
+    int length;               // of q.request, at least 0
+    int r0, count, part, parts;
+    bool alone;               // nothing is to be joined with it
+    int grouped;              // CHUNK_OWN: the request is in a group
+    ChunkSpan range;          // of the tile's rows, all together
+    int first, end;
+};
 __device__ __forceinline__ ChunkDeal chunk_deal(const ChunkArgs &a, const ChunkPass &p, int item, int G) {
     const int n = chunk_sequences(a, p.mode), lane = threadIdx.x & (WAVE - 1);
     ChunkDeal d{};
-    int i;
+    int i, chunk;
     int64_t tile;
     if (n <= WAVE) {
         const ChunkLane l = chunk_lane(a, p, n, G);
@@ -119,12 +126,12 @@ __device__ __forceinline__ ChunkDeal chunk_deal(const ChunkArgs &a, const ChunkP
         const int local = item - __builtin_amdgcn_readlane(before, i), tiles = __builtin_amdgcn_readlane(l.tiles, i);
         d.part = local / tiles;
         tile = tiles - 1 - local % tiles;
-        d.chunk = l.chunk;
+        chunk = l.chunk;
     } else {
         // A sequence of m tokens has at most as many tiles as there are numbers from start G / rows + i up to the next one's.
         const int id = p.tiles - 1 - item % p.tiles;
         d.part = item / p.tiles;
-        d.chunk = p.chunk;
+        chunk = p.chunk;
         if (p.mode == CHUNK_OWN) {
             const int per = (G + p.rows - 1) / p.rows;
             i = id / per;
@@ -138,18 +145,21 @@ __device__ __forceinline__ ChunkDeal chunk_deal(const ChunkArgs &a, const ChunkP
             tile = id - first(i);
         }
     }
-    d.sequence = i;
     d.q = chunk_sequence(a, p.mode, i);
+    d.length = chunk_length(a, d.q.request);
     d.r0 = (int)(tile * p.rows);
-    d.count = (int)max((int64_t)0, min((int64_t)p.rows, (int64_t)d.q.tokens * G - tile * p.rows));
+    const int count = (int)max((int64_t)0, min((int64_t)p.rows, (int64_t)d.q.tokens * G - tile * p.rows));
+    if (count == 0) return d;
+    if (p.mode == CHUNK_OWN) d.grouped = chunk_group(a, i) >= 0;
+    d.range = chunk_range(a, p.mode, i, d.q, d.length, d.r0 / G, (d.r0 + count - 1) / G);
+    const int slots = chunk_slots_of(d.range);
+    d.parts = chunk_parts(slots, chunk);
+    if (d.part >= d.parts) return d;
+    d.count = count;
+    d.alone = p.mode == CHUNK_NEW && d.parts == 1;
+    d.first = chunk_begin(d.range) + d.part * chunk;
+    d.end = d.range.hi - d.first < chunk ? d.range.hi : d.first + chunk;
     return d;
-}
-// Parts of the row `in_head` of token t of sequence i.
-__device__ __forceinline__ int chunk_parts_of(const ChunkArgs &a, const ChunkPass &p, int i, int t, int in_head, int G) {
-    const int n = chunk_sequences(a, p.mode), chunk = n <= WAVE ? chunk_lane(a, p, n, G).chunk : p.chunk;
-    const ChunkSequence q = chunk_sequence(a, p.mode, i);
-    const int64_t r0 = ((int64_t)(t - q.token0) * G + in_head) / p.rows * p.rows, r1 = min(r0 + p.rows, (int64_t)q.tokens * G) - 1;
-    return chunk_parts(chunk_slots_of(chunk_range(a, p.mode, i, q, (int)(r0 / G), (int)(r1 / G))), chunk);
 }
 
 }  // namespace ann

@@ -1125,19 +1125,19 @@ inline int rotate_rows(int T, int heads, int groups) {
 constexpr int64_t CHUNK_ROWS_MAX = 1 << 26;               // query heads of all tokens
 constexpr int64_t CHUNK_GRID = (1 << 24) - 1;             // workgroups of a launch, which has fewer than 2^32 threads
 constexpr size_t CHUNK_WS_MAX = (size_t)256 << 20;        // of workspace
-// Shapes of a workgroup.  FEW: 32 rows, whose slots its waves share out; MORE: 32 rows to each of four waves.
-enum { CHUNK_FEW, CHUNK_MORE };
-constexpr int chunk_rows(bool few) { return few ? 32 : 128; }
-constexpr int chunk_class(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
-constexpr int chunk_slots(int row_bytes, bool few) { return few || row_bytes > 256 ? 32 : 64; }       // slots of a tile
 constexpr int CHUNK_WAVES = 4;
-constexpr int chunk_slot_waves(int row_bytes) { return row_bytes > 512 ? 2 : CHUNK_WAVES; }            // FEW: waves that take slots, as LDS allows
+constexpr int CHUNK_TILE = 128;                           // rows of a workgroup, 32 to each wave, where there are more than a few
+constexpr int chunk_class(int d) { return 16 * attend_ve(d); }
+constexpr int chunk_slots(int row_bytes) { return row_bytes > 256 ? 32 : 64; }                        // slots of a tile
 constexpr int chunk_per_simd(int elem_bytes, int dp) { return elem_bytes == 4 || dp == 256 ? 1 : 2; } // waves, as registers allow
+// A few rows: 16 or, where registers allow, 32.
+constexpr int chunk_few_rows(int elem_bytes, int ve, int64_t rows) { return rows > 16 && attend_head_tiles(elem_bytes, ve, 17) == 2 ? 32 : 16; }
+constexpr int chunk_few_per_simd(int elem_bytes, int ve, int mt) { return ve == 16 || (elem_bytes == 4 && (mt == 2 || ve == 8)) ? 1 : 2; }
 
 // A pass goes through the slots that new tokens attend to, those that groups have in common, or those that are a request's own.
 enum { CHUNK_NEW, CHUNK_COMMON, CHUNK_OWN };
 struct ChunkPass {
-    int mode = CHUNK_NEW, shape = CHUNK_FEW, rows = 32;   // rows of a tile
+    int mode = CHUNK_NEW, rows = 16;                      // rows of a tile
     int items = 0;               // tiles and parts of a cache head that there may be
     int fill = 1;                // workgroups of a cache head that fill the card
     int most_parts = 1, least = 64, part0 = 0;            // parts of a row at most; slots of a part at least; number of a row's first part
@@ -1150,28 +1150,29 @@ struct ChunkPlan {
 };
 constexpr int64_t CHUNK_PARTS = 64;                       // of a row in a pass
 // Sequences of `rows` rows in all, whose tiles go through `range` slots at most.
-inline ChunkPass chunk_pass(int mode, int cus, int elem_bytes, int d, int heads, int64_t rows, int64_t sequences, int64_t range, int64_t most_parts) {
+inline ChunkPass chunk_pass(int mode, int cus, int elem_bytes, int d, int heads, int64_t rows, int64_t sequences, int64_t range, int64_t most_parts, int64_t least_rows = 1) {
     ChunkPass p;
-    const int dp = chunk_class(d);
+    const int ve = attend_ve(d);
+    const int64_t mean = (rows + sequences - 1) / sequences;
+    const bool few = mode == CHUNK_OWN || mean <= 32;
     p.mode = mode;
-    p.shape = mode == CHUNK_OWN || rows <= 32 * sequences ? CHUNK_FEW : CHUNK_MORE;
-    p.rows = chunk_rows(p.shape == CHUNK_FEW);
-    p.fill = cus * chunk_per_simd(elem_bytes, dp) / heads;
+    p.rows = few ? chunk_few_rows(elem_bytes, ve, mean > least_rows ? mean : least_rows) : CHUNK_TILE;
+    p.fill = (few ? 4 : chunk_per_simd(elem_bytes, 16 * ve)) * cus / heads;
     if (p.fill < 1) p.fill = 1;
-    p.least = elem_bytes == 4 ? 64 : p.shape == CHUNK_FEW ? 128 : 256;
+    p.least = few ? (int)(2 * attend_step(elem_bytes, d)) : elem_bytes == 4 ? 64 : 256;
     const int64_t tiles = mode == CHUNK_OWN ? sequences * ((rows / sequences + p.rows - 1) / p.rows) : rows / p.rows + sequences;
-    // nothing is divided where tiles alone keep the card busy
-    const int64_t busy = rows / p.rows;
+    // nothing is divided where tiles alone keep most of the card busy
+    const int64_t busy = few ? sequences : rows / p.rows;
     int64_t parts = (range + p.least - 1) / p.least;
     if (parts > most_parts) parts = most_parts;
     if (parts > CHUNK_PARTS) parts = CHUNK_PARTS;
-    if (busy >= 2 * p.fill || parts < 1) parts = 1;
+    if (4 * busy >= 3 * p.fill || parts < 1) parts = 1;
     p.tiles = (int)tiles;
     if (sequences <= 64) {
         p.most_parts = (int)parts;
         p.items = (int)(parts > 1 && tiles < 2 * p.fill + sequences ? 2 * p.fill + sequences : tiles);
     } else {
-        const int64_t mean = (rows / sequences + p.rows - 1) / p.rows * sequences, wanted = mean >= p.fill ? 1 : p.fill / (mean < 1 ? 1 : mean);
+        const int64_t busy_tiles = (mean + p.rows - 1) / p.rows * sequences, wanted = busy_tiles >= p.fill ? 1 : p.fill / busy_tiles;
         if (parts > wanted) parts = wanted;
         p.chunk = (int)(((range + parts - 1) / parts + 63) / 64 * 64);
         p.most_parts = (int)((range + p.chunk - 1) / p.chunk);
@@ -1179,9 +1180,9 @@ inline ChunkPass chunk_pass(int mode, int cus, int elem_bytes, int d, int heads,
     }
     return p;
 }
-inline size_t chunk_bytes(int64_t rows, int64_t d, int64_t splits) { return splits > 1 ? (size_t)rows * splits * (d + 2) * 4 : 0; }
+inline size_t chunk_bytes(int64_t rows, int64_t d, int64_t splits) { return splits > 1 ? (size_t)rows * splits * (d + 4) * 4 : 0; }
 // Parts that `most` bytes hold.
-inline int64_t chunk_parts_in(int64_t rows, int64_t d, size_t most) { return (int64_t)(most / ((size_t)rows * (d + 2) * 4)); }
+inline int64_t chunk_parts_in(int64_t rows, int64_t d, size_t most) { return (int64_t)(most / ((size_t)rows * (d + 4) * 4)); }
 inline ChunkPlan chunk_plan(int cus, int elem_bytes, int d, int q_heads, int heads, int64_t T, int64_t B, int64_t max_length, int64_t window, size_t most) {
     ChunkPlan pl;
     const int G = q_heads / heads;
@@ -1202,6 +1203,12 @@ inline ChunkPlan shared_plan(int cus, int elem_bytes, int d, int q_heads, int he
     } else {
         pl.own = chunk_pass(CHUNK_OWN, cus, elem_bytes, d, heads, B * G, B, max_own + 31, parts / 2);
         pl.first = chunk_pass(CHUNK_COMMON, cus, elem_bytes, d, heads, B * G, groups, max_shared, parts - pl.own.most_parts);
+        // (one launch for both, if both have few rows)
+        if (pl.first.rows <= 32 && pl.own.rows != pl.first.rows) {
+            const int64_t rows = pl.first.rows > pl.own.rows ? pl.first.rows : pl.own.rows;
+            pl.own = chunk_pass(CHUNK_OWN, cus, elem_bytes, d, heads, B * G, B, max_own + 31, parts / 2, rows);
+            pl.first = chunk_pass(CHUNK_COMMON, cus, elem_bytes, d, heads, B * G, groups, max_shared, parts - pl.own.most_parts, rows);
+        }
         pl.own.part0 = pl.first.most_parts;
         pl.splits = pl.first.most_parts + pl.own.most_parts;
     }
