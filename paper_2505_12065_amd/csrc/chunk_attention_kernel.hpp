@@ -140,17 +140,17 @@ __device__ __forceinline__ f4 not_finite_four(const char *p) {
 
 // Slots of one row of a deal, of token t, the i-th of its sequence
 __device__ __forceinline__ ChunkSpan chunk_row_span(const ChunkArgs &a, int mode, const ChunkDeal &deal, int t, int i) {
-    if (mode == CHUNK_NEW) return chunk_span(a, deal.length, deal.q.tokens - i);
+    if (mode == CHUNK_NEW) return chunk_span(a, deal.k.length, deal.k.q.tokens - i);
     return {deal.range.lo, mode == CHUNK_COMMON ? min(deal.range.hi, chunk_length(a, t)) : deal.range.hi};
 }
 // Four elements of row `in` of a deal: divided and written if the row has no other parts, else left for what joins them.
 template <class T>
 __device__ __forceinline__ void chunk_write(const ChunkArgs &a, const ChunkPass &pass, const ChunkDeal &deal, int head, int in, int at, f4 y, float most, float total) {
     const int G = a.q_heads / a.cache.heads, r = deal.r0 + in;
-    const int64_t row = (int64_t)(deal.q.token0 + r / G) * a.q_heads + head * G + r % G;
+    const int64_t row = (int64_t)(deal.k.q.token0 + r / G) * a.q_heads + head * G + r % G;
     if (a.splits > 1) {
         const int64_t place = row * a.splits + pass.part0 + deal.part;
-        if (at == 0) *reinterpret_cast<f4 *>(a.stats + 4 * place) = f4{most, total, __int_as_float(deal.parts), __int_as_float(deal.grouped)};
+        if (at == 0) *reinterpret_cast<f4 *>(a.stats + 4 * place) = f4{most, total, __int_as_float(deal.parts), __int_as_float(deal.k.grouped)};
         if (!deal.alone) {
             *reinterpret_cast<f4 *>(a.partial + place * a.cache.d + at) = y;
             return;
@@ -187,7 +187,7 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(T::bytes, DP)) v
     const float scale = fmaxf(fabsf(a.scale), 1e-37f);    // (not 0: a score of -infinity stays one)
     const int row0 = wave * 32, row_bytes = a.cache.d * T::bytes;
     {
-        const int in = row0 + m, r = deal.r0 + in, t = deal.q.token0 + r / G;
+        const int in = row0 + m, r = deal.r0 + in, t = deal.k.q.token0 + r / G;
         const bool there = in < deal.count;
         const char *from = static_cast<const char *>(a.q) + t * a.q_row + (head * G + r % G) * a.q_head;
 #pragma unroll
@@ -227,7 +227,7 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(T::bytes, DP)) v
     }
 
     unsigned char *const mine = chunk_lds;
-    const int32_t *table = a.table + (int64_t)deal.q.request * a.width;
+    const int32_t *table = a.table + (int64_t)deal.k.q.request * a.width;
     const int slots_log = a.cache.slots_log, mask = (1 << slots_log) - 1;
     const char *k_head = a.cache.k + head * a.cache.k_head, *v_head = a.cache.v + head * a.cache.v_head;
     // the page of slot k0 + lane % KT, or -1
@@ -509,7 +509,7 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE
     int lo[MT], hi[MT], lo_most = 0, hi_least = INT_MAX;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-        const int in = 16 * mt + m, r = deal.r0 + in, t = deal.q.token0 + r / G;
+        const int in = 16 * mt + m, r = deal.r0 + in, t = deal.k.q.token0 + r / G;
         const bool there = in < deal.count;
         const char *from = static_cast<const char *>(a.q) + t * a.q_row + (head * G + r % G) * a.q_head;
 #pragma unroll
@@ -538,7 +538,7 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE
     lo_most = __builtin_amdgcn_readfirstlane(lo_most);
     hi_least = __builtin_amdgcn_readfirstlane(hi_least);
 
-    const int32_t *table = a.table + (int64_t)deal.q.request * a.width;
+    const int32_t *table = a.table + (int64_t)deal.k.q.request * a.width;
     const int slots_log = a.cache.slots_log, mask = (1 << slots_log) - 1;
     const char *k_head = a.cache.k + head * a.cache.k_head, *v_head = a.cache.v + head * a.cache.v_head;
     auto row_page = [&](int key) {

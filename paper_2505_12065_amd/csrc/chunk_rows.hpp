@@ -7,6 +7,7 @@
 
 #include "launch.hpp"
 #include "packed.hpp"
+#include "paged_attention_kernel.hpp"
 
 namespace ann {
 
@@ -18,22 +19,23 @@ __device__ __forceinline__ int chunk_parts(int slots, int chunk) { return slots 
 
 __device__ __forceinline__ int chunk_length(const ChunkArgs &a, int request) { return max(a.lengths[request], 0); }
 
-// The group of request t, or -1.  By whole waves, whose lanes may ask for different requests.
-__device__ __forceinline__ int chunk_group(const ChunkArgs &a, int t) {
+// The group of request t, or -1, and how many slots it has in common.  By whole waves, whose lanes may ask for different requests.
+struct ChunkGroup { int group, common; };
+__device__ __forceinline__ int chunk_common(const ChunkArgs &a, int g) { return g < 0 ? 0 : min(max(a.shared[g], 0), a.max_shared); }
+__device__ __forceinline__ ChunkGroup chunk_group(const ChunkArgs &a, int t) {
     int n = 0;                                            // starts up to t
     if (a.groups < WAVE) {
-        const int lane = threadIdx.x & (WAVE - 1), start = lane <= a.groups ? packed_start(a.group_starts, lane, a.tokens) : INT_MAX;
+        const int lane = threadIdx.x & (WAVE - 1), start = lane <= a.groups ? packed_start(a.group_starts, lane, a.tokens) : INT_MAX, common = lane < a.groups ? chunk_common(a, lane) : 0;
         for (int g = 0; g <= a.groups; ++g) n += __builtin_amdgcn_readlane(start, g) <= t;
-    } else {
-        for (int left = a.groups + 1; left > 0;) {        // (halves)
-            const int half = left / 2;
-            if (packed_start(a.group_starts, n + half, a.tokens) <= t) { n += half + 1; left -= half + 1; }
-            else left = half;
-        }
+        return n > 0 && n <= a.groups ? ChunkGroup{n - 1, __shfl(common, n - 1)} : ChunkGroup{-1, 0};
     }
-    return n <= a.groups ? n - 1 : -1;
+    for (int left = a.groups + 1; left > 0;) {            // (halves)
+        const int half = left / 2;
+        if (packed_start(a.group_starts, n + half, a.tokens) <= t) { n += half + 1; left -= half + 1; }
+        else left = half;
+    }
+    return n > 0 && n <= a.groups ? ChunkGroup{n - 1, chunk_common(a, n - 1)} : ChunkGroup{-1, 0};
 }
-__device__ __forceinline__ int chunk_common(const ChunkArgs &a, int g) { return g < 0 ? 0 : min(max(a.shared[g], 0), a.max_shared); }
 
 struct ChunkSequence { int token0, tokens, request; };    // request: whose pages are read
 __device__ __forceinline__ int chunk_sequences(const ChunkArgs &a, int mode) { return mode == CHUNK_NEW ? a.requests : mode == CHUNK_COMMON ? a.groups : a.tokens; }
@@ -49,87 +51,109 @@ __device__ __forceinline__ ChunkSpan chunk_span(const ChunkArgs &a, int length, 
     if (slot < 0 || slot >= a.max_length) return {0, 0};
     return {a.window > 0 ? max(slot + 1 - a.window, 0) : 0, slot + 1};
 }
-// ... that tokens t0 to t1 of sequence i, of a request of `length` slots, attend to, all of them together.  By whole waves.
-__device__ __forceinline__ ChunkSpan chunk_range(const ChunkArgs &a, int mode, int i, const ChunkSequence &q, int length, int t0, int t1) {
+// What a wave knows of a sequence: of one, or each lane of another.
+struct ChunkKnown {
+    ChunkSequence q;
+    int length, common;       // slots of q.request, at least 0; of its group in common
+    int grouped;              // q.request is in a group
+};
+__device__ __forceinline__ ChunkKnown chunk_known(const ChunkArgs &a, int mode, int i) {
+    ChunkKnown k{chunk_sequence(a, mode, i), 0, 0, 0};
+    k.length = chunk_length(a, k.q.request);
+    if (mode == CHUNK_COMMON) k.common = chunk_common(a, i);
+    if (mode == CHUNK_OWN) {
+        const ChunkGroup g = chunk_group(a, i);
+        k.common = g.common;
+        k.grouped = g.group >= 0;
+    }
+    return k;
+}
+// Slots that tokens t0 to t1 of a sequence attend to, all of them together.
+__device__ __forceinline__ ChunkSpan chunk_range(const ChunkArgs &a, int mode, const ChunkKnown &k, int t0, int t1) {
     if (mode == CHUNK_NEW) {
-        const int first = length - (q.tokens - t0), last = length - (q.tokens - t1);
+        const int first = k.length - (k.q.tokens - t0), last = k.length - (k.q.tokens - t1);
         return {a.window > 0 ? max(first + 1 - a.window, 0) : 0, min(max(last + 1, 0), a.max_length)};
     }
-    if (mode == CHUNK_COMMON) return {0, chunk_common(a, i)};
-    const int n = min(length, a.max_length), common = min(n, chunk_common(a, chunk_group(a, q.token0)));
+    if (mode == CHUNK_COMMON) return {0, k.common};
+    const int n = min(k.length, a.max_length), common = min(n, k.common);
     return {common, common + min(n - common, a.max_own)};
 }
 
-__device__ __forceinline__ int wave_sum_int(int x) {
-#pragma unroll
-    for (int i = 1; i < WAVE; i *= 2) x += __shfl_xor(x, i);
-    return x;
+// Sums and largest over a wave, without LDS
+__device__ __forceinline__ int wave_sum_of(int x) {
+    x += (int)lane_swap<1>((uint32_t)x);
+    x += (int)lane_swap<2>((uint32_t)x);
+    x += (int)lane_swap<4>((uint32_t)x);
+    x += (int)lane_swap<8>((uint32_t)x);
+    uint32_t a, b;
+    row_pair<16>((uint32_t)x, a, b);
+    x = (int)(a + b);
+    row_pair<32>((uint32_t)x, a, b);
+    return (int)(a + b);
+}
+__device__ __forceinline__ int wave_max_of(int x) {
+    x = max(x, (int)lane_swap<1>((uint32_t)x));
+    x = max(x, (int)lane_swap<2>((uint32_t)x));
+    x = max(x, (int)lane_swap<4>((uint32_t)x));
+    x = max(x, (int)lane_swap<8>((uint32_t)x));
+    uint32_t a, b;
+    row_pair<16>((uint32_t)x, a, b);
+    x = max((int)a, (int)b);
+    row_pair<32>((uint32_t)x, a, b);
+    return max((int)a, (int)b);
 }
 
-// What lane i knows of sequence i, and slots of a part.
-struct ChunkLane { int tiles, slots, chunk; };
-__device__ __forceinline__ ChunkLane chunk_lane(const ChunkArgs &a, const ChunkPass &p, int n, int G) {
-    const int lane = threadIdx.x & (WAVE - 1);
-    ChunkLane l{0, 0, INT_MAX};
-    const int i = min(lane, n - 1);
-    const ChunkSequence q = chunk_sequence(a, p.mode, i);
-    const int64_t rows = (int64_t)q.tokens * G;
-    if (lane < n) l.tiles = (int)((rows + p.rows - 1) / p.rows);
-    // (the last tile has most, but for what a window leaves it)
-    const int t0 = (int)(max(l.tiles - 1, 0) * (int64_t)p.rows / G), t1 = max(q.tokens - 1, 0);
-    const ChunkSpan range = chunk_range(a, p.mode, i, q, chunk_length(a, q.request), t0, t1);
-    if (l.tiles > 0) l.slots = chunk_slots_of(range);
-    if (l.tiles > 0 && p.mode == CHUNK_NEW && a.window > 0) l.slots = (int)max((int64_t)l.slots, min((int64_t)range.hi, (int64_t)a.window + p.rows + 32));
-    if (p.most_parts == 1) return l;
-    const int tiles = wave_sum_int(l.tiles);
-    float slots = (float)l.tiles * (float)l.slots;
-    int most = l.slots;
-#pragma unroll
-    for (int k = 1; k < WAVE; k *= 2) {
-        slots += __shfl_xor(slots, k);
-        most = max(most, __shfl_xor(most, k));
-    }
-    // tiles + slots / chunk workgroups at most: once as many as fill the card, twice if tiles alone make up much of it
-    const int room = (4 * (int64_t)tiles > p.fill ? 2 : 1) * p.fill - tiles;
-    if (room <= 0) return l;
-    const int chunk = max(max((int)min(ceilf(slots / room), 1e9f), p.least), (most - 1) / p.most_parts + 1);
-    l.chunk = (chunk + 63) & ~63;
-    return l;
+// Slots of a part, up to 64 sequences: lane i has so many tiles and slots of sequence i.
+__device__ __forceinline__ int chunk_even(const ChunkPass &p, int tiles, int slots) {
+    if (p.most_parts == 1) return INT_MAX;
+    const int most = __builtin_amdgcn_readfirstlane(wave_max_of(slots)), all_tiles = __builtin_amdgcn_readfirstlane(wave_sum_of(tiles));
+    const float all = wave_sum((float)tiles * (float)slots);
+    // all_tiles + all / chunk workgroups at most: once as many as fill the card, twice if tiles alone make up much of it
+    const int room = (4 * (int64_t)all_tiles > p.fill ? 2 : 1) * p.fill - all_tiles;
+    if (room <= 0) return INT_MAX;
+    const int chunk = max(max((int)min(ceilf(all / (float)room), 1e9f), p.least), (most - 1) / p.most_parts + 1);
+    return __builtin_amdgcn_readfirstlane((chunk + 63) & ~63);
 }
 
 // What a workgroup does: slots first .. end - 1 of the tile that begins with row r0 of a sequence, of whose range they are part `part`; count 0: nothing.
 struct ChunkDeal {
-    ChunkSequence q;
-    int length;               // of q.request, at least 0
+    ChunkKnown k;
     int r0, count, part, parts;
     bool alone;               // nothing is to be joined with it
-    int grouped;              // CHUNK_OWN: the request is in a group
     ChunkSpan range;          // of the tile's rows, all together
     int first, end;
 };
 __device__ __forceinline__ ChunkDeal chunk_deal(const ChunkArgs &a, const ChunkPass &p, int item, int G) {
     const int n = chunk_sequences(a, p.mode), lane = threadIdx.x & (WAVE - 1);
     ChunkDeal d{};
-    int i, chunk;
-    int64_t tile;
+    int chunk;
     if (n <= WAVE) {
-        const ChunkLane l = chunk_lane(a, p, n, G);
-        const int items = l.tiles * chunk_parts(l.slots, l.chunk);
+        const ChunkKnown k = chunk_known(a, p.mode, min(lane, n - 1));
+        const int tiles = lane < n ? (int)(((int64_t)k.q.tokens * G + p.rows - 1) / p.rows) : 0;
+        // (the last tile has most slots, but for what a window leaves it)
+        const ChunkSpan last = chunk_range(a, p.mode, k, (int)(max(tiles - 1, 0) * (int64_t)p.rows / G), max(k.q.tokens - 1, 0));
+        int slots = tiles > 0 ? chunk_slots_of(last) : 0;
+        if (tiles > 0 && p.mode == CHUNK_NEW && a.window > 0) slots = (int)max((int64_t)slots, min((int64_t)last.hi, (int64_t)a.window + p.rows + 32));
+        chunk = chunk_even(p, tiles, slots);
+        const int items = tiles * chunk_parts(slots, chunk);
         int before = 0;                                   // items of longer sequences
-        for (int k = 0; k < n; ++k) {
-            const int other = __builtin_amdgcn_readlane(l.slots, k);
-            before += other > l.slots || (other == l.slots && k < lane) ? __builtin_amdgcn_readlane(items, k) : 0;
+        for (int i = 0; i < n; ++i) {
+            const int other = __builtin_amdgcn_readlane(slots, i);
+            before += other > slots || (other == slots && i < lane) ? __builtin_amdgcn_readlane(items, i) : 0;
         }
         const uint64_t mine = __ballot(item >= before && item < before + items);
         if (mine == 0) return d;
-        i = __ffsll((unsigned long long)mine) - 1;
-        const int local = item - __builtin_amdgcn_readlane(before, i), tiles = __builtin_amdgcn_readlane(l.tiles, i);
-        d.part = local / tiles;
-        tile = tiles - 1 - local % tiles;
-        chunk = l.chunk;
+        const int i = __ffsll((unsigned long long)mine) - 1;
+        auto of = [&](int x) { return __builtin_amdgcn_readlane(x, i); };
+        const int local = item - of(before), its = of(tiles);
+        d.part = local / its;
+        d.r0 = (its - 1 - local % its) * p.rows;
+        d.k = ChunkKnown{{of(k.q.token0), of(k.q.tokens), of(k.q.request)}, of(k.length), of(k.common), of(k.grouped)};
     } else {
         // A sequence of m tokens has at most as many tiles as there are numbers from start G / rows + i up to the next one's.
         const int id = p.tiles - 1 - item % p.tiles;
+        int i;
+        int64_t tile;
         d.part = item / p.tiles;
         chunk = p.chunk;
         if (p.mode == CHUNK_OWN) {
@@ -140,20 +164,19 @@ __device__ __forceinline__ ChunkDeal chunk_deal(const ChunkArgs &a, const ChunkP
         } else {
             const int32_t *starts = p.mode == CHUNK_NEW ? a.starts : a.group_starts;
             auto first = [&](int k) { return (int)((int64_t)packed_start(starts, k, a.tokens) * G / p.rows) + k; };
-            i = count_up_to(first, n + 1, id) - 1;
+            i = __builtin_amdgcn_readfirstlane(count_up_to(first, n + 1, id)) - 1;
             if (i < 0 || i >= n) return d;
             tile = id - first(i);
         }
+        d.r0 = (int)(tile * p.rows);
+        d.k = chunk_known(a, p.mode, i);
+        d.k.common = __builtin_amdgcn_readfirstlane(d.k.common);             // (the same in all lanes, which the compiler cannot know)
+        d.k.grouped = __builtin_amdgcn_readfirstlane(d.k.grouped);
     }
-    d.q = chunk_sequence(a, p.mode, i);
-    d.length = chunk_length(a, d.q.request);
-    d.r0 = (int)(tile * p.rows);
-    const int count = (int)max((int64_t)0, min((int64_t)p.rows, (int64_t)d.q.tokens * G - tile * p.rows));
+    const int count = (int)max((int64_t)0, min((int64_t)p.rows, (int64_t)d.k.q.tokens * G - d.r0));
     if (count == 0) return d;
-    if (p.mode == CHUNK_OWN) d.grouped = chunk_group(a, i) >= 0;
-    d.range = chunk_range(a, p.mode, i, d.q, d.length, d.r0 / G, (d.r0 + count - 1) / G);
-    const int slots = chunk_slots_of(d.range);
-    d.parts = chunk_parts(slots, chunk);
+    d.range = chunk_range(a, p.mode, d.k, d.r0 / G, (d.r0 + count - 1) / G);
+    d.parts = chunk_parts(chunk_slots_of(d.range), chunk);
     if (d.part >= d.parts) return d;
     d.count = count;
     d.alone = p.mode == CHUNK_NEW && d.parts == 1;

@@ -1170,7 +1170,9 @@ inline ChunkPass chunk_pass(int mode, int cus, int elem_bytes, int d, int heads,
     p.tiles = (int)tiles;
     if (sequences <= 64) {
         p.most_parts = (int)parts;
-        p.items = (int)(parts > 1 && tiles < 2 * p.fill + sequences ? 2 * p.fill + sequences : tiles);
+        // (parts that even out to a card's fill, or two, are no more than that and a sequence's last ones)
+        const int64_t even = 2 * p.fill + sequences;
+        p.items = (int)(tiles * parts < even ? tiles * parts : tiles < even ? even : tiles);
     } else {
         const int64_t busy_tiles = (mean + p.rows - 1) / p.rows * sequences, wanted = busy_tiles >= p.fill ? 1 : p.fill / busy_tiles;
         if (parts > wanted) parts = wanted;
