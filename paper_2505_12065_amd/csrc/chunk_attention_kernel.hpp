@@ -143,11 +143,9 @@ __device__ __forceinline__ ChunkSpan chunk_row_span(const ChunkArgs &a, int mode
     if (mode == CHUNK_NEW) return chunk_span(a, deal.k.length, deal.k.q.tokens - i);
     return {deal.range.lo, mode == CHUNK_COMMON ? min(deal.range.hi, chunk_length(a, t)) : deal.range.hi};
 }
-// Four elements of row `in` of a deal: divided and written if the row has no other parts, else left for what joins them.
+// Four elements of a row: divided and written if the row has no other parts, else left for what joins them.
 template <class T>
-__device__ __forceinline__ void chunk_write(const ChunkArgs &a, const ChunkPass &pass, const ChunkDeal &deal, int head, int in, int at, f4 y, float most, float total) {
-    const int G = a.q_heads / a.cache.heads, r = deal.r0 + in;
-    const int64_t row = (int64_t)(deal.k.q.token0 + r / G) * a.q_heads + head * G + r % G;
+__device__ __forceinline__ void chunk_write(const ChunkArgs &a, const ChunkPass &pass, const ChunkDeal &deal, int64_t row, int at, f4 y, float most, float total) {
     if (a.splits > 1) {
         const int64_t place = row * a.splits + pass.part0 + deal.part;
         if (at == 0) *reinterpret_cast<f4 *>(a.stats + 4 * place) = f4{most, total, __int_as_float(deal.parts), __int_as_float(deal.k.grouped)};
@@ -161,6 +159,11 @@ __device__ __forceinline__ void chunk_write(const ChunkArgs &a, const ChunkPass 
     for (int i = 0; i < 4; ++i) y[i] = total == 0.f ? 0.f : y[i] * by;
     store_four<T>(static_cast<char *>(a.out) + (row * a.cache.d + at) * T::bytes, y);
     if (at == 0 && a.lse) a.lse[row] = chunk_lse(most, total, a.lift);
+}
+// Row `in` of a deal, among those of all tokens.
+__device__ __forceinline__ int64_t chunk_row(const ChunkArgs &a, const ChunkDeal &deal, int head, int G, int in) {
+    const int r = deal.r0 + in;
+    return (int64_t)(deal.k.q.token0 + r / G) * a.q_heads + head * G + r % G;
 }
 
 // ---- 128 rows -------------------------------------------------------------------------------------------------
@@ -473,12 +476,13 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(T::bytes, DP)) v
     }
     const int in = row0 + m;
     if (in < deal.count) {
+        const int64_t row = chunk_row(a, deal, head, G, in);
 #pragma unroll
         for (int c = 0; c < NC; ++c)
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
                 const int at = 32 * c + 2 * i + 4 * h;
-                if (at < a.cache.d) chunk_write<T>(a, pass, deal, head, in, at, f4{o[c][i], o[c][i + 1], o[c][i + 2], o[c][i + 3]}, top, sum);
+                if (at < a.cache.d) chunk_write<T>(a, pass, deal, row, at, f4{o[c][i], o[c][i + 1], o[c][i + 2], o[c][i + 3]}, top, sum);
             }
     }
 }
@@ -793,7 +797,7 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE
             total += s_sum[w * ROWS + in] * (t == -INFINITY ? 1.f : exp2_fast(t - most));
         }
         for (int w = 0; w < used; ++w) y += *reinterpret_cast<const f4 *>(s_o + (w * deal.count + in) * LD + at);
-        chunk_write<T>(a, pass, deal, head, in, at, y, most, total);
+        chunk_write<T>(a, pass, deal, chunk_row(a, deal, head, G, in), at, y, most, total);
     }
 }
 

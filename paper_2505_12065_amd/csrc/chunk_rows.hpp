@@ -103,16 +103,26 @@ __device__ __forceinline__ int wave_max_of(int x) {
     return max((int)a, (int)b);
 }
 
-// Slots of a part, up to 64 sequences: lane i has so many tiles and slots of sequence i.
+// Slots of a part, up to 64 sequences: lane i has so many tiles and slots of sequence i.  The fewest, in whole tiles of 64, with which no more workgroups have something to do than fill the card,
+// once, or twice if tiles of many rows alone make up much of it.
 __device__ __forceinline__ int chunk_even(const ChunkPass &p, int tiles, int slots) {
     if (p.most_parts == 1) return INT_MAX;
     const int most = __builtin_amdgcn_readfirstlane(wave_max_of(slots)), all_tiles = __builtin_amdgcn_readfirstlane(wave_sum_of(tiles));
+    const int64_t limit = (p.rows == CHUNK_TILE && 4 * (int64_t)all_tiles > p.fill ? 2 : 1) * (int64_t)p.fill;
+    if (most <= p.whole && all_tiles >= p.fill / 4) return INT_MAX;
+    if (limit <= all_tiles) return INT_MAX;
     const float all = wave_sum((float)tiles * (float)slots);
-    // all_tiles + all / chunk workgroups at most: once as many as fill the card, twice if tiles alone make up much of it
-    const int room = (4 * (int64_t)all_tiles > p.fill ? 2 : 1) * p.fill - all_tiles;
-    if (room <= 0) return INT_MAX;
-    const int chunk = max(max((int)min(ceilf(all / (float)room), 1e9f), p.least), (most - 1) / p.most_parts + 1);
-    return __builtin_amdgcn_readfirstlane((chunk + 63) & ~63);
+    // in units of 64 slots: `few` are too few or just enough, `enough` are not too few
+    const int least = (max(p.least, (most - 1) / p.most_parts + 1) + 63) / 64;
+    int few = max((int)min(all / (64.f * (float)limit), 1e7f), least), enough = max((int)min(all / (64.f * (float)(limit - all_tiles)), 1e7f) + 1, least);
+    while (few < enough) {
+        const int half = (few + enough) / 2;
+        if (wave_sum_of(tiles * chunk_parts(slots, 64 * half)) <= limit) enough = half;
+        else few = half + 1;
+        few = __builtin_amdgcn_readfirstlane(few);
+        enough = __builtin_amdgcn_readfirstlane(enough);
+    }
+    return 64 * enough;
 }
 
 // What a workgroup does: slots first .. end - 1 of the tile that begins with row r0 of a sequence, of whose range they are part `part`; count 0: nothing.
@@ -136,11 +146,10 @@ __device__ __forceinline__ ChunkDeal chunk_deal(const ChunkArgs &a, const ChunkP
         if (tiles > 0 && p.mode == CHUNK_NEW && a.window > 0) slots = (int)max((int64_t)slots, min((int64_t)last.hi, (int64_t)a.window + p.rows + 32));
         chunk = chunk_even(p, tiles, slots);
         const int items = tiles * chunk_parts(slots, chunk);
-        int before = 0;                                   // items of longer sequences
-        for (int i = 0; i < n; ++i) {
-            const int other = __builtin_amdgcn_readlane(slots, i);
-            before += other > slots || (other == slots && i < lane) ? __builtin_amdgcn_readlane(items, i) : 0;
-        }
+        // items of longer sequences (of two as long, the first's)
+        const uint32_t key = (uint32_t)min(slots, (1 << 26) - 1) << 6 | (WAVE - 1 - lane);
+        int before = 0;
+        for (int i = 0; i < n; ++i) before += (uint32_t)__builtin_amdgcn_readlane((int)key, i) > key ? __builtin_amdgcn_readlane(items, i) : 0;
         const uint64_t mine = __ballot(item >= before && item < before + items);
         if (mine == 0) return d;
         const int i = __ffsll((unsigned long long)mine) - 1;

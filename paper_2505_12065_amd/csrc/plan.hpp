@@ -1141,6 +1141,7 @@ struct ChunkPass {
     int items = 0;               // tiles and parts of a cache head that there may be
     int fill = 1;                // workgroups of a cache head that fill the card
     int most_parts = 1, least = 64, part0 = 0;            // parts of a row at most; slots of a part at least; number of a row's first part
+    int whole = 0;               // ranges of up to so many slots are not divided if there is a tile for every compute unit
     int tiles = 0, chunk = 0;    // of more than 64 sequences: tiles that there may be, slots of a part
 };
 struct ChunkPlan {
@@ -1148,18 +1149,25 @@ struct ChunkPlan {
     int splits = 1;
     size_t bytes = 0;            // of workspace
 };
+#ifndef CHUNK_SMALL
+#define CHUNK_SMALL 1.0e9
+#endif
+#ifndef CHUNK_LEAST
+#define CHUNK_LEAST 256
+#endif
 constexpr int64_t CHUNK_PARTS = 64;                       // of a row in a pass
 // Sequences of `rows` rows in all, whose tiles go through `range` slots at most.
-inline ChunkPass chunk_pass(int mode, int cus, int elem_bytes, int d, int heads, int64_t rows, int64_t sequences, int64_t range, int64_t most_parts, int64_t least_rows = 1) {
+inline ChunkPass chunk_pass(int mode, int cus, int elem_bytes, int d, int heads, int64_t rows, int64_t sequences, int64_t range, int64_t most_parts, int64_t least_rows = 1, bool small = false) {
     ChunkPass p;
     const int ve = attend_ve(d);
     const int64_t mean = (rows + sequences - 1) / sequences;
-    const bool few = mode == CHUNK_OWN || mean <= 32;
+    const bool few = mode == CHUNK_OWN || mean <= 32 || small;
     p.mode = mode;
     p.rows = few ? chunk_few_rows(elem_bytes, ve, mean > least_rows ? mean : least_rows) : CHUNK_TILE;
     p.fill = (few ? 4 : chunk_per_simd(elem_bytes, 16 * ve)) * cus / heads;
     if (p.fill < 1) p.fill = 1;
-    p.least = few ? (int)(2 * attend_step(elem_bytes, d)) : elem_bytes == 4 ? 64 : 256;
+    p.least = few ? (int)attend_step(elem_bytes, d) : elem_bytes == 4 ? 64 : CHUNK_LEAST;
+    p.whole = few ? 1024 : 0;
     const int64_t tiles = mode == CHUNK_OWN ? sequences * ((rows / sequences + p.rows - 1) / p.rows) : rows / p.rows + sequences;
     // nothing is divided where tiles alone keep most of the card busy
     const int64_t busy = few ? sequences : rows / p.rows;
@@ -1204,12 +1212,13 @@ inline ChunkPlan shared_plan(int cus, int elem_bytes, int d, int q_heads, int he
         pl.splits = pl.first.most_parts;
     } else {
         pl.own = chunk_pass(CHUNK_OWN, cus, elem_bytes, d, heads, B * G, B, max_own + 31, parts / 2);
-        pl.first = chunk_pass(CHUNK_COMMON, cus, elem_bytes, d, heads, B * G, groups, max_shared, parts - pl.own.most_parts);
+        const bool small = 4.0 * B * q_heads * (double)max_shared * d <= CHUNK_SMALL;
+        pl.first = chunk_pass(CHUNK_COMMON, cus, elem_bytes, d, heads, B * G, groups, max_shared, parts - pl.own.most_parts, 1, small);
         // (one launch for both, if both have few rows)
         if (pl.first.rows <= 32 && pl.own.rows != pl.first.rows) {
             const int64_t rows = pl.first.rows > pl.own.rows ? pl.first.rows : pl.own.rows;
             pl.own = chunk_pass(CHUNK_OWN, cus, elem_bytes, d, heads, B * G, B, max_own + 31, parts / 2, rows);
-            pl.first = chunk_pass(CHUNK_COMMON, cus, elem_bytes, d, heads, B * G, groups, max_shared, parts - pl.own.most_parts, rows);
+            pl.first = chunk_pass(CHUNK_COMMON, cus, elem_bytes, d, heads, B * G, groups, max_shared, parts - pl.own.most_parts, rows, small);
         }
         pl.own.part0 = pl.first.most_parts;
         pl.splits = pl.first.most_parts + pl.own.most_parts;
