@@ -474,16 +474,32 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(T::bytes, DP)) v
         sum = __uint_as_float(b0) + __uint_as_float(b1);
         top *= scale;                                     // an exponent of 2
     }
-    const int in = row0 + m;
-    if (in < deal.count) {
-        const int64_t row = chunk_row(a, deal, head, G, in);
+    // Written by way of LDS, 32 elements of all the wave's rows at a time, so that eight lanes write 128 bytes of a row.
+    constexpr int LD = 36, PER = WAVE / 8;
+    float *turn = reinterpret_cast<float *>(chunk_lds) + wave * 32 * LD;
+    int64_t rows[32 / PER];
+    float tops[32 / PER], sums[32 / PER];
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
+    for (int k = 0; k < 32 / PER; ++k) {
+        const int in = k * PER + lane / 8;
+        rows[k] = chunk_row(a, deal, head, G, min(row0 + in, deal.count - 1));
+        tops[k] = __shfl(top, in);
+        sums[k] = __shfl(sum, in);
+    }
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const int at = 32 * c + 2 * i + 4 * h;
-                if (at < a.cache.d) chunk_write<T>(a, pass, deal, row, at, f4{o[c][i], o[c][i + 1], o[c][i + 2], o[c][i + 3]}, top, sum);
-            }
+    for (int c = 0; c < NC; ++c) {
+        if (32 * c >= a.cache.d) break;
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) *reinterpret_cast<f4 *>(turn + m * LD + 2 * i + 4 * h) = f4{o[c][i], o[c][i + 1], o[c][i + 2], o[c][i + 3]};
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");              // (what the wave itself wrote)
+        const int at = 32 * c + lane % 8 * 4;
+#pragma unroll
+        for (int k = 0; k < 32 / PER; ++k) {
+            const int in = k * PER + lane / 8;
+            const f4 y = *reinterpret_cast<const f4 *>(turn + in * LD + lane % 8 * 4);
+            if (row0 + in < deal.count && at < a.cache.d) chunk_write<T>(a, pass, deal, rows[k], at, y, tops[k], sums[k]);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }
 
@@ -567,7 +583,7 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE
         }
     };
     auto load_k = [&](int k0, const Pages &pg) __attribute__((always_inline)) {
-        auto load = [&](auto whole) __attribute__((always_inline)) {
+        auto load = [&](auto whole, auto once) __attribute__((always_inline)) {
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 const int p = max(pg.k[t], 0);
@@ -575,13 +591,14 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE
 #pragma unroll
                 for (int s = 0; s < NS; ++s) {
                     const int at = (4 * s + g) * 16;
-                    if (decltype(whole)::value || at < row_bytes) kr[t][s] = load_chunk(row + at);
+                    if (decltype(whole)::value || at < row_bytes) kr[t][s] = stream_load<decltype(once)::value>(reinterpret_cast<const u4 *>(row + at));
                     else kr[t][s] = zero_chunk();
                 }
             }
         };
-        if (full) load(std::true_type{});
-        else load(std::false_type{});
+        if (full && pass.once) load(std::true_type{}, std::true_type{});
+        else if (full) load(std::true_type{}, std::false_type{});
+        else load(std::false_type{}, std::false_type{});
     };
 
     f4 o[MT][VE];
@@ -603,7 +620,7 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE
         const bool more = k0 + STEP < end;
         if (more) pages_of(k0 + STEP, page_next);
         VChunk vr[NT][4][NU];
-        auto load_v = [&](auto whole) __attribute__((always_inline)) {
+        auto load_v = [&](auto whole, auto once) __attribute__((always_inline)) {
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -613,13 +630,14 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE
 #pragma unroll
                     for (int u = 0; u < NU; ++u) {
                         const int at = (u * 16 + m) * CE;
-                        if (decltype(whole)::value || at < a.cache.d) vr[t][i][u] = *reinterpret_cast<const VChunk *>(row + at * T::bytes);
+                        if (decltype(whole)::value || at < a.cache.d) vr[t][i][u] = stream_load<decltype(once)::value>(reinterpret_cast<const VChunk *>(row + at * T::bytes));
                         else vr[t][i][u] = VChunk(0);
                     }
                 }
         };
-        if (full) load_v(std::true_type{});
-        else load_v(std::false_type{});
+        if (full && pass.once) load_v(std::true_type{}, std::true_type{});
+        else if (full) load_v(std::true_type{}, std::false_type{});
+        else load_v(std::false_type{}, std::false_type{});
         if constexpr (Q_LDS) asm volatile("" ::: "memory");                 // (the queries stay where they are)
         f4 x[MT][NT];
 #pragma unroll

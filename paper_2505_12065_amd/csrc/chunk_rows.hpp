@@ -137,7 +137,7 @@ __device__ __forceinline__ ChunkDeal chunk_deal(const ChunkArgs &a, const ChunkP
     const int n = chunk_sequences(a, p.mode), lane = threadIdx.x & (WAVE - 1);
     ChunkDeal d{};
     int chunk;
-    if (n <= WAVE) {
+    if (n <= WAVE && !(p.mode == CHUNK_OWN && p.most_parts == 1)) {         // (own slots that are not divided: all have as many items)
         const ChunkKnown k = chunk_known(a, p.mode, min(lane, n - 1));
         const int tiles = lane < n ? (int)(((int64_t)k.q.tokens * G + p.rows - 1) / p.rows) : 0;
         // (the last tile has most slots, but for what a window leaves it)

@@ -1141,8 +1141,9 @@ struct ChunkPass {
     int items = 0;               // tiles and parts of a cache head that there may be
     int fill = 1;                // workgroups of a cache head that fill the card
     int most_parts = 1, least = 64, part0 = 0;            // parts of a row at most; slots of a part at least; number of a row's first part
+    bool once = false;           // keys and values are read once, and may be more than the last cache holds
     int whole = 0;               // ranges of up to so many slots are not divided if there is a tile for every compute unit
-    int tiles = 0, chunk = 0;    // of more than 64 sequences: tiles that there may be, slots of a part
+    int tiles = 0, chunk = 0;    // tiles that there may be; slots of a part, of more than 64 sequences
 };
 struct ChunkPlan {
     ChunkPass first, own;        // new tokens or slots in common; own slots
@@ -1157,13 +1158,14 @@ struct ChunkPlan {
 #endif
 constexpr int64_t CHUNK_PARTS = 64;                       // of a row in a pass
 // Sequences of `rows` rows in all, whose tiles go through `range` slots at most.
-inline ChunkPass chunk_pass(int mode, int cus, int elem_bytes, int d, int heads, int64_t rows, int64_t sequences, int64_t range, int64_t most_parts, int64_t least_rows = 1, bool small = false) {
+inline ChunkPass chunk_pass(int mode, int cus, int elem_bytes, int d, int heads, int64_t rows, int64_t sequences, int64_t range, int64_t most_parts, bool small = false,
+                            int few_rows = 0) {
     ChunkPass p;
     const int ve = attend_ve(d);
     const int64_t mean = (rows + sequences - 1) / sequences;
     const bool few = mode == CHUNK_OWN || mean <= 32 || small;
     p.mode = mode;
-    p.rows = few ? chunk_few_rows(elem_bytes, ve, mean > least_rows ? mean : least_rows) : CHUNK_TILE;
+    p.rows = !few ? CHUNK_TILE : few_rows ? few_rows : chunk_few_rows(elem_bytes, ve, mean);
     p.fill = (few ? 4 : chunk_per_simd(elem_bytes, 16 * ve)) * cus / heads;
     if (p.fill < 1) p.fill = 1;
     p.least = few ? (int)attend_step(elem_bytes, d) : elem_bytes == 4 ? 64 : CHUNK_LEAST;
@@ -1174,12 +1176,13 @@ inline ChunkPass chunk_pass(int mode, int cus, int elem_bytes, int d, int heads,
     int64_t parts = (range + p.least - 1) / p.least;
     if (parts > most_parts) parts = most_parts;
     if (parts > CHUNK_PARTS) parts = CHUNK_PARTS;
-    if (4 * busy >= 3 * p.fill || parts < 1) parts = 1;
+    if (4 * busy >= 3 * p.fill || (sequences * heads >= cus && range <= p.whole + 31) || parts < 1) parts = 1;
     p.tiles = (int)tiles;
+    p.once = mode == CHUNK_OWN && 2.0 * range * sequences * heads * d * elem_bytes > ATTEND_CACHED;
     if (sequences <= 64) {
         p.most_parts = (int)parts;
-        // (parts that even out to a card's fill, or two, are no more than that and a sequence's last ones)
-        const int64_t even = 2 * p.fill + sequences;
+        p.chunk = INT_MAX;
+        const int64_t even = few ? p.fill : 2 * p.fill;
         p.items = (int)(tiles * parts < even ? tiles * parts : tiles < even ? even : tiles);
     } else {
         const int64_t busy_tiles = (mean + p.rows - 1) / p.rows * sequences, wanted = busy_tiles >= p.fill ? 1 : p.fill / busy_tiles;
@@ -1213,13 +1216,8 @@ inline ChunkPlan shared_plan(int cus, int elem_bytes, int d, int q_heads, int he
     } else {
         pl.own = chunk_pass(CHUNK_OWN, cus, elem_bytes, d, heads, B * G, B, max_own + 31, parts / 2);
         const bool small = 4.0 * B * q_heads * (double)max_shared * d <= CHUNK_SMALL;
-        pl.first = chunk_pass(CHUNK_COMMON, cus, elem_bytes, d, heads, B * G, groups, max_shared, parts - pl.own.most_parts, 1, small);
-        // (one launch for both, if both have few rows)
-        if (pl.first.rows <= 32 && pl.own.rows != pl.first.rows) {
-            const int64_t rows = pl.first.rows > pl.own.rows ? pl.first.rows : pl.own.rows;
-            pl.own = chunk_pass(CHUNK_OWN, cus, elem_bytes, d, heads, B * G, B, max_own + 31, parts / 2, rows);
-            pl.first = chunk_pass(CHUNK_COMMON, cus, elem_bytes, d, heads, B * G, groups, max_shared, parts - pl.own.most_parts, rows, small);
-        }
+        // (one launch for both where there are few rows in common, or little work: tiles of as many rows)
+        pl.first = chunk_pass(CHUNK_COMMON, cus, elem_bytes, d, heads, B * G, groups, max_shared, parts - pl.own.most_parts, small, pl.own.rows);
         pl.own.part0 = pl.first.most_parts;
         pl.splits = pl.first.most_parts + pl.own.most_parts;
     }
