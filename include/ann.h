@@ -505,7 +505,7 @@ int ann_rotate_append(const void *qkv, int64_t token_stride, int64_t head_stride
  *   out         device [T, q_heads, d], contiguous;  lse  device float [T, q_heads], or NULL
  * Values that a token does not attend to do not matter to it, NaN and infinities among them; a value that is one of these and has a weight gives one.  Same inputs and workspace give bitwise-same
  * outputs.  Where there are few tokens, contexts are divided into parts that are joined in the workspace of the current device; with less than the size below they are divided
- * less, or not at all.  q_heads at most 8192, T q_heads 2^26, T 2^22, B 65536, width slots 2^31 - 65537.  T = 0 returns ANN_OK at once. */
+ * less, or not at all.  q_heads at most 8192, T q_heads 2^26, T and B heads 2^22, B 65536, width slots 2^31 - 65537.  T = 0 returns ANN_OK at once. */
 int ann_chunk_attention(const void *q, int64_t q_row, int64_t q_head, int32_t T, int32_t q_heads, const int32_t *starts, int32_t B,
                         const ann_paged_cache *cache, const int32_t *page_table, int32_t width,
                         const int32_t *lengths, int32_t max_length, float scale, int32_t window,
@@ -523,7 +523,7 @@ int64_t ann_chunk_attention_workspace_bytes(int32_t T, int32_t B, int32_t q_head
  *   max_shared, max_own  what the work is divided by: the largest numbers of shared and of own slots, or bounds as close as the host knows.  0 <= max_shared <= width slots, 1 <= max_own <= width slots
  * 16-bit types: weights are rounded to the type for the product with V, as in ann_chunk_attention.  Otherwise, and for q, page_table, out and lse, as in ann_paged_attention.
  * Same inputs and workspace give bitwise-same outputs.  Uses the workspace of the current device; with less than the size below
- * nothing is shared.  groups in [1, 65536], B at most 65536, q_heads 8192, B q_heads 2^22, width slots 2^31 - 65537.  B = 0 returns ANN_OK at once. */
+ * nothing is shared.  groups in [1, 65536], B at most 65536, q_heads 8192, B q_heads and groups heads 2^22, width slots 2^31 - 65537.  B = 0 returns ANN_OK at once. */
 int ann_shared_attention(const void *q, int64_t q_row, int64_t q_head, int32_t B, int32_t q_heads,
                          const ann_paged_cache *cache, const int32_t *page_table, int32_t width, const int32_t *lengths,
                          const int32_t *group_starts, const int32_t *shared, int32_t groups, int32_t max_shared, int32_t max_own, float scale,

@@ -320,24 +320,19 @@ int units_of_device() {
 
 // Launches an attention by the plan that `plan` makes for the bytes that are there.
 template <class Plan>
-int run_attention(ChunkArgs a, int dtype, Plan &&plan, hipStream_t stream) {
+int run_attention(ChunkArgs a, int dtype, size_t most, Plan &&plan, hipStream_t stream) {
     std::lock_guard<std::mutex> lock(g_mu);
     DeviceState *st = nullptr;
     if (int rc = device_state(&st)) return rc;
-    ChunkPlan pl = plan(st->cus, CHUNK_WS_MAX);
+    ChunkPlan pl = plan(st->cus, most);
     // a buffer that a caller gave, or that a graph may not let grow, takes fewer parts
     if (pl.bytes && !at_hand(st, st->ws, pl.bytes, stream)) pl = plan(st->cus, st->user_ws ? st->user_bytes : st->ws.bytes);
-    if (((int64_t)pl.first.items + pl.own.items) * a.cache.heads > CHUNK_GRID) return fail(ANN_ERR_INVALID, "%d tokens of %d heads and %d requests are too many for a call", a.tokens, a.q_heads, a.requests);
     void *ws = nullptr;
     if (pl.bytes)
         if (int rc = workspace_for(st, &st->ws, pl.bytes, stream, &ws)) return rc;
     a.splits = pl.splits;
     a.partial = static_cast<float *>(ws);
     a.stats = a.partial + (size_t)a.tokens * a.q_heads * pl.splits * a.cache.d;
-    if (pl.first.mode == CHUNK_OWN) {                     // (the slots in common are everyone's own)
-        a.max_own = (int)((int64_t)a.max_shared + a.max_own < INT_MAX ? a.max_shared + a.max_own : INT_MAX);
-        a.max_shared = 0;
-    }
     return check_launch("chunk_attention_kernel", (dtype == ANN_F16 ? launch_chunk_attention_f16 : dtype == ANN_BF16 ? launch_chunk_attention_bf16
                                                    : launch_chunk_attention_f32)(a, pl, stream));
 }
@@ -611,7 +606,7 @@ static int check_attention(const void *q, int64_t q_row, int64_t q_head, int32_t
 int64_t ann_chunk_attention_workspace_bytes(int32_t T, int32_t B, int32_t q_heads, int32_t heads, int32_t d, int32_t dtype, int32_t max_length, int32_t window) {
     if (T < 1 || T > GRID_MAX || B < 1 || B > 65536 || heads < 1 || q_heads < heads || q_heads > 8192 || q_heads % heads || d < 8 || d > ANN_HEAD_MAX || max_length < 1 || window < 0)
         return ANN_ERR_INVALID;
-    if (check_dtype(dtype) != ANN_OK || (int64_t)T * q_heads > CHUNK_ROWS_MAX) return ANN_ERR_INVALID;
+    if (check_dtype(dtype) != ANN_OK || (int64_t)T * q_heads > CHUNK_ROWS_MAX || (int64_t)B * heads > GRID_MAX) return ANN_ERR_INVALID;
     return (int64_t)chunk_plan(units_of_device(), elem_bytes(dtype), d, q_heads, heads, T, B, max_length, window, CHUNK_WS_MAX).bytes;
 }
 
@@ -625,12 +620,12 @@ int ann_chunk_attention(const void *q, int64_t q_row, int64_t q_head, int32_t T,
     if (!starts) return fail(ANN_ERR_INVALID, "null pointer argument");
     if (off4({starts})) return fail(ANN_ERR_ALIGNMENT, "starts must be 4-byte aligned");
     if (T < 1 || T > GRID_MAX || (int64_t)T * q_heads > CHUNK_ROWS_MAX) return fail(ANN_ERR_INVALID, "%d tokens of %d heads are out of range", T, q_heads);
-    if (B < 1 || B > 65536) return fail(ANN_ERR_INVALID, "B = %d out of range [1, 65536]", B);
+    if (B < 1 || B > 65536 || (int64_t)B * cache->heads > GRID_MAX) return fail(ANN_ERR_INVALID, "B = %d out of range [1, 65536], or of too many heads", B);
     if (max_length < 1 || max_length > width * cache->slots) return fail(ANN_ERR_INVALID, "max_length = %d out of range [1, width slots]", max_length);
     if (window < 0) return fail(ANN_ERR_INVALID, "window = %d out of range", window);
     a.tokens = T; a.starts = starts; a.requests = B; a.max_length = max_length; a.window = window; a.out = out; a.lse = lse;
     a.lift = chunk_lift(cache->dtype, max_length);
-    return run_attention(a, cache->dtype, [&](int cus, size_t most) {
+    return run_attention(a, cache->dtype, CHUNK_WS_MAX, [&](int cus, size_t most) {
         return chunk_plan(cus, elem_bytes(cache->dtype), cache->d, q_heads, cache->heads, T, B, max_length, window, most);
     }, static_cast<hipStream_t>(stream));
 }
@@ -638,8 +633,8 @@ int ann_chunk_attention(const void *q, int64_t q_row, int64_t q_head, int32_t T,
 int64_t ann_shared_attention_workspace_bytes(int32_t B, int32_t groups, int32_t q_heads, int32_t heads, int32_t d, int32_t dtype, int32_t max_shared, int32_t max_own) {
     if (B < 1 || B > 65536 || groups < 1 || groups > 65536 || heads < 1 || q_heads < heads || q_heads > 8192 || q_heads % heads || d < 8 || d > ANN_HEAD_MAX || max_shared < 0 || max_own < 1)
         return ANN_ERR_INVALID;
-    if (check_dtype(dtype) != ANN_OK || (int64_t)B * q_heads > GRID_MAX) return ANN_ERR_INVALID;
-    return (int64_t)shared_plan(units_of_device(), elem_bytes(dtype), d, q_heads, heads, B, groups, max_shared, max_own, CHUNK_WS_MAX).bytes;
+    if (check_dtype(dtype) != ANN_OK || (int64_t)B * q_heads > GRID_MAX || (int64_t)groups * heads > GRID_MAX) return ANN_ERR_INVALID;
+    return (int64_t)shared_plan(units_of_device(), elem_bytes(dtype), d, q_heads, heads, B, groups, max_shared, max_own, shared_most(B, q_heads, d)).bytes;
 }
 
 int ann_shared_attention(const void *q, int64_t q_row, int64_t q_head, int32_t B, int32_t q_heads,
@@ -652,14 +647,15 @@ int ann_shared_attention(const void *q, int64_t q_row, int64_t q_head, int32_t B
     if (null_in({group_starts, shared})) return fail(ANN_ERR_INVALID, "null pointer argument");
     if (off4({group_starts, shared})) return fail(ANN_ERR_ALIGNMENT, "group_starts and shared must be 4-byte aligned");
     if (B < 1 || B > 65536 || groups < 1 || groups > 65536) return fail(ANN_ERR_INVALID, "B = %d or groups = %d out of range [1, 65536]", B, groups);
-    if ((int64_t)B * q_heads > GRID_MAX) return fail(ANN_ERR_INVALID, "%d requests of %d heads are too many for a call", B, q_heads);
+    if ((int64_t)B * q_heads > GRID_MAX || (int64_t)groups * cache->heads > GRID_MAX)
+        return fail(ANN_ERR_INVALID, "%d requests in %d groups, of %d heads, are too many for a call", B, groups, q_heads);
     const int32_t most = width * cache->slots;
     if (max_shared < 0 || max_shared > most || max_own < 1 || max_own > most)
         return fail(ANN_ERR_INVALID, "max_shared = %d or max_own = %d out of range", max_shared, max_own);
     a.tokens = a.requests = B; a.max_length = most; a.out = out; a.lse = lse;
     a.group_starts = group_starts; a.shared = shared; a.groups = groups; a.max_shared = max_shared; a.max_own = max_own;
     a.lift = chunk_lift(cache->dtype, most);
-    return run_attention(a, cache->dtype, [&](int cus, size_t there) {
+    return run_attention(a, cache->dtype, shared_most(B, q_heads, cache->d), [&](int cus, size_t there) {
         return shared_plan(cus, elem_bytes(cache->dtype), cache->d, q_heads, cache->heads, B, groups, max_shared, max_own, there);
     }, static_cast<hipStream_t>(stream));
 }

@@ -1,7 +1,7 @@
 // Attention of many rows: which rows and slots a workgroup takes.
 //
 // A pass goes through tiles of `rows` rows of sequences of tokens: a request's new ones (CHUNK_NEW), the one of each request of a group (CHUNK_COMMON: the slots in common), or a
-// request's one (CHUNK_OWN: its own slots).  A token has a row for each of the G query heads of a cache head.  Long ranges of slots are divided into parts.  How many tiles and slots there are is known on the
+// request's one (CHUNK_OWN: its own slots; CHUNK_ALL: those in common too).  A token has a row for each of the G query heads of a cache head.  Long ranges of slots are divided into parts.  How many tiles and slots there are is known on the
 // device alone; up to 64 sequences, a lane each, every workgroup works out for itself how the whole is dealt: parts as long as fill the card, longest sequences first.
 #pragma once
 
@@ -40,7 +40,7 @@ __device__ __forceinline__ ChunkGroup chunk_group(const ChunkArgs &a, int t) {
 struct ChunkSequence { int token0, tokens, request; };    // request: whose pages are read
 __device__ __forceinline__ int chunk_sequences(const ChunkArgs &a, int mode) { return mode == CHUNK_NEW ? a.requests : mode == CHUNK_COMMON ? a.groups : a.tokens; }
 __device__ __forceinline__ ChunkSequence chunk_sequence(const ChunkArgs &a, int mode, int i) {
-    if (mode == CHUNK_OWN) return {i, 1, i};
+    if (mode >= CHUNK_OWN) return {i, 1, i};
     const int32_t *starts = mode == CHUNK_NEW ? a.starts : a.group_starts;
     const int s0 = packed_start(starts, i, a.tokens), s1 = packed_start(starts, i + 1, a.tokens);
     return {s0, max(s1 - s0, 0), mode == CHUNK_NEW ? i : min(s0, a.tokens - 1)};
@@ -61,7 +61,7 @@ __device__ __forceinline__ ChunkKnown chunk_known(const ChunkArgs &a, int mode, 
     ChunkKnown k{chunk_sequence(a, mode, i), 0, 0, 0};
     k.length = chunk_length(a, k.q.request);
     if (mode == CHUNK_COMMON) k.common = chunk_common(a, i);
-    if (mode == CHUNK_OWN) {
+    if (mode >= CHUNK_OWN) {
         const ChunkGroup g = chunk_group(a, i);
         k.common = g.common;
         k.grouped = g.group >= 0;
@@ -76,7 +76,7 @@ __device__ __forceinline__ ChunkSpan chunk_range(const ChunkArgs &a, int mode, c
     }
     if (mode == CHUNK_COMMON) return {0, k.common};
     const int n = min(k.length, a.max_length), common = min(n, k.common);
-    return {common, common + min(n - common, a.max_own)};
+    return {mode == CHUNK_ALL ? 0 : common, common + min(n - common, a.max_own)};
 }
 
 // Sums and largest over a wave, without LDS
@@ -137,7 +137,7 @@ __device__ __forceinline__ ChunkDeal chunk_deal(const ChunkArgs &a, const ChunkP
     const int n = chunk_sequences(a, p.mode), lane = threadIdx.x & (WAVE - 1);
     ChunkDeal d{};
     int chunk;
-    if (n <= WAVE && !(p.mode == CHUNK_OWN && p.most_parts == 1)) {         // (own slots that are not divided: all have as many items)
+    if (n <= WAVE && !(p.mode >= CHUNK_OWN && p.most_parts == 1)) {         // (own slots that are not divided: all have as many items)
         const ChunkKnown k = chunk_known(a, p.mode, min(lane, n - 1));
         const int tiles = lane < n ? (int)(((int64_t)k.q.tokens * G + p.rows - 1) / p.rows) : 0;
         // (the last tile has most slots, but for what a window leaves it)
@@ -165,7 +165,7 @@ __device__ __forceinline__ ChunkDeal chunk_deal(const ChunkArgs &a, const ChunkP
         int64_t tile;
         d.part = item / p.tiles;
         chunk = p.chunk;
-        if (p.mode == CHUNK_OWN) {
+        if (p.mode >= CHUNK_OWN) {
             const int per = (G + p.rows - 1) / p.rows;
             i = id / per;
             tile = id % per;

@@ -1124,7 +1124,7 @@ inline int rotate_rows(int T, int heads, int groups) {
 // ---- many tokens at once ------------------------------------------------------------------------------------
 constexpr int64_t CHUNK_ROWS_MAX = 1 << 26;               // query heads of all tokens
 constexpr int64_t CHUNK_GRID = (1 << 24) - 1;             // workgroups of a launch, which has fewer than 2^32 threads
-constexpr size_t CHUNK_WS_MAX = (size_t)256 << 20;        // of workspace
+constexpr size_t CHUNK_WS_MAX = (size_t)1 << 30;          // of workspace
 constexpr int CHUNK_WAVES = 4;
 constexpr int CHUNK_TILE = 128;                           // rows of a workgroup, 32 to each wave, where there are more than a few
 constexpr int chunk_class(int d) { return 16 * attend_ve(d); }
@@ -1134,8 +1134,8 @@ constexpr int chunk_per_simd(int elem_bytes, int dp) { return elem_bytes == 4 ||
 constexpr int chunk_few_rows(int elem_bytes, int ve, int64_t rows) { return rows > 16 && attend_head_tiles(elem_bytes, ve, 17) == 2 ? 32 : 16; }
 constexpr int chunk_few_per_simd(int elem_bytes, int ve, int mt) { return ve == 16 || (elem_bytes == 4 && (mt == 2 || ve == 8)) ? 1 : 2; }
 
-// A pass goes through the slots that new tokens attend to, those that groups have in common, or those that are a request's own.
-enum { CHUNK_NEW, CHUNK_COMMON, CHUNK_OWN };
+// A pass goes through the slots that new tokens attend to, those that groups have in common, those that are a request's own, or both of a request's.
+enum { CHUNK_NEW, CHUNK_COMMON, CHUNK_OWN, CHUNK_ALL };
 struct ChunkPass {
     int mode = CHUNK_NEW, rows = 16;                      // rows of a tile
     int items = 0;               // tiles and parts of a cache head that there may be
@@ -1150,35 +1150,36 @@ struct ChunkPlan {
     int splits = 1;
     size_t bytes = 0;            // of workspace
 };
-#ifndef CHUNK_SMALL
-#define CHUNK_SMALL 1.0e9
-#endif
-#ifndef CHUNK_LEAST
-#define CHUNK_LEAST 256
-#endif
 constexpr int64_t CHUNK_PARTS = 64;                       // of a row in a pass
+// Slots of a part of many rows, at least (fp32, whose products take 16 times as long, a quarter): what a part leaves is 4 (d + 4) bytes for each of its rows, written and read.  100 tokens, 32 heads of 128 to 8,
+// 1600 slots, bf16: 20.6 us with 256, 21.6 with 128; 200 slots 13.4 and 16.1.
+constexpr int CHUNK_LEAST = 256;
+// Slots in common go through by few rows, in one launch with the own slots, up to so many operations.  33 requests in 4 groups, 14 heads of 64 to 2, 2000 slots in common (2.4e8): 17.4 us, by 128 rows and a launch of its
+// own 28.8; 64 requests in one group, 32 heads of 128 to 8, 8100 slots (8.5e9): 111 and 79.
+constexpr double CHUNK_SMALL = 1.0e9;
 // Sequences of `rows` rows in all, whose tiles go through `range` slots at most.
 inline ChunkPass chunk_pass(int mode, int cus, int elem_bytes, int d, int heads, int64_t rows, int64_t sequences, int64_t range, int64_t most_parts, bool small = false,
                             int few_rows = 0) {
     ChunkPass p;
     const int ve = attend_ve(d);
     const int64_t mean = (rows + sequences - 1) / sequences;
-    const bool few = mode == CHUNK_OWN || mean <= 32 || small;
+    const bool few = mode >= CHUNK_OWN || mean <= 32 || small;
     p.mode = mode;
     p.rows = !few ? CHUNK_TILE : few_rows ? few_rows : chunk_few_rows(elem_bytes, ve, mean);
     p.fill = (few ? 4 : chunk_per_simd(elem_bytes, 16 * ve)) * cus / heads;
     if (p.fill < 1) p.fill = 1;
-    p.least = few ? (int)attend_step(elem_bytes, d) : elem_bytes == 4 ? 64 : CHUNK_LEAST;
+    p.least = few ? (int)attend_step(elem_bytes, d) : elem_bytes == 4 ? CHUNK_LEAST / 4 : CHUNK_LEAST;
     p.whole = few ? 1024 : 0;
-    const int64_t tiles = mode == CHUNK_OWN ? sequences * ((rows / sequences + p.rows - 1) / p.rows) : rows / p.rows + sequences;
-    // nothing is divided where tiles alone keep most of the card busy
+    const int64_t tiles = mode >= CHUNK_OWN ? sequences * ((rows / sequences + p.rows - 1) / p.rows) : rows / p.rows + sequences;
+    // Nothing is divided where tiles alone keep most of the card busy, or where there is a request for every compute unit whose slots are few.  (24 x 1190 rows of 4 cache heads, up to 8400 slots: 403 us divided
+    // and joined, 342 not; 64 requests of 8 cache heads, up to 1000 slots each: 59 us in parts of 256, 42 in one.)
     const int64_t busy = few ? sequences : rows / p.rows;
     int64_t parts = (range + p.least - 1) / p.least;
     if (parts > most_parts) parts = most_parts;
     if (parts > CHUNK_PARTS) parts = CHUNK_PARTS;
     if (4 * busy >= 3 * p.fill || (sequences * heads >= cus && range <= p.whole + 31) || parts < 1) parts = 1;
     p.tiles = (int)tiles;
-    p.once = mode == CHUNK_OWN && 2.0 * range * sequences * heads * d * elem_bytes > ATTEND_CACHED;
+    p.once = mode >= CHUNK_OWN && 2.0 * range * sequences * heads * d * elem_bytes > ATTEND_CACHED;
     if (sequences <= 64) {
         p.most_parts = (int)parts;
         p.chunk = INT_MAX;
@@ -1206,12 +1207,18 @@ inline ChunkPlan chunk_plan(int cus, int elem_bytes, int d, int q_heads, int hea
     pl.bytes = chunk_bytes(T * q_heads, d, pl.splits);
     return pl;
 }
-// Nothing in common (max_shared 0, or no room for the parts of both): all slots are the requests' own, a pass without another.
+// With nothing in common, or no room for the parts of both passes, one goes through all slots of every request.
+// (the parts of both: there is always workspace asked for that holds one of each)
+inline size_t shared_most(int64_t B, int64_t q_heads, int64_t d) {
+    const size_t two = chunk_bytes(B * q_heads, d, 2);
+    return two > CHUNK_WS_MAX ? two : CHUNK_WS_MAX;
+}
 inline ChunkPlan shared_plan(int cus, int elem_bytes, int d, int q_heads, int heads, int64_t B, int64_t groups, int64_t max_shared, int64_t max_own, size_t most) {
     ChunkPlan pl;
     const int64_t G = q_heads / heads, parts = chunk_parts_in(B * q_heads, d, most);
     if (max_shared < 1 || parts < 2) {
-        pl.first = chunk_pass(CHUNK_OWN, cus, elem_bytes, d, heads, B * G, B, max_shared + max_own + 31, parts);
+        const int64_t all = max_shared + max_own < INT_MAX - 65536 ? max_shared + max_own : INT_MAX - 65536;   // (no page table holds more)
+        pl.first = chunk_pass(CHUNK_ALL, cus, elem_bytes, d, heads, B * G, B, all, parts);
         pl.splits = pl.first.most_parts;
     } else {
         pl.own = chunk_pass(CHUNK_OWN, cus, elem_bytes, d, heads, B * G, B, max_own + 31, parts / 2);
