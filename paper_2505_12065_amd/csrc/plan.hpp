@@ -1127,7 +1127,6 @@ constexpr int64_t CHUNK_GRID = (1 << 24) - 1;             // workgroups of a lau
 constexpr size_t CHUNK_WS_MAX = (size_t)1 << 30;          // of workspace
 constexpr int CHUNK_WAVES = 4;
 constexpr int CHUNK_TILE = 128;                           // rows of a workgroup, 32 to each wave, where there are more than a few
-constexpr int chunk_class(int d) { return 16 * attend_ve(d); }
 constexpr int chunk_slots(int row_bytes) { return row_bytes > 256 ? 32 : 64; }                        // slots of a tile
 constexpr int chunk_per_simd(int elem_bytes, int dp) { return elem_bytes == 4 || dp == 256 ? 1 : 2; } // waves, as registers allow
 // A few rows: 16 or, where registers allow, 32.
