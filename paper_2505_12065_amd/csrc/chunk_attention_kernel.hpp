@@ -522,6 +522,8 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE
     if (deal.count <= 0) return;
     const int first = deal.first, end = deal.end, row_bytes = a.cache.d * T::bytes;
     const bool full = a.cache.d == 16 * VE;
+    const uint32_t flip = a.scale < 0.f ? (T::bytes == 4 ? 0x80000000u : 0x80008000u) : 0u;
+    const float scale = fmaxf(fabsf(a.scale), 1e-37f);
 
     float *s_top = few_lds, *s_sum = few_lds + WAVES * ROWS, *s_o = few_lds + 2 * WAVES * ROWS;
     constexpr bool Q_LDS = attend_q_in_lds(VE);
@@ -537,6 +539,8 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE
             const int at = (4 * s + g) * 16;
             u4 x = zero_chunk();
             if (there && at < row_bytes) x = load_chunk(from + at);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] ^= flip;
             if constexpr (!Q_LDS) q[mt][s] = x;
             else if ((mt * NS + s) % WAVES == wave) s_q[(mt * NS + s) * WAVE + lane] = x;
         }
@@ -647,7 +651,6 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE
                 x[mt][t] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int s = 0; s < NS; ++s) x[mt][t] = scores_step<T>(kr[t][s], Q_LDS ? s_q[(mt * NS + s) * WAVE + lane] : q[Q_LDS ? 0 : mt][Q_LDS ? 0 : s], x[mt][t]);
-                x[mt][t] *= a.scale;
             }
         if (more) load_k(k0 + STEP, page_next);
         bool whole = k0 >= lo_most && k0 + 16 * NT <= hi_least && k0 + 16 * NT <= end;
@@ -692,14 +695,14 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) most = fmaxf(most, x[mt][t][i]);
-            const float now = fmaxf(top[mt], column_max(most)), keep = top[mt] == now ? 1.f : exp2_fast(top[mt] - now), off = (now == -INFINITY ? 0.f : now) - a.lift;
+            const float now = fmaxf(top[mt], column_max(most)), keep = top[mt] == now ? 1.f : exp2_fast((top[mt] - now) * scale), off = (now == -INFINITY ? 0.f : now * scale) - a.lift;
             top[mt] = now;
             sum[mt] *= keep;
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    x[mt][t][i] = exp2_fast(x[mt][t][i] - off);
+                    x[mt][t][i] = exp2_fast(fmaf(x[mt][t][i], scale, -off));
                     sum[mt] += x[mt][t][i];
                 }
 #pragma unroll
@@ -776,6 +779,7 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
         sum[mt] = column_sum(sum[mt]);
+        top[mt] *= scale;                                 // an exponent of 2
         if (g == 0) {
             s_top[wave * ROWS + 16 * mt + m] = top[mt];
             s_sum[wave * ROWS + 16 * mt + m] = sum[mt];
