@@ -445,7 +445,7 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(T::bytes, DP)) v
         u4 p[NU][2];
         scores(at_k, k0, seen, x);
         // Weights and their products go before other waves' scores, which need the matrix cores alone: of two waves on a SIMD one has something for each unit.  (d = 128, 16 bits: a prompt of 16384 tokens,
-        // 32 heads to 8, 2216 us without and 2105 with it; d = 64 2464 and 2520, d = 256, one wave on a SIMD, 1191 and 1214.)
+        // 32 heads to 8, 2216 us without and 2105 with it; d = 64 2464 and 2520.  With one wave on a SIMD, as at d = 256, there is none to go before.)
         constexpr bool FIRST = DP == 128 && !WIDE;
         if constexpr (FIRST) __builtin_amdgcn_s_setprio(1);
         weights(x, p);

@@ -1123,11 +1123,11 @@ inline int rotate_rows(int T, int heads, int groups) {
 
 // ---- many tokens at once ------------------------------------------------------------------------------------
 constexpr int64_t CHUNK_ROWS_MAX = 1 << 26;               // query heads of all tokens
-constexpr int64_t CHUNK_GRID = (1 << 24) - 1;             // workgroups of a launch, which has fewer than 2^32 threads
 constexpr size_t CHUNK_WS_MAX = (size_t)1 << 30;          // of workspace
 constexpr int CHUNK_WAVES = 4;
 constexpr int CHUNK_TILE = 128;                           // rows of a workgroup, 32 to each wave, where there are more than a few
-constexpr int chunk_slots(int row_bytes) { return row_bytes > 256 ? 32 : 64; }                        // slots of a tile
+// Slots of a tile: 64 wherever two tiles each of keys and values fit a compute unit's shared memory.  (16 bits, d = 256, 4 x 1024 tokens of 8192, with 64 and 32: 955 us and 1189; fp32, d = 128, 2 x 1024 of 4096: 716 and 771.)
+constexpr int chunk_slots(int row_bytes) { return row_bytes > 512 ? 32 : 64; }
 constexpr int chunk_per_simd(int elem_bytes, int dp) { return elem_bytes == 4 || dp == 256 ? 1 : 2; } // waves, as registers allow
 // A few rows: 16 or, where registers allow, 32.
 constexpr int chunk_few_rows(int elem_bytes, int ve, int64_t rows) { return rows > 16 && attend_head_tiles(elem_bytes, ve, 17) == 2 ? 32 : 16; }
