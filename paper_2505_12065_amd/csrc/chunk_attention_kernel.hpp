@@ -57,7 +57,7 @@ __device__ __forceinline__ void wait_outstanding() {
 template <class T, int DP_>
 struct ChunkShape {
     static constexpr int DP = DP_, RB = DP * T::bytes;                  // largest d; bytes of a row in LDS
-    static constexpr int KT = chunk_slots(RB), WAVES = CHUNK_WAVES;
+    static constexpr int KT = chunk_slots(RB, chunk_per_simd(DP)), WAVES = CHUNK_WAVES;
     static constexpr int CPR = RB / 16, RPI = 64 / CPR;                 // chunks of a row, rows that a load brings
     static constexpr int LOADS = KT * RB / 1024 / WAVES;                // of K, and of V, that a wave issues for a tile of slots
     static constexpr int TILE = KT * RB, LDS = 4 * TILE;                // K and V, twice
@@ -169,7 +169,7 @@ __device__ __forceinline__ int64_t chunk_row(const ChunkArgs &a, const ChunkDeal
 // ---- 128 rows -------------------------------------------------------------------------------------------------
 
 template <class T, int DP>
-__global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(T::bytes, DP)) void chunk_attention_kernel(ChunkArgs a, ChunkPass pass) {
+__global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(DP)) void chunk_attention_kernel(ChunkArgs a, ChunkPass pass) {
     typedef ChunkShape<T, DP> Sh;
     constexpr int KT = Sh::KT, RB = Sh::RB, NS = Sh::NS, NC = Sh::NC, NU = Sh::NU, LOADS = Sh::LOADS, CPR = Sh::CPR, RPI = Sh::RPI, WAVES = Sh::WAVES;
     constexpr bool WIDE = T::bytes == 4;
@@ -287,7 +287,7 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(T::bytes, DP)) v
 #pragma unroll
     for (int c = 0; c < NC; ++c) o[c] = zero16();
     float top = -INFINITY, sum = 0.f;                     // a score that the weights go by; the sum of this lane's slots alone
-    const int k_lane = m * RB, k_turn = (h ^ chunk_swizzle<RB>(m)) << 4;    // a lane's part of the places of its operands
+    const int k_lane = m * RB, k_turn_of_lane = (h ^ chunk_swizzle<RB>(m)) << 4;    // a lane's part of the places of its operands
     const int i16 = lane & 15, v_row = 4 * h + (i16 >> 2), v_lane = v_row * RB;
     const int v_turn = ((2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1)) ^ chunk_swizzle<RB>(v_row)) << 4 | (i16 & 1) << 3;
     constexpr uint64_t ALL = KT == 64 ? ~0ull : (1ull << (KT & 63)) - 1;
@@ -295,6 +295,8 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(T::bytes, DP)) v
     auto scores = [&](unsigned char *at_k, int k0, uint64_t seen, f16v (&x)[NU]) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < NU; ++u) x[u] = zero16();
+        int k_turn = k_turn_of_lane;
+        if constexpr (WIDE) asm volatile("" : "+v"(k_turn));   // (or the places of all operands stay in registers from tile to tile: at d = 256 93 were spilled, and 2 x 1024 tokens of 4096 took 2601 us, 1647 so)
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
             if (WIDE && 32 * s >= row_bytes) break;       // (uniform; a product of 32 bits takes 16 times as long)
@@ -367,6 +369,8 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(T::bytes, DP)) v
         }
     };
     auto times_v = [&](unsigned char *at_v, const f16v (&x)[NU], const u4 (&p)[NU][2]) __attribute__((always_inline)) {
+        int m = lane & 31;
+        if constexpr (WIDE) asm volatile("" : "+v"(m));
 #pragma unroll
         for (int u = 0; u < NU; ++u) {
             if constexpr (WIDE) {
@@ -444,9 +448,9 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(T::bytes, DP)) v
         f16v x[NU];
         u4 p[NU][2];
         scores(at_k, k0, seen, x);
-        // Weights and their products go before other waves' scores, which need the matrix cores alone: of two waves on a SIMD one has something for each unit.  (d = 128, 16 bits: a prompt of 16384 tokens,
-        // 32 heads to 8, 2216 us without and 2105 with it; d = 64 2464 and 2520.  With one wave on a SIMD, as at d = 256, there is none to go before.)
-        constexpr bool FIRST = DP == 128 && !WIDE;
+        // Weights and their products go before another wave's scores, which need the matrix cores alone: of two waves on a SIMD one has something for each unit.  (A prompt of 16384 tokens, 32 heads of 128 to 8,
+        // bf16: 2216 us without and 2105 with it; of 8192, 16 heads to 8, fp32: d = 128 2619 and 2550, d = 64 1309 and 1174; d = 64, bf16, 4 x 1024 of 8192 206 and 199, but 24 x 170 of 4400 235 and 241.)
+        constexpr bool FIRST = chunk_per_simd(DP) > 1;
         if constexpr (FIRST) __builtin_amdgcn_s_setprio(1);
         weights(x, p);
         times_v(at_k + Sh::TILE, x, p);

@@ -1126,9 +1126,10 @@ constexpr int64_t CHUNK_ROWS_MAX = 1 << 26;               // query heads of all 
 constexpr size_t CHUNK_WS_MAX = (size_t)1 << 30;          // of workspace
 constexpr int CHUNK_WAVES = 4;
 constexpr int CHUNK_TILE = 128;                           // rows of a workgroup, 32 to each wave, where there are more than a few
-// Slots of a tile: 64 wherever two tiles each of keys and values fit a compute unit's shared memory.  (16 bits, d = 256, 4 x 1024 tokens of 8192, with 64 and 32: 955 us and 1189; fp32, d = 128, 2 x 1024 of 4096: 716 and 771.)
-constexpr int chunk_slots(int row_bytes) { return row_bytes > 512 ? 32 : 64; }
-constexpr int chunk_per_simd(int elem_bytes, int dp) { return elem_bytes == 4 || dp == 256 ? 1 : 2; } // waves, as registers allow
+// Waves on a SIMD, as registers allow, and so workgroups on a compute unit (2 x 1024 tokens of 4096, fp32, d = 128: 684 us, with one wave 727; the prompt of 8192 2626 and 2928).
+constexpr int chunk_per_simd(int dp) { return dp == 256 ? 1 : 2; }
+// Slots of a tile: 64 wherever two tiles each of keys and values, for all the workgroups, fit a compute unit's shared memory (16 bits, d = 256, 4 x 1024 tokens of 8192, with 64 and 32: 955 us and 1189).
+constexpr int chunk_slots(int row_bytes, int per_simd) { return 4 * 64 * row_bytes * per_simd > 160 * 1024 ? 32 : 64; }
 // A few rows: 16 or, where registers allow, 32.
 constexpr int chunk_few_rows(int elem_bytes, int ve, int64_t rows) { return rows > 16 && attend_head_tiles(elem_bytes, ve, 17) == 2 ? 32 : 16; }
 constexpr int chunk_few_per_simd(int elem_bytes, int ve, int mt) { return ve == 16 || (elem_bytes == 4 && (mt == 2 || ve == 8)) ? 1 : 2; }
@@ -1165,7 +1166,7 @@ inline ChunkPass chunk_pass(int mode, int cus, int elem_bytes, int d, int heads,
     const bool few = mode >= CHUNK_OWN || mean <= 32 || small;
     p.mode = mode;
     p.rows = !few ? CHUNK_TILE : few_rows ? few_rows : chunk_few_rows(elem_bytes, ve, mean);
-    p.fill = (few ? 4 : chunk_per_simd(elem_bytes, 16 * ve)) * cus / heads;
+    p.fill = (few ? 4 : chunk_per_simd(16 * ve)) * cus / heads;
     if (p.fill < 1) p.fill = 1;
     p.least = few ? (int)attend_step(elem_bytes, d) : elem_bytes == 4 ? CHUNK_LEAST / 4 : CHUNK_LEAST;
     p.whole = few ? 1024 : 0;
