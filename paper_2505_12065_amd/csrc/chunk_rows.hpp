@@ -15,7 +15,12 @@ struct ChunkSpan { int lo, hi; };                         // slots lo .. hi - 1
 // Parts begin with multiples of 32 slots, so that 16 rows from a multiple of 16 on are loaded together.
 __device__ __forceinline__ int chunk_begin(ChunkSpan range) { return min(range.lo, range.hi) & ~31; }
 __device__ __forceinline__ int chunk_slots_of(ChunkSpan range) { return range.hi - chunk_begin(range); }
-__device__ __forceinline__ int chunk_parts(int slots, int chunk) { return slots > 0 ? (slots - 1) / chunk + 1 : 1; }     // (the first part of nothing says so)
+// Parts of `chunk` slots; the first part of nothing says so.  (There are few: of a quotient below 2^20 a float is off by less than one.)
+__device__ __forceinline__ int chunk_parts(int slots, int chunk) {
+    if (slots <= chunk) return 1;
+    const int guess = (int)((float)(slots - 1) * __builtin_amdgcn_rcpf((float)chunk)), left = (int)((uint32_t)(slots - 1) - (uint32_t)guess * (uint32_t)chunk);
+    return guess + 1 + (left >= chunk) - (left < 0);
+}
 
 __device__ __forceinline__ int chunk_length(const ChunkArgs &a, int request) { return max(a.lengths[request], 0); }
 
@@ -91,6 +96,22 @@ __device__ __forceinline__ int wave_sum_of(int x) {
     row_pair<32>((uint32_t)x, a, b);
     return (int)(a + b);
 }
+// ... over the lanes below each
+__device__ __forceinline__ int wave_sum_before(int x) {
+    const int lane = threadIdx.x & (WAVE - 1);
+    int all = x, before = 0;                              // of a block of lanes, and of those of it below this one
+    auto step = [&](int mask, int other) { before += lane & mask ? other : 0; all += other; };
+    step(1, (int)lane_swap<1>((uint32_t)all));
+    step(2, (int)lane_swap<2>((uint32_t)all));
+    step(4, (int)lane_swap<4>((uint32_t)all));
+    step(8, (int)lane_swap<8>((uint32_t)all));
+    uint32_t a, b;
+    row_pair<16>((uint32_t)all, a, b);
+    step(16, (int)(a + b) - all);
+    row_pair<32>((uint32_t)all, a, b);
+    step(32, (int)(a + b) - all);
+    return before;
+}
 __device__ __forceinline__ int wave_max_of(int x) {
     x = max(x, (int)lane_swap<1>((uint32_t)x));
     x = max(x, (int)lane_swap<2>((uint32_t)x));
@@ -109,7 +130,7 @@ __device__ __forceinline__ int chunk_even(const ChunkPass &p, int tiles, int slo
     if (p.most_parts == 1) return INT_MAX;
     const int most = __builtin_amdgcn_readfirstlane(wave_max_of(slots)), all_tiles = __builtin_amdgcn_readfirstlane(wave_sum_of(tiles));
     const int64_t limit = (p.rows == CHUNK_TILE && 4 * (int64_t)all_tiles > p.fill ? 2 : 1) * (int64_t)p.fill;
-    if (most <= p.whole && all_tiles >= p.fill / 4) return INT_MAX;
+    if (most <= p.whole && all_tiles >= p.units) return INT_MAX;
     if (limit <= all_tiles) return INT_MAX;
     const float all = wave_sum((float)tiles * (float)slots);
     // in units of 64 slots: `few` are too few or just enough, `enough` are not too few
@@ -129,27 +150,32 @@ __device__ __forceinline__ int chunk_even(const ChunkPass &p, int tiles, int slo
 struct ChunkDeal {
     ChunkKnown k;
     int r0, count, part, parts;
-    bool alone;               // nothing is to be joined with it
+    int alone;                // nothing is to be joined with it
     ChunkSpan range;          // of the tile's rows, all together
     int first, end;
 };
-__device__ __forceinline__ ChunkDeal chunk_deal(const ChunkArgs &a, const ChunkPass &p, int item, int G) {
-    const int n = chunk_sequences(a, p.mode), lane = threadIdx.x & (WAVE - 1);
+__device__ __forceinline__ ChunkDeal chunk_deal_of(const ChunkArgs &a, const ChunkPass &p, int item, int G) {
+    const int n = chunk_sequences(a, p.mode), lane = threadIdx.x & (WAVE - 1), rows_log = __ffs(p.rows) - 1;
     ChunkDeal d{};
     int chunk;
     if (n <= WAVE && !(p.mode >= CHUNK_OWN && p.most_parts == 1)) {         // (own slots that are not divided: all have as many items)
         const ChunkKnown k = chunk_known(a, p.mode, min(lane, n - 1));
-        const int tiles = lane < n ? (int)(((int64_t)k.q.tokens * G + p.rows - 1) / p.rows) : 0;
+        const int tiles = lane < n ? (k.q.tokens * G + p.rows - 1) >> rows_log : 0;
         // (the last tile has most slots, but for what a window leaves it)
-        const ChunkSpan last = chunk_range(a, p.mode, k, (int)(max(tiles - 1, 0) * (int64_t)p.rows / G), max(k.q.tokens - 1, 0));
+        const int t0 = p.mode == CHUNK_NEW ? (int)((uint32_t)max(tiles - 1, 0) * p.rows / (uint32_t)G) : 0;
+        const ChunkSpan last = chunk_range(a, p.mode, k, t0, max(k.q.tokens - 1, 0));
         int slots = tiles > 0 ? chunk_slots_of(last) : 0;
         if (tiles > 0 && p.mode == CHUNK_NEW && a.window > 0) slots = (int)max((int64_t)slots, min((int64_t)last.hi, (int64_t)a.window + p.rows + 32));
         chunk = chunk_even(p, tiles, slots);
         const int items = tiles * chunk_parts(slots, chunk);
-        // items of longer sequences (of two as long, the first's)
-        const uint32_t key = (uint32_t)min(slots, (1 << 26) - 1) << 6 | (WAVE - 1 - lane);
-        int before = 0;
-        for (int i = 0; i < n; ++i) before += (uint32_t)__builtin_amdgcn_readlane((int)key, i) > key ? __builtin_amdgcn_readlane(items, i) : 0;
+        int before;
+        if (p.items > p.fill) {                           // items of longer sequences go first (of two as long, the first's)
+            const uint32_t key = (uint32_t)min(slots, (1 << 26) - 1) << 6 | (WAVE - 1 - lane);
+            before = 0;
+            for (int i = 0; i < n; ++i) before += (uint32_t)__builtin_amdgcn_readlane((int)key, i) > key ? __builtin_amdgcn_readlane(items, i) : 0;
+        } else {                                          // all are on the card at once
+            before = wave_sum_before(items);
+        }
         const uint64_t mine = __ballot(item >= before && item < before + items);
         if (mine == 0) return d;
         const int i = __ffsll((unsigned long long)mine) - 1;
@@ -162,27 +188,27 @@ __device__ __forceinline__ ChunkDeal chunk_deal(const ChunkArgs &a, const ChunkP
         // A sequence of m tokens has at most as many tiles as there are numbers from start G / rows + i up to the next one's.
         const int id = p.tiles - 1 - item % p.tiles;
         int i;
-        int64_t tile;
+        int tile;
         d.part = item / p.tiles;
         chunk = p.chunk;
         if (p.mode >= CHUNK_OWN) {
-            const int per = (G + p.rows - 1) / p.rows;
+            const int per = (G + p.rows - 1) >> rows_log;
             i = id / per;
             tile = id % per;
             if (i >= n) return d;
         } else {
             const int32_t *starts = p.mode == CHUNK_NEW ? a.starts : a.group_starts;
-            auto first = [&](int k) { return (int)((int64_t)packed_start(starts, k, a.tokens) * G / p.rows) + k; };
+            auto first = [&](int k) { return (packed_start(starts, k, a.tokens) * G >> rows_log) + k; };
             i = __builtin_amdgcn_readfirstlane(count_up_to(first, n + 1, id)) - 1;
             if (i < 0 || i >= n) return d;
             tile = id - first(i);
         }
-        d.r0 = (int)(tile * p.rows);
+        d.r0 = tile * p.rows;
         d.k = chunk_known(a, p.mode, i);
         d.k.common = __builtin_amdgcn_readfirstlane(d.k.common);             // (the same in all lanes, which the compiler cannot know)
         d.k.grouped = __builtin_amdgcn_readfirstlane(d.k.grouped);
     }
-    const int count = (int)max((int64_t)0, min((int64_t)p.rows, (int64_t)d.k.q.tokens * G - d.r0));
+    const int count = max(0, min(p.rows, d.k.q.tokens * G - d.r0));
     if (count == 0) return d;
     d.range = chunk_range(a, p.mode, d.k, d.r0 / G, (d.r0 + count - 1) / G);
     d.parts = chunk_parts(chunk_slots_of(d.range), chunk);
@@ -192,6 +218,24 @@ __device__ __forceinline__ ChunkDeal chunk_deal(const ChunkArgs &a, const ChunkP
     d.first = chunk_begin(d.range) + d.part * chunk;
     d.end = d.range.hi - d.first < chunk ? d.range.hi : d.first + chunk;
     return d;
+}
+// ... worked out by one wave: a SIMD has waves of several workgroups and issues for one at a time (8 requests of 2000 slots, 8 heads of 128: 20.4 us by each wave, 19.2 so; 128 x 125 slots 18.4 and 17.4).
+__device__ __forceinline__ ChunkDeal chunk_deal(const ChunkArgs &a, const ChunkPass &p, int item, int G) {
+    constexpr int WORDS = sizeof(ChunkDeal) / 4;
+    struct Words { int w[WORDS]; };
+    __shared__ int s_deal[WORDS];
+    if (threadIdx.x < WAVE) {
+        const Words words = __builtin_bit_cast(Words, chunk_deal_of(a, p, item, G));
+        if (threadIdx.x == 0) {
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) s_deal[i] = words.w[i];
+        }
+    }
+    __syncthreads();
+    Words words;
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) words.w[i] = __builtin_amdgcn_readfirstlane(s_deal[i]);
+    return __builtin_bit_cast(ChunkDeal, words);
 }
 
 }  // namespace ann

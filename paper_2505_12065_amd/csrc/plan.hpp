@@ -1132,7 +1132,8 @@ constexpr int chunk_per_simd(int dp) { return dp == 256 ? 1 : 2; }
 constexpr int chunk_slots(int row_bytes, int per_simd) { return 4 * 64 * row_bytes * per_simd > 160 * 1024 ? 32 : 64; }
 // A few rows: 16 or, where registers allow, 32.
 constexpr int chunk_few_rows(int elem_bytes, int ve, int64_t rows) { return rows > 16 && attend_head_tiles(elem_bytes, ve, 17) == 2 ? 32 : 16; }
-constexpr int chunk_few_per_simd(int elem_bytes, int ve, int mt) { return ve == 16 || (elem_bytes == 4 && (mt == 2 || ve == 8)) ? 1 : 2; }
+// Waves on a SIMD, as registers allow; the workgroups that fill the card are as many to a compute unit (8 requests of 2000 slots, 8 heads of 128, 3 to a unit: 16.5 us, 4 of which 3 run at once 19.2).
+constexpr int chunk_few_per_simd(int elem_bytes, int ve, int mt) { return ve == 16 || (elem_bytes == 4 && (mt == 2 || ve == 8)) ? 1 : mt == 2 ? 2 : 3; }
 
 // A pass goes through the slots that new tokens attend to, those that groups have in common, those that are a request's own, or both of a request's.
 enum { CHUNK_NEW, CHUNK_COMMON, CHUNK_OWN, CHUNK_ALL };
@@ -1142,7 +1143,7 @@ struct ChunkPass {
     int fill = 1;                // workgroups of a cache head that fill the card
     int most_parts = 1, least = 64, part0 = 0;            // parts of a row at most; slots of a part at least; number of a row's first part
     bool once = false;           // keys and values are read once, and may be more than the last cache holds
-    int whole = 0;               // ranges of up to so many slots are not divided if there is a tile for every compute unit
+    int whole = 0, units = 1;    // ranges of up to so many slots are not divided if there is a tile for every compute unit, of which a cache head has so many
     int tiles = 0, chunk = 0;    // tiles that there may be; slots of a part, of more than 64 sequences
 };
 struct ChunkPlan {
@@ -1166,13 +1167,14 @@ inline ChunkPass chunk_pass(int mode, int cus, int elem_bytes, int d, int heads,
     const bool few = mode >= CHUNK_OWN || mean <= 32 || small;
     p.mode = mode;
     p.rows = !few ? CHUNK_TILE : few_rows ? few_rows : chunk_few_rows(elem_bytes, ve, mean);
-    p.fill = (few ? 4 : chunk_per_simd(16 * ve)) * cus / heads;
+    p.fill = (few ? chunk_few_per_simd(elem_bytes, ve, p.rows / 16) : chunk_per_simd(16 * ve)) * cus / heads;
     if (p.fill < 1) p.fill = 1;
+    p.units = cus > heads ? cus / heads : 1;
     p.least = few ? (int)attend_step(elem_bytes, d) : elem_bytes == 4 ? CHUNK_LEAST / 4 : CHUNK_LEAST;
     p.whole = few ? 1024 : 0;
     const int64_t tiles = mode >= CHUNK_OWN ? sequences * ((rows / sequences + p.rows - 1) / p.rows) : rows / p.rows + sequences;
     // Nothing is divided where tiles alone keep most of the card busy, or where there is a request for every compute unit whose slots are few.  (24 x 1190 rows of 4 cache heads, up to 8400 slots: 403 us divided
-    // and joined, 342 not; 64 requests of 8 cache heads, up to 1000 slots each: 59 us in parts of 256, 42 in one.)
+    // and joined, 342 not; 64 requests of 8 cache heads, 1000 slots each: 47 us in parts, 42 in one; of 125 to 1000 slots 35 and 31.)
     const int64_t busy = few ? sequences : rows / p.rows;
     int64_t parts = (range + p.least - 1) / p.least;
     if (parts > most_parts) parts = most_parts;
