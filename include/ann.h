@@ -501,7 +501,8 @@ int ann_rotate_append(const void *qkv, int64_t token_stride, int64_t head_stride
  * product with V (each is off by at most half a unit in its last place; fp16: or 2^-32 of the largest), out is rounded once.
  *   q           device [T, q_heads, d] of the cache's type; strides q_row, q_head (multiples of 16 bytes)
  *   lengths     device int32 [B], with the new tokens; as 0 if negative.  A token has its slot only if that is in [0, max_length), 1 <= max_length <= width slots
- *   max_length  what the work is divided by, as no length is read on the host: the largest length, or a bound as close as the host knows
+ *   max_length  what the work is divided by, as no length is read on the host: the largest length, or a bound as close as the host knows; it or the window at most 2^26 (products with V are summed in
+ *               binary32, eight slots at a time)
  *   out         device [T, q_heads, d], contiguous;  lse  device float [T, q_heads], or NULL
  * Values that a token does not attend to do not matter to it, NaN and infinities among them; a value that is one of these and has a weight gives one.  Same inputs and workspace give bitwise-same
  * outputs.  Where there are few tokens, contexts are divided into parts that are joined in the workspace of the current device; with less than the size below they are divided
@@ -520,7 +521,8 @@ int64_t ann_chunk_attention_workspace_bytes(int32_t T, int32_t B, int32_t q_head
  *   shared        device int32 [groups]: the first shared[g] slots of the group's requests are the same slots of the same pages (they are read by the page table of the group's first request).
  *                 It counts as no more than max_shared, as 0 if negative, and for a request as no more than its length
  *   lengths       device int32 [B]; the slots of request b from the shared ones on are its own, of which no more than max_own count; as 0 if negative
- *   max_shared, max_own  what the work is divided by: the largest numbers of shared and of own slots, or bounds as close as the host knows.  0 <= max_shared <= width slots, 1 <= max_own <= width slots
+ *   max_shared, max_own  what the work is divided by: the largest numbers of shared and of own slots, or bounds as close as the host knows.  0 <= max_shared <= width slots, 1 <= max_own <= width slots,
+ *                 both at most 2^26
  * 16-bit types: weights are rounded to the type for the product with V, as in ann_chunk_attention.  Otherwise, and for q, page_table, out and lse, as in ann_paged_attention.
  * Same inputs and workspace give bitwise-same outputs.  Uses the workspace of the current device; with less than the size below
  * nothing is shared.  groups in [1, 65536], B at most 65536, q_heads 8192, B q_heads and groups heads 2^22, width slots 2^31 - 65537.  B = 0 returns ANN_OK at once. */

@@ -603,10 +603,12 @@ static int check_attention(const void *q, int64_t q_row, int64_t q_head, int32_t
     return ANN_OK;
 }
 
+static bool too_many_slots(int32_t max_length, int32_t window) { return max_length > CHUNK_SLOTS_MAX && (window == 0 || window > CHUNK_SLOTS_MAX); }
+
 int64_t ann_chunk_attention_workspace_bytes(int32_t T, int32_t B, int32_t q_heads, int32_t heads, int32_t d, int32_t dtype, int32_t max_length, int32_t window) {
     if (T < 1 || T > GRID_MAX || B < 1 || B > 65536 || heads < 1 || q_heads < heads || q_heads > 8192 || q_heads % heads || d < 8 || d > ANN_HEAD_MAX || max_length < 1 || window < 0)
         return ANN_ERR_INVALID;
-    if (check_dtype(dtype) != ANN_OK || (int64_t)T * q_heads > CHUNK_ROWS_MAX || (int64_t)B * heads > GRID_MAX) return ANN_ERR_INVALID;
+    if (check_dtype(dtype) != ANN_OK || (int64_t)T * q_heads > CHUNK_ROWS_MAX || (int64_t)B * heads > GRID_MAX || too_many_slots(max_length, window)) return ANN_ERR_INVALID;
     return (int64_t)chunk_plan(units_of_device(), elem_bytes(dtype), d, q_heads, heads, T, B, max_length, window, CHUNK_WS_MAX).bytes;
 }
 
@@ -623,6 +625,8 @@ int ann_chunk_attention(const void *q, int64_t q_row, int64_t q_head, int32_t T,
     if (B < 1 || B > 65536 || (int64_t)B * cache->heads > GRID_MAX) return fail(ANN_ERR_INVALID, "B = %d out of range [1, 65536], or of too many heads", B);
     if (max_length < 1 || max_length > width * cache->slots) return fail(ANN_ERR_INVALID, "max_length = %d out of range [1, width slots]", max_length);
     if (window < 0) return fail(ANN_ERR_INVALID, "window = %d out of range", window);
+    if (too_many_slots(max_length, window))
+        return fail(ANN_ERR_INVALID, "max_length = %d without a window: at most %d slots may be attended to", max_length, CHUNK_SLOTS_MAX);
     a.tokens = T; a.starts = starts; a.requests = B; a.max_length = max_length; a.window = window; a.out = out; a.lse = lse;
     a.lift = chunk_lift(cache->dtype, max_length);
     return run_attention(a, cache->dtype, CHUNK_WS_MAX, [&](int cus, size_t most) {
@@ -633,7 +637,7 @@ int ann_chunk_attention(const void *q, int64_t q_row, int64_t q_head, int32_t T,
 int64_t ann_shared_attention_workspace_bytes(int32_t B, int32_t groups, int32_t q_heads, int32_t heads, int32_t d, int32_t dtype, int32_t max_shared, int32_t max_own) {
     if (B < 1 || B > 65536 || groups < 1 || groups > 65536 || heads < 1 || q_heads < heads || q_heads > 8192 || q_heads % heads || d < 8 || d > ANN_HEAD_MAX || max_shared < 0 || max_own < 1)
         return ANN_ERR_INVALID;
-    if (check_dtype(dtype) != ANN_OK || (int64_t)B * q_heads > GRID_MAX || (int64_t)groups * heads > GRID_MAX) return ANN_ERR_INVALID;
+    if (check_dtype(dtype) != ANN_OK || (int64_t)B * q_heads > GRID_MAX || (int64_t)groups * heads > GRID_MAX || max_shared > CHUNK_SLOTS_MAX || max_own > CHUNK_SLOTS_MAX) return ANN_ERR_INVALID;
     return (int64_t)shared_plan(units_of_device(), elem_bytes(dtype), d, q_heads, heads, B, groups, max_shared, max_own, shared_most(B, q_heads, d)).bytes;
 }
 
@@ -650,7 +654,7 @@ int ann_shared_attention(const void *q, int64_t q_row, int64_t q_head, int32_t B
     if ((int64_t)B * q_heads > GRID_MAX || (int64_t)groups * cache->heads > GRID_MAX)
         return fail(ANN_ERR_INVALID, "%d requests in %d groups, of %d heads, are too many for a call", B, groups, q_heads);
     const int32_t most = width * cache->slots;
-    if (max_shared < 0 || max_shared > most || max_own < 1 || max_own > most)
+    if (max_shared < 0 || max_shared > std::min(most, CHUNK_SLOTS_MAX) || max_own < 1 || max_own > std::min(most, CHUNK_SLOTS_MAX))
         return fail(ANN_ERR_INVALID, "max_shared = %d or max_own = %d out of range", max_shared, max_own);
     a.tokens = a.requests = B; a.max_length = most; a.out = out; a.lse = lse;
     a.group_starts = group_starts; a.shared = shared; a.groups = groups; a.max_shared = max_shared; a.max_own = max_own;

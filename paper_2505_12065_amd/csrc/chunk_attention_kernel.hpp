@@ -353,13 +353,14 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(DP)) void chunk_
             for (int c = 0; c < NC; ++c) o[c] *= keep;
         }
         const float off = (top == -INFINITY ? 0.f : top * scale) - a.lift;
+        float tile = 0.f;                                 // (summed alone: a weight at a time, a sum of n of them may be off by n 2^-24)
 #pragma unroll
         for (int u = 0; u < NU; ++u) {
             float w[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 w[i] = exp2_fast(fmaf(x[u][i], scale, -off));
-                sum += w[i];
+                tile += w[i];
                 if constexpr (WIDE) x[u][i] = w[i];
             }
             if constexpr (!WIDE) {
@@ -367,6 +368,7 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(DP)) void chunk_
                 p[u][1] = pack_weights<T>(w + 8);
             }
         }
+        sum += tile;
     };
     auto times_v = [&](unsigned char *at_v, const f16v (&x)[NU], const u4 (&p)[NU][2]) __attribute__((always_inline)) {
         int m = lane & 31;
@@ -706,14 +708,15 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE
                 for (int i = 0; i < 4; ++i) most = fmaxf(most, x[mt][t][i]);
             const float now = fmaxf(top[mt], column_max(most)), keep = top[mt] == now ? 1.f : exp2_fast((top[mt] - now) * scale), off = (now == -INFINITY ? 0.f : now * scale) - a.lift;
             top[mt] = now;
-            sum[mt] *= keep;
+            float tile = 0.f;
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     x[mt][t][i] = exp2_fast(fmaf(x[mt][t][i], scale, -off));
-                    sum[mt] += x[mt][t][i];
+                    tile += x[mt][t][i];
                 }
+            sum[mt] = sum[mt] * keep + tile;
 #pragma unroll
             for (int c = 0; c < VE; ++c) o[mt][c] *= keep;
         }

@@ -133,7 +133,7 @@ __device__ __forceinline__ int chunk_even(const ChunkPass &p, int tiles, int slo
     if (most <= p.whole && all_tiles >= p.units) return INT_MAX;
     if (limit <= all_tiles) return INT_MAX;
     const float all = wave_sum((float)tiles * (float)slots);
-    // in units of 64 slots: `few` are too few or just enough, `enough` are not too few
+    // in units of 64 slots, of which there are 2^20: `few` are too few or just enough, `enough` are not too few
     const int least = (max(p.least, (most - 1) / p.most_parts + 1) + 63) / 64;
     int few = max((int)min(all / (64.f * (float)limit), 1e7f), least), enough = max((int)min(all / (64.f * (float)(limit - all_tiles)), 1e7f) + 1, least);
     while (few < enough) {

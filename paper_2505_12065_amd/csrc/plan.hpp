@@ -1123,6 +1123,8 @@ inline int rotate_rows(int T, int heads, int groups) {
 
 // ---- many tokens at once ------------------------------------------------------------------------------------
 constexpr int64_t CHUNK_ROWS_MAX = 1 << 26;               // query heads of all tokens
+// Slots that a row attends to.  The matrix cores add the products of 8 slots at a time to sums of 32 bits: of 2^27 equal weights and more, what is added is half a unit of the sum's last place and is lost.
+constexpr int CHUNK_SLOTS_MAX = 1 << 26;
 constexpr size_t CHUNK_WS_MAX = (size_t)1 << 30;          // of workspace
 constexpr int CHUNK_WAVES = 4;
 constexpr int CHUNK_TILE = 128;                           // rows of a workgroup, 32 to each wave, where there are more than a few

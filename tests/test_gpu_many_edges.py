@@ -67,27 +67,49 @@ def test_one_token_of_a_long_context(dtype):
 
 @pytest.mark.parametrize("dtype", [F16, BF16, F32])
 def test_the_longest_contexts(dtype):
-    """As many slots as a page table may hold (its pages are the same three).  All scores are 0 and all values of a column the same, so each weighted sum is the sum of weights times a power of two."""
-    page, d = 1024, 8
+    """As many slots as a token may attend to, and, with a window, as a page table may hold (its pages are the same three).  All scores are 0 and all values of a column the same, so each weighted sum is
+    the sum of weights times a power of two: integers up to 2^26 and eight of them or more at a time, which binary32 holds."""
+    page, d, n = 1024, 8, 2 ** 26 - 5
     width = (MOST - 65536) // page
-    n = width * page - 5
-    k, v = torch.randn(3, 1, page, d, device=DEV).to(dtype), torch.zeros(3, 1, page, d, dtype=dtype, device=DEV)
+    k, v = torch.randn(3, 4, page, d, device=DEV).to(dtype), torch.zeros(3, 4, page, d, dtype=dtype, device=DEV)
     v[..., 0], v[..., 1] = 1, -0.5
     table = torch.zeros(2, width, dtype=torch.int32, device=DEV)
     table[:, 1::3], table[:, 2::3] = 1, 2
-    q = torch.zeros(2, 1, d, dtype=dtype, device=DEV)
-    lengths = torch.tensor([n, 100], dtype=torch.int32, device=DEV)
-    starts = torch.tensor([0, 1, 2], dtype=torch.int32, device=DEV)
-    out, lse = ann.ann_chunk_attention(q, k, v, table, lengths, starts)
-    # sums of up to 2^26 equal weights in binary32 by a lane may each be short by a part of 2^-24 at every step beyond 2^24 of them; out is a quotient of two that are alike
-    assert (out[:, 0, 0].float() - 1).abs().max() <= 2 * D.HALF_ULP[dtype] + 2.0 ** -20 and (out[:, 0, 1].float() + 0.5).abs().max() <= 2 * D.HALF_ULP[dtype] + 2.0 ** -20
-    assert abs(float(lse[0, 0]) - math.log(n)) < 1e-3 and abs(float(lse[1, 0]) - math.log(100)) < 1e-5
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+
+    def exact(out, lse, slots):
+        assert (out[..., 0].float() - 1).abs().max() <= 2 * D.HALF_ULP[dtype] and (out[..., 1].float() + 0.5).abs().max() <= 2 * D.HALF_ULP[dtype]
+        assert (lse.double() - torch.tensor(slots, dtype=torch.float64, device=DEV).log().view(-1, 1)).abs().max() <= 2.0 ** -17
+
+    q = torch.zeros(2, 4, d, dtype=dtype, device=DEV)
+    exact(*ann.ann_chunk_attention(q, k, v, table, ints(n, 100), ints(0, 1, 2), max_length=2 ** 26), [n, 100])
+    # many rows: not divided
+    rows = torch.zeros(600, 1024, d, dtype=dtype, device=DEV)[:, :4 if dtype == F32 else 512]
+    exact(*ann.ann_chunk_attention(rows, k, v, table, ints(n, 1000), ints(0, 100, 600), max_length=2 ** 26), [*range(n - 99, n + 1), *range(501, 1001)])
+    n = width * page - 5
+    exact(*ann.ann_chunk_attention(q, k, v, table, ints(n, 100), ints(0, 1, 2), window=5000), [5000, 100])
     # the same slots, a request's first part in common with another
-    lengths = torch.tensor([n, n], dtype=torch.int32, device=DEV)
-    for common in (0, 10 ** 9, MOST):
-        out, lse = ann.ann_shared_attention(q, k, v, table, lengths, torch.tensor([0, 2], dtype=torch.int32, device=DEV), torch.tensor([common], dtype=torch.int32, device=DEV))
-        assert (out[:, 0, 0].float() - 1).abs().max() <= 2 * D.HALF_ULP[dtype] + 2.0 ** -20
-        assert (lse - math.log(n)).abs().max() < 1e-3
+    n = 2 ** 26 + 10_000
+    for common in (0, 20_000, 5 * 10 ** 7, 2 ** 26):
+        exact(*ann.ann_shared_attention(q, k, v, table, ints(n, n), ints(0, 2), ints(common), max_shared=2 ** 26, max_own=2 ** 26), [min(n, common + 2 ** 26)] * 2)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+def test_sums_of_many_small_weights(dtype):
+    """One slot of a large score and many of equal small ones, whose weights are no powers of two: rounded at every one of them, sums would drift."""
+    n, G, T, d = 131_072, 24, 2048, 64
+    page = 256
+    k, v = torch.zeros(n // page, 1, page, d, device=DEV), torch.ones(n // page, 1, page, d, dtype=dtype, device=DEV)
+    k[0, 0, 0, 0] = 1
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    q = torch.zeros(T, G, d, device=DEV)
+    q[:, :, 0] = torch.arange(G, device=DEV) / 8 + 4      # scores of the one slot, exact in every type
+    table = torch.arange(n // page, dtype=torch.int32, device=DEV).view(1, -1)
+    out, lse = ann.ann_chunk_attention(q.to(dtype), k.to(dtype), v, table, ints(n), ints(0, T), scale=1.0, max_length=n)
+    slots = torch.arange(n - T, n, dtype=torch.float64)[:, None]
+    want = (torch.exp(torch.arange(G, dtype=torch.float64) / 8 + 4) + slots).log()
+    # a lane's sum: up to 2^12 tiles, each off by 2^-24 of the sum; a tile's: 32 weights; exponents, exp2 and the logarithm 2^-18 together
+    assert (lse.double().cpu() - want).abs().max() <= 2.0 ** -12 + 2.0 ** -19 + 2.0 ** -18
 
 
 def test_many_tokens():

@@ -46,6 +46,18 @@ def test_argument_errors(name, base, kw, code):
     assert binding.ann_last_error()
 
 
+def test_more_slots_than_a_sum_takes():
+    for most, window, code in ((2 ** 26 + 1, 0, E), (2 ** 27, 2 ** 26 + 1, E)):
+        assert call("ann_chunk_attention", CHUNK, width=2 ** 23, most=most, window=window) == code
+        assert binding.ann_last_error()
+        assert binding.lib().ann_chunk_attention_workspace_bytes(1, 1, 8, 2, 64, 0, most, window) == code
+    for kw in (dict(max_shared=2 ** 26 + 1), dict(max_own=2 ** 26 + 1)):
+        assert call("ann_shared_attention", SHARED, width=2 ** 23, **kw) == E
+        assert binding.lib().ann_shared_attention_workspace_bytes(1, 1, 8, 2, 64, 0, kw.get("max_shared", 64), kw.get("max_own", 80)) == E
+    assert binding.lib().ann_chunk_attention_workspace_bytes(1, 1, 8, 2, 64, 0, 2 ** 26, 0) > 0
+    assert binding.lib().ann_chunk_attention_workspace_bytes(1, 1, 8, 2, 64, 0, 2 ** 30, 2 ** 20) > 0
+
+
 def test_nothing_to_do():
     assert call("ann_rotate_append", APPEND, T=0) == 0 and call("ann_chunk_attention", CHUNK, T=0) == 0 and call("ann_shared_attention", SHARED, B=0) == 0
 
