@@ -1155,10 +1155,10 @@ struct ChunkPlan {
 };
 constexpr int64_t CHUNK_PARTS = 64;                       // of a row in a pass
 // Slots of a part of many rows, at least (fp32, whose products take 16 times as long, a quarter): what a part leaves is 4 (d + 4) bytes for each of its rows, written and read.  100 tokens, 32 heads of 128 to 8,
-// 1600 slots, bf16: 20.6 us with 256, 21.6 with 128; 200 slots 13.4 and 16.1.
+// 1600 slots, bf16: 20.2 us with 256, 20.9 with 128; 200 slots 14.4 and 15.7 (d = 64, 600 slots 16.5 and 14.8).
 constexpr int CHUNK_LEAST = 256;
-// Slots in common go through by few rows, in one launch with the own slots, up to so many operations.  33 requests in 4 groups, 14 heads of 64 to 2, 2000 slots in common (2.4e8): 17.4 us, by 128 rows and a launch of its
-// own 28.8; 64 requests in one group, 32 heads of 128 to 8, 8100 slots (8.5e9): 111 and 79.
+// Slots in common go through by few rows, in one launch with the own slots, up to so many operations.  33 requests in 4 groups, 14 heads of 64 to 2, 2000 slots in common (2.4e8): 15.5 us, by 128 rows and a launch of its
+// own 24.8; 64 requests in one group, 32 heads of 128 to 8, 8100 slots (8.5e9): 96 and 71.
 constexpr double CHUNK_SMALL = 1.0e9;
 // Sequences of `rows` rows in all, whose tiles go through `range` slots at most.
 inline ChunkPass chunk_pass(int mode, int cus, int elem_bytes, int d, int heads, int64_t rows, int64_t sequences, int64_t range, int64_t most_parts, bool small = false,
