@@ -11,7 +11,7 @@
 //
 // What bounds it is the matrix cores, and the power that they and the exponentials draw: 16384 tokens from nothing, 32 heads of 128 to 8, bf16, take 2.09 to 2.17 ms by the card (1.05 to 1.01 PFLOP/s; a large
 // library product reaches 1.36 on such data), at a clock of 1.8 GHz, the matrix cores busy for half of the time and the vector units for somewhat more; 24 passages of up to 300 tokens behind up to 8100
-// slots 347 us (0.82 PFLOP/s: a tenth goes to rows and slots that masks leave out, another to the last workgroups), d = 256 0.54 PFLOP/s, fp32 0.09 to 0.11 (a library product 0.15).
+// slots 347 us (0.82 PFLOP/s: a tenth goes to rows and slots that masks leave out, another to the last workgroups), d = 256 0.54 PFLOP/s, fp32 0.08 to 0.1 (a library product 0.15).
 // With all values 0 the prompt takes 1880 us: the clock.  Why so and not otherwise, the same prompt: 64 rows a wave do not fit its registers (3.5 ms); 256 rows a workgroup, 8 waves: no faster; four tiles of 32 slots
 // in flight for two of 64: 2.75 ms; a tile's sums by dot products of packed weights for sums of 32 bits: 2145 us; a word of each line of the tile behind the next read ahead into the second cache: 2460.
 #pragma once
@@ -382,20 +382,26 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(DP)) void chunk_
     auto times_v = [&](unsigned char *at_v, const f16v (&x)[NU], const u4 (&p)[NU][2]) __attribute__((always_inline)) {
         int m = lane & 31;
         if constexpr (WIDE) asm volatile("" : "+v"(m));
+        // fp32: a tile's products are summed alone, as its weights are, since the matrix cores add two slots at a time to a sum: equal weights over 8192 slots left it 1.2e-4 off without (a library product 3e-5).
+        // (2 x 1024 tokens of 4096: d = 128 742 us, 667 without; d = 64 357 and 340.)
+        if constexpr (WIDE) {
 #pragma unroll
-        for (int u = 0; u < NU; ++u) {
-            if constexpr (WIDE) {
+            for (int c = 0; c < NC; ++c) {
+                if (32 * c >= a.cache.d) break;           // (uniform)
+                f16v y = zero16();
 #pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    if (32 * c >= a.cache.d) break;       // (uniform)
+                for (int u = 0; u < NU; ++u)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int row = 32 * u + 8 * (i / 4) + 4 * h + i % 4;
                         const float v = *reinterpret_cast<const float *>(at_v + row * RB + (((8 * c + (m >> 2)) ^ chunk_swizzle<RB>(row)) << 4) + (m & 3) * 4);
-                        o[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, x[u][i], o[c], 0, 0, 0);
+                        y = __builtin_amdgcn_mfma_f32_32x32x2f32(v, x[u][i], y, 0, 0, 0);
                     }
-                }
-            } else {
+                o[c] += y;
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < NU; ++u)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     unsigned char *from = at_v + (32 * u + 16 * j) * RB + v_lane;
@@ -407,7 +413,6 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(DP)) void chunk_
                         o[c] = mfma32<T>(u4{v0[0], v0[1], v1[0], v1[1]}, p[u][j], o[c]);
                     }
                 }
-            }
         }
     };
     // Rows of V that some rows of queries attend to and others do not must be finite, or they would go into all: 0 times NaN is no 0.  What this wave loaded that is not is taken

@@ -110,6 +110,8 @@ def test_sums_of_many_small_weights(dtype):
     want = (torch.exp(torch.arange(G, dtype=torch.float64) / 8 + 4) + slots).log()
     # a lane's sum: up to 2^12 tiles, each off by 2^-24 of the sum; a tile's: 32 weights; exponents, exp2 and the logarithm 2^-18 together
     assert (lse.double().cpu() - want).abs().max() <= 2.0 ** -12 + 2.0 ** -19 + 2.0 ** -18
+    # products with V: fp32 2^12 tiles of 32, 16 bits eight slots at a time, and the weights' rounding and the output's; and the sum that they are divided by
+    assert (out.double() - 1).abs().max() <= (2.0 ** -12 + 2.0 ** -19 if dtype == F32 else 2.0 ** -10 + 2 * D.HALF_ULP[dtype]) + 2.0 ** -12 + 2.0 ** -18
 
 
 def test_many_tokens():
