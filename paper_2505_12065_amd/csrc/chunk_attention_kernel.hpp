@@ -762,18 +762,20 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE
                         }
                     }
             }
-        } else {
+        } else {                                          // (a step's products summed alone, as by many rows)
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+            for (int u = 0; u < NU; ++u)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int c = 0; c < CE; ++c)
 #pragma unroll
-                    for (int u = 0; u < NU; ++u)
+                    for (int mt = 0; mt < MT; ++mt) {
+                        f4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int c = 0; c < CE; ++c)
+                        for (int t = 0; t < NT; ++t)
 #pragma unroll
-                            for (int mt = 0; mt < MT; ++mt)
-                                o[mt][u * CE + c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[t][i][u][c]), x[mt][t][i], o[mt][u * CE + c], 0, 0, 0);
+                            for (int i = 0; i < 4; ++i) y = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[t][i][u][c]), x[mt][t][i], y, 0, 0, 0);
+                        o[mt][u * CE + c] += y;
+                    }
         }
         page = page_next;
     }

@@ -114,6 +114,24 @@ def test_sums_of_many_small_weights(dtype):
     assert (out.double() - 1).abs().max() <= (2.0 ** -12 + 2.0 ** -19 if dtype == F32 else 2.0 ** -10 + 2 * D.HALF_ULP[dtype]) + 2.0 ** -12 + 2.0 ** -18
 
 
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("common", [0, 131_072])
+def test_sums_of_many_small_weights_of_single_tokens(dtype, common):
+    """The same for so many requests that nothing is divided; all slots in common, or none."""
+    n, G, B, d, page = 131_072, 4, 16_384 if common else 600, 64, 256
+    k, v = torch.zeros(n // page, 1, page, d, device=DEV), torch.ones(n // page, 1, page, d, dtype=dtype, device=DEV)
+    k[0, 0, 0, 0] = 1
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    q = torch.zeros(B, G, d, device=DEV)
+    q[:, :, 0] = torch.arange(G, device=DEV) / 8 + 4.3125
+    table = torch.arange(n // page, dtype=torch.int32, device=DEV).repeat(B, 1)
+    out, lse = ann.ann_shared_attention(q.to(dtype), k.to(dtype), v, table, ints(*[n] * B), ints(0, B), ints(common), max_shared=common, max_own=page if common else n, scale=1.0)
+    want = (torch.exp(torch.arange(G, dtype=torch.float64) / 8 + 4.3125) + n - 1).log()
+    # as above; by few rows a wave has a quarter of the slots, 32 at a time, and weights of 16 bits are two operands
+    assert (lse.double().cpu() - want).abs().max() <= 2.0 ** -12 + 2.0 ** -19 + 2.0 ** -18
+    assert (out.double() - 1).abs().max() <= (2.0 ** -12 + 2.0 ** -19 if dtype == F32 else 2.0 ** -10 + 2 * D.HALF_ULP[dtype]) + 2.0 ** -12 + 2.0 ** -18
+
+
 def test_many_tokens():
     """More tokens than 16 bits number, whose rows are looked at here and there."""
     T, d, held = 70_000, 16, 37
