@@ -1128,7 +1128,7 @@ constexpr int CHUNK_SLOTS_MAX = 1 << 26;
 constexpr size_t CHUNK_WS_MAX = (size_t)1 << 30;          // of workspace
 constexpr int CHUNK_WAVES = 4;
 constexpr int CHUNK_TILE = 128;                           // rows of a workgroup, 32 to each wave, where there are more than a few
-// Waves on a SIMD, as registers allow, and so workgroups on a compute unit (2 x 1024 tokens of 4096, fp32, d = 128: 684 us, with one wave 727; the prompt of 8192 2626 and 2928).
+// Waves on a SIMD, as registers allow, and so workgroups on a compute unit (2 x 1024 tokens of 4096, fp32, d = 128: 751 us, with one wave 760; 8192 from nothing 2824 and 3045).
 constexpr int chunk_per_simd(int dp) { return dp == 256 ? 1 : 2; }
 // Slots of a tile: 64 wherever two tiles each of keys and values, for all the workgroups, fit a compute unit's shared memory (16 bits, d = 256, 4 x 1024 tokens of 8192, with 64 and 32: 955 us and 1189).
 constexpr int chunk_slots(int row_bytes, int per_simd) { return 4 * 64 * row_bytes * per_simd > 160 * 1024 ? 32 : 64; }
