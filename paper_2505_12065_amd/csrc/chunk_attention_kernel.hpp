@@ -9,11 +9,15 @@
 // numbered 8 h + 4 a + i for slot 8 a + 4 h + i: nothing passes between lanes but a maximum, and maxima, sums and factors belong to the lane's own row.  V^T comes from the rows of V as they
 // lie, by reads of LDS that turn 4 x 16 elements.
 //
-// What bounds it is the matrix cores, and the power that they and the exponentials draw: 16384 tokens from nothing, 32 heads of 128 to 8, bf16, take 2.09 to 2.17 ms by the card (1.05 to 1.01 PFLOP/s; a large
-// library product reaches 1.36 on such data), at a clock of 1.8 GHz, the matrix cores busy for half of the time and the vector units for somewhat more; 24 passages of up to 300 tokens behind up to 8100
+// What bounds it is the matrix cores, and the power that they and the exponentials draw: 16384 tokens from nothing, 32 heads of 128 to 8, bf16, take 2.09 to 2.17 ms by the card (1.05 to
+// 1.01 PFLOP/s; a large
+// library product reaches 1.36 on such data), at a clock of 1.8 GHz, the matrix cores busy for half of the time and the vector units for somewhat more; 24 passages of up to 300 tokens
+// behind up to 8100
 // slots 347 us (0.82 PFLOP/s: a tenth goes to rows and slots that masks leave out, another to the last workgroups), d = 256 0.54 PFLOP/s, fp32 0.08 to 0.1 (a library product 0.15).
-// With all values 0 the prompt takes 1880 us: the clock.  Why so and not otherwise, the same prompt: 64 rows a wave do not fit its registers (3.5 ms); 256 rows a workgroup, 8 waves: no faster; four tiles of 32 slots
-// in flight for two of 64: 2.75 ms; a tile's sums by dot products of packed weights for sums of 32 bits: 2145 us; a word of each line of the tile behind the next read ahead into the second cache: 2460.
+// With all values 0 the prompt takes 1880 us: the clock.  Why so and not otherwise, the same prompt: 64 rows a wave do not fit its registers (3.5 ms); 256 rows a workgroup, 8 waves: no
+// faster; four tiles of 32 slots
+// in flight for two of 64: 2.75 ms; a tile's sums by dot products of packed weights for sums of 32 bits: 2145 us; a word of each line of the tile behind the next read ahead into the second
+// cache: 2460.
 #pragma once
 
 #include <type_traits>
@@ -341,7 +345,8 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(DP)) void chunk_
                 if (!((bits >> (8 * (i / 4) + i % 4)) & 1)) x[u][i] = -INFINITY;
         }
     };
-    // Scores become weights; 16 bits: in p, as operands, rounded once.  (Two operands, what rounding the first leaves being the second, as where there are few rows and the matrix cores wait, would make the matrix
+    // Scores become weights; 16 bits: in p, as operands, rounded once.  (Two operands, what rounding the first leaves being the second, as where there are few rows and the matrix cores
+    // wait, would make the matrix
     // instructions that bound this loop half as many again.)
     auto weights = [&](f16v (&x)[NU], u4 (&p)[NU][2]) __attribute__((always_inline)) {
         float most = x[0][0];
@@ -382,7 +387,8 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(DP)) void chunk_
     auto times_v = [&](unsigned char *at_v, const f16v (&x)[NU], const u4 (&p)[NU][2]) __attribute__((always_inline)) {
         int m = lane & 31;
         if constexpr (WIDE) asm volatile("" : "+v"(m));
-        // fp32: a tile's products are summed alone, as its weights are, since the matrix cores add two slots at a time to a sum: equal weights over 8192 slots left it 1.2e-4 off without (a library product 3e-5).
+        // fp32: a tile's products are summed alone, as its weights are, since the matrix cores add two slots at a time to a sum: equal weights over 8192 slots left it 1.2e-4 off without (a
+        // library product 3e-5).
         // (2 x 1024 tokens of 4096: d = 128 742 us, 667 without; d = 64 357 and 340.)
         if constexpr (WIDE) {
 #pragma unroll
@@ -464,8 +470,10 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(DP)) void chunk_
         f16v x[NU];
         u4 p[NU][2];
         scores(at_k, k0, seen, x);
-        // Weights and their products go before another wave's scores, which need the matrix cores alone: of two waves on a SIMD one has something for each unit.  (A prompt of 16384 tokens, 32 heads of 128 to 8,
-        // bf16: 2216 us without and 2105 with it; of 8192, 16 heads to 8, fp32: d = 128 2619 and 2550, d = 64 1309 and 1174; d = 64, bf16, 4 x 1024 of 8192 206 and 199, but 24 x 170 of 4400 235 and 241.)
+        // Weights and their products go before another wave's scores, which need the matrix cores alone: of two waves on a SIMD one has something for each unit.  (A prompt of 16384 tokens,
+        // 32 heads of 128 to 8,
+        // bf16: 2216 us without and 2105 with it; of 8192, 16 heads to 8, fp32: d = 128 2619 and 2550, d = 64 1309 and 1174; d = 64, bf16, 4 x 1024 of 8192 206 and 199, but 24 x 170 of 4400
+        // 235 and 241.)
         constexpr bool FIRST = chunk_per_simd(DP) > 1;
         if constexpr (FIRST) __builtin_amdgcn_s_setprio(1);
         weights(x, p);
@@ -532,7 +540,8 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(DP)) void chunk_
 //
 // Up to 16 MT rows: the waves share the slots out, K and V go from memory to registers, and the tiles are of 16 slots and 16 rows, as in paged_attention_kernel: reading K and V once bounds it
 // (128 requests of 4096 slots, 64 heads of 128 to 8, bf16: 330 us, 6.5 TB/s; ragged ones of up to 2048 4.9 TB/s; fp32, 64 of 2048, 173 us, 6.1 TB/s);
-// with little to read it is a chain of dependent reads (five requests behind 2000 slots in common, 32 heads to 8: 10 us).  A passage of 100 tokens, 400 rows of a cache head, takes 36.8 us so and 20.7 by 128 rows.
+// with little to read it is a chain of dependent reads (five requests behind 2000 slots in common, 32 heads to 8: 10 us).  A passage of 100 tokens, 400 rows of a cache head, takes 36.8 us
+// so and 20.7 by 128 rows.
 // Lane 16 g + m has the scores of row m and slots 4 g .. 4 g + 3 of a tile; weights are operands of two parts.  Both passes of groups go in one launch where both have few rows.
 template <class T, int VE, int MT, bool FINE>
 __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE, MT)) void chunk_few_kernel(ChunkArgs a, ChunkPass first_pass, ChunkPass own_pass) {
@@ -853,7 +862,8 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE
     }
 }
 
-// What the parts of a row left, joined by a wave (bytes, or the launch: 34 MB of parts 8.6 us, the smallest 3.5; a join by the last workgroup of a row would want memory that is cleared beforehand), whose lanes share the parts out where a row takes fewer than there are.  The first part of a pass says how many there are, and the one of own slots whether
+// What the parts of a row left, joined by a wave (bytes, or the launch: 34 MB of parts 8.6 us, the smallest 3.5; a join by the last workgroup of a row would want memory that is cleared
+// beforehand), whose lanes share the parts out where a row takes fewer than there are.  The first part of a pass says how many there are, and the one of own slots whether
 // the row is in a group.
 template <class T>
 __global__ __launch_bounds__(256) void chunk_join_kernel(ChunkArgs a, int own_part0, bool new_tokens) {

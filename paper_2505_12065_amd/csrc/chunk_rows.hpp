@@ -1,7 +1,8 @@
 // Attention of many rows: which rows and slots a workgroup takes.
 //
 // A pass goes through tiles of `rows` rows of sequences of tokens: a request's new ones (CHUNK_NEW), the one of each request of a group (CHUNK_COMMON: the slots in common), or a
-// request's one (CHUNK_OWN: its own slots; CHUNK_ALL: those in common too).  A token has a row for each of the G query heads of a cache head.  Long ranges of slots are divided into parts.  How many tiles and slots there are is known on the
+// request's one (CHUNK_OWN: its own slots; CHUNK_ALL: those in common too).  A token has a row for each of the G query heads of a cache head.  Long ranges of slots are divided into parts.
+// How many tiles and slots there are is known on the
 // device alone; up to 64 sequences, a lane each, every workgroup works out for itself how the whole is dealt: parts as long as fill the card, longest sequences first.
 #pragma once
 
@@ -219,7 +220,8 @@ __device__ __forceinline__ ChunkDeal chunk_deal_of(const ChunkArgs &a, const Chu
     d.end = d.range.hi - d.first < chunk ? d.range.hi : d.first + chunk;
     return d;
 }
-// ... worked out by one wave: a SIMD has waves of several workgroups and issues for one at a time (8 requests of 2000 slots, 8 heads of 128: 20.4 us by each wave, 19.2 so; 128 x 125 slots 18.4 and 17.4).
+// ... worked out by one wave: a SIMD has waves of several workgroups and issues for one at a time (8 requests of 2000 slots, 8 heads of 128: 20.4 us by each wave, 19.2 so; 128 x 125 slots
+// 18.4 and 17.4).
 __device__ __forceinline__ ChunkDeal chunk_deal(const ChunkArgs &a, const ChunkPass &p, int item, int G) {
     constexpr int WORDS = sizeof(ChunkDeal) / 4;
     struct Words { int w[WORDS]; };

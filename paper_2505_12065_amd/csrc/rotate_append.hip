@@ -1,7 +1,8 @@
 // The position rotation of queries and keys, angles from frequencies, and keys and values put behind what each request holds in a paged cache.
 //
 // Every row is read once and written once: bytes bound it where there are many tokens, the launch and a chain of dependent reads (the token's request, its length, its
-// page) where there are few: 14039 tokens, 32 + 8 + 8 heads of 128, bf16, 67.7 us (345 MB, 5.1 TB/s; a copy reaches 4.7 to 5.0), 8 tokens 3.2 us, 5.1 with the host's launch.  An angle is a product in 64 bits, taken in turns and less its whole ones before it is rounded: in 32 bits position 100 000 would be off by 2^-8.
+// page) where there are few: 14039 tokens, 32 + 8 + 8 heads of 128, bf16, 67.7 us (345 MB, 5.1 TB/s; a copy reaches 4.7 to 5.0), 8 tokens 3.2 us, 5.1 with the host's launch.  An angle is a
+// product in 64 bits, taken in turns and less its whole ones before it is rounded: in 32 bits position 100 000 would be off by 2^-8.
 #include "launch.hpp"
 #include "packed.hpp"
 #include "paged.hpp"
