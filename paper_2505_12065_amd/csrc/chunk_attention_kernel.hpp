@@ -155,27 +155,32 @@ __device__ __forceinline__ ChunkSpan chunk_row_span(const ChunkArgs &a, int mode
     if (mode == CHUNK_NEW) return chunk_span(a, deal.k.length, deal.k.q.tokens - i);
     return {deal.range.lo, mode == CHUNK_COMMON ? min(deal.range.hi, chunk_length(a, t)) : deal.range.hi};
 }
+// A row without other parts is divided and written; else what joins the parts reads its elements, its statistics, how many parts there are and whether it is of a group.
+__device__ __forceinline__ bool chunk_whole(const ChunkArgs &a, const ChunkDeal &deal) { return a.splits == 1 || deal.alone; }
+__device__ __forceinline__ float chunk_by(float total) { return total == 0.f ? 0.f : 1.f / total; }
+__device__ __forceinline__ f4 chunk_divided(f4 y, float by) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = by == 0.f ? 0.f : y[i] * by;
+    return y;
+}
+__device__ __forceinline__ int64_t chunk_place(const ChunkArgs &a, const ChunkPass &pass, const ChunkDeal &deal, int row) { return (int64_t)row * a.splits + pass.part0 + deal.part; }
+__device__ __forceinline__ void chunk_statistics(const ChunkArgs &a, const ChunkPass &pass, const ChunkDeal &deal, int row, float most, float total) {
+    if (a.splits > 1) *reinterpret_cast<f4 *>(a.stats + 4 * chunk_place(a, pass, deal, row)) = f4{most, total, __int_as_float(deal.parts), __int_as_float(deal.k.grouped)};
+    if (a.lse && chunk_whole(a, deal)) a.lse[row] = chunk_lse(most, total, a.lift);
+}
 // Four elements of a row: divided and written if the row has no other parts, else left for what joins them.
 template <class T>
-__device__ __forceinline__ void chunk_write(const ChunkArgs &a, const ChunkPass &pass, const ChunkDeal &deal, int64_t row, int at, f4 y, float most, float total) {
-    if (a.splits > 1) {
-        const int64_t place = row * a.splits + pass.part0 + deal.part;
-        if (at == 0) *reinterpret_cast<f4 *>(a.stats + 4 * place) = f4{most, total, __int_as_float(deal.parts), __int_as_float(deal.k.grouped)};
-        if (!deal.alone) {
-            *reinterpret_cast<f4 *>(a.partial + place * a.cache.d + at) = y;
-            return;
-        }
+__device__ __forceinline__ void chunk_write(const ChunkArgs &a, const ChunkPass &pass, const ChunkDeal &deal, int row, int at, f4 y, float by) {
+    if (!chunk_whole(a, deal)) {
+        *reinterpret_cast<f4 *>(a.partial + chunk_place(a, pass, deal, row) * a.cache.d + at) = y;
+        return;
     }
-    const float by = total == 0.f ? 0.f : 1.f / total;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = total == 0.f ? 0.f : y[i] * by;
-    store_four<T>(static_cast<char *>(a.out) + (row * a.cache.d + at) * T::bytes, y);
-    if (at == 0 && a.lse) a.lse[row] = chunk_lse(most, total, a.lift);
+    store_four<T>(static_cast<char *>(a.out) + ((int64_t)row * a.cache.d + at) * T::bytes, chunk_divided(y, by));
 }
 // Row `in` of a deal, among those of all tokens.
-__device__ __forceinline__ int64_t chunk_row(const ChunkArgs &a, const ChunkDeal &deal, int head, int G, int in) {
+__device__ __forceinline__ int chunk_row(const ChunkArgs &a, const ChunkDeal &deal, int head, int G, int in) {
     const int r = deal.r0 + in;
-    return (int64_t)(deal.k.q.token0 + r / G) * a.q_heads + head * G + r % G;
+    return (deal.k.q.token0 + r / G) * a.q_heads + head * G + r % G;
 }
 
 // ---- 128 rows -------------------------------------------------------------------------------------------------
@@ -194,6 +199,16 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(DP)) void chunk_
     const ChunkDeal deal = chunk_deal(a, pass, blockIdx.x / a.cache.heads, G);
     if (deal.count <= 0) return;
     const int first = deal.first, end = deal.end;
+    const int32_t *table = a.table + (int64_t)deal.k.q.request * a.width;
+    const int slots_log = a.cache.slots_log, mask = (1 << slots_log) - 1;
+    // the page of slot k0 + lane % KT, or -1
+    auto look_up = [&](int k0) {
+        const int key = k0 + (lane & (KT - 1));
+        int page = -1;
+        if (key < end) page = table[key >> slots_log];
+        return (unsigned)page < (unsigned)a.cache.pages ? page : -1;
+    };
+    int pages = look_up(first), pages_next = look_up(first + KT);           // (asked for before the queries: they are waited for first)
 
     // this lane's row: its query and the slots that it attends to
     u4 q[NS];
@@ -221,15 +236,9 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(DP)) void chunk_
         }
     }
     int lo_most = lo, hi_least = hi;                      // of all rows of the wave
-#pragma unroll
-    for (int i = 1; i < 32; i *= 2) {
-        lo_most = max(lo_most, __shfl_xor(lo_most, i));
-        hi_least = min(hi_least, __shfl_xor(hi_least, i));
-        hi_most = max(hi_most, __shfl_xor(hi_most, i));
-    }
-    lo_most = __builtin_amdgcn_readfirstlane(lo_most);
-    hi_least = __builtin_amdgcn_readfirstlane(hi_least);
-    hi_most = __builtin_amdgcn_readfirstlane(hi_most);
+    lo_most = __builtin_amdgcn_readfirstlane(wave_max_of(lo_most));
+    hi_least = __builtin_amdgcn_readfirstlane(-wave_max_of(-hi_least));
+    hi_most = __builtin_amdgcn_readfirstlane(wave_max_of(hi_most));
     int all_lo = lo_most, all_hi = hi_least;              // ... of all waves that read the same slots
     {
         if (lane == 0) { s_lo[wave] = lo_most; s_hi[wave] = hi_least; }
@@ -242,16 +251,7 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(DP)) void chunk_
     }
 
     unsigned char *const mine = chunk_lds;
-    const int32_t *table = a.table + (int64_t)deal.k.q.request * a.width;
-    const int slots_log = a.cache.slots_log, mask = (1 << slots_log) - 1;
     const char *k_head = a.cache.k + head * a.cache.k_head, *v_head = a.cache.v + head * a.cache.v_head;
-    // the page of slot k0 + lane % KT, or -1
-    auto look_up = [&](int k0) {
-        const int key = k0 + (lane & (KT - 1));
-        int page = -1;
-        if (key < end) page = table[key >> slots_log];
-        return (unsigned)page < (unsigned)a.cache.pages ? page : -1;
-    };
     // Slots without a row take one of the first page's: their scores do not count, and of their values only that they are finite.
     const int first_row = wave * LOADS * RPI, in_load = lane / CPR, first_at = ((lane & (CPR - 1)) ^ chunk_swizzle<RB>(first_row + in_load)) * 16;
     auto issue = [&](int k0, int pages, unsigned char *to) __attribute__((always_inline)) {
@@ -447,13 +447,12 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(DP)) void chunk_
     };
 
     int k0 = first;
-    int pages = -1, buffer = 0;
+    int buffer = 0;
     uint64_t valid = 0;
     if (k0 < end) {
-        pages = look_up(k0);
         issue(k0, pages, mine);
         valid = __ballot(pages >= 0) & ALL;
-        pages = look_up(k0 + KT);
+        pages = pages_next;
     }
     for (; k0 < end; k0 += KT, buffer ^= 1) {
         unsigned char *at_k = mine + buffer * 2 * Sh::TILE;
@@ -507,33 +506,50 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(DP)) void chunk_
         sum = __uint_as_float(b0) + __uint_as_float(b1);
         top *= scale;                                     // an exponent of 2
     }
-    // Written by way of LDS, 32 elements of all the wave's rows at a time, so that eight lanes write 128 bytes of a row.
-    constexpr int LD = 36, PER = WAVE / 8;
+    // Written by way of LDS, 32 or 64 elements of all the wave's rows at a time, so that eight lanes write 128 bytes of a row.  (A workgroup alone on its compute unit, two tiles: 2 us
+    // of 9, instructions for the most part; 3 while every element's place, division and statistics were worked out where it was written.)
+    constexpr int PER = WAVE / 8, CH = NC > 1 && WAVES * 32 * 68 * 4 <= Sh::LDS ? 2 : 1, LD = 32 * CH + 4;
     float *turn = reinterpret_cast<float *>(chunk_lds) + wave * 32 * LD;
-    int64_t rows[32 / PER];
-    float tops[32 / PER], sums[32 / PER];
-#pragma unroll
-    for (int k = 0; k < 32 / PER; ++k) {
-        const int in = k * PER + lane / 8;
-        rows[k] = chunk_row(a, deal, head, G, min(row0 + in, deal.count - 1));
-        tops[k] = __shfl(top, in);
-        sums[k] = __shfl(sum, in);
-    }
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        if (32 * c >= a.cache.d) break;
-#pragma unroll
-        for (int i = 0; i < 16; i += 4) *reinterpret_cast<f4 *>(turn + m * LD + 2 * i + 4 * h) = f4{o[c][i], o[c][i + 1], o[c][i + 2], o[c][i + 3]};
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");              // (what the wave itself wrote)
-        const int at = 32 * c + lane % 8 * 4;
+    const int my_row = chunk_row(a, deal, head, G, min(row0 + m, deal.count - 1));
+    const float my_by = chunk_by(sum);
+    if (h == 0 && row0 + m < deal.count) chunk_statistics(a, pass, deal, my_row, top, sum);
+    auto write = [&](auto whole) __attribute__((always_inline)) {
+        constexpr int BYTES = decltype(whole)::value ? T::bytes : 4;
+        char *to[32 / PER];
+        float by[32 / PER];
 #pragma unroll
         for (int k = 0; k < 32 / PER; ++k) {
-            const int in = k * PER + lane / 8;
-            const f4 y = *reinterpret_cast<const f4 *>(turn + in * LD + lane % 8 * 4);
-            if (row0 + in < deal.count && at < a.cache.d) chunk_write<T>(a, pass, deal, rows[k], at, y, tops[k], sums[k]);
+            const int in = k * PER + lane / 8, row = __shfl(my_row, in);
+            by[k] = __shfl(my_by, in);
+            if constexpr (decltype(whole)::value) to[k] = static_cast<char *>(a.out) + (int64_t)row * a.cache.d * BYTES;
+            else to[k] = reinterpret_cast<char *>(a.partial + chunk_place(a, pass, deal, row) * a.cache.d);
+            to[k] += lane % 8 * 4 * BYTES;
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    }
+#pragma unroll
+        for (int c = 0; c < NC; c += CH) {
+            if (32 * c >= a.cache.d) break;
+#pragma unroll
+            for (int cc = 0; cc < CH; ++cc)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4)
+                    *reinterpret_cast<f4 *>(turn + m * LD + 32 * cc + 2 * i + 4 * h) = f4{o[c + cc][i], o[c + cc][i + 1], o[c + cc][i + 2], o[c + cc][i + 3]};
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");          // (what the wave itself wrote)
+#pragma unroll
+            for (int k = 0; k < 32 / PER; ++k) {
+                const int in = k * PER + lane / 8;
+#pragma unroll
+                for (int cc = 0; cc < CH; ++cc) {
+                    f4 y = *reinterpret_cast<const f4 *>(turn + in * LD + 32 * cc + lane % 8 * 4);
+                    if (row0 + in >= deal.count || 32 * (c + cc) + lane % 8 * 4 >= a.cache.d) continue;
+                    if constexpr (decltype(whole)::value) store_four<T>(to[k] + 32 * (c + cc) * BYTES, chunk_divided(y, by[k]));
+                    else *reinterpret_cast<f4 *>(to[k] + 32 * (c + cc) * BYTES) = y;
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+    };
+    if (chunk_whole(a, deal)) write(std::true_type{});
+    else write(std::false_type{});
 }
 
 // ---- few rows -------------------------------------------------------------------------------------------------
@@ -549,6 +565,8 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE
     typedef typename Words<Sh::CW>::type VChunk;
     constexpr int NT = Sh::NT, NS = Sh::NS, NU = Sh::NU, CE = Sh::CE, WAVES = CHUNK_WAVES, STEP = 16 * NT * WAVES, ROWS = 16 * MT, LD = attend_lds_row(VE);
     extern __shared__ __align__(16) float few_lds[];
+    __shared__ int s_row[ROWS];
+    __shared__ float s_by[ROWS];
     const int lane = threadIdx.x & (WAVE - 1), g = lane >> 4, m = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const int G = a.q_heads / a.cache.heads, head = blockIdx.x % a.cache.heads, item = blockIdx.x / a.cache.heads;
@@ -844,12 +862,9 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE
                     }
         }
     }
-    __syncthreads();
-    const int per_row = a.cache.d / 4;
-    for (int i = threadIdx.x; i < deal.count * per_row; i += WAVES * WAVE) {
-        const int in = i / per_row, at = i % per_row * 4;
+    if ((int)threadIdx.x < deal.count) {                  // (wave 0: what belongs to a row)
+        const int in = threadIdx.x, row = chunk_row(a, deal, head, G, in);
         float most = -INFINITY, total = 0.f;
-        f4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) most = fmaxf(most, s_top[w * ROWS + in]);
 #pragma unroll
@@ -857,8 +872,17 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE
             const float t = s_top[w * ROWS + in];
             total += s_sum[w * ROWS + in] * (t == -INFINITY ? 1.f : exp2_fast(t - most));
         }
+        s_row[in] = row;
+        s_by[in] = chunk_by(total);
+        chunk_statistics(a, pass, deal, row, most, total);
+    }
+    __syncthreads();
+    const int per_row = a.cache.d / 4;
+    for (int i = threadIdx.x; i < deal.count * per_row; i += WAVES * WAVE) {
+        const int in = i / per_row, at = i % per_row * 4;
+        f4 y = {0.f, 0.f, 0.f, 0.f};
         for (int w = 0; w < used; ++w) y += *reinterpret_cast<const f4 *>(s_o + (w * deal.count + in) * LD + at);
-        chunk_write<T>(a, pass, deal, chunk_row(a, deal, head, G, in), at, y, most, total);
+        chunk_write<T>(a, pass, deal, s_row[in], at, y, s_by[in]);
     }
 }
 
