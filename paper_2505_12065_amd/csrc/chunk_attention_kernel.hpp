@@ -51,9 +51,9 @@ __device__ __forceinline__ void store_four<BF16>(char *to, f4 y) {
     typedef __bf16 b4 __attribute__((ext_vector_type(4)));
     *reinterpret_cast<b4 *>(to) = b4{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
 }
-// From the largest score, as an exponent of 2, and the sum of weights, 2^lift times as large.
-__device__ __forceinline__ float chunk_lse(float most, float total, float lift) {
-    return total == 0.f ? -INFINITY : ((most == -INFINITY ? 0.f : most) - lift) * 0.6931471805599453f + logf(total);
+// From what the weights' exponents are less (the largest score as an exponent of 2, or one near it, less the lift) and their sum.
+__device__ __forceinline__ float chunk_lse(float less, float total) {
+    return total == 0.f ? -INFINITY : (less == -INFINITY ? 0.f : less) * 0.6931471805599453f + logf(total);
 }
 
 // until at most n of this wave's loads are outstanding
@@ -157,7 +157,17 @@ __device__ __forceinline__ ChunkSpan chunk_row_span(const ChunkArgs &a, int mode
 }
 // A row without other parts is divided and written; else what joins the parts reads its elements, its statistics, how many parts there are and whether it is of a group.
 __device__ __forceinline__ bool chunk_whole(const ChunkArgs &a, const ChunkDeal &deal) { return a.splits == 1 || deal.alone; }
-__device__ __forceinline__ float chunk_by(float total) { return total == 0.f ? 0.f : 1.f / total; }
+// Weights are 2^lift times what they are.  16 bits: by their exponents, before they are rounded.  fp32: exponents would be rounded to the lift's last place (20: 2^-20, and not the 2^-23 of those that count, which
+// left outputs and statistics twice as far off): they are less by 2^-6, so that 64 slots' products are no larger than the largest value, and sums of these are multiplied by the rest.
+constexpr float CHUNK_LIFT_F32 = -6.f;
+template <class T>
+__device__ __forceinline__ float chunk_lift_exponent(const ChunkArgs &a) { return T::bytes == 4 ? CHUNK_LIFT_F32 : a.lift; }
+template <class T>
+__device__ __forceinline__ float chunk_lift_factor(const ChunkArgs &a) {
+    return T::bytes == 4 ? __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((127 + (int)(a.lift - CHUNK_LIFT_F32)) << 23)) : 1.f;
+}
+template <class T>
+__device__ __forceinline__ float chunk_by(const ChunkArgs &a, float total) { return total == 0.f ? 0.f : 1.f / (total * chunk_lift_factor<T>(a)); }
 __device__ __forceinline__ f4 chunk_divided(f4 y, float by) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) y[i] = by == 0.f ? 0.f : y[i] * by;
@@ -166,7 +176,7 @@ __device__ __forceinline__ f4 chunk_divided(f4 y, float by) {
 __device__ __forceinline__ int64_t chunk_place(const ChunkArgs &a, const ChunkPass &pass, const ChunkDeal &deal, int row) { return (int64_t)row * a.splits + pass.part0 + deal.part; }
 __device__ __forceinline__ void chunk_statistics(const ChunkArgs &a, const ChunkPass &pass, const ChunkDeal &deal, int row, float most, float total) {
     if (a.splits > 1) *reinterpret_cast<f4 *>(a.stats + 4 * chunk_place(a, pass, deal, row)) = f4{most, total, __int_as_float(deal.parts), __int_as_float(deal.k.grouped)};
-    if (a.lse && chunk_whole(a, deal)) a.lse[row] = chunk_lse(most, total, a.lift);
+    if (a.lse && chunk_whole(a, deal)) a.lse[row] = chunk_lse(most, total);
 }
 // Four elements of a row: divided and written if the row has no other parts, else left for what joins them.
 template <class T>
@@ -190,6 +200,7 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(DP)) void chunk_
     typedef ChunkShape<T, DP> Sh;
     constexpr int KT = Sh::KT, RB = Sh::RB, NS = Sh::NS, NC = Sh::NC, NU = Sh::NU, LOADS = Sh::LOADS, CPR = Sh::CPR, RPI = Sh::RPI, WAVES = Sh::WAVES;
     constexpr bool WIDE = T::bytes == 4;
+    constexpr float RISE = WIDE ? 0.f : 8.f;
     constexpr int AHEAD = DP == 128 ? 6 : 4;              // reads of LDS in flight before a product
     extern __shared__ __align__(16) unsigned char chunk_lds[];
     __shared__ int s_lo[WAVES], s_hi[WAVES], s_bad[2];
@@ -298,7 +309,9 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(DP)) void chunk_
     f16v o[NC];
 #pragma unroll
     for (int c = 0; c < NC; ++c) o[c] = zero16();
-    float top = -INFINITY, sum = 0.f;                     // a score that the weights go by; the sum of this lane's slots alone
+    // What exponents are less, of a score that the weights go by; the sum of this lane's slots alone.  (Everything that compares weights goes by this one rounded number, not by the score: they would differ by
+    // its rounding, 2^-24 of a score times 1 / ln 2.)
+    float off = -INFINITY, sum = 0.f;
     const int k_lane = m * RB, k_turn_of_lane = (h ^ chunk_swizzle<RB>(m)) << 4;    // a lane's part of the places of its operands
     const int i16 = lane & 15, v_row = 4 * h + (i16 >> 2), v_lane = v_row * RB;
     const int v_turn = ((2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1)) ^ chunk_swizzle<RB>(v_row)) << 4 | (i16 & 1) << 3;
@@ -357,23 +370,24 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(DP)) void chunk_
         uint32_t b0, b1;
         row_pair<32>(__float_as_uint(most), b0, b1);
         most = fmaxf(__uint_as_float(b0), __uint_as_float(b1));
-        // The largest score may pass the one that the weights go by by a factor of 2^8 before all that there is of the row is scaled again.
-        const bool rise = (most - top) * scale > 8.f;
+        // 16 bits: the largest score may pass the one that the weights go by by a factor of 2^8 before all that there is of the row is scaled again.
+        const float next = fmaf(most, scale, -chunk_lift_exponent<T>(a));
+        const bool rise = next - off > RISE;
         if (__ballot(rise)) {
-            const float keep = rise ? exp2_fast((top - most) * scale) : 1.f;
-            if (rise) top = most;
+            const float keep = rise ? exp2_fast(off - next) : 1.f;
+            if (rise) off = next;
             sum *= keep;
 #pragma unroll
             for (int c = 0; c < NC; ++c) o[c] *= keep;
         }
-        const float off = (top == -INFINITY ? 0.f : top * scale) - a.lift;
+        const float less = off == -INFINITY ? 0.f : off;
         float tile = 0.f;                                 // (summed alone: a weight at a time, a sum of n of them may be off by n 2^-24)
 #pragma unroll
         for (int u = 0; u < NU; ++u) {
             float w[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                w[i] = exp2_fast(fmaf(x[u][i], scale, -off));
+                w[i] = exp2_fast(fmaf(x[u][i], scale, -less));
                 tile += w[i];
                 if constexpr (WIDE) x[u][i] = w[i];
             }
@@ -391,6 +405,7 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(DP)) void chunk_
         // library product 3e-5).
         // (2 x 1024 tokens of 4096: d = 128 742 us, 667 without; d = 64 357 and 340.)
         if constexpr (WIDE) {
+            const float up = chunk_lift_factor<T>(a);
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 if (32 * c >= a.cache.d) break;           // (uniform)
@@ -403,7 +418,7 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(DP)) void chunk_
                         const float v = *reinterpret_cast<const float *>(at_v + row * RB + (((8 * c + (m >> 2)) ^ chunk_swizzle<RB>(row)) << 4) + (m & 3) * 4);
                         y = __builtin_amdgcn_mfma_f32_32x32x2f32(v, x[u][i], y, 0, 0, 0);
                     }
-                o[c] += y;
+                o[c] += y * up;
             }
         } else {
 #pragma unroll
@@ -504,15 +519,14 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(DP)) void chunk_
         uint32_t b0, b1;
         row_pair<32>(__float_as_uint(sum), b0, b1);
         sum = __uint_as_float(b0) + __uint_as_float(b1);
-        top *= scale;                                     // an exponent of 2
     }
     // Written by way of LDS, 32 or 64 elements of all the wave's rows at a time, so that eight lanes write 128 bytes of a row.  (A workgroup alone on its compute unit, two tiles: 2 us
     // of 9, instructions for the most part; 3 while every element's place, division and statistics were worked out where it was written.)
     constexpr int PER = WAVE / 8, CH = NC > 1 && WAVES * 32 * 68 * 4 <= Sh::LDS ? 2 : 1, LD = 32 * CH + 4;
     float *turn = reinterpret_cast<float *>(chunk_lds) + wave * 32 * LD;
     const int my_row = chunk_row(a, deal, head, G, min(row0 + m, deal.count - 1));
-    const float my_by = chunk_by(sum);
-    if (h == 0 && row0 + m < deal.count) chunk_statistics(a, pass, deal, my_row, top, sum);
+    const float my_by = chunk_by<T>(a, sum);
+    if (h == 0 && row0 + m < deal.count) chunk_statistics(a, pass, deal, my_row, off, sum);
     auto write = [&](auto whole) __attribute__((always_inline)) {
         constexpr int BYTES = decltype(whole)::value ? T::bytes : 4;
         char *to[32 / PER];
@@ -749,14 +763,14 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) most = fmaxf(most, x[mt][t][i]);
-            const float now = fmaxf(top[mt], column_max(most)), keep = top[mt] == now ? 1.f : exp2_fast((top[mt] - now) * scale), off = (now == -INFINITY ? 0.f : now * scale) - a.lift;
-            top[mt] = now;
+            const float now = fmaxf(top[mt], fmaf(column_max(most), scale, -chunk_lift_exponent<T>(a))), keep = top[mt] == now ? 1.f : exp2_fast(top[mt] - now), less = now == -INFINITY ? 0.f : now;
+            top[mt] = now;                                // (as by many rows: what exponents are less)
             float tile = 0.f;
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    x[mt][t][i] = exp2_fast(fmaf(x[mt][t][i], scale, -off));
+                    x[mt][t][i] = exp2_fast(fmaf(x[mt][t][i], scale, -less));
                     tile += x[mt][t][i];
                 }
             sum[mt] = sum[mt] * keep + tile;
@@ -790,6 +804,7 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE
                     }
             }
         } else {                                          // (a step's products summed alone, as by many rows)
+            static_assert(16 * NT <= 64, "as the lift is for");
 #pragma unroll
             for (int u = 0; u < NU; ++u)
 #pragma unroll
@@ -801,7 +816,7 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE
                         for (int t = 0; t < NT; ++t)
 #pragma unroll
                             for (int i = 0; i < 4; ++i) y = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[t][i][u][c]), x[mt][t][i], y, 0, 0, 0);
-                        o[mt][u * CE + c] += y;
+                        o[mt][u * CE + c] += y * chunk_lift_factor<T>(a);
                     }
         }
         page = page_next;
@@ -836,7 +851,6 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
         sum[mt] = column_sum(sum[mt]);
-        top[mt] *= scale;                                 // an exponent of 2
         if (g == 0) {
             s_top[wave * ROWS + 16 * mt + m] = top[mt];
             s_sum[wave * ROWS + 16 * mt + m] = sum[mt];
@@ -873,7 +887,7 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE
             total += s_sum[w * ROWS + in] * (t == -INFINITY ? 1.f : exp2_fast(t - most));
         }
         s_row[in] = row;
-        s_by[in] = chunk_by(total);
+        s_by[in] = chunk_by<T>(a, total);
         chunk_statistics(a, pass, deal, row, most, total);
     }
     __syncthreads();
@@ -939,11 +953,8 @@ __global__ __launch_bounds__(256) void chunk_join_kernel(ChunkArgs a, int own_pa
         for (int j = 0; j < 4; ++j) y[j] += __shfl_xor(y[j], i);
     }
     if (lane >= per || at >= d) return;
-    const float by = total == 0.f ? 0.f : 1.f / total;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = total == 0.f ? 0.f : y[i] * by;
-    store_four<T>(static_cast<char *>(a.out) + (row * d + at) * T::bytes, y);
-    if (lane == 0 && a.lse) a.lse[row] = chunk_lse(most, total, a.lift);
+    store_four<T>(static_cast<char *>(a.out) + (row * d + at) * T::bytes, chunk_divided(y, chunk_by<T>(a, total)));
+    if (lane == 0 && a.lse) a.lse[row] = chunk_lse(most, total);
 }
 
 template <class T, int DP>

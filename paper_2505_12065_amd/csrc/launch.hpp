@@ -198,7 +198,7 @@ struct ChunkArgs {
     int coarse;               // pages of at least 16 slots, whose strides are short
     float lift;               // weights are 2^lift times as large until they are divided
     int splits;               // parts that a row may have, of both passes
-    float *partial, *stats;   // [rows, splits, d], [rows, splits, 4] (largest exponent, sum, parts of its pass, in a group) if there are more than one
+    float *partial, *stats;   // [rows, splits, d], [rows, splits, 4] (what exponents are less, sum, parts of its pass, in a group) if there are more than one
 };
 hipError_t launch_chunk_attention_f16(const ChunkArgs &args, const ChunkPlan &pl, hipStream_t stream);
 hipError_t launch_chunk_attention_bf16(const ChunkArgs &args, const ChunkPlan &pl, hipStream_t stream);

@@ -1128,7 +1128,7 @@ constexpr int CHUNK_SLOTS_MAX = 1 << 26;
 constexpr size_t CHUNK_WS_MAX = (size_t)1 << 30;          // of workspace
 constexpr int CHUNK_WAVES = 4;
 constexpr int CHUNK_TILE = 128;                           // rows of a workgroup, 32 to each wave, where there are more than a few
-// Waves on a SIMD, as registers allow, and so workgroups on a compute unit (2 x 1024 tokens of 4096, fp32, d = 128: 751 us, with one wave 760; 8192 from nothing 2824 and 3045).
+// Waves on a SIMD, as registers allow, and so workgroups on a compute unit (2 x 1024 tokens of 4096, fp32, d = 128: 751 us, with one wave 760; 8192 from nothing 2824 and 3045: before exponents were without the lift, which costs 2 %).
 constexpr int chunk_per_simd(int dp) { return dp == 256 ? 1 : 2; }
 // Slots of a tile: 64 wherever two tiles each of keys and values, for all the workgroups, fit a compute unit's shared memory (16 bits, d = 256, 4 x 1024 tokens of 8192, with 64 and 32: 955 us and 1189).
 constexpr int chunk_slots(int row_bytes, int per_simd) { return 4 * 64 * row_bytes * per_simd > 160 * 1024 ? 32 : 64; }
@@ -1236,7 +1236,7 @@ inline ChunkPlan shared_plan(int cus, int elem_bytes, int d, int q_heads, int he
     return pl;
 }
 // Weights of the product with V.  fp16 has no numbers below 2^-24, and 65504 is its largest: 2^7 times as large they may still be 2^8 times that.  bf16 and fp32 have values up to the largest of the sums' 32
-// bits: as much smaller as there are slots to sum, and by the 2^8.
+// bits: as much smaller as there are slots to sum, and by the 2^8 (which fp32 does without).
 inline float chunk_lift(int dtype, int64_t slots) {
     int bits = 0;
     while (slots >> bits) ++bits;

@@ -132,6 +132,35 @@ def test_sums_of_many_small_weights_of_single_tokens(dtype, common):
     assert (out.double() - 1).abs().max() <= (2.0 ** -12 + 2.0 ** -19 if dtype == F32 else 2.0 ** -10 + 2 * D.HALF_ULP[dtype]) + 2.0 ** -12 + 2.0 ** -18
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T,n,common", [(1, 6000, None), (100, 6000, None), (5, 3000, 2990), (70, 9000, 8000), (600, 700, None)])
+def test_parts_of_large_scores(dtype, T, n, common):
+    """Scores near 1000, exact in every type, a part's largest not another's: what parts say of themselves has to be as exact as their weights."""
+    d, heads, page = 64, 2, 16
+    g = torch.Generator().manual_seed(n)
+    width = (n + page - 1) // page
+    k, v = torch.zeros(width, heads, page, d), torch.randn(width, heads, page, d, generator=g).to(dtype)
+    k[..., 0], k[..., 1] = 1, torch.randint(0, 5, (width, heads, page), generator=g) + 3 * (torch.arange(width) // 16 % 2)[:, None, None]
+    q = torch.zeros(T, heads, d)
+    q[..., 0], q[..., 1] = 992, 1
+    table = torch.randperm(width, generator=g).to(torch.int32).view(1, -1)
+    if common is None:
+        spans = M.chunk_spans([T], [n], n, 0, T)
+        out, lse = ann.ann_chunk_attention(dev(q.to(dtype)), dev(k.to(dtype)), dev(v), dev(table), dev(M.ints([n])), dev(M.ints([0, T])), scale=1.0, max_length=n)
+    else:
+        table = table.repeat(T, 1)
+        spans = [(b, 0, n) for b in range(T)]
+        out, lse = ann.ann_shared_attention(dev(q.to(dtype)), dev(k.to(dtype)), dev(v), dev(table), dev(M.ints([n] * T)), dev(M.ints([0, T])), dev(M.ints([common])), max_shared=common,
+                                            max_own=n - common, scale=1.0)
+    want, want_lse = (torch.from_numpy(x) for x in M.attention(q.to(dtype), k.to(dtype), v, table, spans, 1.0)[:2])
+    # differences of scores up to 7, as exponents of 2 up to 10.1: off by 2^-25 of them as 1 / ln 2 is rounded, 2^-24 each as exponents and as differences of parts; exp2 2^-22; sums 2^-15
+    slack = 10.1 * 3 * 2.0 ** -24 + 2.0 ** -22 + 2.0 ** -15
+    most = float(v.abs().max())
+    assert (out.double().cpu() - want).abs().max() <= (slack + (3 * D.HALF_ULP[dtype] if dtype != F32 else 0)) * most
+    # ... which 1000 / ln 2 is off by 2^-24 of, and its rounding, as ln 2's, and the logarithm's
+    assert (lse.double().cpu() - want_lse).abs().max() <= 1000 * 3 * 2.0 ** -24 + slack
+
+
 def test_many_tokens():
     """More tokens than 16 bits number, whose rows are looked at here and there."""
     T, d, held = 70_000, 16, 37
