@@ -9,15 +9,12 @@
 // numbered 8 h + 4 a + i for slot 8 a + 4 h + i: nothing passes between lanes but a maximum, and maxima, sums and factors belong to the lane's own row.  V^T comes from the rows of V as they
 // lie, by reads of LDS that turn 4 x 16 elements.
 //
-// What bounds it is the matrix cores, and the power that they and the exponentials draw: 16384 tokens from nothing, 32 heads of 128 to 8, bf16, take 2.09 to 2.17 ms by the card (1.05 to
-// 1.01 PFLOP/s; a large
-// library product reaches 1.36 on such data), at a clock of 1.8 GHz, the matrix cores busy for half of the time and the vector units for somewhat more; 24 passages of up to 300 tokens
-// behind up to 8100
-// slots 347 us (0.82 PFLOP/s: a tenth goes to rows and slots that masks leave out, another to the last workgroups), d = 256 0.54 PFLOP/s, fp32 0.08 to 0.1 (a library product 0.15).
-// With all values 0 the prompt takes 1880 us: the clock.  Why so and not otherwise, the same prompt: 64 rows a wave do not fit its registers (3.5 ms); 256 rows a workgroup, 8 waves: no
-// faster; four tiles of 32 slots
-// in flight for two of 64: 2.75 ms; a tile's sums by dot products of packed weights for sums of 32 bits: 2145 us; a word of each line of the tile behind the next read ahead into the second
-// cache: 2460.
+// What bounds it is the matrix cores, and the power that they and the exponentials draw: 16384 tokens from nothing, 32 heads of 128 to 8, bf16, take 2.09 to 2.23 ms by the card (1.05 to 0.99 PFLOP/s;
+// a large library product reaches 1.36 on such data), at a clock of 1.8 GHz, the matrix cores busy for half of the time and the vector units for somewhat more; 24 passages of up to 300 tokens behind
+// up to 8100 slots 347 to 388 us (0.82 to 0.73 PFLOP/s: a tenth goes to rows and slots that masks leave out, another to the last workgroups), d = 256 0.54 PFLOP/s, fp32 0.08 to 0.1 (a library product
+// 0.15). With all values 0 the prompt takes 1880 us: the clock.
+// Why so and not otherwise, the same prompt: 64 rows a wave do not fit its registers (3.5 ms); 256 rows a workgroup, 8 waves: no faster; four tiles of 32 slots in flight for two of 64: 2.75 ms; a
+// tile's sums by dot products of packed weights for sums of 32 bits: 2145 us; a word of each line of the tile behind the next read ahead into the second cache: 2460.
 #pragma once
 
 #include <type_traits>
@@ -358,9 +355,8 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(DP)) void chunk_
                 if (!((bits >> (8 * (i / 4) + i % 4)) & 1)) x[u][i] = -INFINITY;
         }
     };
-    // Scores become weights; 16 bits: in p, as operands, rounded once.  (Two operands, what rounding the first leaves being the second, as where there are few rows and the matrix cores
-    // wait, would make the matrix
-    // instructions that bound this loop half as many again.)
+    // Scores become weights; 16 bits: in p, as operands, rounded once.  (Two operands, what rounding the first leaves being the second, as where there are few rows and the matrix cores wait, would make the
+    // matrix instructions that bound this loop half as many again.)
     auto weights = [&](f16v (&x)[NU], u4 (&p)[NU][2]) __attribute__((always_inline)) {
         float most = x[0][0];
 #pragma unroll
@@ -484,10 +480,8 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(DP)) void chunk_
         f16v x[NU];
         u4 p[NU][2];
         scores(at_k, k0, seen, x);
-        // Weights and their products go before another wave's scores, which need the matrix cores alone: of two waves on a SIMD one has something for each unit.  (A prompt of 16384 tokens,
-        // 32 heads of 128 to 8,
-        // bf16: 2216 us without and 2105 with it; of 8192, 16 heads to 8, fp32: d = 128 2619 and 2550, d = 64 1309 and 1174; d = 64, bf16, 4 x 1024 of 8192 206 and 199, but 24 x 170 of 4400
-        // 235 and 241.)
+        // Weights and their products go before another wave's scores, which need the matrix cores alone: of two waves on a SIMD one has something for each unit.  (A prompt of 16384 tokens, 32 heads of 128 to 8,
+        // bf16: 2216 us without and 2105 with it; of 8192, 16 heads to 8, fp32: d = 128 2619 and 2550, d = 64 1309 and 1174; d = 64, bf16, 4 x 1024 of 8192 206 and 199, but 24 x 170 of 4400 235 and 241.)
         constexpr bool FIRST = chunk_per_simd(DP) > 1;
         if constexpr (FIRST) __builtin_amdgcn_s_setprio(1);
         weights(x, p);
