@@ -33,7 +33,9 @@ __device__ __forceinline__ ChunkGroup chunk_group(const ChunkArgs &a, int t) {
     if (a.groups < WAVE) {
         const int lane = threadIdx.x & (WAVE - 1), start = lane <= a.groups ? packed_start(a.group_starts, lane, a.tokens) : INT_MAX, common = lane < a.groups ? chunk_common(a, lane) : 0;
         for (int g = 0; g <= a.groups; ++g) n += __builtin_amdgcn_readlane(start, g) <= t;
-        return n > 0 && n <= a.groups ? ChunkGroup{n - 1, __shfl(common, n - 1)} : ChunkGroup{-1, 0};
+        const bool in = n > 0 && n <= a.groups;
+        const int mine = __shfl(common, in ? n - 1 : 0);  // (by all lanes: a lane whose request is in no group may hold what others ask for, and a lane that does not take part gives 0)
+        return in ? ChunkGroup{n - 1, mine} : ChunkGroup{-1, 0};
     }
     for (int left = a.groups + 1; left > 0;) {            // (halves)
         const int half = left / 2;

@@ -1,0 +1,39 @@
+"""Calls of the operators that take many tokens at once which their documentation allows and that meet a corner of how work is dealt or numbers are held."""
+import pytest
+import torch
+
+from test_gpu_many import shared
+
+pytestmark = pytest.mark.gpu
+F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
+
+
+# ---- requests in no group -------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("sizes,common,starts,of", [([1, 4], [0, 400], [1, 5], [1]), ([2, 4, 2], [0, 400, 0], [2, 6], [1]), ([3, 2, 4], [0, 320, 800], [3, 5, 9], [1, 2]),
+                                                    ([1, 5], [480, 0], [0, 0, 0, 1], [None, None, 0]), ([20, 1, 30], [0, 160, 0], [5, 5, 20, 21], [None, None, 1])])
+@pytest.mark.parametrize("heads", [1, 4])
+def test_leading_requests_in_no_group(dtype, sizes, common, starts, of, heads):
+    """A group's number is that of a request that is in none; own slots in several parts, and bounds as close as they may be."""
+    own = [(97 * b) % 700 + 300 for b in range(sum(sizes))]
+    group = {b: of[g] for g in range(len(of)) for b in range(starts[g], starts[g + 1])}
+    together = [0 if g is None else common[g] for g in of]
+    of_request = [g for g, n in enumerate(sizes) for _ in range(n)]
+    lengths = [common[of_request[b]] + own[b] for b in range(len(own))]
+    most_own = max(n - (common[group[b]] if group.get(b) is not None else 0) for b, n in enumerate(lengths))
+
+    def edit(q, k, v, table, lengths, *_):
+        return q, k, v, table, lengths, starts, together
+    for kw in (dict(), dict(max_shared=max(common), max_own=most_own)):
+        shared(dtype, common, own, sizes, 4 * heads, heads, 64, 16, edit=edit, **kw)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+def test_leading_requests_in_no_group_and_many_rows_in_common(dtype):
+    """The same where slots in common go by tiles of 128 rows."""
+    own = [(53 * b) % 500 + 200 for b in range(42)]
+
+    def edit(q, k, v, table, lengths, *_):
+        return q, k, v, table, lengths, [2, 42], [3504]
+    shared(dtype, [0, 3504], own, [2, 40], 32, 4, 128, 16, edit=edit, max_shared=3504, max_own=max(own))
