@@ -80,7 +80,7 @@ __device__ __forceinline__ ChunkKnown chunk_known(const ChunkArgs &a, int mode, 
 __device__ __forceinline__ ChunkSpan chunk_range(const ChunkArgs &a, int mode, const ChunkKnown &k, int t0, int t1) {
     if (mode == CHUNK_NEW) {
         const int first = k.length - (k.q.tokens - t0), last = k.length - (k.q.tokens - t1);
-        return {a.window > 0 ? max(first + 1 - a.window, 0) : 0, min(max(last + 1, 0), a.max_length)};
+        return {a.window > 0 ? max(max(first, 0) + 1 - a.window, 0) : 0, min(max(last + 1, 0), a.max_length)};     // (first is below 0 where tokens have no slot, and the window may be the largest number)
     }
     if (mode == CHUNK_COMMON) return {0, k.common};
     const int n = min(k.length, a.max_length), common = min(n, k.common);

@@ -2,10 +2,11 @@
 import pytest
 import torch
 
-from test_gpu_many import shared
+from test_gpu_many import chunk, shared
 
 pytestmark = pytest.mark.gpu
 F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
+MOST = 2 ** 31 - 1
 
 
 # ---- requests in no group -------------------------------------------------------------------------
@@ -37,3 +38,16 @@ def test_leading_requests_in_no_group_and_many_rows_in_common(dtype):
     def edit(q, k, v, table, lengths, *_):
         return q, k, v, table, lengths, [2, 42], [3504]
     shared(dtype, [0, 3504], own, [2, 40], 32, 4, 128, 16, edit=edit, max_shared=3504, max_own=max(own))
+
+
+# ---- windows as large as there are ----------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("window", [40, 1000, MOST - 100, MOST])
+def test_windows_where_some_tokens_have_no_slot(dtype, window):
+    """Lengths below the number of new tokens: what a tile's first token has no slot for does not matter to its others; by many rows, and by few."""
+    def edit(*lengths):
+        return lambda q, k, v, table, _: (q, k, v, table, list(lengths))
+    chunk(dtype, [180], [0], 4, 2, 64, 16, window=window, edit=edit(150))
+    chunk(dtype, [300, 128, 70], [0, 0, 0], 2, 2, 128, 16, window=window, edit=edit(290, 100, 1), max_length=280)
+    chunk(dtype, [60] + [1] * 9, [0] + [40] * 9, 1, 1, 64, 16, window=window, edit=edit(50, *[41] * 9))
