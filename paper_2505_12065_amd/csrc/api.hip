@@ -628,7 +628,7 @@ int ann_chunk_attention(const void *q, int64_t q_row, int64_t q_head, int32_t T,
     if (too_many_slots(max_length, window))
         return fail(ANN_ERR_INVALID, "max_length = %d without a window: at most %d slots may be attended to", max_length, CHUNK_SLOTS_MAX);
     a.tokens = T; a.starts = starts; a.requests = B; a.max_length = max_length; a.window = window; a.out = out; a.lse = lse;
-    a.lift = chunk_lift(cache->dtype, max_length);
+    a.lift = chunk_lift(cache->dtype, window > 0 ? std::min(window, max_length) : max_length);
     return run_attention(a, cache->dtype, CHUNK_WS_MAX, [&](int cus, size_t most) {
         return chunk_plan(cus, elem_bytes(cache->dtype), cache->d, q_heads, cache->heads, T, B, max_length, window, most);
     }, static_cast<hipStream_t>(stream));
@@ -658,7 +658,7 @@ int ann_shared_attention(const void *q, int64_t q_row, int64_t q_head, int32_t B
         return fail(ANN_ERR_INVALID, "max_shared = %d or max_own = %d out of range", max_shared, max_own);
     a.tokens = a.requests = B; a.max_length = most; a.out = out; a.lse = lse;
     a.group_starts = group_starts; a.shared = shared; a.groups = groups; a.max_shared = max_shared; a.max_own = max_own;
-    a.lift = chunk_lift(cache->dtype, most);
+    a.lift = chunk_lift(cache->dtype, std::min<int64_t>(most, (int64_t)max_shared + max_own));
     return run_attention(a, cache->dtype, shared_most(B, q_heads, cache->d), [&](int cus, size_t there) {
         return shared_plan(cus, elem_bytes(cache->dtype), cache->d, q_heads, cache->heads, B, groups, max_shared, max_own, there);
     }, static_cast<hipStream_t>(stream));

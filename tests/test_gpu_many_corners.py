@@ -51,3 +51,23 @@ def test_windows_where_some_tokens_have_no_slot(dtype, window):
     chunk(dtype, [180], [0], 4, 2, 64, 16, window=window, edit=edit(150))
     chunk(dtype, [300, 128, 70], [0, 0, 0], 2, 2, 128, 16, window=window, edit=edit(290, 100, 1), max_length=280)
     chunk(dtype, [60] + [1] * 9, [0] + [40] * 9, 1, 1, 64, 16, window=window, edit=edit(50, *[41] * 9))
+
+
+# ---- small values ---------------------------------------------------------------------------------
+
+def small(v, exponent):
+    """v becomes values of sizes 1 to 2 times a power of two, which both types of 8 bits of exponent hold."""
+    return torch.where(v < 0, -1.0, 1.0).to(v.dtype) * (1 + v.abs().clamp(max=7) / 8) * 2.0 ** exponent
+
+
+@pytest.mark.parametrize("dtype,exponent", [(BF16, -105), (F32, -104)])
+def test_small_values_behind_a_wide_table(dtype, exponent):
+    """What a page table could hold, and slots that a window leaves out, cost no digits of small values."""
+    width = (MOST - 65536) // 1024
+
+    def wide(q, k, v, table, *rest):
+        return q, k, v.copy_(small(v, exponent)), torch.cat([table, torch.full((len(table), width - table.shape[1]), -1, dtype=torch.int32)], 1), *rest
+    chunk(dtype, [3, 1], [2500, 90], 4, 2, 64, 1024, window=100, edit=wide)
+    chunk(dtype, [150, 40], [1000, 0], 4, 2, 64, 1024, window=100, edit=wide)
+    shared(dtype, [2048], [300, 600, 20], [3], 4, 2, 64, 1024, max_shared=2048, max_own=600, edit=wide)
+    shared(dtype, [2048], [300, 600, 20], [3], 4, 2, 64, 1024, max_shared=0, max_own=2648, edit=wide)
