@@ -157,11 +157,13 @@ __device__ __forceinline__ bool chunk_whole(const ChunkArgs &a, const ChunkDeal 
 // Weights are 2^lift times what they are.  16 bits: by their exponents, before they are rounded.  fp32: exponents would be rounded to the lift's last place (20: 2^-20, and not the 2^-23 of those that count, which
 // left outputs and statistics twice as far off): they are less by 2^-6, so that 64 slots' products are no larger than the largest value, and sums of these are multiplied by the rest.
 constexpr float CHUNK_LIFT_F32 = -6.f;
+// Of the 2^8 by which a weight of 16 bits may pass the one of the score it goes by, fp32, whose scores pass none, keeps a factor of 2 for the roundings of its sums.
+constexpr int CHUNK_ROOM_F32 = 7;
 template <class T>
 __device__ __forceinline__ float chunk_lift_exponent(const ChunkArgs &a) { return T::bytes == 4 ? CHUNK_LIFT_F32 : a.lift; }
 template <class T>
 __device__ __forceinline__ float chunk_lift_factor(const ChunkArgs &a) {
-    return T::bytes == 4 ? __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((127 + (int)(a.lift - CHUNK_LIFT_F32)) << 23)) : 1.f;
+    return T::bytes == 4 ? __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((127 + CHUNK_ROOM_F32 + (int)(a.lift - CHUNK_LIFT_F32)) << 23)) : 1.f;
 }
 template <class T>
 __device__ __forceinline__ float chunk_by(const ChunkArgs &a, float total) { return total == 0.f ? 0.f : 1.f / (total * chunk_lift_factor<T>(a)); }

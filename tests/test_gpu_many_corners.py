@@ -2,7 +2,10 @@
 import pytest
 import torch
 
-from test_gpu_many import chunk, shared
+import decode as D                                        # (beside this file)
+import many as M
+import paper_2505_12065_amd as ann
+from test_gpu_many import chunk, dev, shared
 
 pytestmark = pytest.mark.gpu
 F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
@@ -71,3 +74,20 @@ def test_small_values_behind_a_wide_table(dtype, exponent):
     chunk(dtype, [150, 40], [1000, 0], 4, 2, 64, 1024, window=100, edit=wide)
     shared(dtype, [2048], [300, 600, 20], [3], 4, 2, 64, 1024, max_shared=2048, max_own=600, edit=wide)
     shared(dtype, [2048], [300, 600, 20], [3], 4, 2, 64, 1024, max_shared=0, max_own=2648, edit=wide)
+
+
+@pytest.mark.parametrize("T", [2, 90])
+def test_small_values_that_have_all_the_weight(T):
+    """fp32, near its smallest normal number (2^-126): of 9000 slots, which take 14 bits of the sums' range and one is left, one has all the weight."""
+    n, d, page = 9000, 64, 64
+    g = torch.Generator().manual_seed(T)
+    pages = (n + page - 1) // page
+    k, v = torch.zeros(pages, 1, page, d), small(torch.randn(pages, 1, page, d, generator=g), -115)
+    k[77, 0, 5, 0] = 1
+    q = torch.zeros(T, 2, d)
+    q[..., 0] = 100                                       # (e^-100 2^13 is below 2^-130)
+    table = torch.arange(pages, dtype=torch.int32).view(1, -1)
+    out, _ = ann.ann_chunk_attention(dev(q), dev(k), dev(v), dev(table), dev(M.ints([n])), dev(M.ints([0, T])), scale=1.0, max_length=n)
+    want = v[77, 0, 5].double()
+    # a tile's sum, its factor, the row's sum, a joined part's factor and sum: numbers from 2^-115 2^-15 on, whose last place is 2^-149; weight, sums, division and product 2^-24 each
+    assert ((out.double().cpu() - want).abs() <= 5 * 2.0 ** (-150 + 15) + 16 * D.U * want.abs()).all()
