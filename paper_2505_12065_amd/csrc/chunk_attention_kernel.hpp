@@ -155,8 +155,9 @@ __device__ __forceinline__ ChunkSpan chunk_row_span(const ChunkArgs &a, int mode
 // A row without other parts is divided and written; else what joins the parts reads its elements, its statistics, how many parts there are and whether it is of a group.
 __device__ __forceinline__ bool chunk_whole(const ChunkArgs &a, const ChunkDeal &deal) { return a.splits == 1 || deal.alone; }
 // Weights are 2^lift times what they are.  16 bits: by their exponents, before they are rounded.  fp32: exponents would be rounded to the lift's last place (20: 2^-20, and not the 2^-23 of those that count, which
-// left outputs and statistics twice as far off): they are less by 2^-6, so that 64 slots' products are no larger than the largest value, and sums of these are multiplied by the rest.
-constexpr float CHUNK_LIFT_F32 = -6.f;
+// left outputs and statistics twice as far off): they are less by 2^-7, so that 64 slots' products are half as large as the largest value, and sums of these are multiplied by the rest.  (Half:
+// weights are as far above 2^-7 as the largest score's exponent is rounded down, by 2^(2^-7) at scores of 100 000.)
+constexpr float CHUNK_LIFT_F32 = -7.f;
 // Of the 2^8 by which a weight of 16 bits may pass the one of the score it goes by, fp32, whose scores pass none, keeps a factor of 2 for the roundings of its sums.
 constexpr int CHUNK_ROOM_F32 = 7;
 template <class T>

@@ -8,6 +8,7 @@ import paper_2505_12065_amd as ann
 from test_gpu_many import chunk, dev, shared
 
 pytestmark = pytest.mark.gpu
+DEV = "cuda"
 F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
 MOST = 2 ** 31 - 1
 
@@ -91,3 +92,24 @@ def test_small_values_that_have_all_the_weight(T):
     want = v[77, 0, 5].double()
     # a tile's sum, its factor, the row's sum, a joined part's factor and sum: numbers from 2^-115 2^-15 on, whose last place is 2^-149; weight, sums, division and product 2^-24 each
     assert ((out.double().cpu() - want).abs() <= 5 * 2.0 ** (-150 + 15) + 16 * D.U * want.abs()).all()
+
+
+# ---- fp32 values near the largest -----------------------------------------------------------------
+
+@pytest.mark.parametrize("T,common", [(9, None), (70, None), (5, 160), (130, 160)])
+def test_values_near_the_largest_and_large_scores(T, common):
+    """fp32: scores near 100 000, which exponents hold to 2^-7, so that weights of the largest score are up to 2^(2^-7) times what they are by it.  A row's scores are all the same, and so are its weights."""
+    n, d, page = 200, 64, 16
+    value = torch.finfo(F32).max * 0.999
+    k, v = torch.zeros(13, 1, page, d, device=DEV), torch.full((13, 1, page, d), value, device=DEV)
+    k[..., 0] = 1
+    q = torch.zeros(T, 2, d, device=DEV)
+    q[..., 0] = torch.arange(2 * T, device=DEV).view(T, 2) + 100_000
+    table = torch.arange(13, dtype=torch.int32, device=DEV)
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    if common is None:
+        out, _ = ann.ann_chunk_attention(q, k, v, table.view(1, -1), ints(n), ints(0, T), scale=1.0, max_length=n)
+    else:
+        out, _ = ann.ann_shared_attention(q, k, v, table.repeat(T, 1), ints(*[n] * T), ints(0, T), ints(common), max_shared=common, max_own=n - common, scale=1.0)
+    # sums of up to 200 products and of 200 weights, in any order, a division and a product: 2^-24 each
+    assert bool(torch.isfinite(out).all()) and (out.double() / value - 1).abs().max() <= (2 * n + 8) * D.U
