@@ -158,8 +158,8 @@ __device__ __forceinline__ bool chunk_whole(const ChunkArgs &a, const ChunkDeal 
 // left outputs and statistics twice as far off): they are less by 2^-7, so that 64 slots' products are half as large as the largest value, and sums of these are multiplied by the rest.  (Half:
 // weights are as far above 2^-7 as the largest score's exponent is rounded down, by 2^(2^-7) at scores of 100 000.)
 constexpr float CHUNK_LIFT_F32 = -7.f;
-// Of the 2^8 by which a weight of 16 bits may pass the one of the score it goes by, fp32, whose scores pass none, keeps a factor of 2 for the roundings of its sums.
-constexpr int CHUNK_ROOM_F32 = 7;
+// (a weight of 16 bits may pass the one of the score it goes by by 2^8, one of fp32 by nothing)
+constexpr int CHUNK_ROOM_F32 = 8;
 template <class T>
 __device__ __forceinline__ float chunk_lift_exponent(const ChunkArgs &a) { return T::bytes == 4 ? CHUNK_LIFT_F32 : a.lift; }
 template <class T>

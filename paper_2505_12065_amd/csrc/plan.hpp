@@ -1236,12 +1236,12 @@ inline ChunkPlan shared_plan(int cus, int elem_bytes, int d, int q_heads, int he
     return pl;
 }
 // Weights of the product with V, of up to so many slots that a row attends to (not those that its page table could hold: each bit is one that small values lose).  fp16 has no numbers below 2^-24, and
-// 65504 is its largest: 2^7 times as large they may still be 2^8 times that.  bf16 and fp32 have values up to the largest of the sums' 32 bits: as much smaller as there are slots to sum, and by the 2^8 (of which
-// fp32 takes most back: CHUNK_ROOM_F32).
+// 65504 is its largest: 2^7 times as large they may still be 2^8 times that.  bf16 and fp32 have values up to the largest of the sums' 32 bits: as much smaller as there are slots to sum, by the 2^8 (which fp32
+// takes back: CHUNK_ROOM_F32), and by 2 for what exponents and sums are rounded by.
 inline float chunk_lift(int dtype, int64_t slots) {
     int bits = 0;
     while (slots >> bits) ++bits;
-    return dtype == ANN_F16 ? 7.f : -(float)(bits + 8);
+    return dtype == ANN_F16 ? 7.f : -(float)(bits + 9);
 }
 
 // Frequencies of a rotation; scaling: an ANN_ROTATION_* code.

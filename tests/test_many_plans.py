@@ -137,3 +137,9 @@ def test_few_rows_fit_a_compute_unit(plans):
         for ve in (4, 8, 16):
             for mt in (1, 2):
                 assert plans.lds(eb, ve, mt) <= 160 * 1024
+
+
+def test_sums_of_weights_leave_room_for_roundings(plans):
+    """Weights are as far above their power of two as the exponent of the score they go by is rounded down (2^(2^-7) at scores of 100 000), and sums are rounded too: sums stay below half of the largest value."""
+    for n in (1, 63, 64, 4095, 65_535, 2 ** 20, 2 ** 26):
+        assert n * 2.0 ** (plans.lift(1, n) + 8) <= 0.5
