@@ -48,9 +48,12 @@ __device__ __forceinline__ void store_four<BF16>(char *to, f4 y) {
     typedef __bf16 b4 __attribute__((ext_vector_type(4)));
     *reinterpret_cast<b4 *>(to) = b4{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
 }
-// From what the weights' exponents are less (the largest score as an exponent of 2, or one near it, less the lift) and their sum.
+// From what the weights' exponents are less (the largest score as an exponent of 2, or one near it, less the lift) and their sum.  The sum's exponent is added to them before the product with ln 2: the lift is in
+// both, and of two logarithms of its size that cancel each other lse would keep the roundings (16 bits, up to 2048 slots, scores of deviations from 0.3 to 2: off by 2.0e-6 to 2.8e-6 at most, 0.4e-6 to 1.4e-6 so).
 __device__ __forceinline__ float chunk_lse(float less, float total) {
-    return total == 0.f ? -INFINITY : (less == -INFINITY ? 0.f : less) * 0.6931471805599453f + logf(total);
+    int exponent;
+    const float fraction = frexpf(total, &exponent);
+    return total == 0.f ? -INFINITY : fmaf(less == -INFINITY ? 0.f : less + (float)exponent, 0.6931471805599453f, logf(fraction));
 }
 
 // until at most n of this wave's loads are outstanding

@@ -113,3 +113,30 @@ def test_values_near_the_largest_and_large_scores(T, common):
         out, _ = ann.ann_shared_attention(q, k, v, table.repeat(T, 1), ints(*[n] * T), ints(0, T), ints(common), max_shared=common, max_own=n - common, scale=1.0)
     # sums of up to 200 products and of 200 weights, in any order, a division and a product: 2^-24 each
     assert bool(torch.isfinite(out).all()) and (out.double() / value - 1).abs().max() <= (2 * n + 8) * D.U
+
+
+# ---- lse ------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+def test_lse_of_equal_scores(dtype):
+    """Scores of 0: weights are one power of two and sums of them exact, so lse is the logarithm of a whole number, off by 2 units in the last place of a logarithm at most (2^-22 of it): by many
+    rows, by few, in parts and with slots in common."""
+    d, page = 64, 16
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+
+    def near(lse, slots):
+        want = torch.tensor(slots, dtype=torch.float64, device=DEV).log()[:, None]
+        assert bool(((lse.double() - want).abs() <= 2.0 ** -22 * want).all()), (lse.double() - want).abs().max()
+
+    k = torch.randn(600, 1, page, d, device=DEV).to(dtype)
+    for T, n in ((2048, 2048), (300, 9000), (4, 9000), (1, 1)):
+        table = torch.arange(600, dtype=torch.int32, device=DEV).view(1, -1)
+        q = torch.zeros(T, 2, d, dtype=dtype, device=DEV)
+        near(ann.ann_chunk_attention(q, k, k, table, ints([n]), ints([0, T]), max_length=n)[1], list(range(n - T + 1, n + 1)))
+    for B in (7, 60, 300):
+        lengths = [1 + 31 * b for b in range(B)]
+        table = torch.arange(600, dtype=torch.int32, device=DEV).repeat(B, 1)
+        q = torch.zeros(B, 2, d, dtype=dtype, device=DEV)
+        near(ann.ann_chunk_attention(q, k, k, table, ints(lengths), ints(list(range(B + 1))))[1], lengths)
+        for common in (0, 160, 4000):
+            near(ann.ann_shared_attention(q, k, k, table, ints(lengths), ints([0, B]), ints([common]), max_shared=common)[1], lengths)
