@@ -140,3 +140,15 @@ def test_lse_of_equal_scores(dtype):
         near(ann.ann_chunk_attention(q, k, k, table, ints(lengths), ints(list(range(B + 1))))[1], lengths)
         for common in (0, 160, 4000):
             near(ann.ann_shared_attention(q, k, k, table, ints(lengths), ints([0, B]), ints([common]), max_shared=common)[1], lengths)
+
+
+# ---- more requests than a wave has lanes -----------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("common,most_own", [(48, 1000), (16, 993), (80, 1024)])
+def test_own_slots_of_more_than_64_requests_in_parts(dtype, common, most_own):
+    """Own slots that begin off a multiple of 32 and are as many as may count: the last part holds what the beginning was moved by."""
+    own = [most_own + common % 16 if b % 3 == 0 else (37 * b) % most_own for b in range(70)]
+    shared(dtype, [common], own, [70], 2, 1, 64, 16, max_shared=common, max_own=most_own)
+    # by the same plan, with all requests in no group but one
+    shared(dtype, [common], own, [70], 2, 1, 64, 16, max_shared=common, max_own=most_own, edit=lambda *x: (*x[:5], [69, 70], x[6]))

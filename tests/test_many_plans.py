@@ -143,3 +143,18 @@ def test_sums_of_weights_leave_room_for_roundings(plans):
     """Weights are as far above their power of two as the exponent of the score they go by is rounded down (2^(2^-7) at scores of 100 000), and sums are rounded too: sums stay below half of the largest value."""
     for n in (1, 63, 64, 4095, 65_535, 2 ** 20, 2 ** 26):
         assert n * 2.0 ** (plans.lift(1, n) + 8) <= 0.5
+
+
+def test_parts_of_own_slots_cover_where_they_begin(plans):
+    """A request's own slots are read from a multiple of 32 on, up to 31 below the first: parts of more than 64 requests, whose length the host says, have to hold these too."""
+    rng = random.Random(3)
+    divided = 0
+    for _ in range(6000):
+        heads, G, B, groups = log(rng, 1, 16), log(rng, 1, 32), log(rng, 65, 2000), log(rng, 1, 2000)
+        if heads * G > 8192 or B * heads * G > 2 ** 22:
+            continue
+        shared, own_slots, d, eb = log(rng, 1, 100_000), rng.choice([64, 65, 512, log(rng, 1, 100_000)]), 8 * rng.randint(1, 32), rng.choice([2, 4])
+        first, own, _, _ = plan(plans.shared, eb, d, heads * G, heads, B, groups, shared, own_slots, plans.enough(B, heads * G, d))
+        assert own["chunk"] * own["most_parts"] >= own_slots + 31
+        divided += own["most_parts"] > 1
+    assert divided > 100
