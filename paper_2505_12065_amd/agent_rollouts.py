@@ -44,7 +44,7 @@ class Rollouts:
         self.v = [torch.zeros_like(k) for k in self.k]
         self.context = self._ints([list(range(common))])
         self.own_pages = [list(range(common + b * each, common + (b + 1) * each)) for b in range(answers)]
-        self.length, self.said = 0, 0                     # slots of the context; tokens of every answer
+        self.length, self.said, self.begun = 0, 0, False  # slots of the context; tokens of every answer; whether these share it as it is
 
     def _ints(self, x) -> torch.Tensor:
         return torch.tensor(x, dtype=torch.int32, device=self.device)
@@ -60,7 +60,7 @@ class Rollouts:
 
     def take(self, tokens: torch.Tensor) -> torch.Tensor:
         """Tokens that the context grows by; the hidden state of the last."""
-        if self.said:
+        if self.begun:
             raise ValueError("the answers have begun")
         if self.length + len(tokens) > self.limit:
             raise ValueError(f"a context of more than {self.limit} tokens")
@@ -79,6 +79,7 @@ class Rollouts:
 
     def begin(self) -> None:
         """Answers begin: whole pages of the context are everyone's, and its last tokens, where they fill no page, are copied to each answer's first one."""
+        self.begun = True
         whole, rest = self.length // self.page, self.length % self.page
         self.common = whole * self.page
         table = torch.tensor([list(range(whole)) + own for own in self.own_pages], dtype=torch.int32)
