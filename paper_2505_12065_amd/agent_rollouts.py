@@ -92,10 +92,10 @@ class Rollouts:
 
     def step(self, tokens: torch.Tensor) -> torch.Tensor:
         """One new token of every answer: logits [answers, vocabulary]."""
-        self.said += 1
-        n = self.length + self.said
+        n = self.length + self.said + 1
         if n > self.table.shape[1] * self.page:
             raise ValueError("the answers' pages are full")
+        self.said += 1
         lengths = torch.full((self.answers,), n, dtype=torch.int32, device=self.device)
         hidden = self._forward(tokens, self.starts, lengths, self.table, lambda q, k, v: ann.ann_shared_attention(
             q, k, v, self.table, lengths, self.groups, self.shared, max_shared=self.common, max_own=n - self.common)[0])

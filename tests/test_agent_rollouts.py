@@ -17,3 +17,15 @@ def test_the_context_does_not_grow_once_answers_have_begun():
     with pytest.raises(ValueError, match="begun"):
         r.take(torch.tensor([1, 2]))
     assert r.length == 20
+
+
+def test_a_step_that_is_refused_leaves_the_answers_as_they_were():
+    r = small()
+    r.length = 20
+    r.begin()
+    room = r.table.shape[1] * r.page - r.length
+    r.said = room
+    for _ in range(2):
+        with pytest.raises(ValueError, match="full"):
+            r.step(torch.tensor([1, 2]))
+    assert r.said == room
