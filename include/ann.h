@@ -488,7 +488,7 @@ int ann_rotation_frequencies(int32_t rot, double base, int32_t scaling, double f
  *   lengths, page_table  device int32 [B], [B, width]: a token's keys and values go to its slot; one that is not in the table, or whose page is empty, is dropped
  *   positions    device int32 [T], or NULL: a token's position is its slot.  A token of a negative position is padding: its row of q is zero and nothing is put into the cache
  *   frequencies  device double [rot / 2]; rot a multiple of 16 in [0, d] (0: nothing is rotated; NULL)
- *   q            device, [T, q_heads, d]
+ *   q            device, [T, q_heads, d]; not in the place of qkv
  * T at most 2^22, B, q_heads and heads 65536, width slots 2^31 - 65537.  Two tokens with one slot of one page: either's row is left, or a mixture.  T = 0 returns ANN_OK at once.  No workspace. */
 int ann_rotate_append(const void *qkv, int64_t token_stride, int64_t head_stride, int32_t T, int32_t q_heads,
                       const int32_t *starts, int32_t B, const int32_t *lengths, const int32_t *page_table, int32_t width,
@@ -503,7 +503,7 @@ int ann_rotate_append(const void *qkv, int64_t token_stride, int64_t head_stride
  *   lengths     device int32 [B], with the new tokens; as 0 if negative.  A token has its slot only if that is in [0, max_length), 1 <= max_length <= width slots
  *   max_length  what the work is divided by, as no length is read on the host: the largest length, or a bound as close as the host knows; it or the window at most 2^26 (products with V are summed in
  *               binary32, eight slots at a time)
- *   out         device [T, q_heads, d], contiguous;  lse  device float [T, q_heads], or NULL
+ *   out         device [T, q_heads, d], contiguous (a contiguous q may be its own out, but for that they may not overlap);  lse  device float [T, q_heads], or NULL
  * Values that a token does not attend to do not matter to it, NaN and infinities among them; a value that is one of these and has a weight gives one.  Same inputs and workspace give bitwise-same
  * outputs.  Where there are few tokens, contexts are divided into parts that are joined in the workspace of the current device; with less than the size below they are divided
  * less, or not at all.  q_heads at most 8192, T q_heads 2^26, T and B heads 2^22, B 65536, width slots 2^31 - 65537.  T = 0 returns ANN_OK at once. */

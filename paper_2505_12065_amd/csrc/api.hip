@@ -312,6 +312,13 @@ int check_rows(const char *what, int64_t row, int64_t head, int e) {
     return ANN_OK;
 }
 
+// Bytes of n x heads rows; whether outputs of so many, one behind the other, lie in the place of inputs that workgroups go on reading.  (In their very place every row is read by those who write it.)
+int64_t row_bytes(int64_t n, int64_t heads, int64_t row, int64_t head, int64_t d, int e) { return ((n - 1) * row + (heads - 1) * head + d) * e; }
+bool in_place_of(const void *out, int64_t out_bytes, const void *in, int64_t in_bytes) {
+    const uintptr_t o = reinterpret_cast<uintptr_t>(out), i = reinterpret_cast<uintptr_t>(in);
+    return o < i + (uint64_t)in_bytes && i < o + (uint64_t)out_bytes;
+}
+
 int units_of_device() {
     std::lock_guard<std::mutex> lock(g_mu);
     DeviceState *st = nullptr;
@@ -578,6 +585,9 @@ int ann_rotate_append(const void *qkv, int64_t token_stride, int64_t head_stride
     if (off16(qkv) || off16(q)) return fail(ANN_ERR_ALIGNMENT, "qkv and q must be 16-byte aligned");
     if (off4({starts, lengths, page_table, positions})) return fail(ANN_ERR_ALIGNMENT, "starts, lengths, page_table and positions must be 4-byte aligned");
     if (reinterpret_cast<uintptr_t>(frequencies) & 7) return fail(ANN_ERR_ALIGNMENT, "frequencies must be 8-byte aligned");
+    if (!(T == 1 && q == qkv && head_stride == cache->d) &&
+        in_place_of(q, (int64_t)T * q_heads * cache->d * e, qkv, row_bytes(T, q_heads + 2 * (int64_t)cache->heads, token_stride, head_stride, cache->d, e)))
+        return fail(ANN_ERR_INVALID, "q may not lie in the place of qkv");
     a.qkv = qkv; a.token = token_stride * e; a.head = head_stride * e; a.tokens = T; a.q_heads = q_heads;
     a.starts = starts; a.requests = B; a.lengths = lengths; a.table = page_table; a.width = width;
     a.positions = positions; a.frequencies = frequencies; a.rot = rot; a.amplitude = amplitude; a.interleaved = interleaved != 0; a.q = q;
@@ -600,6 +610,16 @@ static int check_attention(const void *q, int64_t q_row, int64_t q_head, int32_t
     a->q = q; a->q_row = q_row * e; a->q_head = q_head * e; a->q_heads = q_heads;
     a->table = page_table; a->width = width; a->lengths = lengths; a->scale = scale * 1.4426950408889634f;
     a->coarse = cache->slots >= 16 && a->cache.k_slot < 1 << 27 && a->cache.v_slot < 1 << 27;
+    return ANN_OK;
+}
+
+// `tokens` rows of q and out, checked otherwise
+static int check_in_place(const void *q, int64_t q_row, int64_t q_head, const void *out, int64_t tokens, int64_t q_heads, const ann_paged_cache *cache) {
+    const int64_t d = cache->d;
+    const int e = elem_bytes(cache->dtype);
+    if (out == q && (tokens == 1 || q_row == q_heads * d) && (q_heads == 1 || q_head == d)) return ANN_OK;
+    if (in_place_of(out, tokens * q_heads * d * e, q, row_bytes(tokens, q_heads, q_row, q_head, d, e)))
+        return fail(ANN_ERR_INVALID, "out may lie in the place of q only if q is contiguous and they begin with the same row");
     return ANN_OK;
 }
 
@@ -627,6 +647,7 @@ int ann_chunk_attention(const void *q, int64_t q_row, int64_t q_head, int32_t T,
     if (window < 0) return fail(ANN_ERR_INVALID, "window = %d out of range", window);
     if (too_many_slots(max_length, window))
         return fail(ANN_ERR_INVALID, "max_length = %d without a window: at most %d slots may be attended to", max_length, CHUNK_SLOTS_MAX);
+    if (int rc = check_in_place(q, q_row, q_head, out, T, q_heads, cache)) return rc;
     a.tokens = T; a.starts = starts; a.requests = B; a.max_length = max_length; a.window = window; a.out = out; a.lse = lse;
     a.lift = chunk_lift(cache->dtype, window > 0 ? std::min(window, max_length) : max_length);
     return run_attention(a, cache->dtype, CHUNK_WS_MAX, [&](int cus, size_t most) {
@@ -656,6 +677,7 @@ int ann_shared_attention(const void *q, int64_t q_row, int64_t q_head, int32_t B
     const int32_t most = width * cache->slots;
     if (max_shared < 0 || max_shared > std::min(most, CHUNK_SLOTS_MAX) || max_own < 1 || max_own > std::min(most, CHUNK_SLOTS_MAX))
         return fail(ANN_ERR_INVALID, "max_shared = %d or max_own = %d out of range", max_shared, max_own);
+    if (int rc = check_in_place(q, q_row, q_head, out, B, q_heads, cache)) return rc;
     a.tokens = a.requests = B; a.max_length = most; a.out = out; a.lse = lse;
     a.group_starts = group_starts; a.shared = shared; a.groups = groups; a.max_shared = max_shared; a.max_own = max_own;
     a.lift = chunk_lift(cache->dtype, std::min<int64_t>(most, (int64_t)max_shared + max_own));

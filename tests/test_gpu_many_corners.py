@@ -152,3 +152,36 @@ def test_own_slots_of_more_than_64_requests_in_parts(dtype, common, most_own):
     shared(dtype, [common], own, [70], 2, 1, 64, 16, max_shared=common, max_own=most_own)
     # by the same plan, with all requests in no group but one
     shared(dtype, [common], own, [70], 2, 1, 64, 16, max_shared=common, max_own=most_own, edit=lambda *x: (*x[:5], [69, 70], x[6]))
+
+
+# ---- outputs in the place of inputs ----------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("new,held", [([180, 3], [100, 700]), ([2, 5], [3000, 10]), ([1] * 80, [100] * 80)])
+def test_attention_in_the_place_of_queries(dtype, new, held):
+    """By many rows and by few, in parts and whole; a token's q where its rows of qkv begin."""
+    lengths = [n + h for n, h in zip(new, held)]
+    k, v, table = D.paged(lengths, 16, 2, 64, dtype, 3)
+    q = D.rows(sum(new), 4, 64, dtype=dtype, seed=4).to(DEV)
+    args = dev(k), dev(v), dev(table), dev(M.ints(lengths))
+    want, want_lse = ann.ann_chunk_attention(q, *args, dev(M.starts_of(new)))
+    own = q.clone()
+    out, lse = ann.ann_chunk_attention(own, *args, dev(M.starts_of(new)), out=own)
+    assert out is own and torch.equal(out, want) and torch.equal(lse, want_lse)
+    B = len(new)
+    groups = dev(M.ints([0, B])), dev(M.ints([0]))
+    want, want_lse = ann.ann_shared_attention(q[:B], *args, *groups)
+    own = q[:B].clone()
+    out, lse = ann.ann_shared_attention(own, *args, *groups, out=own)
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+def test_append_of_one_token_in_the_place_of_its_rows():
+    x = torch.randn(1, 8, 64, device=DEV)
+    i = lambda *a: torch.tensor(a, dtype=torch.int32, device=DEV)  # noqa: E731
+    frequencies, _ = ann.ann_rotation_frequencies(64, device=DEV)
+    caches = [torch.zeros(1, 2, 16, 64, device=DEV) for _ in range(4)]
+    want = ann.ann_rotate_append(x, i(0, 1), i(8), i(0).view(1, 1), frequencies, *caches[:2])
+    own = x.clone()
+    q = ann.ann_rotate_append(own, i(0, 1), i(8), i(0).view(1, 1), frequencies, *caches[2:], q=own[:, :4])
+    assert torch.equal(q, want) and torch.equal(own[:, 4:], x[:, 4:]) and torch.equal(caches[0], caches[2]) and torch.equal(caches[1], caches[3])
