@@ -498,7 +498,8 @@ int ann_rotate_append(const void *qkv, int64_t token_stride, int64_t head_stride
 /* Attention of the new tokens of every request, a passage's or a prompt's, over its paged cache, which holds them: ann_paged_attention with as many queries of a request as it has new
  * tokens.  The token in slot i attends to the slots j <= i whose page is not empty and, with window > 0, of these to j > i - window: x_j, lse and out are those of ann_paged_attention.  A token
  * without a slot, or for which nothing is left, gives out = 0, lse = -inf.  Scores, sums and statistics are binary32; weights of 16-bit types are rounded to the type for the
- * product with V (each is off by at most half a unit in its last place; fp16: or 2^-32 of the largest), out is rounded once.
+ * product with V (each is off by at most half a unit in its last place; fp16: or 2^-32 of the largest; where a request has few rows it is two such numbers), out is rounded once.  Weights are held times a power of
+ * two for that product: exponents of 2 are rounded at its size, to 2^-19 at most for the largest (fp32: 2^-22), and bf16 and fp32 values lose digits below about 2^-126 times the slots that a token attends to (bf16: 2^10 times that).
  *   q           device [T, q_heads, d] of the cache's type; strides q_row, q_head (multiples of 16 bytes)
  *   lengths     device int32 [B], with the new tokens; as 0 if negative.  A token has its slot only if that is in [0, max_length), 1 <= max_length <= width slots
  *   max_length  what the work is divided by, as no length is read on the host: the largest length, or a bound as close as the host knows; it or the window at most 2^26 (products with V are summed in

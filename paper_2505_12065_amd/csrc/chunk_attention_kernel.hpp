@@ -157,7 +157,7 @@ __device__ __forceinline__ ChunkSpan chunk_row_span(const ChunkArgs &a, int mode
 }
 // A row without other parts is divided and written; else what joins the parts reads its elements, its statistics, how many parts there are and whether it is of a group.
 __device__ __forceinline__ bool chunk_whole(const ChunkArgs &a, const ChunkDeal &deal) { return a.splits == 1 || deal.alone; }
-// Weights are 2^lift times what they are.  16 bits: by their exponents, before they are rounded.  fp32: exponents would be rounded to the lift's last place (20: 2^-20, and not the 2^-23 of those that count, which
+// Weights are 2^lift times what they are.  16 bits: by their exponents, before they are rounded, which are off by 2^-19 at most so (2^-8 and 2^-11 are the weights' own roundings).  fp32: exponents would be rounded to the lift's last place (20: 2^-20, and not the 2^-23 of those that count, which
 // left outputs and statistics twice as far off): they are less by 2^-7, so that 64 slots' products are half as large as the largest value, and sums of these are multiplied by the rest.  (Half:
 // weights are as far above 2^-7 as the largest score's exponent is rounded down, by 2^(2^-7) at scores of 100 000.)
 constexpr float CHUNK_LIFT_F32 = -7.f;
@@ -570,8 +570,8 @@ __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_per_simd(DP)) void chunk_
 //
 // Up to 16 MT rows: the waves share the slots out, K and V go from memory to registers, and the tiles are of 16 slots and 16 rows, as in paged_attention_kernel: reading K and V once bounds it
 // (128 requests of 4096 slots, 64 heads of 128 to 8, bf16: 330 us, 6.5 TB/s; ragged ones of up to 2048 4.9 TB/s; fp32, 64 of 2048, 173 us, 6.1 TB/s);
-// with little to read it is a chain of dependent reads (five requests behind 2000 slots in common, 32 heads to 8: 10 us).  A passage of 100 tokens, 400 rows of a cache head, takes 36.8 us
-// so and 20.7 by 128 rows.
+// with little to read it is a chain of dependent reads (five requests behind 2000 slots in common, 32 heads to 8: 10 us).  A passage of 100 tokens, 400 rows of a cache head, takes 26.9 us
+// so and 19.8 by 128 rows.
 // Lane 16 g + m has the scores of row m and slots 4 g .. 4 g + 3 of a tile; weights are operands of two parts.  Both passes of groups go in one launch where both have few rows.
 template <class T, int VE, int MT, bool FINE>
 __global__ __launch_bounds__(CHUNK_WAVES * WAVE, chunk_few_per_simd(T::bytes, VE, MT)) void chunk_few_kernel(ChunkArgs a, ChunkPass first_pass, ChunkPass own_pass) {

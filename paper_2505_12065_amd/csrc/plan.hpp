@@ -1155,10 +1155,10 @@ struct ChunkPlan {
 };
 constexpr int64_t CHUNK_PARTS = 64;                       // of a row in a pass
 // Slots of a part of many rows, at least (fp32, whose products take 16 times as long, a quarter): what a part leaves is 4 (d + 4) bytes for each of its rows, written and read.  100 tokens, 32 heads of 128 to 8,
-// 1600 slots, bf16: 20.2 us with 256, 20.9 with 128; 200 slots 14.4 and 15.7 (d = 64, 600 slots 16.5 and 14.8).
+// 1600 slots, bf16: 19.8 us with 256, 20.2 with 128; 200 slots 12.9 and 15.2 (d = 64, 600 slots 15.3 and 14.1).
 constexpr int CHUNK_LEAST = 256;
-// Slots in common go through by few rows, in one launch with the own slots, up to so many operations.  33 requests in 4 groups, 14 heads of 64 to 2, 2000 slots in common (2.4e8): 15.5 us, by 128 rows and a launch of its
-// own 24.8; 64 requests in one group, 32 heads of 128 to 8, 8100 slots (8.5e9): 96 and 71.
+// Slots in common go through by few rows, in one launch with the own slots, up to so many operations.  33 requests in 4 groups, 14 heads of 64 to 2, 2000 slots in common (2.4e8): 15.0 us, by 128 rows and a launch of its
+// own 23.7; 64 requests in one group, 32 heads of 128 to 8, 8100 slots (8.5e9): 94 and 69; 128 in 4 groups, 64 heads, 32 000 slots: 713 and 309.
 constexpr double CHUNK_SMALL = 1.0e9;
 // Sequences of `rows` rows in all, whose tiles go through `range` slots at most.
 inline ChunkPass chunk_pass(int mode, int cus, int elem_bytes, int d, int heads, int64_t rows, int64_t sequences, int64_t range, int64_t most_parts, bool small = false,
@@ -1175,8 +1175,9 @@ inline ChunkPass chunk_pass(int mode, int cus, int elem_bytes, int d, int heads,
     p.least = few ? (int)attend_step(elem_bytes, d) : elem_bytes == 4 ? CHUNK_LEAST / 4 : CHUNK_LEAST;
     p.whole = few ? 1024 : 0;
     const int64_t tiles = mode >= CHUNK_OWN ? sequences * ((rows / sequences + p.rows - 1) / p.rows) : rows / p.rows + sequences;
-    // Nothing is divided where tiles alone keep most of the card busy, or where there is a request for every compute unit whose slots are few.  (24 x 1190 rows of 4 cache heads, up to 8400 slots: 403 us divided
-    // and joined, 342 not; 64 requests of 8 cache heads, 1000 slots each: 47 us in parts, 42 in one; of 125 to 1000 slots 35 and 31.)
+    // Nothing is divided where tiles alone keep most of the card busy, or where there is a request for every compute unit whose slots are few.  (24 x 1190 rows of 4 cache heads, up to 8400 slots: 380 us divided
+    // and joined, 357 not; 64 requests, 32 heads of 128 to 8, 1000 slots each: 56 us in parts, 50 in one; of 125 to 1000 slots 44 and 37.  It is tiles that are counted, not slots: single tokens of long contexts
+    // beside a prompt are not divided either.)
     const int64_t busy = few ? sequences : rows / p.rows;
     int64_t parts = (range + p.least - 1) / p.least;
     if (parts > most_parts) parts = most_parts;
